@@ -290,8 +290,7 @@ def _run_own(s):
         pages.page_tables(s["lens"], s["new_lens"], s["free_pages"], s["free_top"], s["free_top_out"], s["table"],
                           s["cu_new"], s["slots"])
     elif kind == "store":
-        pages.page_store(s["k"], s["v"], s["lens"], s["table"], s["k_pages"], s["v_pages"])
-        pages.page_bounds(s["k_pages"], s["table"], None, s["lens"], s["bounds"])
+        pages.page_store(s["k"], s["v"], s["lens"], s["table"], s["k_pages"], s["v_pages"], s["bounds"])
     elif kind == "append":
         pages.rope_append(s["q"], s["k"], s["v"], s["positions"], s["slots"], s["q_out"], s["k_pages"], s["v_pages"])
     elif kind == "attend":
