@@ -229,7 +229,7 @@ def prepare(case, seed):
                   k_pages=torch.zeros((n_pages, hkv, p, d), dtype=dtype, device="cuda"),
                   v_pages=torch.zeros((n_pages, hkv, p, d), dtype=dtype, device="cuda"))
         if own:
-            st["pages"] = _handle(case, n_pages=n_pages, max_seqs=t, max_seq_pages=1, rope_theta=case["theta"],
+            st["pages"] = _handle(case, n_pages=n_pages, max_seqs=1, max_seq_pages=1, rope_theta=case["theta"],
                                   rope_sections=(case["axis_t"], case["axis_h"], case["axis_w"]), rope_order=case["order"],
                                   rope_pairing=case["pairing"])
         return st
