@@ -205,6 +205,140 @@ meda_status meda_compress_layer(meda_ctx* ctx, int32_t layer, const void* k, con
 meda_status meda_decode_attention(meda_ctx* ctx, int32_t layer, const void* q, const void* k_cache, const void* v_cache,
                                   const int32_t* budgets, int32_t n_rows, int32_t capacity, float* out, void* stream);
 
+/* ---- paged caches: decoding many requests over their compressed caches ----------------------- */
+
+/* The compressed cache of a layer has a length of its own, S_l, so a server that keeps many requests holds
+ * (requests x layers) caches of ragged lengths that grow by a row per decoded token.  The calls below keep them
+ * in pages.  A "sequence" here is one layer of one request.
+ *
+ *   pools     k_pages, v_pages: device, `dtype`, [n_pages][n_kv_heads][page_size][head_dim]
+ *   table     device int32 [n_seqs][max_seq_pages]: entry p of row i is the pool page that holds rows
+ *             [p * page_size, (p + 1) * page_size) of sequence i; entries behind its last page are never read
+ *   lengths   device int32, entry i at lens[i * lens_stride] (lens_stride 3 reads the S column of a budgets
+ *             array in place), 0 <= length <= max_seq_pages * page_size
+ *   slots     device int64: page * page_size + row inside the page, or -1 for "no slot"
+ *   bounds    device, `dtype`, [n_pages][n_kv_heads][2][head_dim]: minimum and maximum of each page's live keys
+ *
+ * The conventions at the top of this file hold: nothing is copied to the host, step calls allocate nothing, a
+ * meda_pages may be used by one host thread and one stream at a time (CUDA graphs captured through the same
+ * meda_pages share its scratch memory and must not run at the same time; give each stream its own).  Row
+ * counts live on the device and are read there, so one captured graph serves every step while its buffers stay
+ * in place.  Pool rows behind a sequence's length are never read: they may hold anything, NaN included, and
+ * stay as they are.  Errors only the device can see are recorded for meda_pages_poll_status: a length out of
+ * range (taken as the nearest valid one; meda_page_tables and meda_page_store skip instead), a page or a slot outside the pool (its rows are skipped), a
+ * free list that runs out.  The calls make the meda_pages' own device current for their duration.  n_seqs may
+ * be 0: nothing is done then, except that meda_page_tables passes the list's front on. */
+typedef struct meda_pages meda_pages; /* opaque: geometry, rotary frequencies and scratch memory */
+
+/* Which axis an element pair's rotary angle follows, and which elements form a pair. */
+enum { MEDA_ROPE_RUNS = 0, MEDA_ROPE_DEALT = 1 };
+enum { MEDA_ROPE_HALVES = 0, MEDA_ROPE_ADJACENT = 1 };
+
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim; /* head_dim in {64, 128, 256}; n_q_heads / n_kv_heads <= 16 */
+  int32_t dtype;                           /* meda_dtype of pools, queries, new rows and outputs */
+  int32_t page_size;                       /* rows per page: 16, 32, 64, 128 or 256 */
+  int32_t n_pages;                         /* pages in each pool */
+  int32_t max_seqs;                        /* most sequences of one call, <= 16384 */
+  int32_t max_seq_pages;                   /* entries of a table row, <= 262144 */
+  double rope_theta;                       /* base of the rotary frequencies, > 1 */
+  int32_t rope_sections[3];                /* frequencies that follow the time, height and width axis; their sum is
+                                            * half the rotated dimensions, a multiple of 8, at most head_dim / 2 */
+  int32_t rope_order;    /* MEDA_ROPE_RUNS: the time frequencies first, then height, then width.  MEDA_ROPE_DEALT:
+                          * frequency i is height's if i % 3 == 1 and i < 3 * rope_sections[1], width's if i % 3 == 2
+                          * and i < 3 * rope_sections[2], else time's */
+  int32_t rope_pairing;  /* MEDA_ROPE_HALVES: (i, i + half); MEDA_ROPE_ADJACENT: (2 i, 2 i + 1) */
+} meda_pages_config;
+
+/* Validates the geometry and allocates scratch memory on the current device (the only allocating call).
+ * max_seqs * max_seq_pages * page_size / 16 * n_kv_heads and n_pages * n_kv_heads * page_size stay below 2^31 and 2^40.
+ * On failure *out is NULL and the status says why. */
+meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out);
+/* Frees the scratch memory.  The caller must have synchronised the streams that used it. */
+void meda_pages_destroy(meda_pages* pages);
+int64_t meda_pages_workspace_bytes(const meda_pages* pages);
+/* Kernels launched since creation. */
+int64_t meda_pages_launch_count(const meda_pages* pages);
+/* Synchronises `stream`, returns the first device-side error recorded since the last poll (or MEDA_OK) and
+ * clears it. */
+meda_status meda_pages_poll_status(meda_pages* pages, void* stream);
+
+/* Page tables and slot maps for one change of lengths, lens -> new_lens (lens NULL: every sequence is new).
+ *   free_pages  device int32 [n_pages], free_top device int32 [1]: entries [*free_top, n_pages) of the list are the
+ *               free pages, taken from the front; entries before *free_top hold nothing
+ * A sequence that needs more pages takes them, in the order of the sequences and inside one by row; one that
+ * needs fewer gives its last pages back (new length 0: it has left).  Pages given back in this call are handed
+ * out first, in the order (sequence, page) they came in; then the free list serves; given pages nobody took go
+ * to the front of the list, so that the first of them ends just before the old front and the others before it.
+ *   free_top_out  device int32 [1]: the list's new front (another address than free_top's)
+ *   table         device int32 [n_seqs][max_seq_pages]: the entries of pages taken are written, no other
+ *   cu_new        device int32 [n_seqs + 1]: exclusive prefix sums of max(0, new_lens - lens)
+ *   slots         device int64 [slots_capacity]: slots of the new rows, sequence by sequence; -1 behind the last.
+ *                 slots_capacity 0 (slots is not read then): no slot map is wanted
+ * When the list runs out (MEDA_ERR_WORKSPACE), slots_capacity is too small (MEDA_ERR_WORKSPACE), or a length or
+ * the list's front is out of range (MEDA_ERR_INVALID_ARG) the table and the list stay as they are, *free_top_out = *free_top,
+ * cu_new is 0 and every slot -1. */
+meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t lens_stride, const int32_t* new_lens,
+                             int32_t new_stride, int32_t n_seqs, int32_t* free_pages, const int32_t* free_top,
+                             int32_t* free_top_out, int32_t* table, int32_t* cu_new, int64_t* slots,
+                             int64_t slots_capacity, void* stream);
+
+/* Rows of dense caches into pages: rows [0, lens[i]) of every head of sequence i, from
+ *   k, v   device, `dtype`: element (i, head, row, dim) at i * seq_stride + head * head_stride + row * head_dim + dim
+ *          (the k_out / v_out of meda_compress_layer for several layers, or full caches), rows_capacity rows per head
+ * to the pages table names.  bounds, if not NULL, gets the minimum and maximum over each written page's rows (a
+ * NaN key makes both NaN).  A sequence longer than rows_capacity records MEDA_ERR_WORKSPACE and is skipped.
+ * k, v, the pools and bounds are 16-byte aligned, both strides multiples of 16 bytes (MEDA_ERR_SHAPE otherwise). */
+meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int64_t seq_stride, int64_t head_stride,
+                            int32_t rows_capacity, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
+                            const int32_t* table, void* k_pages, void* v_pages, void* bounds, void* stream);
+
+/* Key bounds, recomputed for the pages that rows [lens_from[i], lens[i]) of each sequence touch (lens_from NULL: from
+ * row 0), each over all of the page's rows below lens[i].  Both lengths are read with lens_stride. */
+meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32_t* table, const int32_t* lens_from,
+                             const int32_t* lens, int32_t lens_stride, int32_t n_seqs, void* bounds, void* stream);
+
+/* Rotary positions with three axes, and the new rows into their pages.  For every token and every pair of elements
+ * (a, b) of a query or key head, with the pair's frequency i of `half` in all,
+ *   angle = position[axis(i)] * rope_theta^(-i / half),  (a, b) -> (a cos - b sin, b cos + a sin);
+ * dimensions behind the rotated ones pass through.  The angle is reduced in 64-bit fixed point (exact for any
+ * int32 position up to the frequency's own 2^-53), the rotation is fp32, rounded once.
+ *   q, k, v    device, `dtype`: token t's heads at t * stride, [heads][head_dim] dense inside a token (slices of one
+ *              projection's rows); 16-byte aligned, strides multiples of 16 bytes.  q (with q_out) may be NULL.
+ *   positions  device int32 [3][n_tokens], axis a at positions + a * axis_stride.  NULL: nothing is rotated.
+ *   slots      device int64 [n_tokens]: where the token's key and value go.  Slots of one call are distinct.
+ *   q_out      device, `dtype`, [n_tokens][n_q_heads][head_dim]; may be q itself when that is dense
+ * A token with slot -1 is padding: neither q_out nor the pools are written for it. */
+meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const int32_t* positions, int64_t axis_stride,
+                             const int64_t* slots, int32_t n_tokens, void* q_out, void* k_pages, void* v_pages,
+                             void* stream);
+
+/* Pages worth reading: for every sequence and KV head the `keep` pages with the highest score, ascending, as page
+ * numbers inside the sequence (columns of its table row).  The score of a page for KV head g is the largest logit its
+ * key bounds allow any query head h of g,
+ *   max_h sum_d (q_hd >= 0 ? q_hd * max_d : q_hd * min_d),
+ * summed in 64 bits and rounded once to fp32; ties go to the lowest page, a NaN ranks highest.  The first n_first and
+ * the last n_last pages are always among them (n_first + n_last <= keep).
+ *   q      device, `dtype`, [n_seqs][n_q_heads][head_dim];  bounds: 16-byte aligned
+ *   sel    device int32 [n_seqs][n_kv_heads][keep]: min(keep, pages of the sequence) entries, the others untouched */
+meda_status meda_select_pages(meda_pages* pages, const void* q, const void* bounds, const int32_t* table,
+                              const int32_t* lens, int32_t lens_stride, int32_t n_seqs, int32_t n_first,
+                              int32_t n_last, int32_t keep, int32_t* sel, void* stream);
+
+/* Attention of one new token's queries per sequence over its pages (Eq. 3, as meda_decode_attention):
+ *   out[i][h] = softmax(q_ih . K^T / sqrt(head_dim)) V over rows [0, lens[i]) of KV head g of query head h, or, with
+ *   sel (of meda_select_pages, `keep` entries per sequence and KV head), over those rows that lie in the
+ *   min(keep, pages of the sequence) pages it names.
+ *   q    device, `dtype`, [n_seqs][n_q_heads][head_dim]; q and the pools are 16-byte aligned
+ *   out  device, `dtype`, [n_seqs][n_q_heads][head_dim]
+ *   lse  device fp32 [n_seqs][n_q_heads], may be NULL: the logarithm of the softmax's sum, ready to join with the
+ *        attention over rows kept elsewhere
+ * A sequence of length 0 gets out = 0, lse = -inf. */
+meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                                 const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
+                                 const int32_t* sel, int32_t keep, void* out, float* lse, void* stream);
+
 /* ---- entry point that allocates nothing (the paper has no counterpart) ---------------------- */
 
 /* Largest n_q_heads * window the entry point below accepts, and the size of the scratch array

@@ -53,6 +53,16 @@ class meda_config(ctypes.Structure):
     ]
 
 
+class meda_pages_config(ctypes.Structure):
+    _fields_ = [
+        ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("max_seqs", ctypes.c_int32), ("max_seq_pages", ctypes.c_int32),
+        ("rope_theta", ctypes.c_double), ("rope_sections", ctypes.c_int32 * 3),
+        ("rope_order", ctypes.c_int32), ("rope_pairing", ctypes.c_int32),
+    ]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "meda_create": (ctypes.c_int, [ctypes.POINTER(meda_config), ctypes.POINTER(meda_span), ctypes.c_int32,
@@ -83,6 +93,21 @@ EXPORTS = {
                       [ctypes.c_int32, ctypes.c_void_p]),
     "meda_compress_layer": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int32] + [ctypes.c_void_p] * 8 +
                             [ctypes.c_int32, ctypes.c_void_p]),
+    "meda_pages_create": (ctypes.c_int, [ctypes.POINTER(meda_pages_config), ctypes.POINTER(ctypes.c_void_p)]),
+    "meda_pages_destroy": (None, [ctypes.c_void_p]),
+    "meda_pages_workspace_bytes": (ctypes.c_int64, [ctypes.c_void_p]),
+    "meda_pages_launch_count": (ctypes.c_int64, [ctypes.c_void_p]),
+    "meda_pages_poll_status": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "meda_page_tables": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
+                                        ctypes.c_int32] + [ctypes.c_void_p] * 6 + [ctypes.c_int64, ctypes.c_void_p]),
+    "meda_page_store": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p,
+                                       ctypes.c_int32, ctypes.c_int32] + [ctypes.c_void_p] * 5),
+    "meda_page_bounds": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int32] * 2 + [ctypes.c_void_p] * 2),
+    "meda_rope_append": (ctypes.c_int, [ctypes.c_void_p] + [ctypes.c_void_p, ctypes.c_int64] * 4 +
+                         [ctypes.c_void_p, ctypes.c_int32] + [ctypes.c_void_p] * 4),
+    "meda_select_pages": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int32] * 5 + [ctypes.c_void_p] * 2),
+    "meda_paged_attention": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_int32] * 2 + [ctypes.c_void_p, ctypes.c_int32] +
+                             [ctypes.c_void_p] * 3),
 }
 
 
@@ -263,3 +288,177 @@ class Context:
         _check(self._lib.meda_decode_attention(self._h, layer, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(budgets),
                                                int(n_rows), int(cap), _ptr(out), _stream(stream)), "meda_decode_attention")
 
+
+ROPE_RUNS, ROPE_DEALT = 0, 1
+ROPE_HALVES, ROPE_ADJACENT = 0, 1
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+
+
+class Pages:
+    """Owns one meda_pages: the paged caches of many sequences (one layer of one request each) of one geometry.
+    Method names and argument order follow include/meda.h; shapes are read from the tensors and checked
+    against the geometry.  Lengths are 1-D int32 tensors of any stride (`budgets[:, 0]` as it is).  The handle
+    belongs to the device that is current when it is made, and so do the tensors."""
+
+    def __init__(self, *, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_seqs, max_seq_pages,
+                 rope_theta=10000.0, rope_sections=None, rope_order=ROPE_RUNS, rope_pairing=ROPE_HALVES):
+        self._h = None
+        lib = load_library()
+        f32 = dtype in ("f32", torch.float32)
+        if not f32 and dtype not in ("bf16", torch.bfloat16):
+            raise ValueError("dtype is bf16 or f32")
+        sections = (head_dim // 2, 0, 0) if rope_sections is None else tuple(int(x) for x in rope_sections)
+        if len(sections) != 3:
+            raise ValueError("rope_sections has three entries: time, height, width")
+        self.cfg = meda_pages_config(n_q_heads, n_kv_heads, head_dim, MEDA_F32 if f32 else MEDA_BF16, page_size, n_pages,
+                                     max_seqs, max_seq_pages, float(rope_theta), (ctypes.c_int32 * 3)(*sections),
+                                     rope_order, rope_pairing)
+        handle = ctypes.c_void_p()
+        _check(lib.meda_pages_create(ctypes.byref(self.cfg), ctypes.byref(handle)), "meda_pages_create")
+        self._h = handle.value
+        self._lib = lib
+        self._device = torch.cuda.current_device()
+        self._dtype = torch.float32 if f32 else torch.bfloat16
+        self._n_pages, self._width = int(n_pages), int(max_seq_pages)
+        self._hq, self._hkv, self._d = int(n_q_heads), int(n_kv_heads), int(head_dim)
+        self._pool = (self._n_pages, self._hkv, int(page_size), self._d)
+        self._bounds = (self._n_pages, self._hkv, 2, self._d)
+
+    def close(self):
+        if self._h is not None:
+            self._lib.meda_pages_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def workspace_bytes(self) -> int:
+        return int(self._lib.meda_pages_workspace_bytes(self._h))
+
+    def launch_count(self) -> int:
+        return int(self._lib.meda_pages_launch_count(self._h))
+
+    def poll_status(self, stream=None) -> int:
+        return int(self._lib.meda_pages_poll_status(self._h, self._stream(stream)))
+
+    def check(self, stream=None):
+        _check(self.poll_status(stream), "device status")
+
+    def _stream(self, stream):
+        return (torch.cuda.current_stream(self._device) if stream is None else stream).cuda_stream
+
+    def _dense(self, t, shape, dtype, what):
+        """Address of a contiguous tensor of the handle's device with this type and shape."""
+        if t.dtype is not dtype or t.get_device() != self._device or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{self._device} is wanted, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _lens(self, t, what, n=None):
+        if t.dtype is not _I32 or t.get_device() != self._device or t.dim() != 1 or (n is not None and t.shape[0] != n):
+            raise ValueError(f"{what}: a 1-D int32 tensor{'' if n is None else f' of {n}'} on cuda:{self._device} is wanted, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _heads(self, t, n, heads, what):
+        """(address, token stride) of [n][heads][head_dim] rows that are dense inside a token."""
+        if t.dtype is not self._dtype or t.get_device() != self._device or t.shape != (n, heads, self._d):
+            raise ValueError(f"{what}: {self._dtype} of shape {(n, heads, self._d)} on cuda:{self._device} is wanted, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        st = t.stride()
+        if st[2] != 1 or (heads > 1 and st[1] != self._d):
+            raise ValueError(f"{what}: the heads of a token have to be dense, got strides {st}")
+        return t.data_ptr(), st[0] if n > 1 else 0
+
+    def page_tables(self, lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, stream=None):
+        """lens may be None (every sequence is new); an empty slots tensor: no slot map is wanted."""
+        n = new_lens.shape[0]
+        status = self._lib.meda_page_tables(
+            self._h, None if lens is None else self._lens(lens, "lens", n), 0 if lens is None else lens.stride(0),
+            self._lens(new_lens, "new_lens"), new_lens.stride(0), n, self._dense(free_pages, (self._n_pages,), _I32, "free_pages"),
+            self._dense(free_top, (1,), _I32, "free_top"), self._dense(free_top_out, (1,), _I32, "free_top_out"),
+            self._dense(table, (n, self._width), _I32, "table"), self._dense(cu_new, (n + 1,), _I32, "cu_new"),
+            self._dense(slots, (slots.shape[0],), _I64, "slots"), slots.shape[0], self._stream(stream))
+        if status:
+            _check(status, "meda_page_tables")
+
+    def page_store(self, k, v, lens, table, k_pages, v_pages, bounds=None, stream=None):
+        """k, v: [n_seqs][n_kv_heads][capacity][head_dim], rows of a head dense, the outer strides free but alike."""
+        n = lens.shape[0]
+        st = k.stride()
+        for t, what in ((k, "k"), (v, "v")):
+            if t.dtype is not self._dtype or t.get_device() != self._device or t.dim() != 4 or t.shape != k.shape or \
+                    t.shape[0] != n or t.shape[1] != self._hkv or t.shape[3] != self._d:
+                raise ValueError(f"{what}: {self._dtype} [{n}][{self._hkv}][capacity][{self._d}] on cuda:{self._device} is wanted, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+            if t.stride() != st or st[3] != 1 or (t.shape[2] > 1 and st[2] != self._d):
+                raise ValueError(f"{what}: rows have to be dense and k and v laid out alike, got strides {t.stride()}")
+        status = self._lib.meda_page_store(
+            self._h, k.data_ptr(), v.data_ptr(), st[0] if n > 1 else 0, st[1] if self._hkv > 1 else 0, k.shape[2], self._lens(lens, "lens"), lens.stride(0), n,
+            self._dense(table, (n, self._width), _I32, "table"), self._dense(k_pages, self._pool, self._dtype, "k_pages"),
+            self._dense(v_pages, self._pool, self._dtype, "v_pages"),
+            None if bounds is None else self._dense(bounds, self._bounds, self._dtype, "bounds"), self._stream(stream))
+        if status:
+            _check(status, "meda_page_store")
+
+    def page_bounds(self, k_pages, table, lens_from, lens, bounds, stream=None):
+        n = lens.shape[0]
+        if lens_from is not None and lens_from.stride() != lens.stride():
+            raise ValueError("lens_from and lens have to have the same stride")
+        status = self._lib.meda_page_bounds(
+            self._h, self._dense(k_pages, self._pool, self._dtype, "k_pages"), self._dense(table, (n, self._width), _I32, "table"),
+            None if lens_from is None else self._lens(lens_from, "lens_from", n), self._lens(lens, "lens"), lens.stride(0), n,
+            self._dense(bounds, self._bounds, self._dtype, "bounds"), self._stream(stream))
+        if status:
+            _check(status, "meda_page_bounds")
+
+    def rope_append(self, q, k, v, positions, slots, q_out, k_pages, v_pages, stream=None):
+        """q, k, v: [n_tokens][heads][head_dim] with any token stride; positions: int32 [3][n_tokens] or None."""
+        n = slots.shape[0]
+        k_ptr, k_st = self._heads(k, n, self._hkv, "k")
+        v_ptr, v_st = self._heads(v, n, self._hkv, "v")
+        q_ptr, q_st, out_ptr = None, 0, None
+        if q is not None:
+            q_ptr, q_st = self._heads(q, n, self._hq, "q")
+            out_ptr = self._dense(q_out, (n, self._hq, self._d), self._dtype, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        pos_ptr, axis_st = None, 0
+        if positions is not None:
+            if positions.dtype is not _I32 or positions.get_device() != self._device or positions.shape != (3, n) or \
+                    (n > 1 and positions.stride(1) != 1):
+                raise ValueError(f"positions: int32 [3][{n}] with dense axes on cuda:{self._device} is wanted, "
+                                 f"got {positions.dtype} {tuple(positions.shape)} on {positions.device}")
+            pos_ptr, axis_st = positions.data_ptr(), positions.stride(0)
+        status = self._lib.meda_rope_append(
+            self._h, q_ptr, q_st, k_ptr, k_st, v_ptr, v_st, pos_ptr, axis_st, self._dense(slots, (n,), _I64, "slots"), n, out_ptr,
+            self._dense(k_pages, self._pool, self._dtype, "k_pages"), self._dense(v_pages, self._pool, self._dtype, "v_pages"),
+            self._stream(stream))
+        if status:
+            _check(status, "meda_rope_append")
+
+    def select_pages(self, q, bounds, table, lens, n_first, n_last, sel, stream=None):
+        """sel: int32 [n_seqs][n_kv_heads][keep]."""
+        n, keep = lens.shape[0], sel.shape[-1]
+        status = self._lib.meda_select_pages(
+            self._h, self._dense(q, (n, self._hq, self._d), self._dtype, "q"), self._dense(bounds, self._bounds, self._dtype, "bounds"),
+            self._dense(table, (n, self._width), _I32, "table"), self._lens(lens, "lens"), lens.stride(0), n, n_first, n_last, keep,
+            self._dense(sel, (n, self._hkv, keep), _I32, "sel"), self._stream(stream))
+        if status:
+            _check(status, "meda_select_pages")
+
+    def paged_attention(self, q, k_pages, v_pages, table, lens, out, lse=None, sel=None, stream=None):
+        n = lens.shape[0]
+        shape = (n, self._hq, self._d)
+        keep = 0 if sel is None else sel.shape[-1]
+        status = self._lib.meda_paged_attention(
+            self._h, self._dense(q, shape, self._dtype, "q"), self._dense(k_pages, self._pool, self._dtype, "k_pages"),
+            self._dense(v_pages, self._pool, self._dtype, "v_pages"), self._dense(table, (n, self._width), _I32, "table"),
+            self._lens(lens, "lens"), lens.stride(0), n, None if sel is None else self._dense(sel, (n, self._hkv, keep), _I32, "sel"),
+            keep, self._dense(out, shape, self._dtype, "out"), None if lse is None else self._dense(lse, shape[:2], _F32, "lse"),
+            self._stream(stream))
+        if status:
+            _check(status, "meda_paged_attention")

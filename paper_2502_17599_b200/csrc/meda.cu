@@ -1166,3 +1166,5 @@ meda_status meda_compress_layer(meda_ctx* ctx, int32_t layer, const void* k, con
 
 }  // extern "C"
 #pragma GCC visibility pop
+
+#include "pages_api.cuh"     // meda_pages_* and the calls over paged caches

@@ -1,0 +1,423 @@
+// Host side of the paged caches: the handle and the launches behind meda_pages_* and the calls that take a meda_pages
+// (declared in include/meda.h).  Included by meda.cu, which owns the entry points' visibility.
+#pragma once
+
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <new>
+
+#include "page_rows.cuh"
+#include "page_tables.cuh"
+#include "paged_attention.cuh"
+#include "pages_common.cuh"
+#include "rope_append.cuh"
+#include "select_pages.cuh"
+
+namespace {
+
+using namespace meda;
+
+// Makes the handle's device current for one call.
+struct PagesDevice {
+  int before = -1;
+  bool ok = false, switched = false;
+  explicit PagesDevice(const meda_pages* p) {
+    if (cudaGetDevice(&before) != cudaSuccess) return;
+    if (before != p->device) {
+      if (cudaSetDevice(p->device) != cudaSuccess) return;
+      switched = true;
+    }
+    ok = true;
+  }
+  ~PagesDevice() {
+    if (switched) cudaSetDevice(before);
+  }
+};
+
+inline bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
+
+int pages_element(const meda_pages* p) { return p->cfg.dtype == MEDA_F32 ? 4 : 2; }
+
+// meda_* status of the arguments every call over sequences shares.
+meda_status pages_batch_ok(const meda_pages* p, int32_t n_seqs, int32_t lens_stride) {
+  if (n_seqs < 0 || lens_stride < 0) return MEDA_ERR_INVALID_ARG;
+  return n_seqs > p->cfg.max_seqs ? MEDA_ERR_SHAPE : MEDA_OK;
+}
+
+// ---- attention ---------------------------------------------------------------------------------
+template <typename Tile, int D, int W>
+struct AttnKernel {
+  static constexpr auto kernel = paged_attention_kernel<Tile, D, W>;
+  static size_t smem(int n_seqs, int blocks) {
+    return (size_t)(attn_prefix_floats(n_seqs) + attn_merge_floats(W, Tile::kHeads, D, blocks)) * 4;
+  }
+  // Blocks that are resident at once, with the shared memory of the largest batch.
+  static meda_status prepare(meda_pages* p) {
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return MEDA_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem - (int)a.sharedSizeBytes) != cudaSuccess)
+      return MEDA_ERR_CUDA;
+    int per_sm = 0;
+    const size_t need = smem(p->cfg.max_seqs, p->sm_count);
+    if (need > (size_t)(kMaxDynSmem - (int)a.sharedSizeBytes)) return MEDA_ERR_SHAPE;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, W * 32, need) != cudaSuccess || per_sm < 1)
+      return MEDA_ERR_CUDA;
+    p->attn_blocks = p->sm_count;
+    return MEDA_OK;
+  }
+  static meda_status launch(meda_pages* p, const AttnParams& a, cudaStream_t st) {
+    ++p->launches;
+    kernel<<<p->attn_blocks, W * 32, smem(a.n_seqs, p->attn_blocks), st>>>(a);
+    return launch_status();
+  }
+};
+
+// Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
+// (More than eight query heads per KV head at head_dim 256 take two segments: the accumulators of sixteen do not fit.)
+template <typename F>
+meda_status with_attn_kernel(const meda_pages* p, F f) {
+  const int d = p->cfg.head_dim, g = p->group;
+  if (p->cfg.dtype == MEDA_BF16) {
+    if (d == 64) return g <= 8 ? f(AttnKernel<AttnTileBf16<64, 1>, 64, 16>()) : f(AttnKernel<AttnTileBf16<64, 2>, 64, 16>());
+    if (d == 128) return g <= 8 ? f(AttnKernel<AttnTileBf16<128, 1>, 128, 12>()) : f(AttnKernel<AttnTileBf16<128, 2>, 128, 8>());
+    return f(AttnKernel<AttnTileBf16<256, 1>, 256, 8>());
+  }
+  if (d == 64)
+    return g == 1 ? f(AttnKernel<AttnTileF32<64, 1>, 64, 16>()) : g == 2 ? f(AttnKernel<AttnTileF32<64, 2>, 64, 16>())
+         : g <= 4 ? f(AttnKernel<AttnTileF32<64, 4>, 64, 16>()) : f(AttnKernel<AttnTileF32<64, 8>, 64, 16>());
+  if (d == 128)
+    return g == 1 ? f(AttnKernel<AttnTileF32<128, 1>, 128, 16>()) : g == 2 ? f(AttnKernel<AttnTileF32<128, 2>, 128, 16>())
+         : g <= 4 ? f(AttnKernel<AttnTileF32<128, 4>, 128, 8>()) : f(AttnKernel<AttnTileF32<128, 8>, 128, 8>());
+  return g == 1 ? f(AttnKernel<AttnTileF32<256, 1>, 256, 8>()) : g == 2 ? f(AttnKernel<AttnTileF32<256, 2>, 256, 8>())
+                                                                       : f(AttnKernel<AttnTileF32<256, 4>, 256, 8>());
+}
+
+// ---- selection of pages ------------------------------------------------------------------------
+template <typename T, int D, int GP>
+struct SelectPagesKernel {
+  static constexpr auto kernel = select_pages_kernel<T, D, GP>;
+  static meda_status prepare() { return raise_dyn_smem(kernel); }
+  static meda_status launch(meda_pages* p, const SelectPagesParams& a, int cluster, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.n_seqs * a.n_heads * cluster);
+    cfg.blockDim = dim3(kSelThreads);
+    cfg.dynamicSmemBytes = select_pages_smem(a.width, cluster, GP, D).total;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    ++p->launches;
+    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? MEDA_OK : (cudaGetLastError(), MEDA_ERR_CUDA);
+  }
+};
+
+template <typename T, int D, typename F>
+meda_status with_select_group(const meda_pages* p, F f) {
+  const int g = p->group;
+  return g == 1 ? f(SelectPagesKernel<T, D, 1>()) : g == 2 ? f(SelectPagesKernel<T, D, 2>())
+       : g <= 4 ? f(SelectPagesKernel<T, D, 4>()) : g <= 8 ? f(SelectPagesKernel<T, D, 8>()) : f(SelectPagesKernel<T, D, 16>());
+}
+
+template <typename F>
+meda_status with_select_kernel(const meda_pages* p, F f) {
+  const int d = p->cfg.head_dim;
+  if (p->cfg.dtype == MEDA_BF16)
+    return d == 64 ? with_select_group<__nv_bfloat16, 64>(p, f) : d == 128 ? with_select_group<__nv_bfloat16, 128>(p, f)
+                                                                         : with_select_group<__nv_bfloat16, 256>(p, f);
+  return d == 64 ? with_select_group<float, 64>(p, f) : d == 128 ? with_select_group<float, 128>(p, f)
+                                                                 : with_select_group<float, 256>(p, f);
+}
+
+int group_rounded(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
+
+// Blocks per cluster: the largest of 8, 4, 2, 1 that keeps all clusters within one wave and gives a block a
+// few hundred pages, unless the sort keys need more blocks' shared memory than that.
+int select_pages_cluster(const meda_pages* p, int n_seqs) {
+  int c = 8;
+  const int width = p->cfg.max_seq_pages;
+  while (c > 1 && ((width + c - 1) / c < 256 || (int64_t)n_seqs * p->cfg.n_kv_heads * c > p->sm_count) &&
+         select_pages_smem(width, c / 2, group_rounded(p->group), p->cfg.head_dim).total <= kMaxDynSmem - 1024)
+    c /= 2;
+  return c;
+}
+
+// ---- pages of rows -----------------------------------------------------------------------------
+template <bool STORE>
+meda_status launch_page_rows(meda_pages* p, const RowsParams& a, cudaStream_t st) {
+  ++p->launches;
+  const int grid = p->sm_count * 4;
+  const size_t smem = (size_t)(a.n_seqs + 1) * 4;
+  const int vr = p->cfg.head_dim * pages_element(p) / 16;
+  if (p->cfg.dtype == MEDA_F32) {
+    if (vr == 16) page_rows_kernel<float, 16, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+    else if (vr == 32) page_rows_kernel<float, 32, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+    else page_rows_kernel<float, 64, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+  } else {
+    if (vr == 8) page_rows_kernel<__nv_bfloat16, 8, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+    else if (vr == 16) page_rows_kernel<__nv_bfloat16, 16, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+    else page_rows_kernel<__nv_bfloat16, 32, STORE><<<grid, kRowsThreads, smem, st>>>(a);
+  }
+  return launch_status();
+}
+
+template <bool STORE>
+meda_status raise_page_rows_smem() {
+  meda_status r = raise_dyn_smem(page_rows_kernel<float, 16, STORE>);
+  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<float, 32, STORE>);
+  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<float, 64, STORE>);
+  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 8, STORE>);
+  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 16, STORE>);
+  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 32, STORE>);
+  return r;
+}
+
+template <typename T, bool ADJACENT>
+void launch_rope(const RopeParams& a, int d, int grid, cudaStream_t st) {
+  if (d == 64) rope_append_kernel<T, 64, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
+  else if (d == 128) rope_append_kernel<T, 128, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
+  else rope_append_kernel<T, 256, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
+}
+
+void pages_release(meda_pages* p) {
+  cudaFree(p->status);
+  cudaFree(p->rope_freq);
+  cudaFree(p->rope_axis);
+  cudaFree(p->attn_partial);
+  cudaFree(p->attn_counters);
+  delete p;
+}
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out) {
+  if (out) *out = nullptr;
+  if (!config || !out) return MEDA_ERR_INVALID_ARG;
+  const meda_pages_config& c = *config;
+  if (c.dtype != MEDA_BF16 && c.dtype != MEDA_F32) return MEDA_ERR_INVALID_ARG;
+  if (c.rope_order != MEDA_ROPE_RUNS && c.rope_order != MEDA_ROPE_DEALT) return MEDA_ERR_INVALID_ARG;
+  if (c.rope_pairing != MEDA_ROPE_HALVES && c.rope_pairing != MEDA_ROPE_ADJACENT) return MEDA_ERR_INVALID_ARG;
+  if (!(c.rope_theta > 1.0) || !(c.rope_theta < 1e300)) return MEDA_ERR_INVALID_ARG;
+  if (c.n_q_heads < 1 || c.n_kv_heads < 1 || c.n_q_heads % c.n_kv_heads != 0 || c.n_q_heads / c.n_kv_heads > 16 ||
+      c.n_kv_heads > 1024)
+    return MEDA_ERR_SHAPE;
+  if (c.head_dim != 64 && c.head_dim != 128 && c.head_dim != 256) return MEDA_ERR_SHAPE;
+  if (c.page_size < 16 || c.page_size > 256 || (c.page_size & (c.page_size - 1)) != 0) return MEDA_ERR_SHAPE;
+  if (c.n_pages < 1 || c.max_seqs < 1 || c.max_seqs > kPagesMaxSeqs || c.max_seq_pages < 1 || c.max_seq_pages > kPagesMaxSeqPages)
+    return MEDA_ERR_SHAPE;
+  if ((int64_t)c.max_seqs * c.max_seq_pages * (c.page_size / 16) * c.n_kv_heads >= (int64_t(1) << 31) ||
+      (int64_t)c.n_pages * c.n_kv_heads * c.page_size >= (int64_t(1) << 40))
+    return MEDA_ERR_SHAPE;
+  int64_t half = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (c.rope_sections[a] < 0 || c.rope_sections[a] > c.head_dim / 2) return MEDA_ERR_SHAPE;
+    half += c.rope_sections[a];
+  }
+  if (half < 8 || half % 8 != 0 || half > c.head_dim / 2) return MEDA_ERR_SHAPE;
+  int axis[128];
+  for (int i = 0; i < (int)half; ++i) {
+    if (c.rope_order == MEDA_ROPE_RUNS)
+      axis[i] = i < c.rope_sections[0] ? 0 : (i < c.rope_sections[0] + c.rope_sections[1] ? 1 : 2);
+    else
+      axis[i] = i % 3 == 1 && i < 3 * c.rope_sections[1] ? 1 : (i % 3 == 2 && i < 3 * c.rope_sections[2] ? 2 : 0);
+  }
+  for (int a = 1; a < 3; ++a)                                  // dealt out: every section must find its places
+    if (std::count(axis, axis + half, a) != c.rope_sections[a]) return MEDA_ERR_SHAPE;
+  unsigned long long freq[128];
+  for (int i = 0; i < (int)half; ++i)                          // below one turn per position: 2^64 / 2 pi at most
+    freq[i] = (unsigned long long)(pow(c.rope_theta, -(double)i / (double)half) / 6.283185307179586476925 * 18446744073709551616.0);
+
+  meda_pages* p = new (std::nothrow) meda_pages();
+  if (!p) return MEDA_ERR_CUDA;
+  p->cfg = c;
+  p->group = c.n_q_heads / c.n_kv_heads;
+  p->page_shift = 4;
+  while ((1 << p->page_shift) < c.page_size) ++p->page_shift;
+  meda_status st = MEDA_OK;
+  if (cudaGetDevice(&p->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess)
+    st = MEDA_ERR_CUDA;
+  if (st == MEDA_OK) st = with_attn_kernel(p, [&](auto k) { return k.prepare(p); });
+  if (st == MEDA_OK) st = with_select_kernel(p, [](auto k) { return k.prepare(); });
+  if (st == MEDA_OK && select_pages_smem(c.max_seq_pages, 8, group_rounded(p->group), c.head_dim).total > kMaxDynSmem - 1024)
+    st = MEDA_ERR_SHAPE;
+  if (st == MEDA_OK) st = raise_page_rows_smem<true>();
+  if (st == MEDA_OK) st = raise_page_rows_smem<false>();
+  if (st == MEDA_OK) st = raise_dyn_smem(page_tables_kernel);
+  if (st == MEDA_OK) st = carve(&p->status, 1, &p->bytes);
+  if (st == MEDA_OK) st = carve(&p->rope_freq, half, &p->bytes);
+  if (st == MEDA_OK) st = carve(&p->rope_axis, half, &p->bytes);
+  if (st == MEDA_OK) st = carve(&p->attn_partial, (int64_t)p->attn_blocks * 2 * attn_state_floats(p->group, c.head_dim), &p->bytes);
+  const int64_t counters = (int64_t)c.max_seqs * c.n_q_heads;  // segments: at most one per query head
+  if (st == MEDA_OK) st = carve(&p->attn_counters, counters, &p->bytes);
+  if (st == MEDA_OK && (cudaMemset(p->status, 0, sizeof(int)) != cudaSuccess ||
+                        cudaMemset(p->attn_counters, 0, (size_t)counters * 4) != cudaSuccess ||
+                        cudaMemcpy(p->rope_freq, freq, (size_t)half * 8, cudaMemcpyHostToDevice) != cudaSuccess ||
+                        cudaMemcpy(p->rope_axis, axis, (size_t)half * 4, cudaMemcpyHostToDevice) != cudaSuccess ||
+                        cudaStreamSynchronize(nullptr) != cudaSuccess))
+    st = MEDA_ERR_CUDA;
+  if (st != MEDA_OK) {
+    pages_release(p);
+    cudaGetLastError();
+    return st;
+  }
+  *out = p;
+  return MEDA_OK;
+}
+
+void meda_pages_destroy(meda_pages* pages) {
+  if (pages) pages_release(pages);
+}
+
+int64_t meda_pages_workspace_bytes(const meda_pages* pages) { return pages ? pages->bytes : 0; }
+
+int64_t meda_pages_launch_count(const meda_pages* pages) { return pages ? pages->launches : 0; }
+
+meda_status meda_pages_poll_status(meda_pages* pages, void* stream) {
+  if (!pages) return MEDA_ERR_INVALID_ARG;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  int code = 0;
+  MEDA_CUDA_TRY(cudaStreamSynchronize(as_stream(stream)));
+  MEDA_CUDA_TRY(cudaMemcpy(&code, pages->status, sizeof(int), cudaMemcpyDeviceToHost));
+  if (code != 0) MEDA_CUDA_TRY(cudaMemset(pages->status, 0, sizeof(int)));
+  return (meda_status)code;
+}
+
+meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t lens_stride, const int32_t* new_lens,
+                             int32_t new_stride, int32_t n_seqs, int32_t* free_pages, const int32_t* free_top,
+                             int32_t* free_top_out, int32_t* table, int32_t* cu_new, int64_t* slots,
+                             int64_t slots_capacity, void* stream) {
+  if (!pages || !free_pages || !free_top || !free_top_out || !cu_new) return MEDA_ERR_INVALID_ARG;
+  if (free_top == free_top_out || slots_capacity < 0 || new_stride < 0) return MEDA_ERR_INVALID_ARG;
+  if (slots_capacity > INT32_MAX) return MEDA_ERR_SHAPE;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK) return r;
+  if ((n_seqs > 0 && (!new_lens || !table)) || (slots_capacity > 0 && !slots)) return MEDA_ERR_INVALID_ARG;
+  if (slots_capacity == 0) slots = nullptr;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  const meda_pages_config& c = pages->cfg;
+  TablesParams a = {lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, pages->status,
+                    lens_stride, new_stride, n_seqs, c.n_pages, c.max_seq_pages, pages->page_shift, (int)slots_capacity};
+  // a block per 4,096 entries that may be written (every warp two runs of them), one per SM at most: each block repeats the scans
+  const int64_t entries = slots_capacity + std::min<int64_t>(c.n_pages, (int64_t)n_seqs * c.max_seq_pages);
+  const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (entries + 4095) / 4096));
+  ++pages->launches;
+  page_tables_kernel<<<grid, kTabThreads, (size_t)(n_seqs + 1) * 12, as_stream(stream)>>>(a);
+  return launch_status();
+}
+
+meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int64_t seq_stride, int64_t head_stride,
+                            int32_t rows_capacity, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
+                            const int32_t* table, void* k_pages, void* v_pages, void* bounds, void* stream) {
+  if (!pages || rows_capacity < 0 || seq_stride < 0 || head_stride < 0) return MEDA_ERR_INVALID_ARG;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK || n_seqs == 0) return r;
+  if (!k || !v || !lens || !table || !k_pages || !v_pages) return MEDA_ERR_INVALID_ARG;
+  const meda_pages_config& c = pages->cfg;
+  const int e = 16 / pages_element(pages);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(bounds) || seq_stride % e != 0 ||
+      head_stride % e != 0)
+    return MEDA_ERR_SHAPE;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  RowsParams a = {k, v, k_pages, v_pages, bounds, table, nullptr, lens, pages->status, seq_stride / e, head_stride / e,
+                  lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, rows_capacity};
+  return launch_page_rows<true>(pages, a, as_stream(stream));
+}
+
+meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32_t* table, const int32_t* lens_from,
+                             const int32_t* lens, int32_t lens_stride, int32_t n_seqs, void* bounds, void* stream) {
+  if (!pages) return MEDA_ERR_INVALID_ARG;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK || n_seqs == 0) return r;
+  if (!k_pages || !table || !lens || !bounds) return MEDA_ERR_INVALID_ARG;
+  if (!aligned16(k_pages) || !aligned16(bounds)) return MEDA_ERR_SHAPE;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  const meda_pages_config& c = pages->cfg;
+  RowsParams a = {k_pages, nullptr, nullptr, nullptr, bounds, table, lens_from, lens, pages->status, 0, 0,
+                  lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, 0};
+  return launch_page_rows<false>(pages, a, as_stream(stream));
+}
+
+meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const int32_t* positions, int64_t axis_stride,
+                             const int64_t* slots, int32_t n_tokens, void* q_out, void* k_pages, void* v_pages,
+                             void* stream) {
+  if (!pages || n_tokens < 0 || q_stride < 0 || k_stride < 0 || v_stride < 0 || axis_stride < 0) return MEDA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MEDA_OK;
+  if (!k || !v || !slots || !k_pages || !v_pages || (q == nullptr) != (q_out == nullptr)) return MEDA_ERR_INVALID_ARG;
+  const meda_pages_config& c = pages->cfg;
+  const int e = 16 / pages_element(pages);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_pages) || !aligned16(v_pages) ||
+      q_stride % e != 0 || k_stride % e != 0 || v_stride % e != 0)
+    return MEDA_ERR_SHAPE;
+  if (q && q == q_out && n_tokens > 1 && q_stride != (int64_t)c.n_q_heads * c.head_dim) return MEDA_ERR_INVALID_ARG;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  const int half = c.rope_sections[0] + c.rope_sections[1] + c.rope_sections[2];
+  // one token per block while there are fewer tokens than the GPU holds blocks, else enough of them to
+  // share the block's start
+  const int tokens = (int)std::min<int64_t>(kRopeMaxTokens, std::max<int64_t>(1, n_tokens / (pages->sm_count * 8)));
+  RopeParams a = {q, k, v, positions, slots, q_out, k_pages, v_pages, pages->rope_freq, pages->rope_axis, pages->status,
+                  q_stride / e, k_stride / e, v_stride / e, axis_stride, (long long)c.n_pages << pages->page_shift,
+                  n_tokens, c.n_q_heads, c.n_kv_heads, half, pages->page_shift, tokens};
+  const int grid = (n_tokens + tokens - 1) / tokens;
+  ++pages->launches;
+  cudaStream_t st = as_stream(stream);
+  const bool adjacent = c.rope_pairing == MEDA_ROPE_ADJACENT;
+  if (c.dtype == MEDA_F32) {
+    if (adjacent) launch_rope<float, true>(a, c.head_dim, grid, st);
+    else launch_rope<float, false>(a, c.head_dim, grid, st);
+  } else {
+    if (adjacent) launch_rope<__nv_bfloat16, true>(a, c.head_dim, grid, st);
+    else launch_rope<__nv_bfloat16, false>(a, c.head_dim, grid, st);
+  }
+  return launch_status();
+}
+
+meda_status meda_select_pages(meda_pages* pages, const void* q, const void* bounds, const int32_t* table,
+                              const int32_t* lens, int32_t lens_stride, int32_t n_seqs, int32_t n_first, int32_t n_last,
+                              int32_t keep, int32_t* sel, void* stream) {
+  if (!pages || keep < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > keep) return MEDA_ERR_INVALID_ARG;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK || n_seqs == 0) return r;
+  if (!q || !bounds || !table || !lens || !sel) return MEDA_ERR_INVALID_ARG;
+  if (!aligned16(bounds)) return MEDA_ERR_SHAPE;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  const meda_pages_config& c = pages->cfg;
+  SelectPagesParams a = {q, bounds, table, lens, sel, pages->status, lens_stride, n_seqs, c.n_kv_heads, pages->group, c.n_pages,
+                         c.max_seq_pages, pages->page_shift, keep, n_first, n_last};
+  const int cluster = select_pages_cluster(pages, n_seqs);
+  return with_select_kernel(pages, [&](auto kern) { return kern.launch(pages, a, cluster, as_stream(stream)); });
+}
+
+meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                                 const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
+                                 const int32_t* sel, int32_t keep, void* out, float* lse, void* stream) {
+  if (!pages || (sel && keep < 1)) return MEDA_ERR_INVALID_ARG;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK || n_seqs == 0) return r;
+  if (!q || !k_pages || !v_pages || !table || !lens || !out) return MEDA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return MEDA_ERR_SHAPE;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  const meda_pages_config& c = pages->cfg;
+  AttnParams a = {q, k_pages, v_pages, table, lens, sel, out, lse, pages->attn_partial, pages->attn_counters, pages->status,
+                  lens_stride, n_seqs, c.n_kv_heads, pages->group, c.n_pages, c.max_seq_pages, pages->page_shift, keep,
+                  1.4426950408889634f / sqrtf((float)c.head_dim)};
+  return with_attn_kernel(pages, [&](auto kern) { return kern.launch(pages, a, as_stream(stream)); });
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -1,0 +1,95 @@
+// Shared parts of the paged-cache kernels: the handle, and the block-wide prefix sums by which every block finds
+// its share of a ragged batch.  Lengths live on the device, so no launch can be sized by them: grids are fixed by
+// the GPU, every block reads all lengths (16 K at most, from L2) and takes an equal part of the work they add up to.
+#pragma once
+
+#include "meda_common.cuh"
+
+struct meda_pages {
+  meda_pages_config cfg;
+  int device = 0;
+  int sm_count = 0;
+  int group = 1;                       // query heads per KV head
+  int page_shift = 4;                  // log2(page_size)
+  int64_t launches = 0;
+  int64_t bytes = 0;
+  int* status = nullptr;               // device status word (first error wins)
+  unsigned long long* rope_freq = nullptr;   // [half] turns per position, as a 64-bit fraction
+  int* rope_axis = nullptr;            // [half]
+  float* attn_partial = nullptr;       // [blocks][2][group][head_dim + 2] softmax states of segments that cross blocks
+  unsigned int* attn_counters = nullptr;     // [max_seqs * n_kv_heads] arrivals per segment, zero between launches
+  int attn_blocks = 0;                 // blocks of the attention kernel that are resident at once
+};
+
+namespace meda {
+
+constexpr int kPagesMaxSeqs = 16384;
+constexpr int kPagesMaxSeqPages = 262144;
+
+// Exclusive prefix of `v` over a block of THREADS threads in thread order, and the block total.
+// `scratch` holds THREADS / 32 + 1 values.
+template <int THREADS, typename V>
+__device__ __forceinline__ V block_prefix(V v, V* scratch, V& total) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  V incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const V y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  __syncthreads();                      // previous users of scratch are done
+  if (lane == 31) scratch[warp] = incl;
+  __syncthreads();
+  V before = 0, all = 0;
+#pragma unroll
+  for (int x = 0; x < THREADS / 32; ++x) {
+    const V c = scratch[x];
+    before += x < warp ? c : 0;
+    all += c;
+  }
+  total = all;
+  return before + incl - v;
+}
+
+// A sequence's length as the kernels use it: out-of-range values are cut to the nearest valid one.
+__device__ __forceinline__ int clamped_len(const int32_t* lens, int stride, int i, int max_rows, bool& bad) {
+  const int len = lens[(size_t)i * stride];
+  bad |= len < 0 || len > max_rows;
+  return min(max(len, 0), max_rows);
+}
+
+// pre[0 .. n] (shared memory) <- exclusive prefix sums of units(length of sequence i).  A thread takes consecutive
+// sequences, so one block-wide scan serves any n.  Ends with a barrier.
+template <int THREADS, typename F>
+__device__ __forceinline__ void ragged_prefix(int n, int* pre, int* scratch, F units) {
+  const int per = (n + THREADS - 1) / THREADS;
+  const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
+  int sum = 0;
+  for (int i = lo; i < hi; ++i) {
+    const int u = units(i);
+    pre[i + 1] = u;
+    sum += u;
+  }
+  int total;
+  int run = block_prefix<THREADS>(sum, scratch, total);
+  for (int i = lo; i < hi; ++i) {
+    run += pre[i + 1];
+    pre[i + 1] = run;
+  }
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+}
+
+// Largest i in [0, n) with pre[i] <= x, for pre[0] = 0 <= x < pre[n]: the sequence unit x belongs to
+// (sequences without units are passed over).
+__device__ __forceinline__ int ragged_find(const int* pre, int n, int x) {
+  int lo = 0, hi = n;                   // pre[lo] <= x < pre[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pre[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+}  // namespace meda

@@ -224,3 +224,104 @@ class CompressionPass:
             out["counts"].append(torch.empty((wl.n_kv_heads, s), dtype=torch.int32).pin_memory())
             out["idx"].append(torch.empty((wl.n_kv_heads, s), dtype=torch.int32).pin_memory())
         return out
+
+
+class PagedDecoder:
+    """Decoding of many requests over their compressed caches, kept in one pool of pages.
+
+    Sequence `layer * max_requests + request` is one layer of one request, so a layer's batch is a run of
+    table rows.  `admit` moves what a CompressionPass left into pages, `begin_step` makes room for one row per layer
+    and active request, `attend` (once per layer) rotates and appends the new rows and attends, `release` gives
+    a request's pages back.  Everything runs on torch's current stream; nothing is copied to the host, so
+    begin_step and the layers' attend calls can be captured into a CUDA graph (the lengths live on the device).
+
+    `keep_pages` > 0: attention reads at most that many pages per sequence and KV head, the ones whose key
+    bounds promise the largest logits, the first and the last always among them."""
+
+    def __init__(self, wl: Workload, n_pages: int, max_requests: int, max_rows: int, page_size: int = 16,
+                 keep_pages: int = 0, n_first: int = 1, n_last: int = 2, rope_theta: float = 10000.0, rope_sections=None,
+                 rope_order: int = 0, rope_pairing: int = 0, device="cuda"):
+        L, R, hkv, d = wl.n_layers, int(max_requests), wl.n_kv_heads, wl.head_dim
+        self.wl, self.n_layers, self.max_requests = wl, L, R
+        self.keep_pages, self.n_first, self.n_last = int(keep_pages), n_first, n_last
+        width = -(-int(max_rows) // page_size)
+        self.pages = binding.Pages(n_q_heads=wl.n_q_heads, n_kv_heads=hkv, head_dim=d, dtype=wl.dtype, page_size=page_size,
+                                   n_pages=n_pages, max_seqs=L * R, max_seq_pages=width, rope_theta=rope_theta,
+                                   rope_sections=rope_sections, rope_order=rope_order, rope_pairing=rope_pairing)
+        i32 = dict(dtype=torch.int32, device=device)
+        dt = dict(dtype=wl.torch_dtype, device=device)
+        self.k_pages = torch.empty((n_pages, hkv, page_size, d), **dt)
+        self.v_pages = torch.empty((n_pages, hkv, page_size, d), **dt)
+        self.bounds = torch.empty((n_pages, hkv, 2, d), **dt) if self.keep_pages else None
+        self.table = torch.full((L * R, width), -1, **i32)
+        self.lens = torch.zeros(L * R, **i32)              # rows of every sequence
+        self.lens_before = torch.zeros(L * R, **i32)       # ... before the step in progress
+        self.free_pages = torch.arange(n_pages, **i32)
+        self.free_top = torch.zeros(1, **i32)
+        self.active = torch.zeros(R, **i32)                # 1: the request takes part in the next step
+        self._top_out = torch.zeros(1, **i32)
+        self._cu = torch.zeros(L * R + 1, **i32)
+        self._new_slots = torch.empty(L * R, dtype=torch.int64, device=device)
+        self._no_slots = torch.empty(0, dtype=torch.int64, device=device)
+        self.slots = torch.full((L, R), -1, dtype=torch.int64, device=device)
+        self.q_rot = torch.zeros((R, wl.n_q_heads, d), **dt)
+        self.sel = torch.empty((R, hkv, self.keep_pages), **i32) if self.keep_pages else None
+
+    def close(self):
+        self.pages.close()
+
+    def check(self):
+        """Synchronises and raises if a device-side error was recorded (a full pool among them)."""
+        self.pages.check()
+
+    def _move(self, new_lens, slots):
+        """Page tables for lens -> new_lens.  A change the pool cannot serve is recorded and changes nothing."""
+        self.pages.page_tables(self.lens, new_lens, self.free_pages, self.free_top, self._top_out, self.table, self._cu, slots)
+        self.free_top.copy_(self._top_out)
+
+    def admit(self, request: int, cp: CompressionPass):
+        """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back."""
+        L, R = self.n_layers, self.max_requests
+        self.release(request)
+        rows = cp.budgets[:, 0]
+        new_lens = self.lens.clone()
+        new_lens.view(L, R)[:, request] = rows
+        self._move(new_lens, self._no_slots)               # whole pages are stored: no slot map is needed
+        moved = self._cu[-1] > 0                           # stays 0 when the pool could not serve the request
+        self.lens.copy_(torch.where(moved, new_lens, self.lens))
+        held = torch.where(moved, rows, 0).to(torch.int32)
+        table = self.table.view(L, R, -1)[:, request].contiguous()
+        self.pages.page_store(cp.k_out, cp.v_out, held, table, self.k_pages, self.v_pages, self.bounds)
+        self.active[request:request + 1] = moved.to(torch.int32)
+
+    def release(self, request: int):
+        """Gives the request's pages back."""
+        new_lens = self.lens.clone()
+        new_lens.view(self.n_layers, self.max_requests)[:, request] = 0
+        self._move(new_lens, self._no_slots)
+        self.lens.copy_(new_lens)
+        self.active[request] = 0
+
+    def begin_step(self):
+        """Room for one more row in every layer of the active requests."""
+        L, R = self.n_layers, self.max_requests
+        self.lens_before.copy_(self.lens)
+        grow = self.active.repeat(L)
+        self._move(self.lens + grow, self._new_slots)
+        added = self._cu[1:] - self._cu[:-1]               # all 0 when the pool has run out: nothing is appended then
+        self.lens.copy_(self.lens + added)
+        at = self._cu[:-1].long().clamp(max=L * R - 1)
+        self.slots.copy_(torch.where(added > 0, self._new_slots[at], -1).view(L, R))
+
+    def attend(self, layer: int, q, k, v, positions, out, lse=None):
+        """One layer of the step: q [R][Hq][d], k, v [R][Hkv][d] (any token stride) of the new tokens, positions int32
+        [3][R]; out [R][Hq][d], lse fp32 [R][Hq].  Rows of requests that are not active attend to what they hold,
+        with the query of an earlier call; their outputs mean nothing."""
+        R = self.max_requests
+        rows = slice(layer * R, (layer + 1) * R)
+        table, lens = self.table[rows], self.lens[rows]
+        self.pages.rope_append(q, k, v, positions, self.slots[layer], self.q_rot, self.k_pages, self.v_pages)
+        if self.keep_pages:
+            self.pages.page_bounds(self.k_pages, table, self.lens_before[rows], lens, self.bounds)
+            self.pages.select_pages(self.q_rot, self.bounds, table, lens, self.n_first, self.n_last, self.sel)
+        self.pages.paged_attention(self.q_rot, self.k_pages, self.v_pages, table, lens, out, lse, sel=self.sel)
