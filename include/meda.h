@@ -239,7 +239,7 @@ typedef struct {
   int32_t dtype;                           /* meda_dtype of pools, queries, new rows and outputs */
   int32_t page_size;                       /* rows per page: 16, 32, 64, 128 or 256 */
   int32_t n_pages;                         /* pages in each pool */
-  int32_t max_seqs;                        /* most sequences of one call, <= 16384 */
+  int32_t max_seqs;                        /* most sequences of one call, <= 8192 */
   int32_t max_seq_pages;                   /* entries of a table row, <= 262144 */
   double rope_theta;                       /* base of the rotary frequencies, > 1 */
   int32_t rope_sections[3];                /* frequencies that follow the time, height and width axis; their sum is
@@ -251,7 +251,8 @@ typedef struct {
 } meda_pages_config;
 
 /* Validates the geometry and allocates scratch memory on the current device (the only allocating call).
- * max_seqs * max_seq_pages * page_size / 16 * n_kv_heads and n_pages * n_kv_heads * page_size stay below 2^31 and 2^40.
+ * max_seqs * max_seq_pages * page_size / 16 * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query
+ * heads per KV head in bf16 at head_dim 256 or in fp32; times up to four in fp32 at head_dim 256), n_pages * n_kv_heads * page_size below 2^40.
  * On failure *out is NULL and the status says why. */
 meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out);
 /* Frees the scratch memory.  The caller must have synchronised the streams that used it. */

@@ -291,14 +291,32 @@ class Context:
 
 ROPE_RUNS, ROPE_DEALT = 0, 1
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
-_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_NATIVE = None
+
+
+def load_native():
+    """Loads _pages.so (once): the paged calls' argument marshalling.  Raises if it has not been built."""
+    global _NATIVE
+    if _NATIVE is None:
+        import importlib.machinery
+        import importlib.util
+        path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_pages.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2502_17599_b200.build` "
+                               "(or __graft_entry__.build()); there is no fallback implementation")
+        loader = importlib.machinery.ExtensionFileLoader("_pages", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_pages", loader))
+        loader.exec_module(module)
+        _NATIVE = module
+    return _NATIVE
 
 
 class Pages:
     """Owns one meda_pages: the paged caches of many sequences (one layer of one request each) of one geometry.
     Method names and argument order follow include/meda.h; shapes are read from the tensors and checked
-    against the geometry.  Lengths are 1-D int32 tensors of any stride (`budgets[:, 0]` as it is).  The handle
-    belongs to the device that is current when it is made, and so do the tensors."""
+    against the geometry (ValueError).  Lengths are 1-D int32 tensors of any stride (`budgets[:, 0]` as it is).  The handle
+    belongs to the device that is current when it is made, and so do the tensors; without `stream` a call goes to
+    that device's current stream."""
 
     def __init__(self, *, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_seqs, max_seq_pages,
                  rope_theta=10000.0, rope_sections=None, rope_order=ROPE_RUNS, rope_pairing=ROPE_HALVES):
@@ -318,14 +336,17 @@ class Pages:
         self._h = handle.value
         self._lib = lib
         self._device = torch.cuda.current_device()
-        self._dtype = torch.float32 if f32 else torch.bfloat16
-        self._n_pages, self._width = int(n_pages), int(max_seq_pages)
-        self._hq, self._hkv, self._d = int(n_q_heads), int(n_kv_heads), int(head_dim)
-        self._pool = (self._n_pages, self._hkv, int(page_size), self._d)
-        self._bounds = (self._n_pages, self._hkv, 2, self._d)
+        native = load_native()
+        address = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
+        self._n = native.bind(self._h, self._device, f32, (n_pages, max_seq_pages, n_q_heads, n_kv_heads, page_size, head_dim),
+                              tuple(address(f"meda_{name}") for name in ("page_tables", "page_store", "page_bounds", "rope_append",
+                                                                         "select_pages", "paged_attention")))
+        self._native = native
 
     def close(self):
         if self._h is not None:
+            if hasattr(self, "_n"):
+                self._native.unbind(self._n)
             self._lib.meda_pages_destroy(self._h)
             self._h = None
 
@@ -342,123 +363,45 @@ class Pages:
         return int(self._lib.meda_pages_launch_count(self._h))
 
     def poll_status(self, stream=None) -> int:
-        return int(self._lib.meda_pages_poll_status(self._h, self._stream(stream)))
+        s = torch.cuda.current_stream(self._device) if stream is None else stream
+        return int(self._lib.meda_pages_poll_status(self._h, s.cuda_stream))
 
     def check(self, stream=None):
         _check(self.poll_status(stream), "device status")
 
-    def _stream(self, stream):
-        return (torch.cuda.current_stream(self._device) if stream is None else stream).cuda_stream
-
-    def _dense(self, t, shape, dtype, what):
-        """Address of a contiguous tensor of the handle's device with this type and shape."""
-        if t.dtype is not dtype or t.get_device() != self._device or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{self._device} is wanted, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
-
-    def _lens(self, t, what, n=None):
-        if t.dtype is not _I32 or t.get_device() != self._device or t.dim() != 1 or (n is not None and t.shape[0] != n):
-            raise ValueError(f"{what}: a 1-D int32 tensor{'' if n is None else f' of {n}'} on cuda:{self._device} is wanted, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
-
-    def _heads(self, t, n, heads, what):
-        """(address, token stride) of [n][heads][head_dim] rows that are dense inside a token."""
-        if t.dtype is not self._dtype or t.get_device() != self._device or t.shape != (n, heads, self._d):
-            raise ValueError(f"{what}: {self._dtype} of shape {(n, heads, self._d)} on cuda:{self._device} is wanted, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        st = t.stride()
-        if st[2] != 1 or (heads > 1 and st[1] != self._d):
-            raise ValueError(f"{what}: the heads of a token have to be dense, got strides {st}")
-        return t.data_ptr(), st[0] if n > 1 else 0
-
     def page_tables(self, lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, stream=None):
         """lens may be None (every sequence is new); an empty slots tensor: no slot map is wanted."""
-        n = new_lens.shape[0]
-        status = self._lib.meda_page_tables(
-            self._h, None if lens is None else self._lens(lens, "lens", n), 0 if lens is None else lens.stride(0),
-            self._lens(new_lens, "new_lens"), new_lens.stride(0), n, self._dense(free_pages, (self._n_pages,), _I32, "free_pages"),
-            self._dense(free_top, (1,), _I32, "free_top"), self._dense(free_top_out, (1,), _I32, "free_top_out"),
-            self._dense(table, (n, self._width), _I32, "table"), self._dense(cu_new, (n + 1,), _I32, "cu_new"),
-            self._dense(slots, (slots.shape[0],), _I64, "slots"), slots.shape[0], self._stream(stream))
+        status = self._native.page_tables(self._n, lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, stream)
         if status:
             _check(status, "meda_page_tables")
 
     def page_store(self, k, v, lens, table, k_pages, v_pages, bounds=None, stream=None):
         """k, v: [n_seqs][n_kv_heads][capacity][head_dim], rows of a head dense, the outer strides free but alike."""
-        n = lens.shape[0]
-        st = k.stride()
-        for t, what in ((k, "k"), (v, "v")):
-            if t.dtype is not self._dtype or t.get_device() != self._device or t.dim() != 4 or t.shape != k.shape or \
-                    t.shape[0] != n or t.shape[1] != self._hkv or t.shape[3] != self._d:
-                raise ValueError(f"{what}: {self._dtype} [{n}][{self._hkv}][capacity][{self._d}] on cuda:{self._device} is wanted, "
-                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-            if t.stride() != st or st[3] != 1 or (t.shape[2] > 1 and st[2] != self._d):
-                raise ValueError(f"{what}: rows have to be dense and k and v laid out alike, got strides {t.stride()}")
-        status = self._lib.meda_page_store(
-            self._h, k.data_ptr(), v.data_ptr(), st[0] if n > 1 else 0, st[1] if self._hkv > 1 else 0, k.shape[2], self._lens(lens, "lens"), lens.stride(0), n,
-            self._dense(table, (n, self._width), _I32, "table"), self._dense(k_pages, self._pool, self._dtype, "k_pages"),
-            self._dense(v_pages, self._pool, self._dtype, "v_pages"),
-            None if bounds is None else self._dense(bounds, self._bounds, self._dtype, "bounds"), self._stream(stream))
+        status = self._native.page_store(self._n, k, v, lens, table, k_pages, v_pages, bounds, stream)
         if status:
             _check(status, "meda_page_store")
 
     def page_bounds(self, k_pages, table, lens_from, lens, bounds, stream=None):
-        n = lens.shape[0]
-        if lens_from is not None and lens_from.stride() != lens.stride():
-            raise ValueError("lens_from and lens have to have the same stride")
-        status = self._lib.meda_page_bounds(
-            self._h, self._dense(k_pages, self._pool, self._dtype, "k_pages"), self._dense(table, (n, self._width), _I32, "table"),
-            None if lens_from is None else self._lens(lens_from, "lens_from", n), self._lens(lens, "lens"), lens.stride(0), n,
-            self._dense(bounds, self._bounds, self._dtype, "bounds"), self._stream(stream))
+        """lens_from: None, or of the same stride as lens."""
+        status = self._native.page_bounds(self._n, k_pages, table, lens_from, lens, bounds, stream)
         if status:
             _check(status, "meda_page_bounds")
 
     def rope_append(self, q, k, v, positions, slots, q_out, k_pages, v_pages, stream=None):
-        """q, k, v: [n_tokens][heads][head_dim] with any token stride; positions: int32 [3][n_tokens] or None."""
-        n = slots.shape[0]
-        k_ptr, k_st = self._heads(k, n, self._hkv, "k")
-        v_ptr, v_st = self._heads(v, n, self._hkv, "v")
-        q_ptr, q_st, out_ptr = None, 0, None
-        if q is not None:
-            q_ptr, q_st = self._heads(q, n, self._hq, "q")
-            out_ptr = self._dense(q_out, (n, self._hq, self._d), self._dtype, "q_out")
-        elif q_out is not None:
-            raise ValueError("q_out without q")
-        pos_ptr, axis_st = None, 0
-        if positions is not None:
-            if positions.dtype is not _I32 or positions.get_device() != self._device or positions.shape != (3, n) or \
-                    (n > 1 and positions.stride(1) != 1):
-                raise ValueError(f"positions: int32 [3][{n}] with dense axes on cuda:{self._device} is wanted, "
-                                 f"got {positions.dtype} {tuple(positions.shape)} on {positions.device}")
-            pos_ptr, axis_st = positions.data_ptr(), positions.stride(0)
-        status = self._lib.meda_rope_append(
-            self._h, q_ptr, q_st, k_ptr, k_st, v_ptr, v_st, pos_ptr, axis_st, self._dense(slots, (n,), _I64, "slots"), n, out_ptr,
-            self._dense(k_pages, self._pool, self._dtype, "k_pages"), self._dense(v_pages, self._pool, self._dtype, "v_pages"),
-            self._stream(stream))
+        """q, k, v: [n_tokens][heads][head_dim] with any token stride (q and q_out may be None); positions: int32
+        [3][n_tokens] or None."""
+        status = self._native.rope_append(self._n, q, k, v, positions, slots, q_out, k_pages, v_pages, stream)
         if status:
             _check(status, "meda_rope_append")
 
     def select_pages(self, q, bounds, table, lens, n_first, n_last, sel, stream=None):
         """sel: int32 [n_seqs][n_kv_heads][keep]."""
-        n, keep = lens.shape[0], sel.shape[-1]
-        status = self._lib.meda_select_pages(
-            self._h, self._dense(q, (n, self._hq, self._d), self._dtype, "q"), self._dense(bounds, self._bounds, self._dtype, "bounds"),
-            self._dense(table, (n, self._width), _I32, "table"), self._lens(lens, "lens"), lens.stride(0), n, n_first, n_last, keep,
-            self._dense(sel, (n, self._hkv, keep), _I32, "sel"), self._stream(stream))
+        status = self._native.select_pages(self._n, q, bounds, table, lens, n_first, n_last, sel, stream)
         if status:
             _check(status, "meda_select_pages")
 
     def paged_attention(self, q, k_pages, v_pages, table, lens, out, lse=None, sel=None, stream=None):
-        n = lens.shape[0]
-        shape = (n, self._hq, self._d)
-        keep = 0 if sel is None else sel.shape[-1]
-        status = self._lib.meda_paged_attention(
-            self._h, self._dense(q, shape, self._dtype, "q"), self._dense(k_pages, self._pool, self._dtype, "k_pages"),
-            self._dense(v_pages, self._pool, self._dtype, "v_pages"), self._dense(table, (n, self._width), _I32, "table"),
-            self._lens(lens, "lens"), lens.stride(0), n, None if sel is None else self._dense(sel, (n, self._hkv, keep), _I32, "sel"),
-            keep, self._dense(out, shape, self._dtype, "out"), None if lse is None else self._dense(lse, shape[:2], _F32, "lse"),
-            self._stream(stream))
+        """sel: of select_pages, or None for all pages."""
+        status = self._native.paged_attention(self._n, q, k_pages, v_pages, table, lens, out, lse, sel, stream)
         if status:
             _check(status, "meda_paged_attention")

@@ -1,4 +1,5 @@
-"""Builds libmeda.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libmeda.so (the C-ABI CUDA library, nvcc for sm_100a) and _pages.so (the paged calls' argument
+marshalling, g++ with torch's headers) in-tree."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libmeda.so")
+BINDING_PATH = os.path.join(HERE, "_pages.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -39,8 +41,42 @@ def is_stale() -> bool:
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
+def binding_sources() -> list[str]:
+    return [os.path.join(CSRC, "pages_binding.cpp")]
+
+
+def binding_is_stale() -> bool:
+    if not os.path.exists(BINDING_PATH):
+        return True
+    t = os.path.getmtime(BINDING_PATH)
+    header = os.path.join(os.path.dirname(HERE), "include", "meda.h")
+    return any(os.path.getmtime(p) > t for p in binding_sources() + [header])
+
+
+def _binding_command() -> list[str]:
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))
+    cxx = shutil.which("g++")
+    if cxx is None:
+        raise RuntimeError("g++ not found: cannot build _pages.so")
+    abi = f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"
+    return [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", abi,
+            "-I" + os.path.join(base, "include"), "-I" + os.path.join(base, "include", "torch", "csrc", "api", "include"),
+            "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_paths()["include"],
+            *binding_sources(), "-o", BINDING_PATH, "-L" + os.path.join(base, "lib"), "-Wl,-rpath," + os.path.join(base, "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | None = None) -> str:
-    """Compiles the library if it is missing or older than its sources; returns its path."""
+    """Compiles the library and the paged calls' marshalling where they are missing or older than their sources;
+    returns the library's path."""
+    if force or binding_is_stale():
+        res = subprocess.run(_binding_command(), capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
     if not force and not is_stale():
         return LIB_PATH
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"

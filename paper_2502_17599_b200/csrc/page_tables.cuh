@@ -1,7 +1,7 @@
 // Page tables, slot maps and the free list for one change of lengths, in one launch.
 //
 // Every block computes the three prefix sums (pages taken, pages given back, new rows) over all sequences into its
-// shared memory: 16 K sequences are 128 KB of lengths from L2, and doing it in every block costs no more time than doing it
+// shared memory: 8 K sequences are 64 KB of lengths from L2, and doing it in every block costs no more time than doing it
 // in one, while it saves a second launch and the scratch between the two.  After that each entry written is a
 // function of its index alone: the j-th page taken is the j-th page given back, or the free list's entry behind
 // its front; a row's slot follows from its page.  No entry that is read is written in the same launch (the table

@@ -29,6 +29,19 @@ namespace meda {
 
 constexpr int kAttTile = 16;             // rows per tile; a page holds whole tiles
 
+// x / d for 0 <= x < 2^31 by a multiplication: with 2^s < d < 2^(s+1), mul = ceil(2^(32+s) / d) is off by less than d / 2^(32+s),
+// which x below 2^31 cannot turn into a whole unit; powers of two are shifts.
+struct InvariantDiv {
+  unsigned mul = 0;
+  int shift = 0;
+  __host__ void set(unsigned d) {
+    shift = 0;
+    while ((2ull << shift) <= d) ++shift;                      // floor(log2(d))
+    mul = (d & (d - 1)) == 0 ? 0u : (unsigned)(((1ull << (32 + shift)) + d - 1) / d);
+  }
+  __device__ __forceinline__ int of(int x) const { return (mul ? (int)__umulhi((unsigned)x, mul) : x) >> shift; }
+};
+
 struct AttnParams {
   const void* q;
   const void* k;
@@ -43,6 +56,7 @@ struct AttnParams {
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep;
   float scale_log2;                      // log2(e) / sqrt(head_dim)
+  InvariantDiv heads_div, grid_div;      // by the segments of a sequence, by the blocks of the launch
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -51,6 +65,12 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {              // 2^x, off by 2^-22 at most; 0 for x below -126
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
@@ -89,25 +109,24 @@ struct AttnTileBf16 {
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[y][x][n][e] = 0.f;
   }
+  // Rows behind the nv that count are not read: their lanes read the last one that does, and its probability is 0 (its
+  // value cannot add anything the row itself does not: 0 * NaN is NaN in both).
   __device__ __forceinline__ void load_k(const T* rows, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const bool on = t * 8 + r < nv;
+      const T* src = rows + min(t * 8 + r, nv - 1) * D + c * 8;
 #pragma unroll
-      for (int x = 0; x < KC; ++x)
-        k[t][x] = on ? load_stream(reinterpret_cast<const uint4*>(rows + (t * 8 + r) * D + x * 32 + c * 8)) : make_uint4(0, 0, 0, 0);
+      for (int x = 0; x < KC; ++x) k[t][x] = load_stream(reinterpret_cast<const uint4*>(src + x * 32));
     }
   }
   __device__ __forceinline__ void load_v(const T* rows, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int row = 2 * c + (t & 1) + (t >> 1) * 8;
-      const bool on = row < nv;
+      const T* src = rows + min(2 * c + (t & 1) + (t >> 1) * 8, nv - 1) * D + r * 8;
 #pragma unroll
-      for (int y = 0; y < VC; ++y)
-        v[t][y] = on ? load_stream(reinterpret_cast<const uint4*>(rows + row * D + y * 64 + r * 8)) : make_uint4(0, 0, 0, 0);
+      for (int y = 0; y < VC; ++y) v[t][y] = load_stream(reinterpret_cast<const uint4*>(src + y * 64));
     }
   }
   // logits of the tile in k, in the log2 domain: s[t][0..1] head r, rows t * 8 + 2c, + 1; s[t][2..3] head r + 8
@@ -122,10 +141,14 @@ struct AttnTileBf16 {
         mma_bf16(odd, q[0][x].z, NH > 1 ? q[NH - 1][x].z : 0u, q[0][x].w, NH > 1 ? q[NH - 1][x].w : 0u, k[t][x].z, k[t][x].w);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[t][e] = (even[e] + odd[e]) * scale_log2;
-        if (t * 8 + 2 * c + (e & 1) >= nv) s[t][e] = -INFINITY;
-      }
+      for (int e = 0; e < 4; ++e) s[t][e] = (even[e] + odd[e]) * scale_log2;
+    }
+    if (nv < kAttTile) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t * 8 + 2 * c + (e & 1) >= nv) s[t][e] = -INFINITY;
     }
   }
   __device__ __forceinline__ void attend(float (&s)[2][4], int lane) {
@@ -139,7 +162,7 @@ struct AttnTileBf16 {
       const float mn = fmaxf(m[n], top);
       const float ref = mn == -INFINITY ? 0.f : mn;
       if (__any_sync(0xffffffffu, mn > m[n])) {                // the maximum moved: bring the sums to the new one
-        const float f = exp2f(m[n] - ref);
+        const float f = exp2_fast(m[n] - ref);
         m[n] = mn;
         l[n] *= f;
         const float f0 = __shfl_sync(0xffffffffu, f, 8 * c), f1 = __shfl_sync(0xffffffffu, f, 8 * c + 4);   // heads 2c, 2c + 1
@@ -155,7 +178,7 @@ struct AttnTileBf16 {
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float p0 = exp2f(s[t][2 * n] - ref), p1 = exp2f(s[t][2 * n + 1] - ref);
+        const float p0 = exp2_fast(s[t][2 * n] - ref), p1 = exp2_fast(s[t][2 * n + 1] - ref);
         l[n] += p0 + p1;
         const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
         const __nv_bfloat162 l2 = __floats2bfloat162_rn(p0 - __low2float(h2), p1 - __high2float(h2));
@@ -230,19 +253,19 @@ struct AttnTileF32 {
     m = -INFINITY;
     l = 0.f;
   }
+  // Rows r0 .. r0 + 3 of the tile; behind the last of nv that one again (see AttnTileBf16::load_k).
   __device__ __forceinline__ static void load_rows(float (&x)[B][E], const T* rows, int r0, int nv, int lane) {
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-      const bool on = r0 + b < nv;
-      const T* src = rows + (r0 + b) * D + lane * E;
+      const T* src = rows + min(r0 + b, nv - 1) * D + lane * E;
       if constexpr (E == 2) {
-        const float2 t = on ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
+        const float2 t = *reinterpret_cast<const float2*>(src);
         x[b][0] = t.x;
         x[b][1] = t.y;
       } else {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
-          const float4 t = on ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 t = *reinterpret_cast<const float4*>(src + e);
           x[b][e] = t.x;
           x[b][e + 1] = t.y;
           x[b][e + 2] = t.z;
@@ -273,7 +296,7 @@ struct AttnTileF32 {
     mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, 2));
     mn = fmaxf(mn, m);
     const float ref = mn == -INFINITY ? 0.f : mn;
-    const float pr = exp2f(s - ref), f = exp2f(m - ref);
+    const float pr = exp2_fast(s - ref), f = exp2_fast(m - ref);
     float sum = pr;
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -320,14 +343,25 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* dst, const 
   *reinterpret_cast<uint2*>(dst) = w;
 }
 
-// Floats of one softmax state in scratch: values of every head, then maxima, then sums (padded to 16 bytes).
+// Floats of one softmax state in scratch: values of every head, then (maximum, sum) of every head.
 __host__ __device__ inline int attn_state_floats(int heads, int d) { return heads * (d + 4); }
-// Shared memory: prefix of tiles, and the larger of the warps' states and the weights of a join.
-__host__ __device__ inline int attn_prefix_floats(int n_seqs) { return (n_seqs + 1 + 3) / 4 * 4; }
-__host__ __device__ inline int attn_merge_floats(int warps, int heads, int d, int blocks) {
-  const int states = warps * heads * (d + 4 + 2), join = blocks * heads + 2 * heads;
-  return states > join ? states : join;
+// Shared memory: prefix of tiles and row counts, and two sets of the warps' states.
+__host__ __device__ inline int attn_prefix_floats(int n_seqs) { return (2 * n_seqs + 1 + 3) / 4 * 4; }
+__host__ __device__ constexpr int attn_merge_floats(int warps, int heads, int d) { return warps * heads * (d + 4 + 2); }
+
+// a / b for 0 <= a < 2^31, b > 0 and a quotient below 2^20: the fp32 estimate is off by one at most.
+__device__ __forceinline__ int div_small(int a, int b) {
+  int q = (int)((float)a * __frcp_rn((float)b));
+  const int r = a - q * b;
+  q -= r < 0;
+  q += r >= b;
+  return q;
 }
+
+// One crossing segment of a block: its state waits in scratch until the block's tiles are done.
+struct AttnPending {
+  int seg0, seg1, seq, sh, any;
+};
 
 template <typename Tile, int D, int W>
 __global__ void __launch_bounds__(W * 32, 1)
@@ -336,13 +370,14 @@ paged_attention_kernel(AttnParams p) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int HP = Tile::kHeads;
   constexpr int LD = D + 4;
+  constexpr int kStates = attn_merge_floats(W, HP, D);
   extern __shared__ __align__(16) float att_smem[];
   __shared__ int scratch[W + 1];
-  __shared__ int s_last;
-  int* pre = reinterpret_cast<int*>(att_smem);
-  float* sm_m = att_smem + attn_prefix_floats(p.n_seqs);       // [W][HP]
-  float* sm_l = sm_m + W * HP;                                 // [W][HP]
-  float* sm_o = sm_l + W * HP;                                 // [W][HP][LD]
+  __shared__ unsigned int s_arrived[2];
+  __shared__ AttnPending pend[2];                              // the segment that began before the block, the one that goes on behind it
+  int* pre = reinterpret_cast<int*>(att_smem);                 // [n + 1] tiles before sequence i
+  int* rows_of = pre + p.n_seqs + 1;                           // [n] rows of sequence i
+  float* merge = att_smem + attn_prefix_floats(p.n_seqs);      // two sets of [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int max_rows = p.width << p.page_shift, page_size = 1 << p.page_shift;
   const int tile_shift = p.page_shift - 4;                     // log2(tiles per page)
@@ -352,39 +387,38 @@ paged_attention_kernel(AttnParams p) {
   const int state_floats = attn_state_floats(state_heads, D);
   const int n_q_heads = p.n_heads * p.group;
 
+  if (threadIdx.x < 2) pend[threadIdx.x].any = 0;
   ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;
     const int len = clamped_len(p.lens, p.lens_stride, i, max_rows, bad);
     if (bad && blockIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
+    rows_of[i] = len;
     if (!p.sel) return (len + kAttTile - 1) / kAttTile;
     return min(p.keep, (len + page_size - 1) >> p.page_shift) << tile_shift;
   });
 
-  // sequences without rows
-  for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
-    if (pre[i] == pre[i + 1]) {
-      for (int x = threadIdx.x; x < n_q_heads * D / 4; x += W * 32)
-        store4<T>(static_cast<T*>(p.out) + (size_t)i * n_q_heads * D + x * 4, make_float4(0.f, 0.f, 0.f, 0.f));
-      if (p.lse)
-        for (int h = threadIdx.x; h < n_q_heads; h += W * 32) p.lse[(size_t)i * n_q_heads + h] = -INFINITY;
-    }
-
-  const long long total = (long long)pre[p.n_seqs] * H;
-  const long long C = min((long long)gridDim.x, (total + W - 1) / W);        // blocks with work: a tile per warp at least
-  if ((long long)blockIdx.x >= C) return;
-  const long long t0 = total * blockIdx.x / C, t1 = total * (blockIdx.x + 1) / C;
+  // Block b takes base tiles, the first `extra` blocks one more.  (All tile counts stay below 2^31: see meda_pages_create.)
+  const int total = pre[p.n_seqs] * H;
+  // blocks with work: with few tiles one per segment, more where that leaves a warp more than one
+  const int C = min((int)gridDim.x, min(total, max((total + W - 1) / W, p.n_seqs * H)));
+  const int base = C == (int)gridDim.x ? p.grid_div.of(total) : (C > 0 ? div_small(total, C) : 0), extra = total - base * C;
+  auto block_start = [&](int b) { return base * b + min(b, extra); };
+  auto block_of = [&](int x) {
+    return x < extra * (base + 1) ? div_small(x, base + 1) : extra + div_small(x - extra * (base + 1), base);
+  };
+  const bool has_work = (int)blockIdx.x < C;
+  const int t0 = has_work ? block_start(blockIdx.x) : 0, t1 = has_work ? block_start(blockIdx.x + 1) : 0;
 
   // a tile's first row in the pools and the number of its rows that count (0: nothing to read)
-  auto lookup = [&](long long x, long long& row, int& nv) {
+  auto lookup = [&](int x, long long& row, int& nv) {
     row = 0;
     nv = 0;
     if (x >= t1) return;
-    const int i = ragged_find(pre, p.n_seqs, (int)(x / H));
+    const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(x));
     const int tiles = pre[i + 1] - pre[i];
-    const int local = (int)(x - (long long)pre[i] * H);
-    const int sh = local / tiles, tile = local - sh * tiles, g = sh / chunks;
-    bool bad = false;
-    const int len = clamped_len(p.lens, p.lens_stride, i, max_rows, bad);
+    const int local = x - pre[i] * H;
+    const int sh = div_small(local, tiles), tile = local - sh * tiles, g = chunks == 1 ? sh : sh / chunks;
+    const int len = rows_of[i];
     int col = tile >> tile_shift;
     const int r0 = (tile & ((1 << tile_shift) - 1)) * kAttTile;
     bool ok = true;
@@ -406,164 +440,207 @@ paged_attention_kernel(AttnParams p) {
     }
   };
 
-  // lane y holds the look-up of the warp's y-th tile from here, and of the 32 tiles after those
+  int seq = 0, sh = 0, seg0 = 0;
+  if (has_work) {
+    const int row0 = p.heads_div.of(t0);
+    seq = ragged_find(pre, p.n_seqs, row0);
+    sh = div_small(t0 - pre[seq] * H, pre[seq + 1] - pre[seq]);
+    seg0 = pre[seq] * H + sh * (pre[seq + 1] - pre[seq]);
+  }
   const T* kp = static_cast<const T*>(p.k);
   const T* vp = static_cast<const T*>(p.v);
-  long long x = t0 + warp;
-  long long row_now, row_next;
-  int nv_now, nv_next;
-  lookup(x + (long long)lane * W, row_now, nv_now);
-  lookup(x + (long long)(32 + lane) * W, row_next, nv_next);
-  int at = 0;
   Tile tile;
-  long long row = __shfl_sync(0xffffffffu, row_now, 0);
-  int nv = __shfl_sync(0xffffffffu, nv_now, 0);
-  if constexpr (kBf16) {
-    tile.load_k(kp + row * D, nv, lane);
-    tile.load_v(vp + row * D, nv, lane);
-  } else {
-    tile.load_rows(tile.kx[0], kp + row * D, 0, nv, lane);
-    tile.load_rows(tile.vx[0], vp + row * D, 0, nv, lane);
-  }
+  auto begin_segment = [&] {
+    const int g = chunks == 1 ? sh : sh / chunks, h0 = (sh - g * chunks) * HP;
+    tile.begin(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), lane);
+  };
+  if (has_work) begin_segment();
 
-  int seq = ragged_find(pre, p.n_seqs, (int)(t0 / H));
-  int sh = (int)(t0 - (long long)pre[seq] * H) / (pre[seq + 1] - pre[seq]);
-  long long seg0 = (long long)pre[seq] * H + (long long)sh * (pre[seq + 1] - pre[seq]);
+  // One iteration works on tile x, whose keys and values are in registers, and fetches tile x + W; the first one only
+  // fetches.  Lane y holds the look-up of tile y of the 32 the warp is going through; the next 32 are looked up half
+  // way through them.
+  int x = t0 + warp - W, at = -1, buffer = 0, nv = 0;
+  long long row = 0, row_now = 0, row_next = 0;
+  int nv_now = 0, nv_next = 0;
+  bool worked = false, crossing = false;
   while (seg0 < t1) {
-    const int tiles = pre[seq + 1] - pre[seq];
-    const long long seg1 = seg0 + tiles;
-    const long long end = min(seg1, t1);
-    const int g = sh / chunks, h0 = (sh % chunks) * HP;
-    const int heads = min(HP, p.group - h0);
-    const size_t first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
-    tile.begin(static_cast<const T*>(p.q) + first_head * D, heads, lane);
-
-    while (x < end) {
-      // where the warp's next tile lies
-      ++at;
-      if (at == 32) {
+    ++at;
+    if (at == 32) {
+      row_now = row_next;
+      nv_now = nv_next;
+      at = 0;
+    }
+    if (at == 16 || x < t0) {
+      lookup(x + (at == 16 ? 17 : 1) * W + lane * W, row_next, nv_next);
+      if (at != 16) {
         row_now = row_next;
         nv_now = nv_next;
-        at = 0;
-        lookup(x + (long long)(33 + lane) * W, row_next, nv_next);
       }
-      const long long row_after = __shfl_sync(0xffffffffu, row_now, at);
-      const int nv_after = __shfl_sync(0xffffffffu, nv_now, at);
-      if constexpr (kBf16) {
-        float s[2][4];
-        tile.logits(s, p.scale_log2, nv, lane);
-        tile.load_k(kp + row_after * D, nv_after, lane);
-        if (nv > 0) tile.attend(s, lane);
-        tile.load_v(vp + row_after * D, nv_after, lane);
-      } else {
+    }
+    const long long row_after = __shfl_sync(0xffffffffu, row_now, at);
+    const int nv_after = __shfl_sync(0xffffffffu, nv_now, at);
+    if constexpr (kBf16) {
+      float s[2][4];
+      if (nv > 0) tile.logits(s, p.scale_log2, nv, lane);
+      if (nv_after > 0) tile.load_k(kp + row_after * D, nv_after, lane);
+      if (nv > 0) tile.attend(s, lane);
+      if (nv_after > 0) tile.load_v(vp + row_after * D, nv_after, lane);
+    } else {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const T* nk = b < 3 ? kp + row * D : kp + row_after * D;
-          const T* nvp = b < 3 ? vp + row * D : vp + row_after * D;
-          const int r0 = b < 3 ? 4 * (b + 1) : 0, n = b < 3 ? nv : nv_after;
-          tile.load_rows(tile.kx[(b + 1) & 1], nk, r0, n, lane);
-          tile.load_rows(tile.vx[(b + 1) & 1], nvp, r0, n, lane);
-          if (4 * b < nv) tile.rows4(b & 1, 4 * b, nv, p.scale_log2, lane);
+      for (int b = 0; b < 4; ++b) {
+        const int r0 = b < 3 ? 4 * (b + 1) : 0, n = b < 3 ? nv : nv_after;
+        if (r0 < n) {
+          tile.load_rows(tile.kx[(b + 1) & 1], kp + (b < 3 ? row : row_after) * D, r0, n, lane);
+          tile.load_rows(tile.vx[(b + 1) & 1], vp + (b < 3 ? row : row_after) * D, r0, n, lane);
+        }
+        if (4 * b < nv) tile.rows4(b & 1, 4 * b, nv, p.scale_log2, lane);
+      }
+    }
+    worked |= x >= t0;
+    row = row_after;
+    nv = nv_after;
+    x += W;
+
+    while (seg0 < t1 && x >= min(seg0 + pre[seq + 1] - pre[seq], t1)) {
+      const int seg1 = seg0 + pre[seq + 1] - pre[seq];
+      const int g = chunks == 1 ? sh : sh / chunks, h0 = (sh - g * chunks) * HP;
+      const int heads = min(HP, p.group - h0);
+      const size_t first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
+      // ---- the warps' states of this segment, joined in warp order.  The buffers alternate, so that one barrier per
+      // segment is enough.  A warp without tiles leaves a maximum of -inf, a sum of 0 and no values; nobody reads those.
+      float* sm_m = merge + buffer * kStates;
+      float* sm_l = sm_m + W * HP;
+      float* sm_o = sm_l + W * HP;
+      buffer ^= 1;
+      if (worked) tile.put(sm_m + warp * HP, sm_l + warp * HP, sm_o + warp * HP * LD, LD, heads, lane);
+      else if (lane < HP) {
+        sm_m[warp * HP + lane] = -INFINITY;
+        sm_l[warp * HP + lane] = 0.f;
+      }
+      __syncthreads();
+      const bool whole = seg0 >= t0 && seg1 <= t1;
+      const int slot = seg0 < t0 ? 0 : 1;
+      float* state = p.partial + ((size_t)blockIdx.x * 2 + slot) * state_floats;
+      for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
+        const int h = e / (D / 4), d = (e % (D / 4)) * 4;
+        float mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * HP + h]);
+        float ll = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int w = 0; w < W; ++w) {
+          const float mw = sm_m[w * HP + h], lw = sm_l[w * HP + h];
+          if (mw != -INFINITY || lw != 0.f) {                    // (a sum that is NaN has a maximum of -inf when all logits are)
+            const float f = exp2_fast(mw - mm);
+            const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * HP + h) * LD + d);
+            ll = fmaf(f, lw, ll);
+            acc.x = fmaf(f, y.x, acc.x);
+            acc.y = fmaf(f, y.y, acc.y);
+            acc.z = fmaf(f, y.z, acc.z);
+            acc.w = fmaf(f, y.w, acc.w);
+          }
+        }
+        if (whole) {
+          const float inv = ll == 0.f ? 0.f : 1.f / ll;
+          store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+          if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
+        } else {
+          *reinterpret_cast<float4*>(state + h * D + d) = acc;
+          if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
         }
       }
-      row = row_after;
-      nv = nv_after;
-      x += W;
+      if (!whole) {
+        crossing = true;
+        if (threadIdx.x == 0) pend[slot] = {seg0, seg1, seq, sh, 1};
+      }
+      // next segment with tiles
+      seg0 = seg1;
+      if (++sh == H) {
+        sh = 0;
+        do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
+      }
+      if (seg0 < t1) begin_segment();
+      worked = false;
+    }
+  }
+
+  // sequences without rows
+  for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
+    if (pre[i] == pre[i + 1]) {
+      for (int e = threadIdx.x; e < n_q_heads * D / 4; e += W * 32)
+        store4<T>(static_cast<T*>(p.out) + (size_t)i * n_q_heads * D + e * 4, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (p.lse)
+        for (int h = threadIdx.x; h < n_q_heads; h += W * 32) p.lse[(size_t)i * n_q_heads + h] = -INFINITY;
     }
 
-    // ---- the warps' states of this segment, joined in warp order
-    tile.put(sm_m + warp * HP, sm_l + warp * HP, sm_o + warp * HP * LD, LD, heads, lane);
-    __syncthreads();
-    const bool whole = seg0 >= t0 && seg1 <= t1;
-    float* state = p.partial + ((size_t)blockIdx.x * 2 + (seg0 < t0 ? 0 : 1)) * state_floats;
+  // ---- segments that cross the block's borders: the block that arrives last joins all states, in block order
+  if (!crossing) return;
+  __syncthreads();                                             // the states are written ...
+  if (threadIdx.x == 0) {
+    __threadfence();                                           // ... and visible before the arrival is
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+      if (pend[y].any) s_arrived[y] = atomicAdd(p.counters + (size_t)pend[y].seq * H + pend[y].sh, 1u);
+    __threadfence();
+  }
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const AttnPending pd = pend[y];
+    if (!pd.any) continue;
+    const int c0 = block_of(pd.seg0), parts = block_of(pd.seg1 - 1) - c0 + 1;
+    if (s_arrived[y] != (unsigned)(parts - 1)) continue;
+    const int g = chunks == 1 ? pd.sh : pd.sh / chunks, h0 = (pd.sh - g * chunks) * HP;
+    const int heads = min(HP, p.group - h0);
+    const size_t first_head = (size_t)pd.seq * n_q_heads + (size_t)g * p.group + h0;
+    // states: the segment begins inside the first block (slot 1) and before all others (slot 0)
+    const float* first = p.partial + ((size_t)c0 * 2 + 1) * state_floats;
+    const float* rest = p.partial + (size_t)c0 * 2 * state_floats;
     for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
       const int h = e / (D / 4), d = (e % (D / 4)) * 4;
-      float mm = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * HP + h]);
-      const float ref = mm == -INFINITY ? 0.f : mm;
-      float ll = 0.f;
+      float mm = -INFINITY, ll = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      constexpr int kBatch = 8;
+      for (int z0 = 0; z0 < parts; z0 += kBatch) {
+        float2 ml[kBatch];
+        float4 o[kBatch];
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float f = exp2f(sm_m[w * HP + h] - ref);
-        const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * HP + h) * LD + d);
-        ll = fmaf(f, sm_l[w * HP + h], ll);
-        acc.x = fmaf(f, y.x, acc.x);
-        acc.y = fmaf(f, y.y, acc.y);
-        acc.z = fmaf(f, y.z, acc.z);
-        acc.w = fmaf(f, y.w, acc.w);
-      }
-      if (whole) {
-        const float inv = ll == 0.f ? 0.f : 1.f / ll;
-        store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-        if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
-      } else {
-        *reinterpret_cast<float4*>(state + h * D + d) = acc;
-        if (d == 0) {
-          state[state_heads * D + h] = mm;
-          state[state_heads * D + state_heads + h] = ll;
-        }
-      }
-    }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      const int c0 = (int)(((seg0 + 1) * C + total - 1) / total - 1), c1 = (int)((seg1 * C + total - 1) / total - 1);
-      const int parts = c1 - c0 + 1;
-      unsigned int* counter = p.counters + (size_t)seq * H + sh;
-      if (threadIdx.x == 0) s_last = atomicAdd(counter, 1u) == (unsigned)(parts - 1);
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        // state of part y: the first block's segment starts inside it (slot 1) unless it starts exactly at its border too
-        auto part_state = [&](int y) {
-          const long long b0 = total * (c0 + y) / C;
-          return p.partial + ((size_t)(c0 + y) * 2 + (seg0 < b0 ? 0 : 1)) * state_floats;
-        };
-        float* weight = sm_m;                                  // [parts][heads]
-        for (int h = warp; h < heads; h += W) {
-          float mm = -INFINITY;
-          for (int y = lane; y < parts; y += 32) mm = fmaxf(mm, __ldcg(part_state(y) + state_heads * D + h));
-          mm = warp_max(mm);
-          const float ref = mm == -INFINITY ? 0.f : mm;
-          float ll = 0.f;
-          for (int y = lane; y < parts; y += 32) {
-            const float* st = part_state(y) + state_heads * D + h;
-            const float f = exp2f(__ldcg(st) - ref);
-            weight[y * heads + h] = f;
-            ll = fmaf(f, __ldcg(st + state_heads), ll);
+        for (int z = 0; z < kBatch; ++z) {
+          const float* st = z0 + z == 0 ? first : rest + (size_t)(z0 + z) * 2 * state_floats;
+          ml[z] = make_float2(-INFINITY, 0.f);
+          o[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (z0 + z < parts) {
+            ml[z] = __ldcg(reinterpret_cast<const float2*>(st + state_heads * D + 2 * h));
+            o[z] = __ldcg(reinterpret_cast<const float4*>(st + h * D + d));
           }
-          ll = warp_sum(ll);
-          const float inv = ll == 0.f ? 0.f : 1.f / ll;
-          for (int y = lane; y < parts; y += 32) weight[y * heads + h] *= inv;
-          if (p.lse && lane == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
-          const int h = e / (D / 4), d = (e % (D / 4)) * 4;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-          for (int y = 0; y < parts; ++y) {
-            const float4 z = __ldcg(reinterpret_cast<const float4*>(part_state(y) + h * D + d));
-            const float f = weight[y * heads + h];
-            acc.x = fmaf(f, z.x, acc.x);
-            acc.y = fmaf(f, z.y, acc.y);
-            acc.z = fmaf(f, z.z, acc.z);
-            acc.w = fmaf(f, z.w, acc.w);
-          }
-          store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, acc);
+        float mn = mm;
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) mn = fmaxf(mn, ml[z].x);
+        const float ref = mn == -INFINITY ? 0.f : mn;
+        const float f0 = exp2_fast(mm - ref);
+        ll *= f0;
+        acc.x *= f0;
+        acc.y *= f0;
+        acc.z *= f0;
+        acc.w *= f0;
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) {
+          const float f = exp2_fast(ml[z].x - ref);
+          ll = fmaf(f, ml[z].y, ll);
+          acc.x = fmaf(f, o[z].x, acc.x);
+          acc.y = fmaf(f, o[z].y, acc.y);
+          acc.z = fmaf(f, o[z].z, acc.z);
+          acc.w = fmaf(f, o[z].w, acc.w);
         }
-        if (threadIdx.x == 0) *counter = 0u;
+        mm = mn;
       }
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+      store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
     }
-    // next segment with tiles
-    seg0 = seg1;
-    if (++sh == H) {
-      sh = 0;
-      do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
-    }
-    __syncthreads();                                           // the states' shared memory is written again
+    if (threadIdx.x == 0) p.counters[(size_t)pd.seq * H + pd.sh] = 0u;
   }
 }
 

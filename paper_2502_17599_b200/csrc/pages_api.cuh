@@ -50,9 +50,7 @@ meda_status pages_batch_ok(const meda_pages* p, int32_t n_seqs, int32_t lens_str
 template <typename Tile, int D, int W>
 struct AttnKernel {
   static constexpr auto kernel = paged_attention_kernel<Tile, D, W>;
-  static size_t smem(int n_seqs, int blocks) {
-    return (size_t)(attn_prefix_floats(n_seqs) + attn_merge_floats(W, Tile::kHeads, D, blocks)) * 4;
-  }
+  static size_t smem(int n_seqs) { return (size_t)(attn_prefix_floats(n_seqs) + 2 * attn_merge_floats(W, Tile::kHeads, D)) * 4; }
   // Blocks that are resident at once, with the shared memory of the largest batch.
   static meda_status prepare(meda_pages* p) {
     cudaFuncAttributes a;
@@ -60,16 +58,22 @@ struct AttnKernel {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem - (int)a.sharedSizeBytes) != cudaSuccess)
       return MEDA_ERR_CUDA;
     int per_sm = 0;
-    const size_t need = smem(p->cfg.max_seqs, p->sm_count);
+    const size_t need = smem(p->cfg.max_seqs);
     if (need > (size_t)(kMaxDynSmem - (int)a.sharedSizeBytes)) return MEDA_ERR_SHAPE;
+    // tiles of all segments, and as many again for the look-ahead, are counted in 32 bits
+    const int64_t segments = (int64_t)p->cfg.n_kv_heads * ((p->group + Tile::kHeads - 1) / Tile::kHeads);
+    if (segments * p->cfg.max_seqs * p->cfg.max_seq_pages * (p->cfg.page_size / kAttTile) >= (int64_t(1) << 31) - 65536)
+      return MEDA_ERR_SHAPE;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, W * 32, need) != cudaSuccess || per_sm < 1)
       return MEDA_ERR_CUDA;
     p->attn_blocks = p->sm_count;
     return MEDA_OK;
   }
-  static meda_status launch(meda_pages* p, const AttnParams& a, cudaStream_t st) {
+  static meda_status launch(meda_pages* p, AttnParams a, cudaStream_t st) {
     ++p->launches;
-    kernel<<<p->attn_blocks, W * 32, smem(a.n_seqs, p->attn_blocks), st>>>(a);
+    a.heads_div.set((unsigned)(a.n_heads * ((a.group + Tile::kHeads - 1) / Tile::kHeads)));
+    a.grid_div.set((unsigned)p->attn_blocks);
+    kernel<<<p->attn_blocks, W * 32, smem(a.n_seqs), st>>>(a);
     return launch_status();
   }
 };
@@ -415,7 +419,7 @@ meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k
   const meda_pages_config& c = pages->cfg;
   AttnParams a = {q, k_pages, v_pages, table, lens, sel, out, lse, pages->attn_partial, pages->attn_counters, pages->status,
                   lens_stride, n_seqs, c.n_kv_heads, pages->group, c.n_pages, c.max_seq_pages, pages->page_shift, keep,
-                  1.4426950408889634f / sqrtf((float)c.head_dim)};
+                  1.4426950408889634f / sqrtf((float)c.head_dim), {}, {}};
   return with_attn_kernel(pages, [&](auto kern) { return kern.launch(pages, a, as_stream(stream)); });
 }
 

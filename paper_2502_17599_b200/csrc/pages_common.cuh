@@ -1,6 +1,6 @@
 // Shared parts of the paged-cache kernels: the handle, and the block-wide prefix sums by which every block finds
 // its share of a ragged batch.  Lengths live on the device, so no launch can be sized by them: grids are fixed by
-// the GPU, every block reads all lengths (16 K at most, from L2) and takes an equal part of the work they add up to.
+// the GPU, every block reads all lengths (8 K at most, from L2) and takes an equal part of the work they add up to.
 #pragma once
 
 #include "meda_common.cuh"
@@ -23,7 +23,7 @@ struct meda_pages {
 
 namespace meda {
 
-constexpr int kPagesMaxSeqs = 16384;
+constexpr int kPagesMaxSeqs = 8192;
 constexpr int kPagesMaxSeqPages = 262144;
 
 // Exclusive prefix of `v` over a block of THREADS threads in thread order, and the block total.
