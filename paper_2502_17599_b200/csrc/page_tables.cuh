@@ -7,7 +7,10 @@
 // its front; a row's slot follows from its page.  No entry that is read is written in the same launch (the table
 // entries read are pages the sequences already hold, the ones written are new; the list's entries read lie behind its
 // front, the ones written before it), so blocks need no order among themselves.
-// Bound by latency for decoding steps (a launch, the lengths, two scans), by the 8-byte slots for whole prompts.
+// The unit of work is a page that gets new rows: a lane finds its page, the warp's 32 pages then cover one run of the slot
+// map, which the warp writes in full lines (a slot's page comes from the lane that holds it, by a search over the lanes).
+// Bound by latency for decoding steps (a launch, the lengths, a scan, two searches, one look-up), by the 8-byte slots for whole
+// prompts.
 #pragma once
 
 #include "pages_common.cuh"
@@ -15,7 +18,6 @@
 namespace meda {
 
 constexpr int kTabThreads = 512;
-constexpr int kTabWarpRows = 256;        // consecutive new rows whose slots one warp writes
 
 struct TablesParams {
   const int32_t* lens;
@@ -30,44 +32,90 @@ struct TablesParams {
   int lens_stride, new_stride, n_seqs, n_pages, width, page_shift, slots_capacity;
 };
 
+// Shared memory: six arrays over the sequences.
+__host__ __device__ inline size_t tables_smem(int n_seqs) { return (size_t)(n_seqs + 1) * 24; }
+
 __device__ __forceinline__ int pages_of(int rows, int shift) { return (int)(((unsigned)rows + (1u << shift) - 1u) >> shift); }
 
 __global__ void __launch_bounds__(kTabThreads)
 page_tables_kernel(TablesParams p) {
   extern __shared__ __align__(16) int tab_smem[];
-  __shared__ long long scratch[kTabThreads / 32 + 1];
-  const int n = p.n_seqs;
+  __shared__ long long warp_moves[kTabThreads / 32], warp_rows[kTabThreads / 32];
+  __shared__ int warp_touched[kTabThreads / 32];
+  const int n = p.n_seqs, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int* pops = tab_smem;                 // [n + 1] pages taken before sequence i
   int* pushes = pops + n + 1;           // [n + 1] pages given back before sequence i
   int* fresh = pushes + n + 1;          // [n + 1] new rows before sequence i
+  int* units = fresh + n + 1;           // [n + 1] pages with new rows before sequence i
+  int* was = units + n + 1;             // [n] rows before
+  int* will = was + n + 1;              // [n] rows after
   const int max_rows = p.width << p.page_shift;
 
-  auto old_len = [&](int i) { return p.lens ? p.lens[(size_t)i * p.lens_stride] : 0; };
-  auto new_len = [&](int i) { return p.new_lens[(size_t)i * p.new_stride]; };
-
-  const int per = (n + kTabThreads - 1) / kTabThreads;
-  const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
-  long long s_pop = 0, s_push = 0, s_new = 0;
-  int bad = 0;
-  for (int i = lo; i < hi; ++i) {
-    const int a = old_len(i), b = new_len(i);
-    const bool off = a < 0 || b < 0 || a > max_rows || b > max_rows;
-    bad |= off;
-    const int have = off ? 0 : pages_of(a, p.page_shift), need = off ? 0 : pages_of(b, p.page_shift);
-    const int up = max(0, need - have), down = max(0, have - need), rows = off ? 0 : max(0, b - a);
-    pops[i + 1] = up;
-    pushes[i + 1] = down;
-    fresh[i + 1] = rows;
-    s_pop += up;
-    s_push += down;
-    s_new += rows;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kTabThreads) {
+    was[i] = p.lens ? p.lens[(size_t)i * p.lens_stride] : 0;
+    will[i] = p.new_lens[(size_t)i * p.new_stride];
   }
   const int top = *p.free_top;
-  long long n_pops, n_pushes, n_fresh;
-  long long r_pop = block_prefix<kTabThreads>(s_pop, scratch, n_pops);
-  long long r_push = block_prefix<kTabThreads>(s_push, scratch, n_pushes);
-  long long r_new = block_prefix<kTabThreads>(s_new, scratch, n_fresh);
+  __syncthreads();
+  // a thread's consecutive sequences, then the block: pages taken and given back (below 2^31 each: see meda_pages_create) share
+  // one 64-bit sum
+  const int per = (n + kTabThreads - 1) / kTabThreads;
+  const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
+  long long moves = 0, rows = 0;
+  int touched = 0;
+  int bad = 0;
+  for (int i = lo; i < hi; ++i) {
+    const int a = was[i], b = will[i];
+    const bool off = a < 0 || b < 0 || a > max_rows || b > max_rows;
+    bad |= off;
+    const int step = off ? 0 : pages_of(b, p.page_shift) - pages_of(a, p.page_shift), more = off ? 0 : max(0, b - a);
+    pops[i + 1] = max(0, step);
+    pushes[i + 1] = max(0, -step);
+    const int pages = more ? pages_of(b, p.page_shift) - (a >> p.page_shift) : 0;
+    fresh[i + 1] = more;
+    units[i + 1] = pages;
+    touched += pages;
+    moves += ((long long)max(0, step) << 32) + max(0, -step);
+    rows += more;
+  }
+  long long incl_moves = moves, incl_rows = rows;
+  int incl_touched = touched;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl_moves, o), z = __shfl_up_sync(0xffffffffu, incl_rows, o);
+    const int t = __shfl_up_sync(0xffffffffu, incl_touched, o);
+    if (lane >= o) {
+      incl_moves += y;
+      incl_rows += z;
+      incl_touched += t;
+    }
+  }
+  if (lane == 31) {
+    warp_moves[warp] = incl_moves;
+    warp_rows[warp] = incl_rows;
+    warp_touched[warp] = incl_touched;
+  }
   bad = __syncthreads_or(bad);
+  long long all_moves = 0, n_fresh = 0;
+  incl_moves -= moves;
+  incl_rows -= rows;
+  incl_touched -= touched;
+  int total_units = 0;
+#pragma unroll
+  for (int w = 0; w < kTabThreads / 32; ++w) {
+    const long long y = warp_moves[w], z = warp_rows[w];
+    const int t = warp_touched[w];
+    if (w < warp) {
+      incl_moves += y;
+      incl_rows += z;
+      incl_touched += t;
+    }
+    all_moves += y;
+    n_fresh += z;
+    total_units += t;
+  }
+  const long long n_pops = all_moves >> 32, n_pushes = all_moves & 0xffffffffll;
   const bool first = blockIdx.x == 0 && threadIdx.x == 0;
   int code = MEDA_OK;
   if (bad || top < 0 || top > p.n_pages || top + n_pops - n_pushes < 0) code = MEDA_ERR_INVALID_ARG;
@@ -82,16 +130,19 @@ page_tables_kernel(TablesParams p) {
     }
     return;
   }
+  int r_pop = (int)(incl_moves >> 32), r_push = (int)(incl_moves & 0xffffffffll), r_new = (int)incl_rows, r_unit = incl_touched;
   for (int i = lo; i < hi; ++i) {
     r_pop += pops[i + 1];
     r_push += pushes[i + 1];
     r_new += fresh[i + 1];
-    pops[i + 1] = (int)r_pop;
-    pushes[i + 1] = (int)r_push;
-    fresh[i + 1] = (int)r_new;
-    if (blockIdx.x == 0) p.cu_new[i + 1] = (int)r_new;
+    r_unit += units[i + 1];
+    units[i + 1] = r_unit;
+    pops[i + 1] = r_pop;
+    pushes[i + 1] = r_push;
+    fresh[i + 1] = r_new;
+    if (blockIdx.x == 0) p.cu_new[i + 1] = r_new;
   }
-  if (threadIdx.x == 0) pops[0] = pushes[0] = fresh[0] = 0;
+  if (threadIdx.x == 0) pops[0] = pushes[0] = fresh[0] = units[0] = 0;
   if (first) {
     p.cu_new[0] = 0;
     *p.free_top_out = (int)(top + n_pops - n_pushes);
@@ -106,42 +157,58 @@ page_tables_kernel(TablesParams p) {
     }
     return page;
   };
-  auto pushed = [&](int j) {            // j-th page given back
-    const int i = ragged_find(pushes, n, j);
-    return checked(p.table[(size_t)i * p.width + pages_of(new_len(i), p.page_shift) + (j - pushes[i])]);
+  const int top_bit = n > 1 ? 1 << (31 - __clz(n - 1)) : 0;    // first step of a search over n entries
+  auto find = [&](const int* pre, int x) {                     // largest i < n with pre[i] <= x
+    int i = 0;
+    for (int step = top_bit; step > 0; step >>= 1)
+      if (i + step < n && pre[i + step] <= x) i += step;
+    return i;
   };
-  auto popped = [&](int j) {            // j-th page taken
-    return j < total_pushes ? pushed(j) : checked(p.free_pages[top + (j - total_pushes)]);
+  auto pushed = [&](int j) -> const int32_t* {                 // where the j-th page given back stands
+    const int i = find(pushes, j);
+    return p.table + (size_t)i * p.width + pages_of(will[i], p.page_shift) + (j - pushes[i]);
   };
 
-  // pages taken into the table, pages left over onto the list
-  for (int j = blockIdx.x * kTabThreads + threadIdx.x; j < total_pops; j += stride) {
-    const int i = ragged_find(pops, n, j);
-    p.table[(size_t)i * p.width + pages_of(old_len(i), p.page_shift) + (j - pops[i])] = popped(j);
-  }
-  for (int j = total_pops + blockIdx.x * kTabThreads + threadIdx.x; j < total_pushes; j += stride)
-    p.free_pages[top - 1 - (j - total_pops)] = pushed(j);
-
-  // slots of the new rows: a warp finds the sequence of its first row and walks on from there
-  const int lane = threadIdx.x % 32;
+  // pages that get new rows: the page, its table entry if it was taken, and its rows' slots
   const int mask = (1 << p.page_shift) - 1;
   const int warps = gridDim.x * (kTabThreads / 32);
-  for (long long c0 = (long long)(blockIdx.x * (kTabThreads / 32) + threadIdx.x / 32) * kTabWarpRows; c0 < p.slots_capacity;
-       c0 += (long long)warps * kTabWarpRows) {
-    const int end = (int)min(c0 + kTabWarpRows, (long long)p.slots_capacity);
-    int i = c0 < total_new ? ragged_find(fresh, n, (int)c0) : 0;
-    for (int t = (int)c0 + lane; t < end; t += 32) {
-      int64_t slot = -1;
-      if (t < total_new) {
-        while (t >= fresh[i + 1]) ++i;
-        const int have = old_len(i);
-        const int row = have + (t - fresh[i]), col = row >> p.page_shift, held = pages_of(have, p.page_shift);
-        const int page = col < held ? checked(p.table[(size_t)i * p.width + col]) : popped(pops[i] + (col - held));
-        if (page >= 0) slot = ((int64_t)page << p.page_shift) + (row & mask);
+  for (long long u0 = (long long)(blockIdx.x * (kTabThreads / 32) + warp) * 32; u0 < total_units; u0 += (long long)warps * 32) {
+    const int u = (int)u0 + lane;
+    int first_slot = total_new, rows_here = 0, page = -1, row0 = 0;
+    if (u < total_units) {
+      const int i = find(units, u);
+      const int a = was[i], b = will[i], col = (a >> p.page_shift) + (u - units[i]), held = pages_of(a, p.page_shift);
+      const int32_t* src = p.table + (size_t)i * p.width + col;
+      if (col >= held) {
+        const int j = pops[i] + (col - held);
+        src = j < total_pushes ? pushed(j) : p.free_pages + top + (j - total_pushes);
       }
-      p.slots[t] = slot;
+      page = checked(*src);
+      if (col >= held) p.table[(size_t)i * p.width + col] = page;
+      const int r0 = max(a, col << p.page_shift), r1 = min(b, (col + 1) << p.page_shift);
+      row0 = r0 & mask;
+      rows_here = r1 - r0;
+      first_slot = fresh[i] + (r0 - a);
+    }
+    if (!p.slots) continue;
+    const int begin = __shfl_sync(0xffffffffu, first_slot, 0);
+    const int last = 31 - __clz(__ballot_sync(0xffffffffu, rows_here > 0));
+    const int end = __shfl_sync(0xffffffffu, first_slot + rows_here, last);
+#pragma unroll 4
+    for (int t0 = begin; t0 < end; t0 += 32) {
+      const int t = t0 + lane;
+      int owner = 0;                                           // the lane whose page holds slot t
+#pragma unroll
+      for (int step = 16; step > 0; step >>= 1)
+        if (__shfl_sync(0xffffffffu, first_slot, owner + step) <= t) owner += step;
+      const int pg = __shfl_sync(0xffffffffu, page, owner), r = __shfl_sync(0xffffffffu, row0, owner) + t - __shfl_sync(0xffffffffu, first_slot, owner);
+      if (t < end) p.slots[t] = pg < 0 ? -1 : ((int64_t)pg << p.page_shift) + r;
     }
   }
+  // pages given back that nobody took onto the list; nothing in the slots behind the last row
+  for (int j = total_pops + blockIdx.x * kTabThreads + threadIdx.x; j < total_pushes; j += stride)
+    p.free_pages[top - 1 - (j - total_pops)] = checked(*pushed(j));
+  for (long long t = (long long)total_new + blockIdx.x * kTabThreads + threadIdx.x; t < p.slots_capacity; t += stride) p.slots[t] = -1;
 }
 
 }  // namespace meda

@@ -311,11 +311,12 @@ meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t len
   const meda_pages_config& c = pages->cfg;
   TablesParams a = {lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, pages->status,
                     lens_stride, new_stride, n_seqs, c.n_pages, c.max_seq_pages, pages->page_shift, (int)slots_capacity};
-  // a block per 4,096 entries that may be written (every warp two runs of them), one per SM at most: each block repeats the scans
-  const int64_t entries = slots_capacity + std::min<int64_t>(c.n_pages, (int64_t)n_seqs * c.max_seq_pages);
-  const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (entries + 4095) / 4096));
+  // one page that gets rows per lane, one block per SM at most: each block repeats the scans
+  const int64_t units = slots_capacity ? (slots_capacity >> pages->page_shift) + 2 * (int64_t)n_seqs
+                                       : std::min<int64_t>(c.n_pages, (int64_t)n_seqs * c.max_seq_pages);
+  const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (units + kTabThreads - 1) / kTabThreads));
   ++pages->launches;
-  page_tables_kernel<<<grid, kTabThreads, (size_t)(n_seqs + 1) * 12, as_stream(stream)>>>(a);
+  page_tables_kernel<<<grid, kTabThreads, tables_smem(n_seqs), as_stream(stream)>>>(a);
   return launch_status();
 }
 
