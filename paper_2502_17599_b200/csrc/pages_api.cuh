@@ -106,7 +106,7 @@ struct SelectPagesKernel {
   static meda_status launch(meda_pages* p, const SelectPagesParams& a, int cluster, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.n_seqs * a.n_heads * cluster);
-    cfg.blockDim = dim3(kSelThreads);
+    cfg.blockDim = dim3(kPselThreads);
     cfg.dynamicSmemBytes = select_pages_smem(a.width, cluster, GP, D).total;
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
