@@ -100,35 +100,29 @@ meda_status with_attn_kernel(const meda_pages* p, F f) {
 
 // ---- selection of pages ------------------------------------------------------------------------
 template <typename T, int D, int GP>
-struct SelectPagesKernel {
-  static constexpr auto kernel = select_pages_kernel<T, D, GP>;
-  static meda_status prepare() { return raise_dyn_smem(kernel); }
-  static meda_status launch(meda_pages* p, const SelectPagesParams& a, int cluster, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.n_seqs * a.n_heads * cluster);
-    cfg.blockDim = dim3(kPselThreads);
-    cfg.dynamicSmemBytes = select_pages_smem(a.width, cluster, GP, D).total;
-    cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = cluster;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    ++p->launches;
-    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? MEDA_OK : (cudaGetLastError(), MEDA_ERR_CUDA);
+struct SelectPagesKernels {
+  static meda_status prepare() {
+    const meda_status r = raise_dyn_smem(page_scores_kernel<T, D, GP>);
+    return r == MEDA_OK ? raise_dyn_smem(choose_pages_kernel<T, D>) : r;
+  }
+  static meda_status launch(meda_pages* p, const SelectPagesParams& a, cudaStream_t st) {
+    p->launches += 2;
+    page_scores_kernel<T, D, GP><<<p->sm_count * 2, kPscoreThreads, (size_t)(a.n_seqs + 1) * 4, st>>>(a);
+    choose_pages_kernel<T, D><<<a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width), st>>>(a);
+    return launch_status();
   }
 };
 
 template <typename T, int D, typename F>
 meda_status with_select_group(const meda_pages* p, F f) {
   const int g = p->group;
-  return g == 1 ? f(SelectPagesKernel<T, D, 1>()) : g == 2 ? f(SelectPagesKernel<T, D, 2>())
-       : g <= 4 ? f(SelectPagesKernel<T, D, 4>()) : g <= 8 ? f(SelectPagesKernel<T, D, 8>()) : f(SelectPagesKernel<T, D, 16>());
+  if (sizeof(T) == 2) return g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
+  return g == 1 ? f(SelectPagesKernels<T, D, 1>()) : g <= 4 ? f(SelectPagesKernels<T, D, 4>())
+       : g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
 }
 
 template <typename F>
-meda_status with_select_kernel(const meda_pages* p, F f) {
+meda_status with_select_kernels(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim;
   if (p->cfg.dtype == MEDA_BF16)
     return d == 64 ? with_select_group<__nv_bfloat16, 64>(p, f) : d == 128 ? with_select_group<__nv_bfloat16, 128>(p, f)
@@ -137,17 +131,13 @@ meda_status with_select_kernel(const meda_pages* p, F f) {
                                                                  : with_select_group<float, 256>(p, f);
 }
 
-int group_rounded(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
-
-// Blocks per cluster: the largest of 8, 4, 2, 1 that keeps all clusters within one wave and gives a block a
-// few hundred pages, unless the sort keys need more blocks' shared memory than that.
-int select_pages_cluster(const meda_pages* p, int n_seqs) {
-  int c = 8;
-  const int width = p->cfg.max_seq_pages;
-  while (c > 1 && ((width + c - 1) / c < 256 || (int64_t)n_seqs * p->cfg.n_kv_heads * c > p->sm_count) &&
-         select_pages_smem(width, c / 2, group_rounded(p->group), p->cfg.head_dim).total <= kMaxDynSmem - 1024)
-    c /= 2;
-  return c;
+// Scratch of the selection: one sequence's scores and their bounds, in floats, and how many sequences it holds (at least
+// one, more while that stays below 32 MB; a larger batch goes through it in several launches).
+int64_t select_seq_floats(const meda_pages_config& c) {
+  return (int64_t)c.n_kv_heads * (c.max_seq_pages + pscore_units(c.max_seq_pages));
+}
+int select_scratch_seqs(const meda_pages_config& c) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(c.max_seqs, (int64_t(32) << 20) / 4 / select_seq_floats(c)));
 }
 
 // ---- pages of rows -----------------------------------------------------------------------------
@@ -193,6 +183,7 @@ void pages_release(meda_pages* p) {
   cudaFree(p->rope_axis);
   cudaFree(p->attn_partial);
   cudaFree(p->attn_counters);
+  cudaFree(p->select_scratch);
   delete p;
 }
 
@@ -249,9 +240,7 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
       cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess)
     st = MEDA_ERR_CUDA;
   if (st == MEDA_OK) st = with_attn_kernel(p, [&](auto k) { return k.prepare(p); });
-  if (st == MEDA_OK) st = with_select_kernel(p, [](auto k) { return k.prepare(); });
-  if (st == MEDA_OK && select_pages_smem(c.max_seq_pages, 8, group_rounded(p->group), c.head_dim).total > kMaxDynSmem - 1024)
-    st = MEDA_ERR_SHAPE;
+  if (st == MEDA_OK) st = with_select_kernels(p, [](auto k) { return k.prepare(); });
   if (st == MEDA_OK) st = raise_page_rows_smem<true>();
   if (st == MEDA_OK) st = raise_page_rows_smem<false>();
   if (st == MEDA_OK) st = raise_dyn_smem(page_tables_kernel);
@@ -259,6 +248,7 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
   if (st == MEDA_OK) st = carve(&p->rope_freq, half, &p->bytes);
   if (st == MEDA_OK) st = carve(&p->rope_axis, half, &p->bytes);
   if (st == MEDA_OK) st = carve(&p->attn_partial, (int64_t)p->attn_blocks * 2 * attn_state_floats(p->group, c.head_dim), &p->bytes);
+  if (st == MEDA_OK) st = carve(&p->select_scratch, select_seq_floats(c) * select_scratch_seqs(c), &p->bytes);
   const int64_t counters = (int64_t)c.max_seqs * c.n_q_heads;  // segments: at most one per query head
   if (st == MEDA_OK) st = carve(&p->attn_counters, counters, &p->bytes);
   if (st == MEDA_OK && (cudaMemset(p->status, 0, sizeof(int)) != cudaSuccess ||
@@ -401,10 +391,19 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
   const meda_pages_config& c = pages->cfg;
-  SelectPagesParams a = {q, bounds, table, lens, sel, pages->status, lens_stride, n_seqs, c.n_kv_heads, pages->group, c.n_pages,
-                         c.max_seq_pages, pages->page_shift, keep, n_first, n_last};
-  const int cluster = select_pages_cluster(pages, n_seqs);
-  return with_select_kernel(pages, [&](auto kern) { return kern.launch(pages, a, cluster, as_stream(stream)); });
+  const int some = select_scratch_seqs(c), e = pages_element(pages);
+  for (int i = 0; i < n_seqs; i += some) {
+    const int count = std::min(some, n_seqs - i);
+    float* scores = pages->select_scratch;
+    SelectPagesParams a = {static_cast<const char*>(q) + (size_t)i * c.n_q_heads * c.head_dim * e, bounds,
+                           table + (size_t)i * c.max_seq_pages, lens + (size_t)i * lens_stride, sel + (size_t)i * c.n_kv_heads * keep,
+                           scores, scores + (int64_t)some * c.n_kv_heads * c.max_seq_pages, pages->status, lens_stride, count,
+                           c.n_kv_heads, pages->group, c.n_pages, c.max_seq_pages, pages->page_shift, keep, n_first, n_last, {}};
+    a.heads_div.set((unsigned)c.n_kv_heads);
+    const meda_status done = with_select_kernels(pages, [&](auto kern) { return kern.launch(pages, a, as_stream(stream)); });
+    if (done != MEDA_OK) return done;
+  }
+  return MEDA_OK;
 }
 
 meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,

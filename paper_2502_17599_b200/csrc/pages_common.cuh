@@ -18,6 +18,7 @@ struct meda_pages {
   int* rope_axis = nullptr;            // [half]
   float* attn_partial = nullptr;       // [blocks][2][group][head_dim + 2] softmax states of segments that cross blocks
   unsigned int* attn_counters = nullptr;     // [max_seqs * n_kv_heads] arrivals per segment, zero between launches
+  float* select_scratch = nullptr;     // [sequences][n_kv_heads][max_seq_pages] scores, then a bound per eight pages of them
   int attn_blocks = 0;                 // blocks of the attention kernel that are resident at once
 };
 

@@ -2,32 +2,35 @@
 // logit a page's key bounds allow any of the head's queries, max_h sum_d (q >= 0 ? q * max : q * min).
 //
 // The sum is taken in 64 bits and rounded once: which of two near pages is kept must not hang on the order of an fp32
-// sum, because the whole output follows from it.  64-bit arithmetic on every page would cost several times what reading
-// the bounds does (100 us instead of 4 for 8,064 pages and 28 heads), so bf16 caches go two ways at once:
-//   - every page gets an approximate score from the matrix instructions, max(q, 0) . max + min(q, 0) . min (products of bf16
-//     are exact, the fp32 sum is off by at most eps);
-//   - radix passes over those find the keep-th largest to 22 bits; pages above it by more than 2 eps are kept, pages below it
-//     by more than 2 eps are not (the true keep-th score lies within eps of it), and the few in between are scored
-//     again in 64 bits and ranked among themselves.
-// Where that cannot decide (an infinity or a NaN, more than kPselMaxDoubt pages in between) and for fp32 caches every page is
-// scored in 64 bits and the radix passes go to the last bit.
+// sum, because the whole output follows from it.  64-bit arithmetic on every page would cost far more than reading
+// the bounds does (100 us instead of 4 for 8,067 pages of 4 KV heads with 7 query heads each), so bf16 caches go
+// two ways at once:
+//   - page_scores_kernel gives every page an approximate score from the matrix instructions, max(q, 0) . max + min(q, 0) . min
+//     (products of bf16 are exact, the fp32 sum is off by eps at most), with the whole GPU;
+//   - choose_pages_kernel, one block per (sequence, KV head), finds the keep-th largest of them to one of 2,048 equal bins
+//     between the smallest and the largest score.  A page that stays in a better bin when its score is lowered by 2 eps is kept, one
+//     that stays in a worse bin when it is raised by 2 eps is not (the true keep-th score lies within eps of the
+//     approximate one), and the few in between are scored again in 64 bits and ranked among themselves.
+// Where that cannot decide (an infinity or a NaN, more than kPselMaxDoubt pages in between) the block scores all its
+// pages in 64 bits and finds the keep-th by radix passes to the last bit.  fp32 caches get 64-bit scores at once.
 //
-// One cluster of blocks per (sequence, KV head), in one launch: the blocks hold the sort keys of equal parts of the
-// sequence's pages in shared memory, add up their histograms through distributed shared memory, and write their kept
-// pages in order.  Scores never go to global memory.
+// One block chooses because its work is a handful of block-wide steps over keys in registers; a cluster of blocks per
+// sequence with histograms in distributed shared memory spent 6,000 cycles on each step (31 us against 10).
 #pragma once
 
-#include <cooperative_groups.h>
-
-#include "paged_attention.cuh"   // mma_bf16
+#include "paged_attention.cuh"   // mma_bf16, InvariantDiv, div_small
 #include "pages_common.cuh"
 #include "rope_append.cuh"       // RopeVec
 
 namespace meda {
 
-constexpr int kPselThreads = 512;
-constexpr int kPselBins = 2048;          // 11-bit digits: 11 + 11 + 10 bits of a key
-constexpr int kPselMaxDoubt = 256;       // pages scored again in 64 bits
+constexpr int kPscoreThreads = 256;
+constexpr int kPscoreUnit = 8;           // pages side by side in a warp
+constexpr int kPselThreads = 1024;
+constexpr int kPselItems = 16;           // scores per thread held in registers: 16 K pages in one round
+constexpr int kPselRound = kPselThreads * kPselItems;
+constexpr int kPselBins = 2048;
+constexpr int kPselMaxDoubt = 512;       // pages scored again in 64 bits
 
 struct SelectPagesParams {
   const void* q;
@@ -35,61 +38,193 @@ struct SelectPagesParams {
   const int32_t* table;
   const int32_t* lens;
   int32_t* sel;
+  float* scores;                         // [n_seqs * n_heads][width]
+  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: largest |bound| of a unit's pages, NaN
+                                         // where a score is not finite; 0 where the scores are exact
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep, n_first, n_last;
+  InvariantDiv heads_div;
 };
 
-// Block-shared counters; other blocks of the cluster read some of them.
-struct SelectPagesShared {
-  int scan[kPselThreads / 32 + 1];
-  int digit, remaining;
-  int sure, equal, doubtful;             // this block's pages
-  int undecided;                         // a NaN or an infinity among this block's approximate scores
-  int listed;                            // doubtful pages written to the list (block 0)
-  unsigned int max_abs;                  // largest |bound| of this block's pages, as float bits
-  float q_norm;                          // largest sum |q| over the heads
-};
-
-struct SelectPagesSmem {
-  int keys_off, hist_off, q_off, list_off, total;
-};
-__host__ __device__ inline SelectPagesSmem select_pages_smem(int width, int cluster_size, int gp, int d) {
-  SelectPagesSmem L;
-  int off = 0;
-  L.q_off = off;     off += gp * d * 8;
-  L.hist_off = off;  off += 2 * kPselBins * 4;
-  L.list_off = off;  off += kPselMaxDoubt * 8;
-  L.keys_off = off;  off += ((width + cluster_size - 1) / cluster_size + 3) / 4 * 16;
-  L.total = off;
-  return L;
-}
+__host__ __device__ inline int pscore_units(int pages) { return (pages + kPscoreUnit - 1) / kPscoreUnit; }
 
 __device__ __forceinline__ unsigned int page_key(float score) {
-  if (score != score) return 0xfffffffeu;                      // NaN ranks above every number, below a forced page
+  if (score != score) return 0xffffffffu;                      // NaN ranks highest
   const unsigned int b = __float_as_uint(score + 0.f);         // -0 counts as 0
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
-__device__ __forceinline__ float key_score(unsigned int key) {
-  return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key);
+
+// Place of a page's bounds for KV head g; a page outside the pool is reported and scores as page 0.
+__device__ __forceinline__ size_t bounds_place(const SelectPagesParams& p, int page, int g, int d) {
+  const bool ok = (unsigned)page < (unsigned)p.n_pages;
+  if (!ok) set_status(p.status, MEDA_ERR_INVALID_ARG);
+  return ((size_t)(ok ? page : 0) * p.n_heads + g) * 2 * d;
 }
 
-// The score of one page for one KV head by a whole warp, in 64 bits.  qs: the head's queries [group][D] as doubles.
-template <typename T, int D>
-__device__ __forceinline__ float page_score_warp(const T* lo, const T* hi, const double* qs, int group, int lane) {
-  constexpr int E = D / 32;
-  double mn[E], mx[E];
+// ---- scores of all pages ---------------------------------------------------------------------------------
+// A unit is eight neighbouring pages of one (sequence, KV head); a warp takes a run of units, and reads the queries again
+// where the pair changes.  Four lanes share a page.  D = head_dim, GP = query heads per KV head rounded up to a power of two.
+template <typename T, int D, int GP>
+__global__ void __launch_bounds__(kPscoreThreads)
+page_scores_kernel(SelectPagesParams p) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int E = RopeVec<T>::E;                             // elements per 16-byte vector
+  constexpr int X = D / (4 * E);                               // vectors of a bound per lane
+  constexpr int NH = GP > 8 ? 2 : 1;
+  extern __shared__ __align__(16) int pscore_smem[];
+  __shared__ int scratch[kPscoreThreads / 32 + 1];
+  int* pre = pscore_smem;                                      // [n + 1] units before sequence i (of one KV head)
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, r = lane / 4, c = lane % 4;
+  const int page_size = 1 << p.page_shift, max_rows = p.width << p.page_shift;
+  const T* bounds = static_cast<const T*>(p.bounds);
+  ragged_prefix<kPscoreThreads>(p.n_seqs, pre, scratch, [&](int i) {
+    bool bad = false;
+    const int len = clamped_len(p.lens, p.lens_stride, i, max_rows, bad);
+    if (bad && blockIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
+    const int pages = (len + page_size - 1) >> p.page_shift;
+    return pages > p.keep ? pscore_units(pages) : 0;           // (a sequence that keeps everything needs no scores)
+  });
+  const long long total = (long long)pre[p.n_seqs] * p.n_heads;
+  const long long warps = (long long)gridDim.x * (kPscoreThreads / 32), me = (long long)blockIdx.x * (kPscoreThreads / 32) + warp;
+  const int per = (int)((total + warps - 1) / warps);
+  const int u0 = (int)min(me * per, total), u1 = (int)min((me + 1) * per, total);
+
+  uint4 pos[NH][X], neg[NH][X];                                // bf16: the queries' positive and negative parts as fragments
+  int held = -1, i = 0, g = 0, units = 0, n = 0, first_unit = 0;
+  for (int u = u0; u < u1; ++u) {
+    if (u >= first_unit + units) {                             // the next (sequence, KV head)
+      i = ragged_find(pre, p.n_seqs, p.heads_div.of(u));
+      units = pre[i + 1] - pre[i];
+      g = div_small(u - pre[i] * p.n_heads, units);
+      first_unit = pre[i] * p.n_heads + g * units;
+      bool bad = false;
+      n = (clamped_len(p.lens, p.lens_stride, i, max_rows, bad) + page_size - 1) >> p.page_shift;
+    }
+    const int pair = i * p.n_heads + g, c0 = (u - first_unit) * kPscoreUnit;
+    const T* qh = static_cast<const T*>(p.q) + (size_t)pair * p.group * D;
+    const size_t at = bounds_place(p, p.table[(size_t)i * p.width + min(c0 + r, n - 1)], g, D);
+    if constexpr (kBf16) {
+      const T* src = bounds + at + c * 8;
+      uint4 mn[X], mx[X];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
+      for (int x = 0; x < X; ++x) {
+        mn[x] = load_stream(reinterpret_cast<const uint4*>(src + x * 32));
+        mx[x] = load_stream(reinterpret_cast<const uint4*>(src + D + x * 32));
+      }
+      if (pair != held) {
+        held = pair;
+        const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+        for (int y = 0; y < NH; ++y) {
+          const int h = r + 8 * y;
+#pragma unroll
+          for (int x = 0; x < X; ++x) {
+            const uint4 v = h < p.group ? *reinterpret_cast<const uint4*>(qh + (size_t)h * D + x * 32 + c * 8) : make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t a[4], b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              __nv_bfloat162 t;
+              memcpy(&t, &w[e], 4);
+              const __nv_bfloat162 up = __hmax2_nan(t, zero), down = __hmin2_nan(t, zero);
+              memcpy(&a[e], &up, 4);
+              memcpy(&b[e], &down, 4);
+            }
+            pos[y][x] = make_uint4(a[0], a[1], a[2], a[3]);
+            neg[y][x] = make_uint4(b[0], b[1], b[2], b[3]);
+          }
+        }
+      }
+      // A = queries (row: head), B = bounds (column: page), the contraction index permuted as in paged_attention.cuh
+      float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of dependent instructions
+      __nv_bfloat162 top2 = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+      for (int x = 0; x < X; ++x) {
+        mma_bf16(up, pos[0][x].x, NH > 1 ? pos[NH - 1][x].x : 0u, pos[0][x].y, NH > 1 ? pos[NH - 1][x].y : 0u, mx[x].x, mx[x].y);
+        mma_bf16(down, neg[0][x].x, NH > 1 ? neg[NH - 1][x].x : 0u, neg[0][x].y, NH > 1 ? neg[NH - 1][x].y : 0u, mn[x].x, mn[x].y);
+        mma_bf16(up, pos[0][x].z, NH > 1 ? pos[NH - 1][x].z : 0u, pos[0][x].w, NH > 1 ? pos[NH - 1][x].w : 0u, mx[x].z, mx[x].w);
+        mma_bf16(down, neg[0][x].z, NH > 1 ? neg[NH - 1][x].z : 0u, neg[0][x].w, NH > 1 ? neg[NH - 1][x].w : 0u, mn[x].z, mn[x].w);
+        const uint32_t w[8] = {mn[x].x, mn[x].y, mn[x].z, mn[x].w, mx[x].x, mx[x].y, mx[x].z, mx[x].w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          __nv_bfloat162 t;
+          memcpy(&t, &w[e], 4);
+          top2 = __hmax2_nan(top2, __habs2(t));
+        }
+      }
+      float best[2];                                           // of pages 2c and 2c + 1
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float a = r < p.group ? up[e] + down[e] : -INFINITY;
+        const float b = NH > 1 && r + 8 < p.group ? up[2 + e] + down[2 + e] : -INFINITY;
+        odd |= a != a || b != b;
+        best[e] = fmaxf(a, b);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) best[e] = fmaxf(best[e], __shfl_xor_sync(0xffffffffu, best[e], o));
+      }
+      const float t0 = __low2float(top2), t1 = __high2float(top2);
+      odd |= t0 != t0 || t1 != t1 || t0 == INFINITY || t1 == INFINITY;
+      const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(t0, t1))));
+      odd = __any_sync(0xffffffffu, odd);
+      if (r < 2 && c0 + 2 * c + r < n) p.scores[(size_t)pair * p.width + c0 + 2 * c + r] = best[r];
+      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top;
+    } else {
+      const uint4* src = reinterpret_cast<const uint4*>(bounds + at) + c;
+      double acc[GP];
+#pragma unroll
+      for (int h = 0; h < GP; ++h) acc[h] = 0.0;
+#pragma unroll 2
+      for (int x = 0; x < X; ++x) {
+        float mn[E], mx[E];
+        RopeVec<T>::unpack(src[x * 4], mn);
+        RopeVec<T>::unpack(src[D / E + x * 4], mx);
+#pragma unroll
+        for (int h = 0; h < GP; ++h)
+          if (h < p.group) {
+            float qv[E];
+            RopeVec<T>::unpack(*reinterpret_cast<const uint4*>(qh + (size_t)h * D + (x * 4 + c) * E), qv);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[h] = fma((double)qv[e], (double)(qv[e] >= 0.f ? mx[e] : mn[e]), acc[h]);
+          }
+      }
+      float best = -INFINITY;
+      bool nan = false;
+#pragma unroll
+      for (int h = 0; h < GP; ++h)
+        if (h < p.group) {
+          double s = acc[h];
+          s += __shfl_xor_sync(0xffffffffu, s, 1);
+          s += __shfl_xor_sync(0xffffffffu, s, 2);
+          const float f = (float)s;
+          nan |= f != f;
+          best = fmaxf(best, f);
+        }
+      const bool odd = __any_sync(0xffffffffu, nan || fabsf(best) == INFINITY);
+      if (c == 0 && c0 + r < n) p.scores[(size_t)pair * p.width + c0 + r] = nan ? NAN : best;
+      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : 0.f;
+    }
+  }
+}
+
+// The score of one page for one KV head by a whole warp, in 64 bits.  qh: the head's queries [group][D].
+template <typename T, int D>
+__device__ __forceinline__ float page_score_warp(const T* lo, const T* qh, int group, int lane) {
+  constexpr int N = D / 32;
+  double mn[N], mx[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
     mn[e] = (double)to_f32<T>(lo[e * 32 + lane]);
-    mx[e] = (double)to_f32<T>(hi[e * 32 + lane]);
+    mx[e] = (double)to_f32<T>(lo[D + e * 32 + lane]);
   }
   float best = -INFINITY;
   bool nan = false;
+#pragma unroll 4
   for (int h = 0; h < group; ++h) {
     double s = 0.0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const double q = qs[h * D + e * 32 + lane];
+    for (int e = 0; e < N; ++e) {
+      const double q = (double)to_f32<T>(qh[h * D + e * 32 + lane]);
       s = fma(q, q >= 0.0 ? mx[e] : mn[e], s);
     }
 #pragma unroll
@@ -101,364 +236,253 @@ __device__ __forceinline__ float page_score_warp(const T* lo, const T* hi, const
   return nan ? NAN : best;
 }
 
-// D = head_dim, GP = query heads per KV head rounded up to a power of two.
-template <typename T, int D, int GP>
+// ---- the choice, one block per (sequence, KV head) ---------------------------------------------------------
+__host__ __device__ inline int choose_smem(int width) { return 2 * ((width + 31) / 32) * 4; }     // two bits per page
+
+template <typename T, int D>
 __global__ void __launch_bounds__(kPselThreads, 1)
-select_pages_kernel(SelectPagesParams p) {
-  namespace cg = cooperative_groups;
-  constexpr bool kBf16 = sizeof(T) == 2;
+choose_pages_kernel(SelectPagesParams p) {
+  constexpr bool kExact = sizeof(T) == 4;                      // the scores are the 64-bit ones already
   constexpr int kWarps = kPselThreads / 32;
-  constexpr int E = RopeVec<T>::E;                             // elements per 16-byte vector
-  constexpr int X = D / (4 * E);                               // vectors of a bound per lane, four lanes to a page
-  extern __shared__ __align__(16) unsigned char psel_smem[];
-  __shared__ SelectPagesShared sh;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int rank = (int)cluster.block_rank(), CS = (int)cluster.num_blocks();
-  const SelectPagesSmem L = select_pages_smem(p.width, CS, GP, D);
-  unsigned int* keys = reinterpret_cast<unsigned int*>(psel_smem + L.keys_off);
-  unsigned int* hist = reinterpret_cast<unsigned int*>(psel_smem + L.hist_off);
-  uint2* list = reinterpret_cast<uint2*>(psel_smem + L.list_off);   // (key, page) of doubtful pages, in block 0
-  double* qs = reinterpret_cast<double*>(psel_smem + L.q_off); // [GP][D]
+  extern __shared__ __align__(16) unsigned int choose_bits[];
+  __shared__ unsigned int hist[kPselBins];
+  __shared__ uint2 list[kPselMaxDoubt];                        // (key, page) of the pages in doubt
+  __shared__ int scan[kWarps + 1];
+  __shared__ float red[3][kWarps];
+  __shared__ int s_bin, s_need, s_sure, s_listed;
+  unsigned int* kept = choose_bits;                            // [words]
+  unsigned int* equal = choose_bits + (p.width + 31) / 32;     // [words], the fallback's
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int pair = blockIdx.x / CS, i = pair / p.n_heads, g = pair % p.n_heads;
+  const int pair = blockIdx.x, i = p.heads_div.of(pair), g = pair - i * p.n_heads;
   const int page_size = 1 << p.page_shift;
   bool bad = false;
   const int len = clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad);
-  if (bad && threadIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
   const int n = (len + page_size - 1) >> p.page_shift;         // pages of the sequence
-  int32_t* out = p.sel + ((size_t)i * p.n_heads + g) * p.keep;
-  if (n <= p.keep) {                                           // uniform over the cluster: every page is kept
-    for (int c = rank * kPselThreads + threadIdx.x; c < n; c += CS * kPselThreads) out[c] = c;
+  int32_t* out = p.sel + (size_t)pair * p.keep;
+  if (n <= p.keep) {                                           // every page is kept
+    for (int c = threadIdx.x; c < n; c += kPselThreads) out[c] = c;
     return;
   }
-  const int chunk = (n + CS - 1) / CS;
-  const int lo = min(n, rank * chunk), hi = min(n, lo + chunk);
-  const T* qh = static_cast<const T*>(p.q) + ((size_t)i * p.n_heads + g) * p.group * D;
-  const int32_t* table = p.table + (size_t)i * p.width;
+  const float* scores = p.scores + (size_t)pair * p.width;
+  const T* qh = static_cast<const T*>(p.q) + (size_t)pair * p.group * D;
   const T* bounds = static_cast<const T*>(p.bounds);
+  const int32_t* table = p.table + (size_t)i * p.width;
+  const int want = p.keep - p.n_first - p.n_last;              // pages to choose among those that are not kept anyway
+  const int words = (n + 31) / 32, rounds = (n + kPselRound - 1) / kPselRound;
   auto forced = [&](int c) { return c < p.n_first || c >= n - p.n_last; };
-  // page (column of the table) c's place in the pool of bounds; a page outside the pool is reported and scores as page 0
-  auto place = [&](int c) {
-    const int page = table[c];
-    const bool ok = (unsigned)page < (unsigned)p.n_pages;
-    if (!ok) set_status(p.status, MEDA_ERR_INVALID_ARG);
-    return ((size_t)(ok ? page : 0) * p.n_heads + g) * 2 * D;
-  };
+  auto open_page = [&](int c) { return c < n && !forced(c); };
 
-  if (threadIdx.x == 0) {
-    sh.undecided = kBf16 ? 0 : 1;
-    sh.listed = 0;
-    sh.max_abs = 0u;
-    sh.q_norm = 0.f;
-  }
-  for (int x = threadIdx.x; x < GP * D; x += kPselThreads) qs[x] = x < p.group * D ? (double)to_f32<T>(qh[x]) : 0.0;
-  for (int b = threadIdx.x; b < 2 * kPselBins; b += kPselThreads) hist[b] = 0u;
-  __syncthreads();
-
-  // One radix pass over this block's keys and the cluster's sum of its histogram: narrows prefix / mask / remaining by a digit.
-  unsigned int prefix = 0u, mask = 0u;
-  int remaining = p.keep;
-  auto radix_pass = [&](int pass) {
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
-    const unsigned int bins = pass == 2 ? 1024u : 2048u;
-    unsigned int* h = hist + (pass & 1) * kPselBins;           // alternate passes count into alternate histograms: one cluster
-    for (int c = threadIdx.x; c < hi - lo; c += kPselThreads) {    // barrier per pass is enough
-      const unsigned int key = keys[c];
-      if ((key & mask) == prefix) atomicAdd(&h[(key >> shift) & (bins - 1u)], 1u);
+  // a thread's scores: page (round * items + y) * threads + thread, so that a warp's 32 pages are one word of the bit maps
+  float v[kPselItems];
+  auto load_round = [&](int round) {
+#pragma unroll
+    for (int y = 0; y < kPselItems; ++y) {
+      const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
+      v[y] = c < n ? scores[c] : 0.f;
     }
-    cluster.sync();
-    // a thread owns four bins, from the top down
-    const int b0 = (int)bins - 4 - 4 * (int)threadIdx.x;
-    int c[4] = {0, 0, 0, 0};
-    if (b0 >= 0) {
+  };
+  load_round(0);
+  float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest |bound|, NaN or infinite where that cannot bound eps
+  const float* um = p.unit_max + (size_t)pair * pscore_units(p.width);
+  bool odd = false;
+  for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
+    const float f = um[x];
+    odd |= f != f;
+    limit = fmaxf(limit, f);
+  }
+  float norm = 0.f;                                            // sum |q| of the head this warp looks after
+  for (int h = warp; h < p.group; h += kWarps) {
+    float s = 0.f;
+    for (int d = lane; d < D; d += 32) s += fabsf(to_f32<T>(qh[h * D + d]));
+    norm = fmaxf(norm, warp_sum(s));
+  }
+  for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
+  if (threadIdx.x == 0) s_sure = s_listed = 0;
+  for (int round = 0; round < rounds; ++round) {
+    if (rounds > 1) load_round(round);
+#pragma unroll
+    for (int y = 0; y < kPselItems; ++y) {
+      const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
+      if (open_page(c)) {
+        top = fmaxf(top, v[y]);
+        bottom = fminf(bottom, v[y]);
+      }
+    }
+  }
+  top = warp_max(top);
+  bottom = -warp_max(-bottom);
+  limit = warp_max(limit);
+  if (lane == 0) {
+    red[0][warp] = top;
+    red[1][warp] = bottom;
+    red[2][warp] = limit;
+    scan[warp] = __float_as_int(norm);
+  }
+  odd = __syncthreads_or(odd);
+  norm = 0.f;
 #pragma unroll 8
-      for (int r = 0; r < CS; ++r) {
-        const uint4 four = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(h, r) + b0);
-        c[0] += (int)four.w;
-        c[1] += (int)four.z;
-        c[2] += (int)four.y;
-        c[3] += (int)four.x;
-      }
-    }
-    int all;
-    int above = block_prefix<kPselThreads>(c[0] + c[1] + c[2] + c[3], sh.scan, all);
-    if (above < remaining && above + c[0] + c[1] + c[2] + c[3] >= remaining) {
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        if (above < remaining && above + c[y] >= remaining) {
-          sh.digit = b0 + 3 - y;
-          sh.remaining = remaining - above;
-        }
-        above += c[y];
-      }
-    }
-    // the other histogram is free again (its readers have passed the barrier above): cleared for the next pass
-    unsigned int* other = hist + ((pass + 1) & 1) * kPselBins;
-    if (pass > 0)
-      for (int b = threadIdx.x; b < kPselBins; b += kPselThreads) other[b] = 0u;
+  for (int w = 0; w < kWarps; ++w) {
+    top = fmaxf(top, red[0][w]);
+    bottom = fminf(bottom, red[1][w]);
+    limit = fmaxf(limit, red[2][w]);
+    norm = fmaxf(norm, __int_as_float(scan[w]));
+  }
+  // eps = 2^-16 max_h sum |q| max |bound| covers 2 D products summed in fp32 by two chains of D / 16 instructions, each off
+  // by 2^-21 of the partial sums at most, which stay below sum |q| max |bound|
+  const float slack = 2.01f * 1.52587890625e-5f * norm * limit;
+  const float scale = top > bottom ? (kPselBins - 1) / (top - bottom) : 0.f;
+  // bin 0 holds the best scores; fp32 rounding keeps the order
+  auto bin_of = [&](float s) { return (int)fminf(fmaxf((top - s) * scale, 0.f), (float)(kPselBins - 1)); };
+  bool decided = !odd && slack < 1e30f && scale < 1e30f && top < 1e30f && bottom > -1e30f;
+  if (want == 0) {                                             // nothing to choose
+    for (int w = threadIdx.x; w < words; w += kPselThreads) kept[w] = 0u;
     __syncthreads();
-    prefix |= (unsigned int)sh.digit << shift;
-    mask |= (bins - 1u) << shift;
-    remaining = sh.remaining;
-  };
-
-  unsigned int threshold = 0u;           // pages with a larger key are kept, and the first take_equal of those with this one
-  int take_equal = 0;
-  bool decided = false;
-  if constexpr (kBf16) {
-    // ---- approximate scores: eight pages side by side, A = the queries' positive and negative parts (row: head), B = a page's
-    // bounds (column: page), the contraction index permuted as in paged_attention.cuh
-    constexpr int NH = GP > 8 ? 2 : 1;
-    constexpr int KC = D / 32;
-    uint4 pos[NH][KC], neg[NH][KC];
+    for (int c = threadIdx.x; c < p.n_first + p.n_last; c += kPselThreads) {
+      const int page = c < p.n_first ? c : n - p.n_last + (c - p.n_first);
+      atomicOr(&kept[page / 32], 1u << (page % 32));
+    }
+    __syncthreads();
+  } else if (decided) {
+    for (int round = 0; round < rounds; ++round) {
+      if (rounds > 1) load_round(round);
+#pragma unroll
+      for (int y = 0; y < kPselItems; ++y) {
+        const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
+        if (open_page(c)) atomicAdd(&hist[bin_of(v[y])], 1u);
+      }
+    }
+    __syncthreads();
     {
-      const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
-      const int r = lane / 4, c = lane % 4;
-#pragma unroll
-      for (int y = 0; y < NH; ++y) {
-        const int h = r + 8 * y;
-        float norm = 0.f;
-#pragma unroll
-        for (int x = 0; x < KC; ++x) {
-          const uint4 v = h < p.group ? *reinterpret_cast<const uint4*>(qh + (size_t)h * D + x * 32 + c * 8) : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          uint32_t a[4], b[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            __nv_bfloat162 t;
-            memcpy(&t, &w[e], 4);
-            const __nv_bfloat162 up = __hmax2_nan(t, zero), down = __hmin2_nan(t, zero);
-            memcpy(&a[e], &up, 4);
-            memcpy(&b[e], &down, 4);
-            norm += fabsf(__low2float(t)) + fabsf(__high2float(t));
-          }
-          pos[y][x] = make_uint4(a[0], a[1], a[2], a[3]);
-          neg[y][x] = make_uint4(b[0], b[1], b[2], b[3]);
-        }
-        norm += __shfl_xor_sync(0xffffffffu, norm, 1);
-        norm += __shfl_xor_sync(0xffffffffu, norm, 2);
-        norm = warp_max(norm);
-        if (warp == 0 && lane == 0) sh.q_norm = fmaxf(sh.q_norm, norm);
-      }
-    }
-    __nv_bfloat162 top2 = __floats2bfloat162_rn(0.f, 0.f);     // running max |bound| of this lane's pieces
-    bool odd = false;
-    for (int c0 = lo + warp * 8; c0 < hi; c0 += kWarps * 8) {
-      const int r = lane / 4, c = lane % 4;
-      const T* src = bounds + place(min(c0 + r, hi - 1)) + c * 8;
-      uint4 mn[KC], mx[KC];
-#pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        mn[x] = load_stream(reinterpret_cast<const uint4*>(src + x * 32));
-        mx[x] = load_stream(reinterpret_cast<const uint4*>(src + D + x * 32));
-      }
-      float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of dependent instructions
-#pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        mma_bf16(up, pos[0][x].x, NH > 1 ? pos[NH - 1][x].x : 0u, pos[0][x].y, NH > 1 ? pos[NH - 1][x].y : 0u, mx[x].x, mx[x].y);
-        mma_bf16(down, neg[0][x].x, NH > 1 ? neg[NH - 1][x].x : 0u, neg[0][x].y, NH > 1 ? neg[NH - 1][x].y : 0u, mn[x].x, mn[x].y);
-        mma_bf16(up, pos[0][x].z, NH > 1 ? pos[NH - 1][x].z : 0u, pos[0][x].w, NH > 1 ? pos[NH - 1][x].w : 0u, mx[x].z, mx[x].w);
-        mma_bf16(down, neg[0][x].z, NH > 1 ? neg[NH - 1][x].z : 0u, neg[0][x].w, NH > 1 ? neg[NH - 1][x].w : 0u, mn[x].z, mn[x].w);
-      }
-#pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        const uint32_t w[8] = {mn[x].x, mn[x].y, mn[x].z, mn[x].w, mx[x].x, mx[x].y, mx[x].z, mx[x].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          __nv_bfloat162 t;
-          memcpy(&t, &w[e], 4);
-          top2 = __hmax2_nan(top2, __habs2(t));
-        }
-      }
-      // the best head of pages 2c and 2c + 1
-      float best[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float a = r < p.group ? up[e] + down[e] : -INFINITY;
-        const float b = NH > 1 && r + 8 < p.group ? up[2 + e] + down[2 + e] : -INFINITY;
-        odd |= a != a || b != b;
-        best[e] = fmaxf(a, b);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) best[e] = fmaxf(best[e], __shfl_xor_sync(0xffffffffu, best[e], o));
-      }
-      if (r < 2) {
-        const int at = c0 + 2 * c + r;
-        if (at < hi) keys[at - lo] = forced(at) ? 0xffffffffu : page_key(best[r]);
-      }
-    }
-    const float top_abs = fmaxf(__low2float(top2), __high2float(top2));
-    odd |= __low2float(top2) != __low2float(top2) || __high2float(top2) != __high2float(top2) || top_abs == INFINITY;
-    const unsigned int top_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top_abs));
-    odd = __any_sync(0xffffffffu, odd);
-    if (lane == 0) {
-      atomicMax(&sh.max_abs, top_bits);
-      if (odd) atomicOr(&sh.undecided, 1);
+      const uint2 two = reinterpret_cast<const uint2*>(hist)[threadIdx.x];
+      int all;
+      const int before = block_prefix<kPselThreads>((int)(two.x + two.y), scan, all);
+      if (before < want && before + (int)(two.x + two.y) >= want) s_bin = 2 * threadIdx.x + (before + (int)two.x < want);
     }
     __syncthreads();
-    radix_pass(0);
-    radix_pass(1);
-    // The bounds of all blocks: eps = 2^-16 max_h sum |q| max |bound| covers 2 D products summed in fp32 by two chains of
-    // D / 16 instructions (each off by 2^-21 of the partial sums at most, which stay below sum |q| max |bound|).
-    float top_all = 0.f;
-    bool undecided = false;
-    for (int r = 0; r < CS; ++r) {
-      const SelectPagesShared* o = cluster.map_shared_rank(&sh, r);
-      top_all = fmaxf(top_all, __uint_as_float(o->max_abs));
-      undecided |= o->undecided != 0;
+    const int bin = s_bin;                                     // of the want-th largest approximate score
+    int sure = 0;
+    for (int round = 0; round < rounds; ++round) {
+      if (rounds > 1) load_round(round);
+#pragma unroll
+      for (int y = 0; y < kPselItems; ++y) {
+        const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
+        if (c - lane < n) {                                    // uniform over the warp
+          const bool is_open = open_page(c);
+          const bool better = is_open && bin_of(v[y] - slack) < bin;
+          const unsigned int word = __ballot_sync(0xffffffffu, better || (c < n && forced(c)));
+          if (lane == 0) kept[c / 32] = word;
+          sure += better;
+          if (is_open && !better && bin_of(v[y] + slack) <= bin) {
+            const int e = atomicAdd(&s_listed, 1);
+            if (e < kPselMaxDoubt) list[e] = make_uint2(page_key(v[y]), (unsigned int)c);
+          }
+        }
+      }
     }
-    const float eps = 1.52587890625e-5f * sh.q_norm * top_all;
-    const unsigned int k0 = prefix, k1 = prefix | 1023u;        // the keep-th approximate score lies in [k0, k1]
-    undecided |= !(eps < 1e30f) || k1 >= 0xff7fffffu || k0 <= 0x00800000u;
-    if (!undecided) {
-      const unsigned int low = page_key(key_score(k0) - 2.01f * eps), high = page_key(key_score(k1) + 2.01f * eps);
-      int sure = 0, doubt = 0;
-      for (int c = threadIdx.x; c < hi - lo; c += kPselThreads) {
-        sure += keys[c] > high;
-        doubt += keys[c] >= low && keys[c] <= high;
-      }
-      int all_sure, all_doubt;
-      block_prefix<kPselThreads>(sure, sh.scan, all_sure);
-      const int my_doubt = block_prefix<kPselThreads>(doubt, sh.scan, all_doubt);
-      if (threadIdx.x == 0) {
-        sh.sure = all_sure;
-        sh.doubtful = all_doubt;
-      }
-      cluster.sync();
-      int need = p.keep, before = 0, total = 0;
-      for (int r = 0; r < CS; ++r) {
-        const SelectPagesShared* o = cluster.map_shared_rank(&sh, r);
-        need -= o->sure;
-        if (r < rank) before += o->doubtful;
-        total += o->doubtful;
-      }
-      if (total <= kPselMaxDoubt) {                            // uniform over the cluster
-        // own doubtful pages onto block 0's list (any order), scored there by its owner's warps
-        uint2* all = cluster.map_shared_rank(list, 0);
-        int at = before + my_doubt;
-        for (int c = threadIdx.x; c < hi - lo; c += kPselThreads)
-          if (keys[c] >= low && keys[c] <= high) list[at++ - before].y = (unsigned int)c;      // staged here first
-        __syncthreads();
-        const int mine = all_doubt;
-        unsigned int my_page[(kPselMaxDoubt + kWarps - 1) / kWarps];
-#pragma unroll
-        for (int y = 0; y < (kPselMaxDoubt + kWarps - 1) / kWarps; ++y)
-          my_page[y] = y * kWarps + warp < mine ? list[y * kWarps + warp].y : 0u;
-        cluster.sync();                                        // block 0's own staging has been read
-#pragma unroll
-        for (int y = 0; y < (kPselMaxDoubt + kWarps - 1) / kWarps; ++y) {
-          const int e = y * kWarps + warp;
-          if (e < mine) {
-            const int c = lo + (int)my_page[y];
-            const T* src = bounds + place(c);
-            const float s = page_score_warp<T, D>(src, src + D, qs, p.group, lane);
-            if (lane == 0) all[before + e] = make_uint2(page_key(s), (unsigned int)c);
-          }
+    sure = __reduce_add_sync(0xffffffffu, sure);
+    if (lane == 0) atomicAdd(&s_sure, sure);
+    __syncthreads();
+    const int listed = s_listed, need = want - s_sure;
+    decided = listed <= kPselMaxDoubt;
+    if (decided) {
+      if constexpr (!kExact) {
+        for (int e = warp; e < listed; e += kWarps) {
+          const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[list[e].y], g, D), qh, p.group, lane);
+          if (lane == 0) list[e].x = page_key(s);
         }
-        cluster.sync();
-        // the `need` best of the list, ties to the lowest page: the kept ones get the highest key, the others the lowest
-        for (int e = warp; e < mine; e += kWarps) {
-          const uint2 me = all[before + e];
-          int better = 0;
-          for (int o = lane; o < total; o += 32) {
-            const uint2 x = all[o];
-            better += x.x > me.x || (x.x == me.x && x.y < me.y);
-          }
-          better = __reduce_add_sync(0xffffffffu, better);
-          if (lane == 0) keys[(int)me.y - lo] = better < need ? 0xffffffffu : 0u;
-        }
-        threshold = high;
-        decided = true;
         __syncthreads();
       }
+      if ((int)threadIdx.x < listed) {                         // the `need` best of the list, ties to the lowest page
+        const uint2 me = list[threadIdx.x];
+        int better = 0;
+#pragma unroll 4
+        for (int o = 0; o < listed; ++o) {
+          const uint2 x = list[o];
+          better += x.x > me.x || (x.x == me.x && x.y < me.y);
+        }
+        if (better < need) atomicOr(&kept[me.y / 32], 1u << (me.y % 32));
+      }
+      __syncthreads();
     }
   }
-  if (!decided) {
-    // ---- every page in 64 bits: four lanes to a page, eight pages side by side
-    if constexpr (kBf16) {
-      cluster.sync();                                          // nobody still reads the histograms
-      for (int b = threadIdx.x; b < 2 * kPselBins; b += kPselThreads) hist[b] = 0u;
-      prefix = mask = 0u;
-      remaining = p.keep;
-    }
-    const int sub = lane / 4, quarter = lane % 4;
-    for (int c0 = lo + warp * 8; c0 < hi; c0 += kWarps * 8) {
-      const uint4* src = reinterpret_cast<const uint4*>(bounds + place(min(c0 + sub, hi - 1))) + quarter;
-      double acc[GP];
-#pragma unroll
-      for (int h = 0; h < GP; ++h) acc[h] = 0.0;
-#pragma unroll 1
-      for (int x = 0; x < X; ++x) {
-        float mn[E], mx[E];
-        RopeVec<T>::unpack(src[x * 4], mn);
-        RopeVec<T>::unpack(src[D / E + x * 4], mx);
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const double n0 = (double)mn[e], n1 = (double)mn[e + 1], x0 = (double)mx[e], x1 = (double)mx[e + 1];
-#pragma unroll
-          for (int h = 0; h < GP; ++h) {
-            const double2 qv = *reinterpret_cast<const double2*>(qs + h * D + x * 4 * E + quarter * E + e);
-            acc[h] = fma(qv.x, qv.x >= 0.0 ? x0 : n0, acc[h]);
-            acc[h] = fma(qv.y, qv.y >= 0.0 ? x1 : n1, acc[h]);
-          }
-        }
+  if (want > 0 && !decided) {
+    // ---- every page in 64 bits (into the scores' place), and radix passes to the last bit
+    float* exact = p.scores + (size_t)pair * p.width;
+    if constexpr (!kExact) {
+      for (int c = warp; c < n; c += kWarps) {
+        const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[c], g, D), qh, p.group, lane);
+        if (lane == 0) exact[c] = s;
       }
-      float best = -INFINITY;
-      bool nan = false;
-#pragma unroll
-      for (int h = 0; h < GP; ++h) {
-        double s = acc[h];
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        s += __shfl_xor_sync(0xffffffffu, s, 2);
-        const float f = (float)s;
-        if (h < p.group) {
-          nan |= f != f;
-          best = fmaxf(best, f);
-        }
-      }
-      const int c = c0 + sub;
-      if (quarter == 0 && c < hi) keys[c - lo] = forced(c) ? 0xffffffffu : page_key(nan ? NAN : best);
     }
     __syncthreads();
+    unsigned int prefix = 0u, mask = 0u;
+    int remaining = want;
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) radix_pass(pass);
-    threshold = prefix;
-    take_equal = remaining;                                    // keys equal to the threshold that are kept, lowest pages first
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+      const unsigned int bins = pass == 2 ? 1024u : 2048u;
+      for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
+      __syncthreads();
+      for (int c = threadIdx.x; c < n; c += kPselThreads) {
+        const unsigned int key = page_key(exact[c]);
+        if (!forced(c) && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1u)], 1u);
+      }
+      __syncthreads();
+      const int b0 = (int)bins - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;          // from the top down
+      const int n0 = b1 >= 0 ? (int)hist[b0] : 0, n1 = b1 >= 0 ? (int)hist[b1] : 0;
+      int all;
+      const int above = block_prefix<kPselThreads>(n0 + n1, scan, all);
+      if (above < remaining && above + n0 + n1 >= remaining) {
+        s_bin = above + n0 >= remaining ? b0 : b1;
+        s_need = above + n0 >= remaining ? remaining - above : remaining - above - n0;
+      }
+      __syncthreads();
+      prefix |= (unsigned int)s_bin << shift;
+      mask |= (bins - 1u) << shift;
+      remaining = s_need;
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < words * 32; c += kPselThreads) {             // words * 32 and the stride keep warps whole
+      const unsigned int key = c < n ? page_key(exact[c]) : 0u;
+      const unsigned int above = __ballot_sync(0xffffffffu, c < n && (forced(c) || key > prefix));
+      const unsigned int same = __ballot_sync(0xffffffffu, open_page(c) && key == prefix);
+      if (lane == 0) {
+        kept[c / 32] = above;
+        equal[c / 32] = same;
+      }
+    }
+    __syncthreads();
+    int before = 0;
+    for (int w0 = 0; w0 < words; w0 += kPselThreads) {         // of equal keys the lowest pages
+      const int w = w0 + (int)threadIdx.x;
+      unsigned int same = w < words ? equal[w] : 0u;
+      int all;
+      int rank = before + block_prefix<kPselThreads>(__popc(same), scan, all);
+      before += all;
+      while (same && rank < remaining) {
+        const unsigned int bit = same & (0u - same);
+        kept[w] |= bit;
+        same ^= bit;
+        ++rank;
+      }
+    }
+    __syncthreads();
   }
 
   // ---- kept pages, in order
-  int sure = 0, equal = 0;
-  for (int c = threadIdx.x; c < hi - lo; c += kPselThreads) {
-    sure += keys[c] > threshold;
-    equal += keys[c] == threshold;
+  int before = 0;
+  for (int w0 = 0; w0 < words; w0 += kPselThreads) {
+    const int w = w0 + (int)threadIdx.x;
+    unsigned int bits = w < words ? kept[w] : 0u;
+    int all;
+    int at = before + block_prefix<kPselThreads>(__popc(bits), scan, all);
+    before += all;
+    while (bits) {
+      const int b = __ffs((int)bits) - 1;
+      bits &= bits - 1u;
+      out[at++] = w * 32 + b;
+    }
   }
-  int all_sure, all_equal;
-  block_prefix<kPselThreads>(sure, sh.scan, all_sure);
-  block_prefix<kPselThreads>(equal, sh.scan, all_equal);
-  if (threadIdx.x == 0) {
-    sh.sure = all_sure;
-    sh.equal = all_equal;
-  }
-  cluster.sync();
-  int kept_before = 0, equal_before = 0;
-  for (int r = 0; r < rank; ++r) {
-    const SelectPagesShared* o = cluster.map_shared_rank(&sh, r);
-    const int e = o->equal;
-    kept_before += o->sure + min(max(take_equal - equal_before, 0), e);
-    equal_before += e;
-  }
-  for (int c0 = 0; c0 < hi - lo; c0 += kPselThreads) {
-    const int c = c0 + (int)threadIdx.x;
-    const unsigned int key = c < hi - lo ? keys[c] : 0u;
-    const bool is_equal = c < hi - lo && key == threshold;
-    int eq_total, keep_total;
-    const int eq_rank = equal_before + block_prefix<kPselThreads>((int)is_equal, sh.scan, eq_total);
-    const bool kept = c < hi - lo && (key > threshold || (is_equal && eq_rank < take_equal));
-    const int pos = kept_before + block_prefix<kPselThreads>((int)kept, sh.scan, keep_total);
-    if (kept) out[pos] = lo + c;
-    kept_before += keep_total;
-    equal_before += eq_total;
-  }
-  cluster.sync();                                              // no block leaves while another may still read its counters
 }
 
 }  // namespace meda
