@@ -108,7 +108,7 @@ struct SelectPagesKernels {
   static meda_status launch(meda_pages* p, const SelectPagesParams& a, cudaStream_t st) {
     p->launches += 2;
     page_scores_kernel<T, D, GP><<<p->sm_count * 2, kPscoreThreads, (size_t)(a.n_seqs + 1) * 4, st>>>(a);
-    choose_pages_kernel<T, D><<<a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width), st>>>(a);
+    choose_pages_kernel<T, D><<<a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width, a.group, D), st>>>(a);
     return launch_status();
   }
 };

@@ -27,8 +27,9 @@ namespace meda {
 constexpr int kPagesMaxSeqs = 8192;
 constexpr int kPagesMaxSeqPages = 262144;
 
-// Exclusive prefix of `v` over a block of THREADS threads in thread order, and the block total.
-// `scratch` holds THREADS / 32 + 1 values.
+// Exclusive prefix of `v` over a block of THREADS threads (1024 at most) in thread order, and the block total.
+// `scratch` holds THREADS / 32 values; two barriers.  Every warp scans the warps' sums by itself, one value per lane: reading
+// them all in every thread would keep the shared memory busy for THREADS cycles.
 template <int THREADS, typename V>
 __device__ __forceinline__ V block_prefix(V v, V* scratch, V& total) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -41,15 +42,15 @@ __device__ __forceinline__ V block_prefix(V v, V* scratch, V& total) {
   __syncthreads();                      // previous users of scratch are done
   if (lane == 31) scratch[warp] = incl;
   __syncthreads();
-  V before = 0, all = 0;
+  V sums = lane < THREADS / 32 ? scratch[lane] : 0;
 #pragma unroll
-  for (int x = 0; x < THREADS / 32; ++x) {
-    const V c = scratch[x];
-    before += x < warp ? c : 0;
-    all += c;
+  for (int o = 1; o < THREADS / 32; o <<= 1) {
+    const V y = __shfl_up_sync(0xffffffffu, sums, o);
+    if (lane >= o) sums += y;
   }
-  total = all;
-  return before + incl - v;
+  total = __shfl_sync(0xffffffffu, sums, 31);
+  const V before = __shfl_sync(0xffffffffu, sums, (warp + 31) % 32);
+  return (warp ? before : 0) + incl - v;
 }
 
 // A sequence's length as the kernels use it: out-of-range values are cut to the nearest valid one.

@@ -39,8 +39,8 @@ struct SelectPagesParams {
   const int32_t* lens;
   int32_t* sel;
   float* scores;                         // [n_seqs * n_heads][width]
-  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: largest |bound| of a unit's pages, NaN
-                                         // where a score is not finite; 0 where the scores are exact
+  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: max_h sum |q| times the largest |bound|
+                                         // of a unit's pages, NaN where a score is not finite; 0 where the scores are exact
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep, n_first, n_last;
   InvariantDiv heads_div;
@@ -90,6 +90,7 @@ page_scores_kernel(SelectPagesParams p) {
   const int u0 = (int)min(me * per, total), u1 = (int)min((me + 1) * per, total);
 
   uint4 pos[NH][X], neg[NH][X];                                // bf16: the queries' positive and negative parts as fragments
+  float norm = 0.f;                                            // max_h sum |q|
   int held = -1, i = 0, g = 0, units = 0, n = 0, first_unit = 0;
   for (int u = u0; u < u1; ++u) {
     if (u >= first_unit + units) {                             // the next (sequence, KV head)
@@ -114,9 +115,11 @@ page_scores_kernel(SelectPagesParams p) {
       if (pair != held) {
         held = pair;
         const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+        norm = 0.f;
 #pragma unroll
         for (int y = 0; y < NH; ++y) {
           const int h = r + 8 * y;
+          float sum = 0.f;
 #pragma unroll
           for (int x = 0; x < X; ++x) {
             const uint4 v = h < p.group ? *reinterpret_cast<const uint4*>(qh + (size_t)h * D + x * 32 + c * 8) : make_uint4(0, 0, 0, 0);
@@ -129,10 +132,14 @@ page_scores_kernel(SelectPagesParams p) {
               const __nv_bfloat162 up = __hmax2_nan(t, zero), down = __hmin2_nan(t, zero);
               memcpy(&a[e], &up, 4);
               memcpy(&b[e], &down, 4);
+              sum += fabsf(__low2float(t)) + fabsf(__high2float(t));
             }
             pos[y][x] = make_uint4(a[0], a[1], a[2], a[3]);
             neg[y][x] = make_uint4(b[0], b[1], b[2], b[3]);
           }
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          norm = fmaxf(norm, warp_max(sum));
         }
       }
       // A = queries (row: head), B = bounds (column: page), the contraction index permuted as in paged_attention.cuh
@@ -168,7 +175,7 @@ page_scores_kernel(SelectPagesParams p) {
       const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(t0, t1))));
       odd = __any_sync(0xffffffffu, odd);
       if (r < 2 && c0 + 2 * c + r < n) p.scores[(size_t)pair * p.width + c0 + 2 * c + r] = best[r];
-      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top;
+      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top * norm;
     } else {
       const uint4* src = reinterpret_cast<const uint4*>(bounds + at) + c;
       double acc[GP];
@@ -207,9 +214,9 @@ page_scores_kernel(SelectPagesParams p) {
   }
 }
 
-// The score of one page for one KV head by a whole warp, in 64 bits.  qh: the head's queries [group][D].
+// The score of one page for one KV head by a whole warp, in 64 bits.  qh: the head's queries [group][D] as floats.
 template <typename T, int D>
-__device__ __forceinline__ float page_score_warp(const T* lo, const T* qh, int group, int lane) {
+__device__ __forceinline__ float page_score_warp(const T* lo, const float* qh, int group, int lane) {
   constexpr int N = D / 32;
   double mn[N], mx[N];
 #pragma unroll
@@ -224,7 +231,7 @@ __device__ __forceinline__ float page_score_warp(const T* lo, const T* qh, int g
     double s = 0.0;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const double q = (double)to_f32<T>(qh[h * D + e * 32 + lane]);
+      const double q = (double)qh[h * D + e * 32 + lane];
       s = fma(q, q >= 0.0 ? mx[e] : mn[e], s);
     }
 #pragma unroll
@@ -237,21 +244,24 @@ __device__ __forceinline__ float page_score_warp(const T* lo, const T* qh, int g
 }
 
 // ---- the choice, one block per (sequence, KV head) ---------------------------------------------------------
-__host__ __device__ inline int choose_smem(int width) { return 2 * ((width + 31) / 32) * 4; }     // two bits per page
+// Shared memory: the queries as floats, two bits per page.
+__host__ __device__ inline int choose_smem(int width, int group, int d) { return (group * d + 2 * ((width + 31) / 32)) * 4; }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kPselThreads, 1)
 choose_pages_kernel(SelectPagesParams p) {
   constexpr bool kExact = sizeof(T) == 4;                      // the scores are the 64-bit ones already
   constexpr int kWarps = kPselThreads / 32;
-  extern __shared__ __align__(16) unsigned int choose_bits[];
+  extern __shared__ __align__(16) float choose_smem_base[];
   __shared__ unsigned int hist[kPselBins];
   __shared__ uint2 list[kPselMaxDoubt];                        // (key, page) of the pages in doubt
-  __shared__ int scan[kWarps + 1];
+  __shared__ int listed_page[kPselMaxDoubt];                   // their table entries
+  __shared__ int scan[kWarps];
   __shared__ float red[3][kWarps];
   __shared__ int s_bin, s_need, s_sure, s_listed;
-  unsigned int* kept = choose_bits;                            // [words]
-  unsigned int* equal = choose_bits + (p.width + 31) / 32;     // [words], the fallback's
+  float* qs = choose_smem_base;                                // [group][D]
+  unsigned int* kept = reinterpret_cast<unsigned int*>(qs + p.group * D);      // [words]
+  unsigned int* equal = kept + (p.width + 31) / 32;            // [words], the fallback's
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int pair = blockIdx.x, i = p.heads_div.of(pair), g = pair - i * p.n_heads;
   const int page_size = 1 << p.page_shift;
@@ -274,15 +284,17 @@ choose_pages_kernel(SelectPagesParams p) {
 
   // a thread's scores: page (round * items + y) * threads + thread, so that a warp's 32 pages are one word of the bit maps
   float v[kPselItems];
+  auto page_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads + (int)threadIdx.x; };
+  auto any_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads < n; };       // uniform
   auto load_round = [&](int round) {
 #pragma unroll
     for (int y = 0; y < kPselItems; ++y) {
-      const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
-      v[y] = c < n ? scores[c] : 0.f;
+      const int c = page_at(round, y);
+      if (any_at(round, y)) v[y] = c < n ? scores[c] : 0.f;
     }
   };
   load_round(0);
-  float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest |bound|, NaN or infinite where that cannot bound eps
+  float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: max_h sum |q| times the largest |bound|
   const float* um = p.unit_max + (size_t)pair * pscore_units(p.width);
   bool odd = false;
   for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
@@ -290,46 +302,34 @@ choose_pages_kernel(SelectPagesParams p) {
     odd |= f != f;
     limit = fmaxf(limit, f);
   }
-  float norm = 0.f;                                            // sum |q| of the head this warp looks after
-  for (int h = warp; h < p.group; h += kWarps) {
-    float s = 0.f;
-    for (int d = lane; d < D; d += 32) s += fabsf(to_f32<T>(qh[h * D + d]));
-    norm = fmaxf(norm, warp_sum(s));
-  }
+  if constexpr (!kExact)
+    for (int x = threadIdx.x; x < p.group * D; x += kPselThreads) qs[x] = to_f32<T>(qh[x]);
   for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
   if (threadIdx.x == 0) s_sure = s_listed = 0;
   for (int round = 0; round < rounds; ++round) {
     if (rounds > 1) load_round(round);
 #pragma unroll
-    for (int y = 0; y < kPselItems; ++y) {
-      const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
-      if (open_page(c)) {
+    for (int y = 0; y < kPselItems; ++y)
+      if (any_at(round, y) && open_page(page_at(round, y))) {
         top = fmaxf(top, v[y]);
         bottom = fminf(bottom, v[y]);
       }
-    }
   }
   top = warp_max(top);
   bottom = -warp_max(-bottom);
   limit = warp_max(limit);
   if (lane == 0) {
     red[0][warp] = top;
-    red[1][warp] = bottom;
+    red[1][warp] = -bottom;
     red[2][warp] = limit;
-    scan[warp] = __float_as_int(norm);
   }
   odd = __syncthreads_or(odd);
-  norm = 0.f;
-#pragma unroll 8
-  for (int w = 0; w < kWarps; ++w) {
-    top = fmaxf(top, red[0][w]);
-    bottom = fminf(bottom, red[1][w]);
-    limit = fmaxf(limit, red[2][w]);
-    norm = fmaxf(norm, __int_as_float(scan[w]));
-  }
+  top = warp_max(red[0][lane]);
+  bottom = -warp_max(red[1][lane]);
+  limit = warp_max(red[2][lane]);
   // eps = 2^-16 max_h sum |q| max |bound| covers 2 D products summed in fp32 by two chains of D / 16 instructions, each off
   // by 2^-21 of the partial sums at most, which stay below sum |q| max |bound|
-  const float slack = 2.01f * 1.52587890625e-5f * norm * limit;
+  const float slack = 2.01f * 1.52587890625e-5f * limit;
   const float scale = top > bottom ? (kPselBins - 1) / (top - bottom) : 0.f;
   // bin 0 holds the best scores; fp32 rounding keeps the order
   auto bin_of = [&](float s) { return (int)fminf(fmaxf((top - s) * scale, 0.f), (float)(kPselBins - 1)); };
@@ -346,10 +346,8 @@ choose_pages_kernel(SelectPagesParams p) {
     for (int round = 0; round < rounds; ++round) {
       if (rounds > 1) load_round(round);
 #pragma unroll
-      for (int y = 0; y < kPselItems; ++y) {
-        const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
-        if (open_page(c)) atomicAdd(&hist[bin_of(v[y])], 1u);
-      }
+      for (int y = 0; y < kPselItems; ++y)
+        if (any_at(round, y) && open_page(page_at(round, y))) atomicAdd(&hist[bin_of(v[y])], 1u);
     }
     __syncthreads();
     {
@@ -365,8 +363,8 @@ choose_pages_kernel(SelectPagesParams p) {
       if (rounds > 1) load_round(round);
 #pragma unroll
       for (int y = 0; y < kPselItems; ++y) {
-        const int c = (round * kPselItems + y) * kPselThreads + (int)threadIdx.x;
-        if (c - lane < n) {                                    // uniform over the warp
+        const int c = page_at(round, y);
+        if (any_at(round, y) && c - lane < n) {                // uniform over the warp
           const bool is_open = open_page(c);
           const bool better = is_open && bin_of(v[y] - slack) < bin;
           const unsigned int word = __ballot_sync(0xffffffffu, better || (c < n && forced(c)));
@@ -374,7 +372,10 @@ choose_pages_kernel(SelectPagesParams p) {
           sure += better;
           if (is_open && !better && bin_of(v[y] + slack) <= bin) {
             const int e = atomicAdd(&s_listed, 1);
-            if (e < kPselMaxDoubt) list[e] = make_uint2(page_key(v[y]), (unsigned int)c);
+            if (e < kPselMaxDoubt) {
+              list[e] = make_uint2(page_key(v[y]), (unsigned int)c);
+              if constexpr (!kExact) listed_page[e] = table[c];
+            }
           }
         }
       }
@@ -387,7 +388,7 @@ choose_pages_kernel(SelectPagesParams p) {
     if (decided) {
       if constexpr (!kExact) {
         for (int e = warp; e < listed; e += kWarps) {
-          const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[list[e].y], g, D), qh, p.group, lane);
+          const float s = page_score_warp<T, D>(bounds + bounds_place(p, listed_page[e], g, D), qs, p.group, lane);
           if (lane == 0) list[e].x = page_key(s);
         }
         __syncthreads();
@@ -410,7 +411,7 @@ choose_pages_kernel(SelectPagesParams p) {
     float* exact = p.scores + (size_t)pair * p.width;
     if constexpr (!kExact) {
       for (int c = warp; c < n; c += kWarps) {
-        const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[c], g, D), qh, p.group, lane);
+        const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[c], g, D), qs, p.group, lane);
         if (lane == 0) exact[c] = s;
       }
     }
