@@ -112,6 +112,7 @@ struct RowsParams {
 template <typename T, int VR, bool STORE>
 __global__ void __launch_bounds__(kRowsThreads)
 page_rows_kernel(RowsParams p) {
+  begin_grid();
   extern __shared__ __align__(16) int rows_smem[];
   __shared__ int scratch[kRowsThreads / 32 + 1];
   constexpr int kCols = VR > 32 ? VR / 32 : 1;           // vectors of a row per lane

@@ -371,6 +371,7 @@ paged_attention_kernel(AttnParams p) {
   constexpr int HP = Tile::kHeads;
   constexpr int LD = D + 4;
   constexpr int kStates = attn_merge_floats(W, HP, D);
+  begin_grid();
   extern __shared__ __align__(16) float att_smem[];
   __shared__ int scratch[W + 1];
   __shared__ unsigned int s_arrived[2];

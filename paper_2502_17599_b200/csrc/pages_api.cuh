@@ -36,6 +36,25 @@ struct PagesDevice {
   }
 };
 
+// A launch that may be set up before the kernels ahead of it in the stream have finished (they and it start with begin_grid).
+template <typename K, typename P>
+meda_status launch_after(meda_pages* p, K kernel, int grid, int block, size_t smem, cudaStream_t st, const P& params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  ++p->launches;
+  if (cudaLaunchKernelEx(&cfg, kernel, params) == cudaSuccess) return MEDA_OK;
+  cudaGetLastError();
+  return MEDA_ERR_CUDA;
+}
+
 inline bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
 
 int pages_element(const meda_pages* p) { return p->cfg.dtype == MEDA_F32 ? 4 : 2; }
@@ -70,11 +89,9 @@ struct AttnKernel {
     return MEDA_OK;
   }
   static meda_status launch(meda_pages* p, AttnParams a, cudaStream_t st) {
-    ++p->launches;
     a.heads_div.set((unsigned)(a.n_heads * ((a.group + Tile::kHeads - 1) / Tile::kHeads)));
     a.grid_div.set((unsigned)p->attn_blocks);
-    kernel<<<p->attn_blocks, W * 32, smem(a.n_seqs), st>>>(a);
-    return launch_status();
+    return launch_after(p, kernel, p->attn_blocks, W * 32, smem(a.n_seqs), st, a);
   }
 };
 
@@ -106,10 +123,11 @@ struct SelectPagesKernels {
     return r == MEDA_OK ? raise_dyn_smem(choose_pages_kernel<T, D>) : r;
   }
   static meda_status launch(meda_pages* p, const SelectPagesParams& a, cudaStream_t st) {
-    p->launches += 2;
-    page_scores_kernel<T, D, GP><<<p->sm_count * 2, kPscoreThreads, (size_t)(a.n_seqs + 1) * 4, st>>>(a);
-    choose_pages_kernel<T, D><<<a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width, a.group, D), st>>>(a);
-    return launch_status();
+    // two blocks per SM, and no more (see tables_smem)
+    const size_t smem = std::max<size_t>((size_t)(a.n_seqs + 1) * 4, 77 * 1024);
+    const meda_status r = launch_after(p, page_scores_kernel<T, D, GP>, p->sm_count * 2, kPscoreThreads, smem, st, a);
+    if (r != MEDA_OK) return r;
+    return launch_after(p, choose_pages_kernel<T, D>, a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width, a.group, D), st, a);
   }
 };
 
@@ -143,20 +161,13 @@ int select_scratch_seqs(const meda_pages_config& c) {
 // ---- pages of rows -----------------------------------------------------------------------------
 template <bool STORE>
 meda_status launch_page_rows(meda_pages* p, const RowsParams& a, cudaStream_t st) {
-  ++p->launches;
-  const int grid = p->sm_count * 4;
-  const size_t smem = (size_t)(a.n_seqs + 1) * 4;
   const int vr = p->cfg.head_dim * pages_element(p) / 16;
-  if (p->cfg.dtype == MEDA_F32) {
-    if (vr == 16) page_rows_kernel<float, 16, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-    else if (vr == 32) page_rows_kernel<float, 32, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-    else page_rows_kernel<float, 64, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-  } else {
-    if (vr == 8) page_rows_kernel<__nv_bfloat16, 8, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-    else if (vr == 16) page_rows_kernel<__nv_bfloat16, 16, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-    else page_rows_kernel<__nv_bfloat16, 32, STORE><<<grid, kRowsThreads, smem, st>>>(a);
-  }
-  return launch_status();
+  auto go = [&](auto kernel) { return launch_after(p, kernel, p->sm_count * 4, kRowsThreads, (size_t)(a.n_seqs + 1) * 4, st, a); };
+  if (p->cfg.dtype == MEDA_F32)
+    return vr == 16 ? go(page_rows_kernel<float, 16, STORE>) : vr == 32 ? go(page_rows_kernel<float, 32, STORE>)
+                                                                        : go(page_rows_kernel<float, 64, STORE>);
+  return vr == 8 ? go(page_rows_kernel<__nv_bfloat16, 8, STORE>) : vr == 16 ? go(page_rows_kernel<__nv_bfloat16, 16, STORE>)
+                                                                           : go(page_rows_kernel<__nv_bfloat16, 32, STORE>);
 }
 
 template <bool STORE>
@@ -171,10 +182,11 @@ meda_status raise_page_rows_smem() {
 }
 
 template <typename T, bool ADJACENT>
-void launch_rope(const RopeParams& a, int d, int grid, cudaStream_t st) {
-  if (d == 64) rope_append_kernel<T, 64, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
-  else if (d == 128) rope_append_kernel<T, 128, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
-  else rope_append_kernel<T, 256, ADJACENT><<<grid, kRopeThreads, 0, st>>>(a);
+meda_status launch_rope(meda_pages* p, const RopeParams& a, int grid, cudaStream_t st) {
+  auto go = [&](auto kernel) { return launch_after(p, kernel, grid, kRopeThreads, 0, st, a); };
+  const int d = p->cfg.head_dim;
+  return d == 64 ? go(rope_append_kernel<T, 64, ADJACENT>) : d == 128 ? go(rope_append_kernel<T, 128, ADJACENT>)
+                                                                    : go(rope_append_kernel<T, 256, ADJACENT>);
 }
 
 void pages_release(meda_pages* p) {
@@ -305,9 +317,7 @@ meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t len
   const int64_t units = slots_capacity ? (slots_capacity >> pages->page_shift) + 2 * (int64_t)n_seqs
                                        : std::min<int64_t>(c.n_pages, (int64_t)n_seqs * c.max_seq_pages);
   const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (units + kTabThreads - 1) / kTabThreads));
-  ++pages->launches;
-  page_tables_kernel<<<grid, kTabThreads, tables_smem(n_seqs), as_stream(stream)>>>(a);
-  return launch_status();
+  return launch_after(pages, page_tables_kernel, grid, kTabThreads, tables_smem(n_seqs), as_stream(stream), a);
 }
 
 meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int64_t seq_stride, int64_t head_stride,
@@ -367,17 +377,10 @@ meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride,
                   q_stride / e, k_stride / e, v_stride / e, axis_stride, (long long)c.n_pages << pages->page_shift,
                   n_tokens, c.n_q_heads, c.n_kv_heads, half, pages->page_shift, tokens};
   const int grid = (n_tokens + tokens - 1) / tokens;
-  ++pages->launches;
   cudaStream_t st = as_stream(stream);
   const bool adjacent = c.rope_pairing == MEDA_ROPE_ADJACENT;
-  if (c.dtype == MEDA_F32) {
-    if (adjacent) launch_rope<float, true>(a, c.head_dim, grid, st);
-    else launch_rope<float, false>(a, c.head_dim, grid, st);
-  } else {
-    if (adjacent) launch_rope<__nv_bfloat16, true>(a, c.head_dim, grid, st);
-    else launch_rope<__nv_bfloat16, false>(a, c.head_dim, grid, st);
-  }
-  return launch_status();
+  if (c.dtype == MEDA_F32) return adjacent ? launch_rope<float, true>(pages, a, grid, st) : launch_rope<float, false>(pages, a, grid, st);
+  return adjacent ? launch_rope<__nv_bfloat16, true>(pages, a, grid, st) : launch_rope<__nv_bfloat16, false>(pages, a, grid, st);
 }
 
 meda_status meda_select_pages(meda_pages* pages, const void* q, const void* bounds, const int32_t* table,

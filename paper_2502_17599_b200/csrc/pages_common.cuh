@@ -27,6 +27,14 @@ namespace meda {
 constexpr int kPagesMaxSeqs = 8192;
 constexpr int kPagesMaxSeqPages = 262144;
 
+// Every kernel of the paged caches starts with this.  The launches are programmatic (see launch_after): the next kernel of
+// the stream may be set up while this one still runs, and waits here, before it touches any memory, until all before it
+// has finished and its writes are visible.  A kernel takes 3 to 10 us on a decoding step; 1 to 2 of them were the gap.
+__device__ __forceinline__ void begin_grid() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Exclusive prefix of `v` over a block of THREADS threads (1024 at most) in thread order, and the block total.
 // `scratch` holds THREADS / 32 values; two barriers.  Every warp scans the warps' sums by itself, one value per lane: reading
 // them all in every thread would keep the shared memory busy for THREADS cycles.

@@ -75,6 +75,7 @@ template <typename T, int D, bool ADJACENT>
 __global__ void __launch_bounds__(kRopeThreads)
 rope_append_kernel(RopeParams p) {
   constexpr int E = RopeVec<T>::E;
+  begin_grid();
   constexpr int VR = D / E;                                    // vectors per head
   __shared__ float2 turn[kRopeMaxTokens][D / 2];               // (cos, sin)
   __shared__ int64_t slot_of[kRopeMaxTokens];

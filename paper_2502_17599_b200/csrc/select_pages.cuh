@@ -6,11 +6,12 @@
 // the bounds does (100 us instead of 4 for 8,067 pages of 4 KV heads with 7 query heads each), so bf16 caches go
 // two ways at once:
 //   - page_scores_kernel gives every page an approximate score from the matrix instructions, max(q, 0) . max + min(q, 0) . min
-//     (products of bf16 are exact, the fp32 sum is off by eps at most), with the whole GPU;
+//     (products of bf16 are exact, the fp32 sum is off by eps at most), with the whole GPU; the same instructions on |min| and |max|
+//     give sum |q| |bound|, which eps is proportional to;
 //   - choose_pages_kernel, one block per (sequence, KV head), finds the keep-th largest of them to one of 2,048 equal bins
-//     between the smallest and the largest score.  A page that stays in a better bin when its score is lowered by 2 eps is kept, one
-//     that stays in a worse bin when it is raised by 2 eps is not (the true keep-th score lies within eps of the
-//     approximate one), and the few in between are scored again in 64 bits and ranked among themselves.
+//     between the smallest and the largest score.  A page more than 2 eps above that bin is kept, one more than 2 eps below it
+//     is not (the true keep-th score lies within eps of the approximate one), and the few in between are scored again
+//     in 64 bits and ranked among themselves.
 // Where that cannot decide (an infinity or a NaN, more than kPselMaxDoubt pages in between) the block scores all its
 // pages in 64 bits and finds the keep-th by radix passes to the last bit.  fp32 caches get 64-bit scores at once.
 //
@@ -39,8 +40,8 @@ struct SelectPagesParams {
   const int32_t* lens;
   int32_t* sel;
   float* scores;                         // [n_seqs * n_heads][width]
-  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: max_h sum |q| times the largest |bound|
-                                         // of a unit's pages, NaN where a score is not finite; 0 where the scores are exact
+  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: largest sum |q| |bound| among a unit's
+                                         // pages and heads, not finite where a score is not; 0 where the scores are exact
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep, n_first, n_last;
   InvariantDiv heads_div;
@@ -71,6 +72,7 @@ page_scores_kernel(SelectPagesParams p) {
   constexpr int E = RopeVec<T>::E;                             // elements per 16-byte vector
   constexpr int X = D / (4 * E);                               // vectors of a bound per lane
   constexpr int NH = GP > 8 ? 2 : 1;
+  begin_grid();
   extern __shared__ __align__(16) int pscore_smem[];
   __shared__ int scratch[kPscoreThreads / 32 + 1];
   int* pre = pscore_smem;                                      // [n + 1] units before sequence i (of one KV head)
@@ -90,7 +92,6 @@ page_scores_kernel(SelectPagesParams p) {
   const int u0 = (int)min(me * per, total), u1 = (int)min((me + 1) * per, total);
 
   uint4 pos[NH][X], neg[NH][X];                                // bf16: the queries' positive and negative parts as fragments
-  float norm = 0.f;                                            // max_h sum |q|
   int held = -1, i = 0, g = 0, units = 0, n = 0, first_unit = 0;
   for (int u = u0; u < u1; ++u) {
     if (u >= first_unit + units) {                             // the next (sequence, KV head)
@@ -115,11 +116,9 @@ page_scores_kernel(SelectPagesParams p) {
       if (pair != held) {
         held = pair;
         const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
-        norm = 0.f;
 #pragma unroll
         for (int y = 0; y < NH; ++y) {
           const int h = r + 8 * y;
-          float sum = 0.f;
 #pragma unroll
           for (int x = 0; x < X; ++x) {
             const uint4 v = h < p.group ? *reinterpret_cast<const uint4*>(qh + (size_t)h * D + x * 32 + c * 8) : make_uint4(0, 0, 0, 0);
@@ -132,50 +131,44 @@ page_scores_kernel(SelectPagesParams p) {
               const __nv_bfloat162 up = __hmax2_nan(t, zero), down = __hmin2_nan(t, zero);
               memcpy(&a[e], &up, 4);
               memcpy(&b[e], &down, 4);
-              sum += fabsf(__low2float(t)) + fabsf(__high2float(t));
             }
             pos[y][x] = make_uint4(a[0], a[1], a[2], a[3]);
             neg[y][x] = make_uint4(b[0], b[1], b[2], b[3]);
           }
-          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-          norm = fmaxf(norm, warp_max(sum));
         }
       }
       // A = queries (row: head), B = bounds (column: page), the contraction index permuted as in paged_attention.cuh
-      float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of dependent instructions
-      __nv_bfloat162 top2 = __floats2bfloat162_rn(0.f, 0.f);
+      float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f};        // four chains of dependent instructions
+      float abs_up[4] = {0.f, 0.f, 0.f, 0.f}, abs_down[4] = {0.f, 0.f, 0.f, 0.f};
+      constexpr uint32_t kAbs = 0x7fff7fffu;
+      auto fragment = [&](float(&s)[4], const uint4(&a)[NH][X], int x, const uint4& b, uint32_t keep) {
+        mma_bf16(s, a[0][x].x, NH > 1 ? a[NH - 1][x].x : 0u, a[0][x].y, NH > 1 ? a[NH - 1][x].y : 0u, b.x & keep, b.y & keep);
+        mma_bf16(s, a[0][x].z, NH > 1 ? a[NH - 1][x].z : 0u, a[0][x].w, NH > 1 ? a[NH - 1][x].w : 0u, b.z & keep, b.w & keep);
+      };
 #pragma unroll
       for (int x = 0; x < X; ++x) {
-        mma_bf16(up, pos[0][x].x, NH > 1 ? pos[NH - 1][x].x : 0u, pos[0][x].y, NH > 1 ? pos[NH - 1][x].y : 0u, mx[x].x, mx[x].y);
-        mma_bf16(down, neg[0][x].x, NH > 1 ? neg[NH - 1][x].x : 0u, neg[0][x].y, NH > 1 ? neg[NH - 1][x].y : 0u, mn[x].x, mn[x].y);
-        mma_bf16(up, pos[0][x].z, NH > 1 ? pos[NH - 1][x].z : 0u, pos[0][x].w, NH > 1 ? pos[NH - 1][x].w : 0u, mx[x].z, mx[x].w);
-        mma_bf16(down, neg[0][x].z, NH > 1 ? neg[NH - 1][x].z : 0u, neg[0][x].w, NH > 1 ? neg[NH - 1][x].w : 0u, mn[x].z, mn[x].w);
-        const uint32_t w[8] = {mn[x].x, mn[x].y, mn[x].z, mn[x].w, mx[x].x, mx[x].y, mx[x].z, mx[x].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          __nv_bfloat162 t;
-          memcpy(&t, &w[e], 4);
-          top2 = __hmax2_nan(top2, __habs2(t));
-        }
+        fragment(up, pos, x, mx[x], 0xffffffffu);
+        fragment(down, neg, x, mn[x], 0xffffffffu);
+        fragment(abs_up, pos, x, mx[x], kAbs);
+        fragment(abs_down, neg, x, mn[x], kAbs);
       }
-      float best[2];                                           // of pages 2c and 2c + 1
+      float best[2], top = 0.f;                                // best: of pages 2c and 2c + 1
       bool odd = false;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float a = r < p.group ? up[e] + down[e] : -INFINITY;
         const float b = NH > 1 && r + 8 < p.group ? up[2 + e] + down[2 + e] : -INFINITY;
-        odd |= a != a || b != b;
+        const float size = fmaxf(abs_up[e] - abs_down[e], abs_up[2 + e] - abs_down[2 + e]);      // (0 for heads there are none of)
+        odd |= a != a || b != b || !(size < INFINITY);
+        top = fmaxf(top, size);
         best[e] = fmaxf(a, b);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) best[e] = fmaxf(best[e], __shfl_xor_sync(0xffffffffu, best[e], o));
       }
-      const float t0 = __low2float(top2), t1 = __high2float(top2);
-      odd |= t0 != t0 || t1 != t1 || t0 == INFINITY || t1 == INFINITY;
-      const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(t0, t1))));
+      top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
       odd = __any_sync(0xffffffffu, odd);
       if (r < 2 && c0 + 2 * c + r < n) p.scores[(size_t)pair * p.width + c0 + 2 * c + r] = best[r];
-      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top * norm;
+      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top;
     } else {
       const uint4* src = reinterpret_cast<const uint4*>(bounds + at) + c;
       double acc[GP];
@@ -252,6 +245,7 @@ __global__ void __launch_bounds__(kPselThreads, 1)
 choose_pages_kernel(SelectPagesParams p) {
   constexpr bool kExact = sizeof(T) == 4;                      // the scores are the 64-bit ones already
   constexpr int kWarps = kPselThreads / 32;
+  begin_grid();
   extern __shared__ __align__(16) float choose_smem_base[];
   __shared__ unsigned int hist[kPselBins];
   __shared__ uint2 list[kPselMaxDoubt];                        // (key, page) of the pages in doubt
@@ -294,7 +288,7 @@ choose_pages_kernel(SelectPagesParams p) {
     }
   };
   load_round(0);
-  float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: max_h sum |q| times the largest |bound|
+  float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest sum |q| |bound|
   const float* um = p.unit_max + (size_t)pair * pscore_units(p.width);
   bool odd = false;
   for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
@@ -327,10 +321,12 @@ choose_pages_kernel(SelectPagesParams p) {
   top = warp_max(red[0][lane]);
   bottom = -warp_max(red[1][lane]);
   limit = warp_max(red[2][lane]);
-  // eps = 2^-16 max_h sum |q| max |bound| covers 2 D products summed in fp32 by two chains of D / 16 instructions, each off
-  // by 2^-21 of the partial sums at most, which stay below sum |q| max |bound|
-  const float slack = 2.01f * 1.52587890625e-5f * limit;
+  // eps: a score is 2 D products summed by D / 8 instructions; each adds 16 products to a sum in fp32, cutting every addend to
+  // 24 bits of the largest at worst, 17 * 2^-24 of sum |q| |bound| in all: D / 8 * 17 * 2^-24 < D 2^-22.  (That sum itself is known to
+  // as much: the 1 % on top covers it.)
+  const float slack = 2.f * 1.01f * (float)D * 2.384185791015625e-7f * limit;
   const float scale = top > bottom ? (kPselBins - 1) / (top - bottom) : 0.f;
+  const float scale_or_one = scale > 0.f ? scale : 1.f;
   // bin 0 holds the best scores; fp32 rounding keeps the order
   auto bin_of = [&](float s) { return (int)fminf(fmaxf((top - s) * scale, 0.f), (float)(kPselBins - 1)); };
   bool decided = !odd && slack < 1e30f && scale < 1e30f && top < 1e30f && bottom > -1e30f;
@@ -357,7 +353,9 @@ choose_pages_kernel(SelectPagesParams p) {
       if (before < want && before + (int)(two.x + two.y) >= want) s_bin = 2 * threadIdx.x + (before + (int)two.x < want);
     }
     __syncthreads();
-    const int bin = s_bin;                                     // of the want-th largest approximate score
+    // the bin of the want-th largest approximate score, widened by the rounding of its own borders, and 2 eps on each side
+    const float round_off = 1e-6f * (fabsf(top) + fabsf(bottom));
+    const float high = top - (float)s_bin / scale_or_one + round_off + slack, low = top - (float)(s_bin + 1) / scale_or_one - round_off - slack;
     int sure = 0;
     for (int round = 0; round < rounds; ++round) {
       if (rounds > 1) load_round(round);
@@ -366,11 +364,11 @@ choose_pages_kernel(SelectPagesParams p) {
         const int c = page_at(round, y);
         if (any_at(round, y) && c - lane < n) {                // uniform over the warp
           const bool is_open = open_page(c);
-          const bool better = is_open && bin_of(v[y] - slack) < bin;
+          const bool better = is_open && v[y] > high;
           const unsigned int word = __ballot_sync(0xffffffffu, better || (c < n && forced(c)));
           if (lane == 0) kept[c / 32] = word;
           sure += better;
-          if (is_open && !better && bin_of(v[y] + slack) <= bin) {
+          if (is_open && !better && v[y] >= low) {
             const int e = atomicAdd(&s_listed, 1);
             if (e < kPselMaxDoubt) {
               list[e] = make_uint2(page_key(v[y]), (unsigned int)c);
