@@ -147,6 +147,7 @@ page_rows_kernel(RowsParams p) {
   });
   const long long total = (long long)rows_smem[p.n_seqs] * p.n_heads;
   const int warps = gridDim.x * (kRowsThreads / 32);
+#pragma unroll 1
   for (long long u = (long long)blockIdx.x * (kRowsThreads / 32) + warp; u < total; u += warps) {
     const int i = ragged_find(rows_smem, p.n_seqs, (int)(u / p.n_heads));
     const int count = rows_smem[i + 1] - rows_smem[i];
@@ -180,6 +181,7 @@ page_rows_kernel(RowsParams p) {
       VecBounds<T> b;
       b.reset();
       const int v0 = c * 32 + vec;
+#pragma unroll 1
       for (int r0 = sub; r0 < live; r0 += kRows * kBatch) {
         uint4 kx[kBatch], vx[kBatch];
 #pragma unroll

@@ -70,6 +70,7 @@ page_tables_kernel(TablesParams p) {
   long long moves = 0, rows = 0;
   int touched = 0;
   int bad = 0;
+#pragma unroll 1
   for (int i = lo; i < hi; ++i) {
     const int a = was[i], b = will[i];
     const bool off = a < 0 || b < 0 || a > max_rows || b > max_rows;
@@ -127,7 +128,9 @@ page_tables_kernel(TablesParams p) {
   else if (top + n_pops - n_pushes > p.n_pages || n_fresh > (p.slots ? p.slots_capacity : INT32_MAX)) code = MEDA_ERR_WORKSPACE;
   const int stride = gridDim.x * kTabThreads;
   if (code != MEDA_OK) {
+#pragma unroll 1
     for (int i = blockIdx.x * kTabThreads + threadIdx.x; i < p.slots_capacity; i += stride) p.slots[i] = -1;
+#pragma unroll 1
     for (int i = blockIdx.x * kTabThreads + threadIdx.x; i <= n; i += stride) p.cu_new[i] = 0;
     if (first) {
       *p.free_top_out = top;
@@ -136,6 +139,7 @@ page_tables_kernel(TablesParams p) {
     return;
   }
   int r_pop = (int)(incl_moves >> 32), r_push = (int)(incl_moves & 0xffffffffll), r_new = (int)incl_rows, r_unit = incl_touched;
+#pragma unroll 1
   for (int i = lo; i < hi; ++i) {
     r_pop += pops[i + 1];
     r_push += pushes[i + 1];
@@ -165,6 +169,7 @@ page_tables_kernel(TablesParams p) {
   const int top_bit = n > 1 ? 1 << (31 - __clz(n - 1)) : 0;    // first step of a search over n entries
   auto find = [&](const int* pre, int x) {                     // largest i < n with pre[i] <= x
     int i = 0;
+#pragma unroll 1
     for (int step = top_bit; step > 0; step >>= 1)
       if (i + step < n && pre[i + step] <= x) i += step;
     return i;
@@ -177,6 +182,7 @@ page_tables_kernel(TablesParams p) {
   // pages that get new rows: the page, its table entry if it was taken, and its rows' slots
   const int mask = (1 << p.page_shift) - 1;
   const int warps = gridDim.x * (kTabThreads / 32);
+#pragma unroll 1
   for (long long u0 = (long long)(blockIdx.x * (kTabThreads / 32) + warp) * 32; u0 < total_units; u0 += (long long)warps * 32) {
     const int u = (int)u0 + lane;
     int first_slot = total_new, rows_here = 0, page = -1, row0 = 0;
@@ -211,8 +217,10 @@ page_tables_kernel(TablesParams p) {
     }
   }
   // pages given back that nobody took onto the list; nothing in the slots behind the last row
+#pragma unroll 1
   for (int j = total_pops + blockIdx.x * kTabThreads + threadIdx.x; j < total_pushes; j += stride)
     p.free_pages[top - 1 - (j - total_pops)] = checked(*pushed(j));
+#pragma unroll 1
   for (long long t = (long long)total_new + blockIdx.x * kTabThreads + threadIdx.x; t < p.slots_capacity; t += stride) p.slots[t] = -1;
 }
 

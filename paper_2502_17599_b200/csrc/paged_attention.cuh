@@ -1,11 +1,12 @@
-// Attention of one new token per sequence over paged caches of ragged lengths (Eq. 3), in one launch.
+// Attention of one new token per sequence over paged caches of ragged lengths (Eq. 3).
 //
 // Work split.  All (sequence, KV head, 16-row tile) triples form one list; block c of C takes the c-th equal part of
 // it, so a batch of one 128K cache and a batch of 64 very different ones load the GPU alike, without the host
 // knowing any length.  Inside a block the warps take tiles in turn.  A segment (sequence, KV head) that lies in one
 // block is finished there; the at most two segments of a block that cross its borders leave softmax states (max, sum,
-// weighted values) in scratch, and the block that arrives last at such a segment joins the states in block order:
-// no second launch, no atomics on values, the same bits every run.
+// weighted values) in scratch, and a second, small launch joins the states of a segment in block order: the same bits
+// every run.  (Joining them in the block that arrives last cost more: a fence and an atomic of 1.3 us, and then one SM
+// reads 37 states of 3.6 KB for each KV head of a long cache in 5 us; the second launch is set up during the first.)
 //
 // Inner loop, bf16.  One pass over K and V with the running maximum and sum.  A warp's tile goes straight from
 // global memory into matrix-instruction fragments: the contraction index of Q K^T may be permuted freely as
@@ -28,6 +29,11 @@
 namespace meda {
 
 constexpr int kAttTile = 16;             // rows per tile; a page holds whole tiles
+// Empty tiles counted with every segment of a batch with many of them: what starting one and joining its warps' states takes,
+// in tiles of a block's time.  Without them a block whose share is many short segments works far longer than one inside
+// a long one (64 sequences of 36 to 18,944 rows: 91 us; 8 tiles: 91, 12: 80, 20: 74, 28: 74).
+constexpr int kAttSegment = 20;
+constexpr int kAttLeast = 8;             // tiles per block where the GPU has more blocks than that fills
 
 // x / d for 0 <= x < 2^31 by a multiplication: with 2^s < d < 2^(s+1), mul = ceil(2^(32+s) / d) is off by less than d / 2^(32+s),
 // which x below 2^31 cannot turn into a whole unit; powers of two are shifts.
@@ -51,8 +57,9 @@ struct AttnParams {
   const int32_t* sel;
   void* out;
   float* lse;
-  float* partial;
-  unsigned int* counters;
+  float* partial;                        // [blocks][2] softmax states of segments that cross borders
+  int4* split;                           // [blocks]: (blocks, first query head of [n_seqs][n_q_heads], query heads) of the segment that
+                                         // starts in the block and goes on behind it; 0 blocks: there is none
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep;
   float scale_log2;                      // log2(e) / sqrt(head_dim)
@@ -89,7 +96,7 @@ struct AttnTileBf16 {
   float o[VC][4][NH][4];
   float m[NH], l[NH];
 
-  __device__ __forceinline__ void begin(const T* qh, int heads, int lane) {      // qh: the segment's first query head
+  __device__ __forceinline__ void load_q(const T* qh, int heads, int lane) {     // qh: the segment's first query head
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
@@ -97,6 +104,11 @@ struct AttnTileBf16 {
 #pragma unroll
       for (int x = 0; x < KC; ++x)
         q[n][x] = h < heads ? *reinterpret_cast<const uint4*>(qh + (size_t)h * D + x * 32 + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
       m[n] = -INFINITY;
       l[n] = 0.f;
     }
@@ -242,14 +254,17 @@ struct AttnTileF32 {
   float acc[GP][E];
   float m, l;                            // of this lane's head
 
-  __device__ __forceinline__ void begin(const T* qh, int heads, int lane) {
+  __device__ __forceinline__ void load_q(const T* qh, int heads, int lane) {
 #pragma unroll
     for (int h = 0; h < GP; ++h)
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        q[h][e] = h < heads ? qh[(size_t)h * D + lane * E + e] : 0.f;
-        acc[h][e] = 0.f;
-      }
+      for (int e = 0; e < E; ++e) q[h][e] = h < heads ? qh[(size_t)h * D + lane * E + e] : 0.f;
+  }
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int h = 0; h < GP; ++h)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[h][e] = 0.f;
     m = -INFINITY;
     l = 0.f;
   }
@@ -358,11 +373,6 @@ __device__ __forceinline__ int div_small(int a, int b) {
   return q;
 }
 
-// One crossing segment of a block: its state waits in scratch until the block's tiles are done.
-struct AttnPending {
-  int seg0, seg1, seq, sh, any;
-};
-
 template <typename Tile, int D, int W>
 __global__ void __launch_bounds__(W * 32, 1)
 paged_attention_kernel(AttnParams p) {
@@ -374,8 +384,6 @@ paged_attention_kernel(AttnParams p) {
   begin_grid();
   extern __shared__ __align__(16) float att_smem[];
   __shared__ int scratch[W + 1];
-  __shared__ unsigned int s_arrived[2];
-  __shared__ AttnPending pend[2];                              // the segment that began before the block, the one that goes on behind it
   int* pre = reinterpret_cast<int*>(att_smem);                 // [n + 1] tiles before sequence i
   int* rows_of = pre + p.n_seqs + 1;                           // [n] rows of sequence i
   float* merge = att_smem + attn_prefix_floats(p.n_seqs);      // two sets of [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
@@ -387,25 +395,30 @@ paged_attention_kernel(AttnParams p) {
   const int state_heads = min(p.group, HP);
   const int state_floats = attn_state_floats(state_heads, D);
   const int n_q_heads = p.n_heads * p.group;
+  const int gap = 2 * p.n_seqs * H > (int)gridDim.x ? kAttSegment : 0;
 
-  if (threadIdx.x < 2) pend[threadIdx.x].any = 0;
   ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;
     const int len = clamped_len(p.lens, p.lens_stride, i, max_rows, bad);
     if (bad && blockIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
     rows_of[i] = len;
-    if (!p.sel) return (len + kAttTile - 1) / kAttTile;
-    return min(p.keep, (len + page_size - 1) >> p.page_shift) << tile_shift;
+    const int tiles = p.sel ? min(p.keep, (len + page_size - 1) >> p.page_shift) << tile_shift : (len + kAttTile - 1) / kAttTile;
+    return tiles ? tiles + gap : 0;
   });
 
   // Block b takes base tiles, the first `extra` blocks one more.  (All tile counts stay below 2^31: see meda_pages_create.)
   const int total = pre[p.n_seqs] * H;
-  // blocks with work: with few tiles one per segment, more where that leaves a warp more than one
-  const int C = min((int)gridDim.x, min(total, max((total + W - 1) / W, p.n_seqs * H)));
+  // Blocks with work: as many to a segment as give each kAttLeast tiles on average, so that segments of one length are cut
+  // alike and no block works on two of them needlessly.  Block b's first tile is b / C of the total, rounded down.
+  const int most = max(p.n_seqs * H, 1), each = most * kAttLeast;
+  const int C = total == 0 ? 0 : min((int)gridDim.x, total <= (long long)each * gridDim.x ? most * (div_small(total - 1, each) + 1) : (int)gridDim.x);
   const int base = C == (int)gridDim.x ? p.grid_div.of(total) : (C > 0 ? div_small(total, C) : 0), extra = total - base * C;
-  auto block_start = [&](int b) { return base * b + min(b, extra); };
+  auto block_start = [&](int b) { return base * b + div_small(extra * b, C); };
   auto block_of = [&](int x) {
-    return x < extra * (base + 1) ? div_small(x, base + 1) : extra + div_small(x - extra * (base + 1), base);
+    int b = min((int)((float)x * ((float)C / (float)total)), C - 1);
+    while (block_start(b) > x) --b;
+    while (b + 1 < C && block_start(b + 1) <= x) ++b;
+    return b;
   };
   const bool has_work = (int)blockIdx.x < C;
   const int t0 = has_work ? block_start(blockIdx.x) : 0, t1 = has_work ? block_start(blockIdx.x + 1) : 0;
@@ -419,6 +432,7 @@ paged_attention_kernel(AttnParams p) {
     const int tiles = pre[i + 1] - pre[i];
     const int local = x - pre[i] * H;
     const int sh = div_small(local, tiles), tile = local - sh * tiles, g = chunks == 1 ? sh : sh / chunks;
+    if (tile >= tiles - gap) return;
     const int len = rows_of[i];
     int col = tile >> tile_shift;
     const int r0 = (tile & ((1 << tile_shift) - 1)) * kAttTile;
@@ -442,20 +456,30 @@ paged_attention_kernel(AttnParams p) {
   };
 
   int seq = 0, sh = 0, seg0 = 0;
+  auto next_segment = [&] {                                    // the next one with tiles
+    seg0 += pre[seq + 1] - pre[seq];
+    if (++sh == H) {
+      sh = 0;
+#pragma unroll 1
+      do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
+    }
+  };
   if (has_work) {
-    const int row0 = p.heads_div.of(t0);
-    seq = ragged_find(pre, p.n_seqs, row0);
-    sh = div_small(t0 - pre[seq] * H, pre[seq + 1] - pre[seq]);
-    seg0 = pre[seq] * H + sh * (pre[seq + 1] - pre[seq]);
+    seq = ragged_find(pre, p.n_seqs, p.heads_div.of(t0));
+    const int tiles = pre[seq + 1] - pre[seq];
+    sh = div_small(t0 - pre[seq] * H, tiles);
+    seg0 = pre[seq] * H + sh * tiles;
+    if (t0 >= seg0 + tiles - gap) next_segment();      // nothing but empty tiles of it here
   }
   const T* kp = static_cast<const T*>(p.k);
   const T* vp = static_cast<const T*>(p.v);
   Tile tile;
-  auto begin_segment = [&] {
+  auto load_q = [&] {
     const int g = chunks == 1 ? sh : sh / chunks, h0 = (sh - g * chunks) * HP;
-    tile.begin(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), lane);
+    tile.load_q(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), lane);
   };
-  if (has_work) begin_segment();
+  if (seg0 < t1) load_q();                                     // (a block may hold nothing but the last segment's empty tiles)
+  tile.reset();
 
   // One iteration works on tile x, whose keys and values are in registers, and fetches tile x + W; the first one only
   // fetches.  Lane y holds the look-up of tile y of the 32 the warp is going through; the next 32 are looked up half
@@ -463,7 +487,9 @@ paged_attention_kernel(AttnParams p) {
   int x = t0 + warp - W, at = -1, buffer = 0, nv = 0;
   long long row = 0, row_now = 0, row_next = 0;
   int nv_now = 0, nv_next = 0;
-  bool worked = false, crossing = false;
+  bool worked = false;
+  int4 split = make_int4(0, 0, 0, 0);
+#pragma unroll 1
   while (seg0 < t1) {
     ++at;
     if (at == 32) {
@@ -502,11 +528,16 @@ paged_attention_kernel(AttnParams p) {
     nv = nv_after;
     x += W;
 
-    while (seg0 < t1 && x >= min(seg0 + pre[seq + 1] - pre[seq], t1)) {
-      const int seg1 = seg0 + pre[seq + 1] - pre[seq];
+    // (empty tiles do not count, so a border among them splits nothing)
+#pragma unroll 1
+    while (seg0 < t1 && x >= min(seg0 + pre[seq + 1] - pre[seq] - gap, t1)) {
+      const int seg1 = seg0 + pre[seq + 1] - pre[seq] - gap, was_seg0 = seg0;
       const int g = chunks == 1 ? sh : sh / chunks, h0 = (sh - g * chunks) * HP;
       const int heads = min(HP, p.group - h0);
       const size_t first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
+      next_segment();                                          // its queries can come already
+      if (seg0 < t1) load_q();
+
       // ---- the warps' states of this segment, joined in warp order.  The buffers alternate, so that one barrier per
       // segment is enough.  A warp without tiles leaves a maximum of -inf, a sum of 0 and no values; nobody reads those.
       float* sm_m = merge + buffer * kStates;
@@ -519,9 +550,11 @@ paged_attention_kernel(AttnParams p) {
         sm_l[warp * HP + lane] = 0.f;
       }
       __syncthreads();
-      const bool whole = seg0 >= t0 && seg1 <= t1;
-      const int slot = seg0 < t0 ? 0 : 1;
+      tile.reset();
+      const bool whole = was_seg0 >= t0 && seg1 <= t1;
+      const int slot = was_seg0 < t0 ? 0 : 1;
       float* state = p.partial + ((size_t)blockIdx.x * 2 + slot) * state_floats;
+#pragma unroll 1
       for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
         const int h = e / (D / 4), d = (e % (D / 4)) * 4;
         float mm = -INFINITY;
@@ -551,98 +584,80 @@ paged_attention_kernel(AttnParams p) {
           if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
         }
       }
-      if (!whole) {
-        crossing = true;
-        if (threadIdx.x == 0) pend[slot] = {seg0, seg1, seq, sh, 1};
-      }
-      // next segment with tiles
-      seg0 = seg1;
-      if (++sh == H) {
-        sh = 0;
-        do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
-      }
-      if (seg0 < t1) begin_segment();
+      if (was_seg0 >= t0 && seg1 > t1) split = make_int4(block_of(seg1 - 1) - (int)blockIdx.x + 1, (int)first_head, heads, 0);
       worked = false;
     }
   }
 
   // sequences without rows
+#pragma unroll 1
   for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
     if (pre[i] == pre[i + 1]) {
+#pragma unroll 1
       for (int e = threadIdx.x; e < n_q_heads * D / 4; e += W * 32)
         store4<T>(static_cast<T*>(p.out) + (size_t)i * n_q_heads * D + e * 4, make_float4(0.f, 0.f, 0.f, 0.f));
       if (p.lse)
+#pragma unroll 1
         for (int h = threadIdx.x; h < n_q_heads; h += W * 32) p.lse[(size_t)i * n_q_heads + h] = -INFINITY;
     }
 
-  // ---- segments that cross the block's borders: the block that arrives last joins all states, in block order
-  if (!crossing) return;
-  __syncthreads();                                             // the states are written ...
-  if (threadIdx.x == 0) {
-    __threadfence();                                           // ... and visible before the arrival is
+  if (threadIdx.x == 0) p.split[blockIdx.x] = split;
+}
+
+// Joins the states of the segment that starts in block blockIdx.x of the launch above, for query head blockIdx.y of it.  Groups
+// of D / 4 threads take every n-th state, four at a time in flight; their results are added in a fixed order.
+constexpr int kAttJoinThreads = 128;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kAttJoinThreads)
+join_attention_kernel(AttnParams p) {
+  constexpr int kGroup = D / 4, kGroups = kAttJoinThreads / kGroup, kBatch = 4;
+  __shared__ float4 s_o[kGroups][kGroup];
+  __shared__ float2 s_ml[kGroups];
+  begin_grid();
+  const int4 split = p.split[blockIdx.x];
+  const int parts = split.x, h = blockIdx.y;
+  if (parts == 0 || h >= split.z) return;
+  const int group = threadIdx.x / kGroup, d = threadIdx.x % kGroup;
+  const int state_heads = gridDim.y, state_floats = attn_state_floats(state_heads, D);
+  // the segment begins inside its first block (slot 1) and before all others (slot 0)
+  auto state_of = [&](int z) { return p.partial + ((size_t)(blockIdx.x + z) * 2 + (z == 0)) * state_floats; };
+  float mm = -INFINITY, ll = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float2 ml, float4 o) {
+    const float mn = fmaxf(mm, ml.x), ref = mn == -INFINITY ? 0.f : mn;
+    const float f0 = exp2_fast(mm - ref), f = exp2_fast(ml.x - ref);
+    mm = mn;
+    ll = fmaf(f, ml.y, ll * f0);
+    acc.x = fmaf(f, o.x, acc.x * f0);
+    acc.y = fmaf(f, o.y, acc.y * f0);
+    acc.z = fmaf(f, o.z, acc.z * f0);
+    acc.w = fmaf(f, o.w, acc.w * f0);
+  };
+#pragma unroll 1
+  for (int z0 = group; z0 < parts; z0 += kGroups * kBatch) {
+    float2 ml[kBatch];
+    float4 o[kBatch];
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
-      if (pend[y].any) s_arrived[y] = atomicAdd(p.counters + (size_t)pend[y].seq * H + pend[y].sh, 1u);
-    __threadfence();
-  }
-  __syncthreads();
-#pragma unroll
-  for (int y = 0; y < 2; ++y) {
-    const AttnPending pd = pend[y];
-    if (!pd.any) continue;
-    const int c0 = block_of(pd.seg0), parts = block_of(pd.seg1 - 1) - c0 + 1;
-    if (s_arrived[y] != (unsigned)(parts - 1)) continue;
-    const int g = chunks == 1 ? pd.sh : pd.sh / chunks, h0 = (pd.sh - g * chunks) * HP;
-    const int heads = min(HP, p.group - h0);
-    const size_t first_head = (size_t)pd.seq * n_q_heads + (size_t)g * p.group + h0;
-    // states: the segment begins inside the first block (slot 1) and before all others (slot 0)
-    const float* first = p.partial + ((size_t)c0 * 2 + 1) * state_floats;
-    const float* rest = p.partial + (size_t)c0 * 2 * state_floats;
-    for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
-      const int h = e / (D / 4), d = (e % (D / 4)) * 4;
-      float mm = -INFINITY, ll = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      constexpr int kBatch = 8;
-      for (int z0 = 0; z0 < parts; z0 += kBatch) {
-        float2 ml[kBatch];
-        float4 o[kBatch];
-#pragma unroll
-        for (int z = 0; z < kBatch; ++z) {
-          const float* st = z0 + z == 0 ? first : rest + (size_t)(z0 + z) * 2 * state_floats;
-          ml[z] = make_float2(-INFINITY, 0.f);
-          o[z] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (z0 + z < parts) {
-            ml[z] = __ldcg(reinterpret_cast<const float2*>(st + state_heads * D + 2 * h));
-            o[z] = __ldcg(reinterpret_cast<const float4*>(st + h * D + d));
-          }
-        }
-        float mn = mm;
-#pragma unroll
-        for (int z = 0; z < kBatch; ++z) mn = fmaxf(mn, ml[z].x);
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        const float f0 = exp2_fast(mm - ref);
-        ll *= f0;
-        acc.x *= f0;
-        acc.y *= f0;
-        acc.z *= f0;
-        acc.w *= f0;
-#pragma unroll
-        for (int z = 0; z < kBatch; ++z) {
-          const float f = exp2_fast(ml[z].x - ref);
-          ll = fmaf(f, ml[z].y, ll);
-          acc.x = fmaf(f, o[z].x, acc.x);
-          acc.y = fmaf(f, o[z].y, acc.y);
-          acc.z = fmaf(f, o[z].z, acc.z);
-          acc.w = fmaf(f, o[z].w, acc.w);
-        }
-        mm = mn;
-      }
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;
-      store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
+    for (int y = 0; y < kBatch; ++y) {
+      const float* st = state_of(min(z0 + y * kGroups, parts - 1));
+      ml[y] = *reinterpret_cast<const float2*>(st + state_heads * D + 2 * h);
+      o[y] = *reinterpret_cast<const float4*>(st + h * D + d * 4);
     }
-    if (threadIdx.x == 0) p.counters[(size_t)pd.seq * H + pd.sh] = 0u;
+#pragma unroll
+    for (int y = 0; y < kBatch; ++y)
+      if (z0 + y * kGroups < parts) add(ml[y], o[y]);
   }
+  s_o[group][d] = acc;
+  if (d == 0) s_ml[group] = make_float2(mm, ll);
+  __syncthreads();
+  if (group != 0) return;
+#pragma unroll
+  for (int y = 1; y < kGroups; ++y)
+    if (y < parts) add(s_ml[y], s_o[y][d]);
+  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  store4<T>(static_cast<T*>(p.out) + ((size_t)split.y + h) * D + d * 4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+  if (p.lse && d == 0) p.lse[split.y + h] = (mm + log2f(ll)) * 0.6931471805599453f;
 }
 
 }  // namespace meda

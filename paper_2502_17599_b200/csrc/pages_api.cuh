@@ -38,9 +38,9 @@ struct PagesDevice {
 
 // A launch that may be set up before the kernels ahead of it in the stream have finished (they and it start with begin_grid).
 template <typename K, typename P>
-meda_status launch_after(meda_pages* p, K kernel, int grid, int block, size_t smem, cudaStream_t st, const P& params) {
+meda_status launch_after(meda_pages* p, K kernel, dim3 grid, int block, size_t smem, cudaStream_t st, const P& params) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -81,7 +81,7 @@ struct AttnKernel {
     if (need > (size_t)(kMaxDynSmem - (int)a.sharedSizeBytes)) return MEDA_ERR_SHAPE;
     // tiles of all segments, and as many again for the look-ahead, are counted in 32 bits
     const int64_t segments = (int64_t)p->cfg.n_kv_heads * ((p->group + Tile::kHeads - 1) / Tile::kHeads);
-    if (segments * p->cfg.max_seqs * p->cfg.max_seq_pages * (p->cfg.page_size / kAttTile) >= (int64_t(1) << 31) - 65536)
+    if (segments * p->cfg.max_seqs * ((int64_t)p->cfg.max_seq_pages * (p->cfg.page_size / kAttTile) + kAttSegment) >= (int64_t(1) << 31) - 65536)
       return MEDA_ERR_SHAPE;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, W * 32, need) != cudaSuccess || per_sm < 1)
       return MEDA_ERR_CUDA;
@@ -91,7 +91,10 @@ struct AttnKernel {
   static meda_status launch(meda_pages* p, AttnParams a, cudaStream_t st) {
     a.heads_div.set((unsigned)(a.n_heads * ((a.group + Tile::kHeads - 1) / Tile::kHeads)));
     a.grid_div.set((unsigned)p->attn_blocks);
-    return launch_after(p, kernel, p->attn_blocks, W * 32, smem(a.n_seqs), st, a);
+    const meda_status r = launch_after(p, kernel, p->attn_blocks, W * 32, smem(a.n_seqs), st, a);
+    if (r != MEDA_OK) return r;
+    return launch_after(p, join_attention_kernel<typename Tile::T, D>, dim3(p->attn_blocks, std::min(a.group, Tile::kHeads)), kAttJoinThreads,
+                        0, st, a);
   }
 };
 
@@ -194,7 +197,7 @@ void pages_release(meda_pages* p) {
   cudaFree(p->rope_freq);
   cudaFree(p->rope_axis);
   cudaFree(p->attn_partial);
-  cudaFree(p->attn_counters);
+  cudaFree(p->attn_split);
   cudaFree(p->select_scratch);
   delete p;
 }
@@ -261,10 +264,8 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
   if (st == MEDA_OK) st = carve(&p->rope_axis, half, &p->bytes);
   if (st == MEDA_OK) st = carve(&p->attn_partial, (int64_t)p->attn_blocks * 2 * attn_state_floats(p->group, c.head_dim), &p->bytes);
   if (st == MEDA_OK) st = carve(&p->select_scratch, select_seq_floats(c) * select_scratch_seqs(c), &p->bytes);
-  const int64_t counters = (int64_t)c.max_seqs * c.n_q_heads;  // segments: at most one per query head
-  if (st == MEDA_OK) st = carve(&p->attn_counters, counters, &p->bytes);
+  if (st == MEDA_OK) st = carve(&p->attn_split, p->attn_blocks, &p->bytes);
   if (st == MEDA_OK && (cudaMemset(p->status, 0, sizeof(int)) != cudaSuccess ||
-                        cudaMemset(p->attn_counters, 0, (size_t)counters * 4) != cudaSuccess ||
                         cudaMemcpy(p->rope_freq, freq, (size_t)half * 8, cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaMemcpy(p->rope_axis, axis, (size_t)half * 4, cudaMemcpyHostToDevice) != cudaSuccess ||
                         cudaStreamSynchronize(nullptr) != cudaSuccess))
@@ -420,7 +421,7 @@ meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
   const meda_pages_config& c = pages->cfg;
-  AttnParams a = {q, k_pages, v_pages, table, lens, sel, out, lse, pages->attn_partial, pages->attn_counters, pages->status,
+  AttnParams a = {q, k_pages, v_pages, table, lens, sel, out, lse, pages->attn_partial, pages->attn_split, pages->status,
                   lens_stride, n_seqs, c.n_kv_heads, pages->group, c.n_pages, c.max_seq_pages, pages->page_shift, keep,
                   1.4426950408889634f / sqrtf((float)c.head_dim), {}, {}};
   return with_attn_kernel(pages, [&](auto kern) { return kern.launch(pages, a, as_stream(stream)); });

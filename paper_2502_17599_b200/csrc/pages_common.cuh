@@ -17,7 +17,7 @@ struct meda_pages {
   unsigned long long* rope_freq = nullptr;   // [half] turns per position, as a 64-bit fraction
   int* rope_axis = nullptr;            // [half]
   float* attn_partial = nullptr;       // [blocks][2][group][head_dim + 2] softmax states of segments that cross blocks
-  unsigned int* attn_counters = nullptr;     // [max_seqs * n_kv_heads] arrivals per segment, zero between launches
+  int4* attn_split = nullptr;          // [blocks] segments that go on behind a block
   float* select_scratch = nullptr;     // [sequences][n_kv_heads][max_seq_pages] scores, then a bound per eight pages of them
   int attn_blocks = 0;                 // blocks of the attention kernel that are resident at once
 };
@@ -69,12 +69,27 @@ __device__ __forceinline__ int clamped_len(const int32_t* lens, int stride, int 
 }
 
 // pre[0 .. n] (shared memory) <- exclusive prefix sums of units(length of sequence i).  A thread takes consecutive
-// sequences, so one block-wide scan serves any n.  Ends with a barrier.
+// sequences, so one block-wide scan serves any n.  Afterwards every thread may read pre (and what units() wrote of its
+// own sequences, as long as every warp writes the same).
 template <int THREADS, typename F>
 __device__ __forceinline__ void ragged_prefix(int n, int* pre, int* scratch, F units) {
+  if (n <= 32) {                        // few sequences: every warp for itself (they write the same values), no barrier
+    const int lane = threadIdx.x % 32;
+    int u = lane < n ? units(lane) : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, u, o);
+      if (lane >= o) u += y;
+    }
+    if (lane < n) pre[lane + 1] = u;
+    if (lane == 0) pre[0] = 0;
+    __syncwarp();
+    return;
+  }
   const int per = (n + THREADS - 1) / THREADS;
   const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
   int sum = 0;
+#pragma unroll 1
   for (int i = lo; i < hi; ++i) {
     const int u = units(i);
     pre[i + 1] = u;
@@ -82,6 +97,7 @@ __device__ __forceinline__ void ragged_prefix(int n, int* pre, int* scratch, F u
   }
   int total;
   int run = block_prefix<THREADS>(sum, scratch, total);
+#pragma unroll 1
   for (int i = lo; i < hi; ++i) {
     run += pre[i + 1];
     pre[i + 1] = run;
@@ -94,6 +110,7 @@ __device__ __forceinline__ void ragged_prefix(int n, int* pre, int* scratch, F u
 // (sequences without units are passed over).
 __device__ __forceinline__ int ragged_find(const int* pre, int n, int x) {
   int lo = 0, hi = n;                   // pre[lo] <= x < pre[hi]
+#pragma unroll 1
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (pre[mid] <= x) lo = mid;

@@ -90,6 +90,7 @@ rope_append_kernel(RopeParams p) {
     }
     slot_of[threadIdx.x] = s;
   }
+#pragma unroll 1
   for (int x = threadIdx.x; x < n_tok * half; x += kRopeThreads) {
     const int tok = x / half, i = x - tok * half;
     const long long pos = p.positions[p.axis[i] * p.axis_stride + t0 + tok];

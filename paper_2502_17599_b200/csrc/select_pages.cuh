@@ -28,7 +28,7 @@ namespace meda {
 constexpr int kPscoreThreads = 256;
 constexpr int kPscoreUnit = 8;           // pages side by side in a warp
 constexpr int kPselThreads = 1024;
-constexpr int kPselItems = 16;           // scores per thread held in registers: 16 K pages in one round
+constexpr int kPselItems = 8;            // scores per thread held in registers: 8 K pages in one round
 constexpr int kPselRound = kPselThreads * kPselItems;
 constexpr int kPselBins = 2048;
 constexpr int kPselMaxDoubt = 512;       // pages scored again in 64 bits
@@ -93,6 +93,7 @@ page_scores_kernel(SelectPagesParams p) {
 
   uint4 pos[NH][X], neg[NH][X];                                // bf16: the queries' positive and negative parts as fragments
   int held = -1, i = 0, g = 0, units = 0, n = 0, first_unit = 0;
+#pragma unroll 1
   for (int u = u0; u < u1; ++u) {
     if (u >= first_unit + units) {                             // the next (sequence, KV head)
       i = ragged_find(pre, p.n_seqs, p.heads_div.of(u));
@@ -209,7 +210,7 @@ page_scores_kernel(SelectPagesParams p) {
 
 // The score of one page for one KV head by a whole warp, in 64 bits.  qh: the head's queries [group][D] as floats.
 template <typename T, int D>
-__device__ __forceinline__ float page_score_warp(const T* lo, const float* qh, int group, int lane) {
+__device__ __noinline__ float page_score_warp(const T* lo, const float* qh, int group, int lane) {
   constexpr int N = D / 32;
   double mn[N], mx[N];
 #pragma unroll
@@ -219,7 +220,7 @@ __device__ __forceinline__ float page_score_warp(const T* lo, const float* qh, i
   }
   float best = -INFINITY;
   bool nan = false;
-#pragma unroll 4
+#pragma unroll 2
   for (int h = 0; h < group; ++h) {
     double s = 0.0;
 #pragma unroll
@@ -264,6 +265,7 @@ choose_pages_kernel(SelectPagesParams p) {
   const int n = (len + page_size - 1) >> p.page_shift;         // pages of the sequence
   int32_t* out = p.sel + (size_t)pair * p.keep;
   if (n <= p.keep) {                                           // every page is kept
+#pragma unroll 1
     for (int c = threadIdx.x; c < n; c += kPselThreads) out[c] = c;
     return;
   }
@@ -291,15 +293,19 @@ choose_pages_kernel(SelectPagesParams p) {
   float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest sum |q| |bound|
   const float* um = p.unit_max + (size_t)pair * pscore_units(p.width);
   bool odd = false;
+#pragma unroll 1
   for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
     const float f = um[x];
     odd |= f != f;
     limit = fmaxf(limit, f);
   }
   if constexpr (!kExact)
+#pragma unroll 1
     for (int x = threadIdx.x; x < p.group * D; x += kPselThreads) qs[x] = to_f32<T>(qh[x]);
+#pragma unroll 1
   for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
   if (threadIdx.x == 0) s_sure = s_listed = 0;
+#pragma unroll 1
   for (int round = 0; round < rounds; ++round) {
     if (rounds > 1) load_round(round);
 #pragma unroll
@@ -331,14 +337,17 @@ choose_pages_kernel(SelectPagesParams p) {
   auto bin_of = [&](float s) { return (int)fminf(fmaxf((top - s) * scale, 0.f), (float)(kPselBins - 1)); };
   bool decided = !odd && slack < 1e30f && scale < 1e30f && top < 1e30f && bottom > -1e30f;
   if (want == 0) {                                             // nothing to choose
+#pragma unroll 1
     for (int w = threadIdx.x; w < words; w += kPselThreads) kept[w] = 0u;
     __syncthreads();
+#pragma unroll 1
     for (int c = threadIdx.x; c < p.n_first + p.n_last; c += kPselThreads) {
       const int page = c < p.n_first ? c : n - p.n_last + (c - p.n_first);
       atomicOr(&kept[page / 32], 1u << (page % 32));
     }
     __syncthreads();
   } else if (decided) {
+#pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
       if (rounds > 1) load_round(round);
 #pragma unroll
@@ -357,6 +366,7 @@ choose_pages_kernel(SelectPagesParams p) {
     const float round_off = 1e-6f * (fabsf(top) + fabsf(bottom));
     const float high = top - (float)s_bin / scale_or_one + round_off + slack, low = top - (float)(s_bin + 1) / scale_or_one - round_off - slack;
     int sure = 0;
+#pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
       if (rounds > 1) load_round(round);
 #pragma unroll
@@ -385,6 +395,7 @@ choose_pages_kernel(SelectPagesParams p) {
     decided = listed <= kPselMaxDoubt;
     if (decided) {
       if constexpr (!kExact) {
+#pragma unroll 1
         for (int e = warp; e < listed; e += kWarps) {
           const float s = page_score_warp<T, D>(bounds + bounds_place(p, listed_page[e], g, D), qs, p.group, lane);
           if (lane == 0) list[e].x = page_key(s);
@@ -408,6 +419,7 @@ choose_pages_kernel(SelectPagesParams p) {
     // ---- every page in 64 bits (into the scores' place), and radix passes to the last bit
     float* exact = p.scores + (size_t)pair * p.width;
     if constexpr (!kExact) {
+#pragma unroll 1
       for (int c = warp; c < n; c += kWarps) {
         const float s = page_score_warp<T, D>(bounds + bounds_place(p, table[c], g, D), qs, p.group, lane);
         if (lane == 0) exact[c] = s;
@@ -420,8 +432,10 @@ choose_pages_kernel(SelectPagesParams p) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
       const unsigned int bins = pass == 2 ? 1024u : 2048u;
+#pragma unroll 1
       for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
       __syncthreads();
+#pragma unroll 1
       for (int c = threadIdx.x; c < n; c += kPselThreads) {
         const unsigned int key = page_key(exact[c]);
         if (!forced(c) && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1u)], 1u);
@@ -441,6 +455,7 @@ choose_pages_kernel(SelectPagesParams p) {
       remaining = s_need;
       __syncthreads();
     }
+#pragma unroll 1
     for (int c = threadIdx.x; c < words * 32; c += kPselThreads) {             // words * 32 and the stride keep warps whole
       const unsigned int key = c < n ? page_key(exact[c]) : 0u;
       const unsigned int above = __ballot_sync(0xffffffffu, c < n && (forced(c) || key > prefix));
@@ -452,12 +467,14 @@ choose_pages_kernel(SelectPagesParams p) {
     }
     __syncthreads();
     int before = 0;
+#pragma unroll 1
     for (int w0 = 0; w0 < words; w0 += kPselThreads) {         // of equal keys the lowest pages
       const int w = w0 + (int)threadIdx.x;
       unsigned int same = w < words ? equal[w] : 0u;
       int all;
       int rank = before + block_prefix<kPselThreads>(__popc(same), scan, all);
       before += all;
+#pragma unroll 1
       while (same && rank < remaining) {
         const unsigned int bit = same & (0u - same);
         kept[w] |= bit;
@@ -470,12 +487,14 @@ choose_pages_kernel(SelectPagesParams p) {
 
   // ---- kept pages, in order
   int before = 0;
+#pragma unroll 1
   for (int w0 = 0; w0 < words; w0 += kPselThreads) {
     const int w = w0 + (int)threadIdx.x;
     unsigned int bits = w < words ? kept[w] : 0u;
     int all;
     int at = before + block_prefix<kPselThreads>(__popc(bits), scan, all);
     before += all;
+#pragma unroll 1
     while (bits) {
       const int b = __ffs((int)bits) - 1;
       bits &= bits - 1u;
