@@ -29,7 +29,7 @@
 namespace meda {
 
 constexpr int kAttTile = 16;             // rows per tile; a page holds whole tiles
-// Empty tiles counted with every segment of a batch with many of them: what starting one and joining its warps' states takes,
+// Empty tiles counted with every segment of a batch of sequences: what starting one and joining its warps' states takes,
 // in tiles of a block's time.  Without them a block whose share is many short segments works far longer than one inside
 // a long one (64 sequences of 36 to 18,944 rows: 91 us; 8 tiles: 91, 12: 80, 20: 74, 28: 74).
 constexpr int kAttSegment = 20;
@@ -395,7 +395,7 @@ paged_attention_kernel(AttnParams p) {
   const int state_heads = min(p.group, HP);
   const int state_floats = attn_state_floats(state_heads, D);
   const int n_q_heads = p.n_heads * p.group;
-  const int gap = 2 * p.n_seqs * H > (int)gridDim.x ? kAttSegment : 0;
+  const int gap = p.n_seqs > 1 ? kAttSegment : 0;
 
   ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;

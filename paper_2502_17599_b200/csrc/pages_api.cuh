@@ -122,15 +122,22 @@ meda_status with_attn_kernel(const meda_pages* p, F f) {
 template <typename T, int D, int GP>
 struct SelectPagesKernels {
   static meda_status prepare() {
-    const meda_status r = raise_dyn_smem(page_scores_kernel<T, D, GP>);
-    return r == MEDA_OK ? raise_dyn_smem(choose_pages_kernel<T, D>) : r;
+    meda_status r = raise_dyn_smem(page_scores_kernel<T, D, GP>);
+    if (r == MEDA_OK) r = raise_dyn_smem(choose_pages_kernel<T, D, 256>);
+    return r == MEDA_OK ? raise_dyn_smem(choose_pages_kernel<T, D, 1024>) : r;
   }
   static meda_status launch(meda_pages* p, const SelectPagesParams& a, cudaStream_t st) {
-    // two blocks per SM, and no more (see tables_smem)
-    const size_t smem = std::max<size_t>((size_t)(a.n_seqs + 1) * 4, 77 * 1024);
-    const meda_status r = launch_after(p, page_scores_kernel<T, D, GP>, p->sm_count * 2, kPscoreThreads, smem, st, a);
+    // fp32 scores are bound by 64-bit arithmetic and want twice the warps (and no third block on an SM: see tables_smem)
+    const int blocks = sizeof(T) == 4 ? 2 : 1;
+    const size_t seqs = (size_t)(a.n_seqs + 1) * 4;
+    const meda_status r = launch_after(p, page_scores_kernel<T, D, GP>, p->sm_count * blocks, kPscoreThreads,
+                                       blocks == 2 ? std::max<size_t>(seqs, 77 * 1024) : seqs, st, a);
     if (r != MEDA_OK) return r;
-    return launch_after(p, choose_pages_kernel<T, D>, a.n_seqs * a.n_heads, kPselThreads, choose_smem(a.width, a.group, D), st, a);
+    // a large block where it has an SM to itself, four small ones to an SM where there are more pairs than SMs
+    const int pairs = a.n_seqs * a.n_heads;
+    const size_t smem = choose_smem(a.width, a.group, D);
+    return pairs <= p->sm_count ? launch_after(p, choose_pages_kernel<T, D, 1024>, pairs, 1024, smem, st, a)
+                                : launch_after(p, choose_pages_kernel<T, D, 256>, pairs, 256, smem, st, a);
   }
 };
 
@@ -155,7 +162,7 @@ meda_status with_select_kernels(const meda_pages* p, F f) {
 // Scratch of the selection: one sequence's scores and their bounds, in floats, and how many sequences it holds (at least
 // one, more while that stays below 32 MB; a larger batch goes through it in several launches).
 int64_t select_seq_floats(const meda_pages_config& c) {
-  return (int64_t)c.n_kv_heads * (c.max_seq_pages + pscore_units(c.max_seq_pages));
+  return (int64_t)c.n_kv_heads * ((c.max_seq_pages + 3) / 4 * 4 + 4 * pscore_units(c.max_seq_pages));
 }
 int select_scratch_seqs(const meda_pages_config& c) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(c.max_seqs, (int64_t(32) << 20) / 4 / select_seq_floats(c)));
@@ -401,7 +408,7 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
     float* scores = pages->select_scratch;
     SelectPagesParams a = {static_cast<const char*>(q) + (size_t)i * c.n_q_heads * c.head_dim * e, bounds,
                            table + (size_t)i * c.max_seq_pages, lens + (size_t)i * lens_stride, sel + (size_t)i * c.n_kv_heads * keep,
-                           scores, scores + (int64_t)some * c.n_kv_heads * c.max_seq_pages, pages->status, lens_stride, count,
+                           scores, reinterpret_cast<float4*>(scores + (int64_t)some * c.n_kv_heads * ((c.max_seq_pages + 3) / 4 * 4)), pages->status, lens_stride, count,
                            c.n_kv_heads, pages->group, c.n_pages, c.max_seq_pages, pages->page_shift, keep, n_first, n_last, {}};
     a.heads_div.set((unsigned)c.n_kv_heads);
     const meda_status done = with_select_kernels(pages, [&](auto kern) { return kern.launch(pages, a, as_stream(stream)); });

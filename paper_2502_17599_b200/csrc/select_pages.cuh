@@ -25,11 +25,9 @@
 
 namespace meda {
 
-constexpr int kPscoreThreads = 256;
+constexpr int kPscoreThreads = 384;
 constexpr int kPscoreUnit = 8;           // pages side by side in a warp
-constexpr int kPselThreads = 1024;
-constexpr int kPselItems = 8;            // scores per thread held in registers: 8 K pages in one round
-constexpr int kPselRound = kPselThreads * kPselItems;
+constexpr int kPselItems = 8;            // scores per thread held in registers in one round
 constexpr int kPselBins = 2048;
 constexpr int kPselMaxDoubt = 512;       // pages scored again in 64 bits
 
@@ -40,8 +38,8 @@ struct SelectPagesParams {
   const int32_t* lens;
   int32_t* sel;
   float* scores;                         // [n_seqs * n_heads][width]
-  float* unit_max;                       // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: largest sum |q| |bound| among a unit's
-                                         // pages and heads, not finite where a score is not; 0 where the scores are exact
+  float4* units;                         // [n_seqs * n_heads][width / kPscoreUnit, rounded up]: of a unit's pages the largest sum |q| |bound|
+                                         // (not finite where a score is not; 0 where the scores are exact), the largest and the smallest score
   int* status;
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep, n_first, n_last;
   InvariantDiv heads_div;
@@ -63,10 +61,11 @@ __device__ __forceinline__ size_t bounds_place(const SelectPagesParams& p, int p
 }
 
 // ---- scores of all pages ---------------------------------------------------------------------------------
-// A unit is eight neighbouring pages of one (sequence, KV head); a warp takes a run of units, and reads the queries again
-// where the pair changes.  Four lanes share a page.  D = head_dim, GP = query heads per KV head rounded up to a power of two.
+// A unit is eight neighbouring pages of one (sequence, KV head); a warp takes a run of units.  It looks up four of them at
+// a time (lane l: page l % 8 of unit l / 8), fetches a unit's bounds while it works on the one before, and reads the queries
+// again where the pair changes.  Four lanes share a page.  D = head_dim, GP = query heads per KV head rounded up to a power of two.
 template <typename T, int D, int GP>
-__global__ void __launch_bounds__(kPscoreThreads)
+__global__ void __launch_bounds__(kPscoreThreads, sizeof(T) == 4 ? 2 : 1)
 page_scores_kernel(SelectPagesParams p) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int E = RopeVec<T>::E;                             // elements per 16-byte vector
@@ -77,7 +76,7 @@ page_scores_kernel(SelectPagesParams p) {
   __shared__ int scratch[kPscoreThreads / 32 + 1];
   int* pre = pscore_smem;                                      // [n + 1] units before sequence i (of one KV head)
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, r = lane / 4, c = lane % 4;
-  const int page_size = 1 << p.page_shift, max_rows = p.width << p.page_shift;
+  const int page_size = 1 << p.page_shift, max_rows = p.width << p.page_shift, row_units = pscore_units(p.width);
   const T* bounds = static_cast<const T*>(p.bounds);
   ragged_prefix<kPscoreThreads>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;
@@ -86,34 +85,51 @@ page_scores_kernel(SelectPagesParams p) {
     const int pages = (len + page_size - 1) >> p.page_shift;
     return pages > p.keep ? pscore_units(pages) : 0;           // (a sequence that keeps everything needs no scores)
   });
-  const long long total = (long long)pre[p.n_seqs] * p.n_heads;
-  const long long warps = (long long)gridDim.x * (kPscoreThreads / 32), me = (long long)blockIdx.x * (kPscoreThreads / 32) + warp;
-  const int per = (int)((total + warps - 1) / warps);
-  const int u0 = (int)min(me * per, total), u1 = (int)min((me + 1) * per, total);
+  const int total = pre[p.n_seqs] * p.n_heads;
+  const int warps = gridDim.x * (kPscoreThreads / 32), me = blockIdx.x * (kPscoreThreads / 32) + warp;
+  const int base = total / warps, extra = total - base * warps;
+  const int u0 = base * me + min(me, extra), u1 = u0 + base + (me < extra);
 
-  uint4 pos[NH][X], neg[NH][X];                                // bf16: the queries' positive and negative parts as fragments
-  int held = -1, i = 0, g = 0, units = 0, n = 0, first_unit = 0;
-#pragma unroll 1
-  for (int u = u0; u < u1; ++u) {
-    if (u >= first_unit + units) {                             // the next (sequence, KV head)
-      i = ragged_find(pre, p.n_seqs, p.heads_div.of(u));
-      units = pre[i + 1] - pre[i];
-      g = div_small(u - pre[i] * p.n_heads, units);
-      first_unit = pre[i] * p.n_heads + g * units;
-      bool bad = false;
-      n = (clamped_len(p.lens, p.lens_stride, i, max_rows, bad) + page_size - 1) >> p.page_shift;
-    }
-    const int pair = i * p.n_heads + g, c0 = (u - first_unit) * kPscoreUnit;
-    const T* qh = static_cast<const T*>(p.q) + (size_t)pair * p.group * D;
-    const size_t at = bounds_place(p, p.table[(size_t)i * p.width + min(c0 + r, n - 1)], g, D);
+  uint4 mn[kBf16 ? X : 1], mx[kBf16 ? X : 1];                  // bf16: the bounds of the next unit
+  uint4 pos[NH][kBf16 ? X : 1], neg[NH][kBf16 ? X : 1];        // bf16: the queries' positive and negative parts as fragments
+  int held = -1;
+  // this lane's page of the four units from `from` on: its bounds' place, its (sequence, KV head), its number in the sequence and that one's pages
+  size_t l_at = 0;
+  int l_pair = 0, l_c0 = 0, l_n = 0;
+  auto look_up = [&](int from) {
+    const int u = min(from + lane / 8, u1 - 1);
+    const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(u)), units = pre[i + 1] - pre[i];
+    const int g = div_small(u - pre[i] * p.n_heads, units);
+    bool bad = false;
+    l_n = (clamped_len(p.lens, p.lens_stride, i, max_rows, bad) + page_size - 1) >> p.page_shift;
+    l_pair = i * p.n_heads + g;
+    l_c0 = (u - pre[i] * p.n_heads - g * units) * kPscoreUnit;
+    l_at = bounds_place(p, p.table[(size_t)i * p.width + min(l_c0 + lane % 8, l_n - 1)], g, D);
+  };
+  auto fetch = [&](int u) {                                    // the bounds of unit u, one of the four looked up
     if constexpr (kBf16) {
-      const T* src = bounds + at + c * 8;
-      uint4 mn[X], mx[X];
+      const T* src = bounds + __shfl_sync(0xffffffffu, l_at, ((u - u0) % 4) * 8 + r) + c * 8;
 #pragma unroll
       for (int x = 0; x < X; ++x) {
         mn[x] = load_stream(reinterpret_cast<const uint4*>(src + x * 32));
         mx[x] = load_stream(reinterpret_cast<const uint4*>(src + D + x * 32));
       }
+    }
+  };
+  if (u0 < u1) {
+    look_up(u0);
+    fetch(u0);
+  }
+#pragma unroll 1
+  for (int u = u0; u < u1; ++u) {
+    const int from = ((u - u0) % 4) * 8;
+    const int pair = __shfl_sync(0xffffffffu, l_pair, from), c0 = __shfl_sync(0xffffffffu, l_c0, from);
+    const int n = __shfl_sync(0xffffffffu, l_n, from);
+    const size_t at = __shfl_sync(0xffffffffu, l_at, from + r);
+    const T* qh = static_cast<const T*>(p.q) + (size_t)pair * p.group * D;
+    float size, best[2];                                       // best: bf16, of pages 2c and 2c + 1; fp32, best[0] of page r
+    bool odd = false;
+    if constexpr (kBf16) {
       if (pair != held) {
         held = pair;
         const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
@@ -153,23 +169,23 @@ page_scores_kernel(SelectPagesParams p) {
         fragment(abs_up, pos, x, mx[x], kAbs);
         fragment(abs_down, neg, x, mn[x], kAbs);
       }
-      float best[2], top = 0.f;                                // best: of pages 2c and 2c + 1
-      bool odd = false;
+      if (u + 1 < u1) {
+        if ((u + 1 - u0) % 4 == 0) look_up(u + 1);
+        fetch(u + 1);
+      }
+      size = 0.f;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float a = r < p.group ? up[e] + down[e] : -INFINITY;
         const float b = NH > 1 && r + 8 < p.group ? up[2 + e] + down[2 + e] : -INFINITY;
-        const float size = fmaxf(abs_up[e] - abs_down[e], abs_up[2 + e] - abs_down[2 + e]);      // (0 for heads there are none of)
-        odd |= a != a || b != b || !(size < INFINITY);
-        top = fmaxf(top, size);
+        const float s = fmaxf(abs_up[e] - abs_down[e], abs_up[2 + e] - abs_down[2 + e]);         // (0 for heads there are none of)
+        odd |= a != a || b != b || !(s < INFINITY);
+        size = fmaxf(size, s);
         best[e] = fmaxf(a, b);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) best[e] = fmaxf(best[e], __shfl_xor_sync(0xffffffffu, best[e], o));
       }
-      top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-      odd = __any_sync(0xffffffffu, odd);
       if (r < 2 && c0 + 2 * c + r < n) p.scores[(size_t)pair * p.width + c0 + 2 * c + r] = best[r];
-      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : top;
     } else {
       const uint4* src = reinterpret_cast<const uint4*>(bounds + at) + c;
       double acc[GP];
@@ -177,19 +193,19 @@ page_scores_kernel(SelectPagesParams p) {
       for (int h = 0; h < GP; ++h) acc[h] = 0.0;
 #pragma unroll 2
       for (int x = 0; x < X; ++x) {
-        float mn[E], mx[E];
-        RopeVec<T>::unpack(src[x * 4], mn);
-        RopeVec<T>::unpack(src[D / E + x * 4], mx);
+        float lo[E], hi[E];
+        RopeVec<T>::unpack(src[x * 4], lo);
+        RopeVec<T>::unpack(src[D / E + x * 4], hi);
 #pragma unroll
         for (int h = 0; h < GP; ++h)
           if (h < p.group) {
             float qv[E];
             RopeVec<T>::unpack(*reinterpret_cast<const uint4*>(qh + (size_t)h * D + (x * 4 + c) * E), qv);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[h] = fma((double)qv[e], (double)(qv[e] >= 0.f ? mx[e] : mn[e]), acc[h]);
+            for (int e = 0; e < E; ++e) acc[h] = fma((double)qv[e], (double)(qv[e] >= 0.f ? hi[e] : lo[e]), acc[h]);
           }
       }
-      float best = -INFINITY;
+      float top = -INFINITY;
       bool nan = false;
 #pragma unroll
       for (int h = 0; h < GP; ++h)
@@ -199,18 +215,26 @@ page_scores_kernel(SelectPagesParams p) {
           s += __shfl_xor_sync(0xffffffffu, s, 2);
           const float f = (float)s;
           nan |= f != f;
-          best = fmaxf(best, f);
+          top = fmaxf(top, f);
         }
-      const bool odd = __any_sync(0xffffffffu, nan || fabsf(best) == INFINITY);
-      if (c == 0 && c0 + r < n) p.scores[(size_t)pair * p.width + c0 + r] = nan ? NAN : best;
-      if (lane == 0) p.unit_max[(size_t)pair * pscore_units(p.width) + c0 / kPscoreUnit] = odd ? NAN : 0.f;
+      odd = nan || fabsf(top) == INFINITY;
+      size = 0.f;
+      best[0] = best[1] = top;
+      if (c == 0 && c0 + r < n) p.scores[(size_t)pair * p.width + c0 + r] = nan ? NAN : top;
+      if (u + 1 < u1 && (u + 1 - u0) % 4 == 0) look_up(u + 1);
     }
+    // (pages behind the last repeat it)
+    const float high = warp_max(fmaxf(best[0], best[1])), low = -warp_max(-fminf(best[0], best[1]));
+    size = warp_max(size);
+    odd = __any_sync(0xffffffffu, odd);
+    if (lane == 0) p.units[(size_t)pair * row_units + c0 / kPscoreUnit] = make_float4(odd ? NAN : size, high, low, 0.f);
   }
 }
 
-// The score of one page for one KV head by a whole warp, in 64 bits.  qh: the head's queries [group][D] as floats.
+// The score of one page for one KV head by a whole warp, in 64 bits.  qs: the head's queries [group][D] as floats.  A lane
+// holds D / 32 dimensions; the sums of eight heads are exchanged so that four lanes end up with each.
 template <typename T, int D>
-__device__ __noinline__ float page_score_warp(const T* lo, const float* qh, int group, int lane) {
+__device__ __noinline__ float page_score_warp(const T* lo, const float* qs, int group, int lane) {
   constexpr int N = D / 32;
   double mn[N], mx[N];
 #pragma unroll
@@ -220,29 +244,43 @@ __device__ __noinline__ float page_score_warp(const T* lo, const float* qh, int 
   }
   float best = -INFINITY;
   bool nan = false;
-#pragma unroll 2
-  for (int h = 0; h < group; ++h) {
-    double s = 0.0;
+#pragma unroll 1
+  for (int h0 = 0; h0 < group; h0 += 8) {
+    double s[8];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const double q = (double)qh[h * D + e * 32 + lane];
-      s = fma(q, q >= 0.0 ? mx[e] : mn[e], s);
+    for (int y = 0; y < 8; ++y) {
+      s[y] = 0.0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const double q = (double)qs[min(h0 + y, group - 1) * D + e * 32 + lane];
+        s[y] = fma(q, q >= 0.0 ? mx[e] : mn[e], s[y]);
+      }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const float f = (float)s;
+    for (int o = 4; o >= 1; o >>= 1) {                         // lanes 4 o apart keep the upper or the lower half of what is left
+      const bool upper = (lane & (4 * o)) != 0;
+#pragma unroll
+      for (int y = 0; y < o; ++y) {
+        const double give = upper ? s[y] : s[y + o], keep = upper ? s[y + o] : s[y];
+        s[y] = keep + __shfl_xor_sync(0xffffffffu, give, 4 * o);
+      }
+    }
+    s[0] += __shfl_xor_sync(0xffffffffu, s[0], 2);
+    s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
+    const float f = (float)s[0];                               // of head h0 + lane / 4 (of the last head again behind it)
     nan |= f != f;
     best = fmaxf(best, f);
   }
-  return nan ? NAN : best;
+  best = warp_max(best);
+  return __any_sync(0xffffffffu, nan) ? NAN : best;
 }
 
 // ---- the choice, one block per (sequence, KV head) ---------------------------------------------------------
 // Shared memory: the queries as floats, two bits per page.
 __host__ __device__ inline int choose_smem(int width, int group, int d) { return (group * d + 2 * ((width + 31) / 32)) * 4; }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kPselThreads, 1)
+template <typename T, int D, int kPselThreads>
+__global__ void __launch_bounds__(kPselThreads, 1024 / kPselThreads)
 choose_pages_kernel(SelectPagesParams p) {
   constexpr bool kExact = sizeof(T) == 4;                      // the scores are the 64-bit ones already
   constexpr int kWarps = kPselThreads / 32;
@@ -260,6 +298,19 @@ choose_pages_kernel(SelectPagesParams p) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int pair = blockIdx.x, i = p.heads_div.of(pair), g = pair - i * p.n_heads;
   const int page_size = 1 << p.page_shift;
+  // a thread's scores: page (round * items + y) * threads + thread, so that a warp's 32 pages are one word of the bit maps;
+  // the first round is fetched before the sequence's length is known
+  const float* scores = p.scores + (size_t)pair * p.width;
+  float v[kPselItems];
+  auto page_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads + (int)threadIdx.x; };
+  auto load_round = [&](int round) {
+#pragma unroll
+    for (int y = 0; y < kPselItems; ++y) {
+      const int c = page_at(round, y);
+      v[y] = c < p.width ? scores[c] : 0.f;
+    }
+  };
+  load_round(0);
   bool bad = false;
   const int len = clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad);
   const int n = (len + page_size - 1) >> p.page_shift;         // pages of the sequence
@@ -269,35 +320,25 @@ choose_pages_kernel(SelectPagesParams p) {
     for (int c = threadIdx.x; c < n; c += kPselThreads) out[c] = c;
     return;
   }
-  const float* scores = p.scores + (size_t)pair * p.width;
   const T* qh = static_cast<const T*>(p.q) + (size_t)pair * p.group * D;
   const T* bounds = static_cast<const T*>(p.bounds);
   const int32_t* table = p.table + (size_t)i * p.width;
   const int want = p.keep - p.n_first - p.n_last;              // pages to choose among those that are not kept anyway
-  const int words = (n + 31) / 32, rounds = (n + kPselRound - 1) / kPselRound;
+  const int words = (n + 31) / 32, rounds = (n + kPselThreads * kPselItems - 1) / (kPselThreads * kPselItems);
   auto forced = [&](int c) { return c < p.n_first || c >= n - p.n_last; };
   auto open_page = [&](int c) { return c < n && !forced(c); };
 
-  // a thread's scores: page (round * items + y) * threads + thread, so that a warp's 32 pages are one word of the bit maps
-  float v[kPselItems];
-  auto page_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads + (int)threadIdx.x; };
   auto any_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads < n; };       // uniform
-  auto load_round = [&](int round) {
-#pragma unroll
-    for (int y = 0; y < kPselItems; ++y) {
-      const int c = page_at(round, y);
-      if (any_at(round, y)) v[y] = c < n ? scores[c] : 0.f;
-    }
-  };
-  load_round(0);
   float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest sum |q| |bound|
-  const float* um = p.unit_max + (size_t)pair * pscore_units(p.width);
+  const float4* units = p.units + (size_t)pair * pscore_units(p.width);
   bool odd = false;
 #pragma unroll 1
   for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
-    const float f = um[x];
-    odd |= f != f;
-    limit = fmaxf(limit, f);
+    const float4 f = units[x];
+    odd |= f.x != f.x;
+    limit = fmaxf(limit, f.x);
+    top = fmaxf(top, f.y);
+    bottom = fminf(bottom, f.z);
   }
   if constexpr (!kExact)
 #pragma unroll 1
@@ -305,16 +346,6 @@ choose_pages_kernel(SelectPagesParams p) {
 #pragma unroll 1
   for (int x = threadIdx.x; x < kPselBins; x += kPselThreads) hist[x] = 0u;
   if (threadIdx.x == 0) s_sure = s_listed = 0;
-#pragma unroll 1
-  for (int round = 0; round < rounds; ++round) {
-    if (rounds > 1) load_round(round);
-#pragma unroll
-    for (int y = 0; y < kPselItems; ++y)
-      if (any_at(round, y) && open_page(page_at(round, y))) {
-        top = fmaxf(top, v[y]);
-        bottom = fminf(bottom, v[y]);
-      }
-  }
   top = warp_max(top);
   bottom = -warp_max(-bottom);
   limit = warp_max(limit);
@@ -324,9 +355,9 @@ choose_pages_kernel(SelectPagesParams p) {
     red[2][warp] = limit;
   }
   odd = __syncthreads_or(odd);
-  top = warp_max(red[0][lane]);
-  bottom = -warp_max(red[1][lane]);
-  limit = warp_max(red[2][lane]);
+  top = warp_max(red[0][lane % kWarps]);
+  bottom = -warp_max(red[1][lane % kWarps]);
+  limit = warp_max(red[2][lane % kWarps]);
   // eps: a score is 2 D products summed by D / 8 instructions; each adds 16 products to a sum in fp32, cutting every addend to
   // 24 bits of the largest at worst, 17 * 2^-24 of sum |q| |bound| in all: D / 8 * 17 * 2^-24 < D 2^-22.  (That sum itself is known to
   // as much: the 1 % on top covers it.)
@@ -356,10 +387,20 @@ choose_pages_kernel(SelectPagesParams p) {
     }
     __syncthreads();
     {
-      const uint2 two = reinterpret_cast<const uint2*>(hist)[threadIdx.x];
+      constexpr int kOwn = kPselBins / kPselThreads;           // a thread's bins
+      int own[kOwn], sum = 0;
+#pragma unroll
+      for (int y = 0; y < kOwn; ++y) {
+        own[y] = (int)hist[kOwn * threadIdx.x + y];
+        sum += own[y];
+      }
       int all;
-      const int before = block_prefix<kPselThreads>((int)(two.x + two.y), scan, all);
-      if (before < want && before + (int)(two.x + two.y) >= want) s_bin = 2 * threadIdx.x + (before + (int)two.x < want);
+      int before = block_prefix<kPselThreads>(sum, scan, all);
+#pragma unroll
+      for (int y = 0; y < kOwn; ++y) {
+        if (before < want && before + own[y] >= want) s_bin = kOwn * threadIdx.x + y;
+        before += own[y];
+      }
     }
     __syncthreads();
     // the bin of the want-th largest approximate score, widened by the rounding of its own borders, and 2 eps on each side
@@ -402,8 +443,9 @@ choose_pages_kernel(SelectPagesParams p) {
         }
         __syncthreads();
       }
-      if ((int)threadIdx.x < listed) {                         // the `need` best of the list, ties to the lowest page
-        const uint2 me = list[threadIdx.x];
+#pragma unroll 1
+      for (int e = threadIdx.x; e < listed; e += kPselThreads) {     // the `need` best of the list, ties to the lowest page
+        const uint2 me = list[e];
         int better = 0;
 #pragma unroll 4
         for (int o = 0; o < listed; ++o) {
@@ -441,13 +483,20 @@ choose_pages_kernel(SelectPagesParams p) {
         if (!forced(c) && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1u)], 1u);
       }
       __syncthreads();
-      const int b0 = (int)bins - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;          // from the top down
-      const int n0 = b1 >= 0 ? (int)hist[b0] : 0, n1 = b1 >= 0 ? (int)hist[b1] : 0;
-      int all;
-      const int above = block_prefix<kPselThreads>(n0 + n1, scan, all);
-      if (above < remaining && above + n0 + n1 >= remaining) {
-        s_bin = above + n0 >= remaining ? b0 : b1;
-        s_need = above + n0 >= remaining ? remaining - above : remaining - above - n0;
+      constexpr int kOwn = kPselBins / kPselThreads;           // a thread's bins, from the top down
+      const int b0 = (int)bins - 1 - kOwn * (int)threadIdx.x;
+      int sum = 0, all;
+#pragma unroll 1
+      for (int y = 0; y < kOwn; ++y) sum += b0 - y >= 0 ? (int)hist[b0 - y] : 0;
+      int above = block_prefix<kPselThreads>(sum, scan, all);
+#pragma unroll 1
+      for (int y = 0; y < kOwn && b0 - y >= 0; ++y) {
+        const int here = (int)hist[b0 - y];
+        if (above < remaining && above + here >= remaining) {
+          s_bin = b0 - y;
+          s_need = remaining - above;
+        }
+        above += here;
       }
       __syncthreads();
       prefix |= (unsigned int)s_bin << shift;
