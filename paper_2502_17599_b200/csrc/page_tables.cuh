@@ -17,7 +17,8 @@
 
 namespace meda {
 
-constexpr int kTabThreads = 512;
+constexpr int kTabThreads = 1024;
+constexpr int kTabPer = kPagesMaxSeqs / kTabThreads;     // sequences of a thread, at most
 
 struct TablesParams {
   const int32_t* lens;
@@ -68,22 +69,24 @@ page_tables_kernel(TablesParams p) {
   const int per = (n + kTabThreads - 1) / kTabThreads;
   const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
   long long moves = 0, rows = 0;
-  int touched = 0;
-  int bad = 0;
-#pragma unroll 1
-  for (int i = lo; i < hi; ++i) {
-    const int a = was[i], b = will[i];
-    const bool off = a < 0 || b < 0 || a > max_rows || b > max_rows;
-    bad |= off;
-    const int step = off ? 0 : pages_of(b, p.page_shift) - pages_of(a, p.page_shift), more = off ? 0 : max(0, b - a);
-    pops[i + 1] = max(0, step);
-    pushes[i + 1] = max(0, -step);
-    const int pages = more ? pages_of(b, p.page_shift) - (a >> p.page_shift) : 0;
-    fresh[i + 1] = more;
-    units[i + 1] = pages;
-    touched += pages;
-    moves += ((long long)max(0, step) << 32) + max(0, -step);
-    rows += more;
+  int touched = 0, bad = 0;
+  int step[kTabPer], more[kTabPer], pages[kTabPer];             // pages taken (given back: negative), new rows, pages they touch
+#pragma unroll
+  for (int y = 0; y < kTabPer; ++y) {
+    step[y] = more[y] = pages[y] = 0;
+    if (lo + y < hi) {
+      const int a = was[lo + y], b = will[lo + y];
+      if (a < 0 || b < 0 || a > max_rows || b > max_rows) {
+        bad = 1;
+      } else {
+        step[y] = pages_of(b, p.page_shift) - pages_of(a, p.page_shift);
+        more[y] = max(0, b - a);
+        pages[y] = more[y] ? pages_of(b, p.page_shift) - (a >> p.page_shift) : 0;
+      }
+    }
+    moves += ((long long)max(0, step[y]) << 32) + max(0, -step[y]);
+    rows += more[y];
+    touched += pages[y];
   }
   long long incl_moves = moves, incl_rows = rows;
   int incl_touched = touched;
@@ -103,24 +106,28 @@ page_tables_kernel(TablesParams p) {
     warp_touched[warp] = incl_touched;
   }
   bad = __syncthreads_or(bad);
-  long long all_moves = 0, n_fresh = 0;
-  incl_moves -= moves;
-  incl_rows -= rows;
-  incl_touched -= touched;
-  int total_units = 0;
+  // every warp scans the warps' sums by itself, one per lane
+  constexpr int kWarps = kTabThreads / 32;
+  long long sum_moves = lane < kWarps ? warp_moves[lane] : 0, sum_rows = lane < kWarps ? warp_rows[lane] : 0;
+  int sum_touched = lane < kWarps ? warp_touched[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kTabThreads / 32; ++w) {
-    const long long y = warp_moves[w], z = warp_rows[w];
-    const int t = warp_touched[w];
-    if (w < warp) {
-      incl_moves += y;
-      incl_rows += z;
-      incl_touched += t;
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, sum_moves, o), z = __shfl_up_sync(0xffffffffu, sum_rows, o);
+    const int t = __shfl_up_sync(0xffffffffu, sum_touched, o);
+    if (lane >= o) {
+      sum_moves += y;
+      sum_rows += z;
+      sum_touched += t;
     }
-    all_moves += y;
-    n_fresh += z;
-    total_units += t;
   }
+  const long long all_moves = __shfl_sync(0xffffffffu, sum_moves, 31), n_fresh = __shfl_sync(0xffffffffu, sum_rows, 31);
+  const int total_units = __shfl_sync(0xffffffffu, sum_touched, 31);
+  const long long before_moves = __shfl_sync(0xffffffffu, sum_moves, (warp + 31) % 32);
+  const long long before_rows = __shfl_sync(0xffffffffu, sum_rows, (warp + 31) % 32);
+  const int before_touched = __shfl_sync(0xffffffffu, sum_touched, (warp + 31) % 32);
+  incl_moves += (warp ? before_moves : 0) - moves;
+  incl_rows += (warp ? before_rows : 0) - rows;
+  incl_touched += (warp ? before_touched : 0) - touched;
   const long long n_pops = all_moves >> 32, n_pushes = all_moves & 0xffffffffll;
   const bool first = blockIdx.x == 0 && threadIdx.x == 0;
   int code = MEDA_OK;
@@ -139,18 +146,19 @@ page_tables_kernel(TablesParams p) {
     return;
   }
   int r_pop = (int)(incl_moves >> 32), r_push = (int)(incl_moves & 0xffffffffll), r_new = (int)incl_rows, r_unit = incl_touched;
-#pragma unroll 1
-  for (int i = lo; i < hi; ++i) {
-    r_pop += pops[i + 1];
-    r_push += pushes[i + 1];
-    r_new += fresh[i + 1];
-    r_unit += units[i + 1];
-    units[i + 1] = r_unit;
-    pops[i + 1] = r_pop;
-    pushes[i + 1] = r_push;
-    fresh[i + 1] = r_new;
-    if (blockIdx.x == 0) p.cu_new[i + 1] = r_new;
-  }
+#pragma unroll
+  for (int y = 0; y < kTabPer; ++y)
+    if (lo + y < hi) {
+      r_pop += max(0, step[y]);
+      r_push += max(0, -step[y]);
+      r_new += more[y];
+      r_unit += pages[y];
+      pops[lo + y + 1] = r_pop;
+      pushes[lo + y + 1] = r_push;
+      fresh[lo + y + 1] = r_new;
+      units[lo + y + 1] = r_unit;
+      if (blockIdx.x == 0) p.cu_new[lo + y + 1] = r_new;
+    }
   if (threadIdx.x == 0) pops[0] = pushes[0] = fresh[0] = units[0] = 0;
   if (first) {
     p.cu_new[0] = 0;
@@ -183,7 +191,7 @@ page_tables_kernel(TablesParams p) {
   const int mask = (1 << p.page_shift) - 1;
   const int warps = gridDim.x * (kTabThreads / 32);
 #pragma unroll 1
-  for (long long u0 = (long long)(blockIdx.x * (kTabThreads / 32) + warp) * 32; u0 < total_units; u0 += (long long)warps * 32) {
+  for (long long u0 = (long long)(warp * gridDim.x + blockIdx.x) * 32; u0 < total_units; u0 += (long long)warps * 32) {
     const int u = (int)u0 + lane;
     int first_slot = total_new, rows_here = 0, page = -1, row0 = 0;
     if (u < total_units) {
@@ -205,15 +213,21 @@ page_tables_kernel(TablesParams p) {
     const int begin = __shfl_sync(0xffffffffu, first_slot, 0);
     const int last = 31 - __clz(__ballot_sync(0xffffffffu, rows_here > 0));
     const int end = __shfl_sync(0xffffffffu, first_slot + rows_here, last);
-#pragma unroll 4
-    for (int t0 = begin; t0 < end; t0 += 32) {
-      const int t = t0 + lane;
-      int owner = 0;                                           // the lane whose page holds slot t
+#pragma unroll 1
+    for (int t0 = begin; t0 < end; t0 += 128) {                // four slots of a lane at a time: their searches run side by side
+      int owner[4] = {0, 0, 0, 0};                             // the lane whose page holds the slot
 #pragma unroll
       for (int step = 16; step > 0; step >>= 1)
-        if (__shfl_sync(0xffffffffu, first_slot, owner + step) <= t) owner += step;
-      const int pg = __shfl_sync(0xffffffffu, page, owner), r = __shfl_sync(0xffffffffu, row0, owner) + t - __shfl_sync(0xffffffffu, first_slot, owner);
-      if (t < end) p.slots[t] = pg < 0 ? -1 : ((int64_t)pg << p.page_shift) + r;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (__shfl_sync(0xffffffffu, first_slot, owner[y] + step) <= t0 + 32 * y + lane) owner[y] += step;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int t = t0 + 32 * y + lane;
+        const int pg = __shfl_sync(0xffffffffu, page, owner[y]);
+        const int r = __shfl_sync(0xffffffffu, row0 - first_slot, owner[y]) + t;
+        if (t < end) p.slots[t] = pg < 0 ? -1 : ((int64_t)pg << p.page_shift) + r;
+      }
     }
   }
   // pages given back that nobody took onto the list; nothing in the slots behind the last row

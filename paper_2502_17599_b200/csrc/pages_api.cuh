@@ -321,10 +321,11 @@ meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t len
   const meda_pages_config& c = pages->cfg;
   TablesParams a = {lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, pages->status,
                     lens_stride, new_stride, n_seqs, c.n_pages, c.max_seq_pages, pages->page_shift, (int)slots_capacity};
-  // one page that gets rows per lane, one block per SM at most: each block repeats the scans
+  // every page that gets rows is a lane's; the warps that hold them are spread over blocks, two to each, one block per SM at most
+  // (each block repeats the scans)
   const int64_t units = slots_capacity ? (slots_capacity >> pages->page_shift) + 2 * (int64_t)n_seqs
                                        : std::min<int64_t>(c.n_pages, (int64_t)n_seqs * c.max_seq_pages);
-  const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (units + kTabThreads - 1) / kTabThreads));
+  const int grid = (int)std::min<int64_t>(pages->sm_count, std::max<int64_t>(1, (units + 63) / 64));
   return launch_after(pages, page_tables_kernel, grid, kTabThreads, tables_smem(n_seqs), as_stream(stream), a);
 }
 
