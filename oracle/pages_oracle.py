@@ -78,10 +78,11 @@ def rope(x, positions, sections, order, pairing, theta):
 
 def page_scores(q_heads, bounds):
     """q_heads [G][D], bounds [pages][2][D] -> fp32 scores of one KV head's pages."""
-    per = np.where(q_heads[:, None] >= 0, q_heads[:, None] * bounds[None, :, 1], q_heads[:, None] * bounds[None, :, 0])
-    s = per.sum(-1)
-    s = np.where(np.isnan(s).any(0), np.nan, s.max(0))
-    return s.astype(np.float32)
+    with np.errstate(invalid="ignore", over="ignore"):
+        per = np.where(q_heads[:, None] >= 0, q_heads[:, None] * bounds[None, :, 1], q_heads[:, None] * bounds[None, :, 0])
+        s = per.sum(-1)
+        s = np.where(np.isnan(s).any(0), np.nan, s.max(0))
+        return s.astype(np.float32)
 
 
 def select_pages(scores, keep, n_first, n_last):

@@ -4,8 +4,10 @@
 
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 
 #include "page_rows.cuh"
@@ -57,6 +59,18 @@ meda_status launch_after(meda_pages* p, K kernel, dim3 grid, int block, size_t s
 
 inline bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
 
+// raise_dyn_smem, once for each kernel and device: a server makes handles while others are in use.
+template <auto kernel>
+meda_status raise_once() {
+  static std::atomic<unsigned long long> done{0};              // a bit per device, up to 64 of them
+  int device = 0;
+  MEDA_CUDA_TRY(cudaGetDevice(&device));
+  if (device < 64 && (done.load(std::memory_order_acquire) >> device & 1u)) return MEDA_OK;
+  const meda_status r = raise_dyn_smem(kernel);
+  if (r == MEDA_OK && device < 64) done.fetch_or(1ull << device, std::memory_order_release);
+  return r;
+}
+
 int pages_element(const meda_pages* p) { return p->cfg.dtype == MEDA_F32 ? 4 : 2; }
 
 // meda_* status of the arguments every call over sequences shares.
@@ -70,23 +84,15 @@ template <typename Tile, int D, int W>
 struct AttnKernel {
   static constexpr auto kernel = paged_attention_kernel<Tile, D, W>;
   static size_t smem(int n_seqs) { return (size_t)(attn_prefix_floats(n_seqs) + 2 * attn_merge_floats(W, Tile::kHeads, D)) * 4; }
-  // Blocks that are resident at once, with the shared memory of the largest batch.
+  // One block per SM, with the shared memory of the largest batch.
   static meda_status prepare(meda_pages* p) {
-    cudaFuncAttributes a;
-    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return MEDA_ERR_CUDA;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem - (int)a.sharedSizeBytes) != cudaSuccess)
-      return MEDA_ERR_CUDA;
-    int per_sm = 0;
-    const size_t need = smem(p->cfg.max_seqs);
-    if (need > (size_t)(kMaxDynSmem - (int)a.sharedSizeBytes)) return MEDA_ERR_SHAPE;
+    if (smem(p->cfg.max_seqs) > (size_t)kMaxDynSmem - 1024) return MEDA_ERR_SHAPE;
     // tiles of all segments, and as many again for the look-ahead, are counted in 32 bits
     const int64_t segments = (int64_t)p->cfg.n_kv_heads * ((p->group + Tile::kHeads - 1) / Tile::kHeads);
     if (segments * p->cfg.max_seqs * ((int64_t)p->cfg.max_seq_pages * (p->cfg.page_size / kAttTile) + kAttSegment) >= (int64_t(1) << 31) - 65536)
       return MEDA_ERR_SHAPE;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, W * 32, need) != cudaSuccess || per_sm < 1)
-      return MEDA_ERR_CUDA;
     p->attn_blocks = p->sm_count;
-    return MEDA_OK;
+    return raise_once<kernel>();
   }
   static meda_status launch(meda_pages* p, AttnParams a, cudaStream_t st) {
     a.heads_div.set((unsigned)(a.n_heads * ((a.group + Tile::kHeads - 1) / Tile::kHeads)));
@@ -122,9 +128,9 @@ meda_status with_attn_kernel(const meda_pages* p, F f) {
 template <typename T, int D, int GP>
 struct SelectPagesKernels {
   static meda_status prepare() {
-    meda_status r = raise_dyn_smem(page_scores_kernel<T, D, GP>);
-    if (r == MEDA_OK) r = raise_dyn_smem(choose_pages_kernel<T, D, 256>);
-    return r == MEDA_OK ? raise_dyn_smem(choose_pages_kernel<T, D, 1024>) : r;
+    meda_status r = raise_once<page_scores_kernel<T, D, GP>>();
+    if (r == MEDA_OK) r = raise_once<choose_pages_kernel<T, D, 256>>();
+    return r == MEDA_OK ? raise_once<choose_pages_kernel<T, D, 1024>>() : r;
   }
   static meda_status launch(meda_pages* p, const SelectPagesParams& a, cudaStream_t st) {
     // fp32 scores are bound by 64-bit arithmetic and want twice the warps (and no third block on an SM: see tables_smem)
@@ -160,12 +166,12 @@ meda_status with_select_kernels(const meda_pages* p, F f) {
 }
 
 // Scratch of the selection: one sequence's scores and their bounds, in floats, and how many sequences it holds (at least
-// one, more while that stays below 32 MB; a larger batch goes through it in several launches).
+// one, more while that stays below 8 MB; a larger batch goes through it in several launches).
 int64_t select_seq_floats(const meda_pages_config& c) {
   return (int64_t)c.n_kv_heads * ((c.max_seq_pages + 3) / 4 * 4 + 4 * pscore_units(c.max_seq_pages));
 }
 int select_scratch_seqs(const meda_pages_config& c) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(c.max_seqs, (int64_t(32) << 20) / 4 / select_seq_floats(c)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(c.max_seqs, (int64_t(8) << 20) / 4 / select_seq_floats(c)));
 }
 
 // ---- pages of rows -----------------------------------------------------------------------------
@@ -180,16 +186,8 @@ meda_status launch_page_rows(meda_pages* p, const RowsParams& a, cudaStream_t st
                                                                            : go(page_rows_kernel<__nv_bfloat16, 32, STORE>);
 }
 
-template <bool STORE>
-meda_status raise_page_rows_smem() {
-  meda_status r = raise_dyn_smem(page_rows_kernel<float, 16, STORE>);
-  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<float, 32, STORE>);
-  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<float, 64, STORE>);
-  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 8, STORE>);
-  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 16, STORE>);
-  if (r == MEDA_OK) r = raise_dyn_smem(page_rows_kernel<__nv_bfloat16, 32, STORE>);
-  return r;
-}
+// (32 KB of prefixes at most: below the limit every kernel starts with)
+static_assert((kPagesMaxSeqs + 1) * 4 <= 48 * 1024, "page_rows_kernel would have to raise its shared memory");
 
 template <typename T, bool ADJACENT>
 meda_status launch_rope(meda_pages* p, const RopeParams& a, int grid, cudaStream_t st) {
@@ -200,12 +198,7 @@ meda_status launch_rope(meda_pages* p, const RopeParams& a, int grid, cudaStream
 }
 
 void pages_release(meda_pages* p) {
-  cudaFree(p->status);
-  cudaFree(p->rope_freq);
-  cudaFree(p->rope_axis);
-  cudaFree(p->attn_partial);
-  cudaFree(p->attn_split);
-  cudaFree(p->select_scratch);
+  cudaFree(p->slab);
   delete p;
 }
 
@@ -263,20 +256,32 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
     st = MEDA_ERR_CUDA;
   if (st == MEDA_OK) st = with_attn_kernel(p, [&](auto k) { return k.prepare(p); });
   if (st == MEDA_OK) st = with_select_kernels(p, [](auto k) { return k.prepare(); });
-  if (st == MEDA_OK) st = raise_page_rows_smem<true>();
-  if (st == MEDA_OK) st = raise_page_rows_smem<false>();
-  if (st == MEDA_OK) st = raise_dyn_smem(page_tables_kernel);
-  if (st == MEDA_OK) st = carve(&p->status, 1, &p->bytes);
-  if (st == MEDA_OK) st = carve(&p->rope_freq, half, &p->bytes);
-  if (st == MEDA_OK) st = carve(&p->rope_axis, half, &p->bytes);
-  if (st == MEDA_OK) st = carve(&p->attn_partial, (int64_t)p->attn_blocks * 2 * attn_state_floats(p->group, c.head_dim), &p->bytes);
-  if (st == MEDA_OK) st = carve(&p->select_scratch, select_seq_floats(c) * select_scratch_seqs(c), &p->bytes);
-  if (st == MEDA_OK) st = carve(&p->attn_split, p->attn_blocks, &p->bytes);
-  if (st == MEDA_OK && (cudaMemset(p->status, 0, sizeof(int)) != cudaSuccess ||
-                        cudaMemcpy(p->rope_freq, freq, (size_t)half * 8, cudaMemcpyHostToDevice) != cudaSuccess ||
-                        cudaMemcpy(p->rope_axis, axis, (size_t)half * 4, cudaMemcpyHostToDevice) != cudaSuccess ||
-                        cudaStreamSynchronize(nullptr) != cudaSuccess))
-    st = MEDA_ERR_CUDA;
+  if (st == MEDA_OK) st = raise_once<page_tables_kernel>();
+  if (st == MEDA_OK) {
+    // one allocation: [status | frequencies | axes | splits | states | scores]; the first three from the host, the others need no start
+    const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
+    const int64_t freq_at = 256, axis_at = freq_at + up(half * 8), split_at = axis_at + up(half * 4);
+    const int64_t partial_at = split_at + up((int64_t)p->attn_blocks * (int64_t)sizeof(int4));
+    const int64_t scores_at = partial_at + up((int64_t)p->attn_blocks * 2 * attn_state_floats(p->group, c.head_dim) * 4);
+    const int64_t bytes = scores_at + up(select_seq_floats(c) * select_scratch_seqs(c) * 4);
+    alignas(8) unsigned char host[256 + 1024 + 512] = {0};
+    memcpy(host + freq_at, freq, (size_t)half * 8);
+    memcpy(host + axis_at, axis, (size_t)half * 4);
+    char* slab = nullptr;
+    if (cudaMalloc(reinterpret_cast<void**>(&slab), (size_t)bytes) != cudaSuccess) st = MEDA_ERR_CUDA;
+    else {
+      p->slab = slab;
+      p->bytes = bytes;
+      p->status = reinterpret_cast<int*>(slab);
+      p->rope_freq = reinterpret_cast<unsigned long long*>(slab + freq_at);
+      p->rope_axis = reinterpret_cast<int*>(slab + axis_at);
+      p->attn_split = reinterpret_cast<int4*>(slab + split_at);
+      p->attn_partial = reinterpret_cast<float*>(slab + partial_at);
+      p->select_scratch = reinterpret_cast<float*>(slab + scores_at);
+      if (cudaMemcpy(slab, host, (size_t)split_at, cudaMemcpyHostToDevice) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess)
+        st = MEDA_ERR_CUDA;
+    }
+  }
   if (st != MEDA_OK) {
     pages_release(p);
     cudaGetLastError();

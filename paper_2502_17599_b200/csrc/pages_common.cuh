@@ -13,6 +13,7 @@ struct meda_pages {
   int page_shift = 4;                  // log2(page_size)
   int64_t launches = 0;
   int64_t bytes = 0;
+  void* slab = nullptr;                // the one allocation all pointers below lead into
   int* status = nullptr;               // device status word (first error wins)
   unsigned long long* rope_freq = nullptr;   // [half] turns per position, as a 64-bit fraction
   int* rope_axis = nullptr;            // [half]
@@ -86,15 +87,14 @@ __device__ __forceinline__ void ragged_prefix(int n, int* pre, int* scratch, F u
     __syncwarp();
     return;
   }
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += THREADS) pre[i + 1] = units(i);         // neighbouring threads, neighbouring lengths
+  __syncthreads();
   const int per = (n + THREADS - 1) / THREADS;
   const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
   int sum = 0;
 #pragma unroll 1
-  for (int i = lo; i < hi; ++i) {
-    const int u = units(i);
-    pre[i + 1] = u;
-    sum += u;
-  }
+  for (int i = lo; i < hi; ++i) sum += pre[i + 1];
   int total;
   int run = block_prefix<THREADS>(sum, scratch, total);
 #pragma unroll 1

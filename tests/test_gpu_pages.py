@@ -170,6 +170,23 @@ def test_page_tables_steps_never_share_a_page(B):
     pg.close()
 
 
+def test_page_tables_largest_batch(B):
+    """8,192 sequences (all the shared memory the scans take), most of them untouched."""
+    rng = np.random.default_rng(9)
+    n, page, width = 8192, 16, 6
+    lens = rng.integers(0, 90, n)
+    new = np.where(rng.random(n) < 0.9, lens, rng.integers(0, 97, n))
+    used = sum(O.n_pages_of(int(x), page) for x in lens)
+    table = table_for(lens, page, width, used, 1)
+    n_pages = used + 9000
+    free = np.concatenate([np.zeros(used), np.arange(used, n_pages)]).astype(np.int64)
+    capacity = int(np.maximum(new - lens, 0).sum()) + 1000
+    want = O.page_tables(lens, new, free, used, table, page, capacity)
+    got, status = run_tables(B, lens.tolist(), new.tolist(), page, width, n_pages, used, table, free, capacity)
+    assert want[5] and status == 0
+    same_tables(got, want)
+
+
 # ------------------------------------------------------------------------------------------------- store
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -600,6 +617,67 @@ def test_select_pages_ties_zeros_and_nan(B):
     pg.close()
 
 
+def test_select_pages_many_rounds_and_many_pairs(B):
+    """More pages than a block holds at once (one large block per pair, and small blocks for many pairs), and more sequences than
+    the scratch holds scores of at once."""
+    for lens, hq, hkv, d, keep in (([150_011], 2, 1, 64, 700), ([41_000] * 38 + [3, 0], 8, 4, 64, 37)):
+        pg, q, kp, vp, table, out, lse = attention_case(B, lens, hq, hkv, d, "bf16", 16, seed=31)
+        t, n = i32(table.tolist()), i32(lens)
+        bd = torch.zeros((kp.shape[0], hkv, 2, d), dtype=torch.bfloat16, device="cuda")
+        sel = torch.full((len(lens), hkv, keep), -1, dtype=torch.int32, device="cuda")
+        pg.page_bounds(kp, t, None, n, bd)
+        pg.select_pages(q, bd, t, n, 1, 2, sel)
+        pg.check()
+        check_selection(sel, q, bd, table, lens, 16, keep, 1, 2)
+        # the same query everywhere 0: every page ties, the 64-bit path decides by the page's number
+        q.zero_()
+        sel.fill_(-1)
+        pg.select_pages(q, bd, t, n, 1, 2, sel)
+        pg.check()
+        check_selection(sel, q, bd, table, lens, 16, keep, 1, 2)
+        pg.close()
+    # a table row of 65,536 entries: the scratch holds few sequences, the batch goes through it in turns
+    rng = np.random.default_rng(0)
+    lens = rng.integers(0, 1500, 60).tolist()
+    width, hkv, d = 65_536, 2, 64
+    n_pages = sum(O.n_pages_of(x, 16) for x in lens)
+    table = table_for(lens, 16, width, n_pages, 3)
+    pg = make(B, n_q_heads=6, n_kv_heads=hkv, head_dim=d, n_pages=n_pages, max_seqs=60, max_seq_pages=width)
+    q, kp = normal((60, 6, d), DT["bf16"], 1), normal((n_pages, hkv, 16, d), DT["bf16"], 2, 0.3)
+    bd = torch.zeros((n_pages, hkv, 2, d), dtype=torch.bfloat16, device="cuda")
+    sel = torch.full((60, hkv, 11), -1, dtype=torch.int32, device="cuda")
+    t, n = i32(table.tolist()), i32(lens)
+    pg.page_bounds(kp, t, None, n, bd)
+    before = pg.launch_count()
+    pg.select_pages(q, bd, t, n, 1, 2, sel)
+    assert pg.launch_count() - before > 2
+    pg.check()
+    check_selection(sel, q, bd, table, lens, 16, 11, 1, 2)
+    pg.close()
+
+
+def test_select_pages_infinite_and_huge_bounds(B):
+    """Scores that are infinite or NaN, or so large that an fp32 sum overflows on the way, go to the 64-bit path."""
+    for dtype in ("bf16", "f32"):
+        lens, page, d, keep = [16 * 300] * 4, 16, 64, 9
+        pg, q, kp, vp, table, out, lse = attention_case(B, lens, 3, 1, d, dtype, page, seed=6)
+        t, n = i32(table.tolist()), i32(lens)
+        bd = torch.zeros((kp.shape[0], 1, 2, d), dtype=DT[dtype], device="cuda")
+        pg.page_bounds(kp, t, None, n, bd)
+        pages = t.long()
+        bd[pages[0, 17], 0, 1, 5] = math.inf
+        bd[pages[0, 18], 0, 0, 5] = -math.inf
+        q[0, :, 5] = torch.tensor([1.0, -1.0, 2.0], device="cuda")
+        bd[pages[1, 40], 0, 0, 3] = -math.inf                      # 0 times it, or a score of -inf: never among the best
+        q[1, :, 3] = torch.tensor([-0.5, 0.5, 0.0], device="cuda")
+        bd[pages[2, :300], 0] = bd[pages[2, :300], 0] * 1e37       # sums near the largest float
+        sel = torch.full((4, 1, keep), -1, dtype=torch.int32, device="cuda")
+        pg.select_pages(q, bd, t, n, 0, 1, sel)
+        pg.check()
+        check_selection(sel, q, bd, table, lens, page, keep, 0, 1)
+        pg.close()
+
+
 # ---------------------------------------------------------------------------------------------- refusals
 
 def test_refusals(B):
@@ -814,6 +892,61 @@ def test_paged_attention_agrees_with_attention_over_the_dense_cache(B):
     dec.close()
     for cp in cps:
         cp.close()
+
+
+def test_calls_behind_copies_joins_and_other_kernels_in_a_graph(B):
+    """The launches may be set up ahead of the work before them; that must wait all the same, whatever it is: a memset, a copy,
+    another stream's kernel, an ordinary kernel, and it must hold inside one captured graph."""
+    lens = [700, 33]
+    pg, q, kp, vp, table, out, lse = attention_case(B, lens, 8, 2, 128, "bf16", 16, seed=14)
+    t, n = i32(table.tolist()), i32(lens)
+    source, live = torch.stack([n, n - 5, n - 20]), n.clone()
+    wants = []
+    for i in range(3):
+        o = torch.empty_like(out)
+        pg.paged_attention(q, kp, vp, t, source[i].contiguous(), o)
+        wants.append(o)
+    torch.cuda.synchronize()
+    pick = torch.zeros(1, dtype=torch.int64, device="cuda")
+    big = torch.zeros(32 << 20, device="cuda")
+    side = torch.cuda.Stream()
+    outs = [torch.empty_like(out) for _ in range(4)]
+
+    def body():
+        main = torch.cuda.current_stream()
+        live.zero_()
+        big.add_(1.0)                                              # something long, so that an early start would read zeros
+        live.copy_(source.index_select(0, pick)[0])
+        pg.paged_attention(q, kp, vp, t, live, outs[0])
+        live.zero_()
+        pg.paged_attention(q, kp, vp, t, live, outs[1])
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            big.add_(1.0)
+            live.copy_(source.index_select(0, pick)[0])
+        main.wait_stream(side)
+        pg.paged_attention(q, kp, vp, t, live, outs[2])
+        outs[3].copy_(outs[2])
+
+    body()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        body()
+    for i in (0, 2, 1, 0):
+        pick.fill_(i)
+        for o in outs:
+            o.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], wants[i]) and torch.equal(outs[2], wants[i]) and torch.equal(outs[3], wants[i]) and (outs[1] == 0).all()
+        for o in outs:
+            o.fill_(math.nan)
+        body()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], wants[i]) and torch.equal(outs[2], wants[i]) and (outs[1] == 0).all()
+    pg.check()
+    pg.close()
 
 
 def test_two_handles_on_two_streams_and_two_graphs(B):
