@@ -299,8 +299,9 @@ choose_pages_kernel(SelectPagesParams p) {
   const int pair = blockIdx.x, i = p.heads_div.of(pair), g = pair - i * p.n_heads;
   const int page_size = 1 << p.page_shift;
   // a thread's scores: page (round * items + y) * threads + thread, so that a warp's 32 pages are one word of the bit maps;
-  // the first round is fetched before the sequence's length is known
+  // what the first round needs is fetched before the sequence's length is known
   const float* scores = p.scores + (size_t)pair * p.width;
+  const float4* units = p.units + (size_t)pair * pscore_units(p.width);
   float v[kPselItems];
   auto page_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads + (int)threadIdx.x; };
   auto load_round = [&](int round) {
@@ -311,6 +312,7 @@ choose_pages_kernel(SelectPagesParams p) {
     }
   };
   load_round(0);
+  const float4 first_unit = (int)threadIdx.x < pscore_units(p.width) ? units[threadIdx.x] : make_float4(0.f, 0.f, 0.f, 0.f);
   bool bad = false;
   const int len = clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad);
   const int n = (len + page_size - 1) >> p.page_shift;         // pages of the sequence
@@ -329,12 +331,19 @@ choose_pages_kernel(SelectPagesParams p) {
   auto open_page = [&](int c) { return c < n && !forced(c); };
 
   auto any_at = [&](int round, int y) { return (round * kPselItems + y) * kPselThreads < n; };       // uniform
+  // pages kept anyway count as +inf from here on, what lies behind the last page as -inf
+  auto settle = [&](int round) {
+#pragma unroll
+    for (int y = 0; y < kPselItems; ++y) {
+      const int c = page_at(round, y);
+      if (any_at(round, y)) v[y] = c >= n ? -INFINITY : (forced(c) ? INFINITY : v[y]);
+    }
+  };
   float top = -INFINITY, bottom = INFINITY, limit = 0.f;       // limit: largest sum |q| |bound|
-  const float4* units = p.units + (size_t)pair * pscore_units(p.width);
   bool odd = false;
 #pragma unroll 1
   for (int x = threadIdx.x; x < pscore_units(n); x += kPselThreads) {
-    const float4 f = units[x];
+    const float4 f = x == (int)threadIdx.x ? first_unit : units[x];
     odd |= f.x != f.x;
     limit = fmaxf(limit, f.x);
     top = fmaxf(top, f.y);
@@ -380,10 +389,11 @@ choose_pages_kernel(SelectPagesParams p) {
   } else if (decided) {
 #pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
-      if (rounds > 1) load_round(round);
+      if (round > 0) load_round(round);
+      settle(round);
 #pragma unroll
       for (int y = 0; y < kPselItems; ++y)
-        if (any_at(round, y) && open_page(page_at(round, y))) atomicAdd(&hist[bin_of(v[y])], 1u);
+        if (any_at(round, y) && v[y] != -INFINITY) atomicAdd(&hist[bin_of(v[y])], 1u);
     }
     __syncthreads();
     {
@@ -398,28 +408,31 @@ choose_pages_kernel(SelectPagesParams p) {
       int before = block_prefix<kPselThreads>(sum, scan, all);
 #pragma unroll
       for (int y = 0; y < kOwn; ++y) {
-        if (before < want && before + own[y] >= want) s_bin = kOwn * threadIdx.x + y;
+        if (before < p.keep && before + own[y] >= p.keep) s_bin = kOwn * threadIdx.x + y;
         before += own[y];
       }
     }
     __syncthreads();
-    // the bin of the want-th largest approximate score, widened by the rounding of its own borders, and 2 eps on each side
+    // the bin of the keep-th largest approximate score, widened by the rounding of its own borders, and 2 eps on each side
     const float round_off = 1e-6f * (fabsf(top) + fabsf(bottom));
     const float high = top - (float)s_bin / scale_or_one + round_off + slack, low = top - (float)(s_bin + 1) / scale_or_one - round_off - slack;
-    int sure = 0;
+    int sure = 0;                                              // of the warp's pages (lane 0 counts)
 #pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
-      if (rounds > 1) load_round(round);
+      if (rounds > 1) {
+        load_round(round);
+        settle(round);
+      }
 #pragma unroll
       for (int y = 0; y < kPselItems; ++y) {
         const int c = page_at(round, y);
         if (any_at(round, y) && c - lane < n) {                // uniform over the warp
-          const bool is_open = open_page(c);
-          const bool better = is_open && v[y] > high;
-          const unsigned int word = __ballot_sync(0xffffffffu, better || (c < n && forced(c)));
-          if (lane == 0) kept[c / 32] = word;
-          sure += better;
-          if (is_open && !better && v[y] >= low) {
+          const unsigned int word = __ballot_sync(0xffffffffu, v[y] > high);
+          if (lane == 0) {
+            kept[c / 32] = word;
+            sure += __popc(word);
+          }
+          if (v[y] <= high && v[y] >= low) {
             const int e = atomicAdd(&s_listed, 1);
             if (e < kPselMaxDoubt) {
               list[e] = make_uint2(page_key(v[y]), (unsigned int)c);
@@ -429,10 +442,9 @@ choose_pages_kernel(SelectPagesParams p) {
         }
       }
     }
-    sure = __reduce_add_sync(0xffffffffu, sure);
     if (lane == 0) atomicAdd(&s_sure, sure);
     __syncthreads();
-    const int listed = s_listed, need = want - s_sure;
+    const int listed = s_listed, need = p.keep - s_sure;
     decided = listed <= kPselMaxDoubt;
     if (decided) {
       if constexpr (!kExact) {
