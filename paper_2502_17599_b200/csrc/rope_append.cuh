@@ -14,7 +14,7 @@
 namespace meda {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 8;        // tokens per block
+constexpr int kRopeMaxTokens = 4;        // tokens per block
 
 struct RopeParams {
   const void* q;
