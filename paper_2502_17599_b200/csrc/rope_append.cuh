@@ -77,7 +77,10 @@ rope_append_kernel(RopeParams p) {
   constexpr int E = RopeVec<T>::E;
   begin_grid();
   constexpr int VR = D / E;                                    // vectors per head
-  __shared__ float2 turn[kRopeMaxTokens][D / 2];               // (cos, sin)
+  // (cos, sin) of the block's tokens: the frequencies an item works on one after the other lie `items` apart, so that neighbouring
+  // threads, which have neighbouring items, read neighbouring words (side by side in an item they met in two banks of 32)
+  __shared__ float2 turn[kRopeMaxTokens][D / 2];
+  constexpr int kPerItem = ADJACENT ? E / 2 : E;
   __shared__ int64_t slot_of[kRopeMaxTokens];
   const int t0 = blockIdx.x * p.tokens_per_block;
   const int n_tok = min(p.tokens_per_block, p.n_tokens - t0);
@@ -98,7 +101,7 @@ rope_append_kernel(RopeParams p) {
     const float half_turns = (float)(int)(frac >> 32) * 4.656612873077393e-10f;       // 2^-31: twice the turns, for sincospi
     float s, c;
     sincospif(half_turns, &s, &c);
-    turn[tok][i] = make_float2(c, s);
+    turn[tok][(i % kPerItem) * (half / kPerItem) + i / kPerItem] = make_float2(c, s);
   }
   __syncthreads();
 
@@ -149,7 +152,7 @@ rope_append_kernel(RopeParams p) {
       RopeVec<T>::unpack(src[item], f);
 #pragma unroll
       for (int e = 0; e < E / 2; ++e) {
-        const float2 cs = turn[tok][item * (E / 2) + e];
+        const float2 cs = turn[tok][e * rot + item];
         const float a = f[2 * e], b = f[2 * e + 1];
         f[2 * e] = a * cs.x - b * cs.y;
         f[2 * e + 1] = b * cs.x + a * cs.y;
@@ -163,7 +166,7 @@ rope_append_kernel(RopeParams p) {
       RopeVec<T>::unpack(xb, b);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float2 cs = turn[tok][item * E + e];
+        const float2 cs = turn[tok][e * rot + item];
         const float y = a[e] * cs.x - b[e] * cs.y;
         b[e] = b[e] * cs.x + a[e] * cs.y;
         a[e] = y;
