@@ -251,7 +251,7 @@ typedef struct {
 } meda_pages_config;
 
 /* Validates the geometry and allocates scratch memory on the current device (the only allocating call).
- * max_seqs * (max_seq_pages * page_size / 16 + 12) * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query
+ * max_seqs * (max_seq_pages * page_size / 16 + 20) * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query
  * heads per KV head in bf16 at head_dim 256 or in fp32; times up to four in fp32 at head_dim 256), n_pages * n_kv_heads * page_size below 2^40.
  * On failure *out is NULL and the status says why. */
 meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out);
