@@ -372,7 +372,9 @@ __host__ __device__ constexpr int attn_merge_floats(int warps, int heads, int d)
 
 // a / b for 0 <= a < 2^31, b > 0 and a quotient below 2^20: the fp32 estimate is off by one at most.
 __device__ __forceinline__ int div_small(int a, int b) {
-  int q = (int)((float)a * __frcp_rn((float)b));
+  float inverse;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"((float)b));             // off by 2^-23 at most
+  int q = (int)((float)a * inverse);
   const int r = a - q * b;
   q -= r < 0;
   q += r >= b;
