@@ -37,9 +37,11 @@ namespace meda {
 constexpr int kAttTile = 16;             // rows per tile; a page holds whole tiles
 // Empty tiles counted with every segment of a batch of sequences: what starting one and joining its warps' states takes,
 // in tiles of a block's time.  Without them a block whose share is many short segments works far longer than one inside
-// a long one (64 sequences of 36 to 18,944 rows: 91 us; 8 tiles: 91, 12: 80, 20: 74, 28: 74).
+// a long one (64 sequences of 36 to 18,944 rows: 96 us; 8 tiles: 87, 12: 80, 20: 71, 28: 72).
 constexpr int kAttSegment = 20;
-constexpr int kAttLeast = 8;             // tiles per block where the GPU has more blocks than that fills
+// Tiles per block where the GPU has more blocks than that fills.  One sequence of 947 rows, 4 KV heads: 4 tiles 7.2 us, 8: 7.6,
+// 16: 9.1; of 4,000 rows: 9.0, 8.5, 9.3.
+constexpr int kAttLeast = 8;
 
 // x / d for 0 <= x < 2^31 by a multiplication: with 2^s < d < 2^(s+1), mul = ceil(2^(32+s) / d) is off by less than d / 2^(32+s),
 // which x below 2^31 cannot turn into a whole unit; powers of two are shifts.
@@ -414,7 +416,7 @@ paged_attention_kernel(AttnParams p) {
     return tiles ? tiles + gap : 0;
   });
 
-  // Block b takes base tiles, the first `extra` blocks one more.  (All tile counts stay below 2^31: see meda_pages_create.)
+  // (All tile counts stay below 2^31: see meda_pages_create.)
   const int total = pre[p.n_seqs] * H;
   // Blocks with work: as many to a segment as give each kAttLeast tiles on average, so that segments of one length are cut
   // alike and no block works on two of them needlessly.  Block b's first tile is b / C of the total, rounded down.

@@ -19,7 +19,7 @@ struct meda_pages {
   int* rope_axis = nullptr;            // [half]
   float* attn_partial = nullptr;       // [blocks][2][group][head_dim + 2] softmax states of segments that cross blocks
   int4* attn_split = nullptr;          // [blocks] segments that go on behind a block
-  float* select_scratch = nullptr;     // [sequences][n_kv_heads][max_seq_pages] scores, then a bound per eight pages of them
+  float* select_scratch = nullptr;     // [sequences][n_kv_heads][max_seq_pages] scores, then four floats per eight pages: bound, largest, smallest, unused
   int attn_blocks = 0;                 // blocks of the attention kernel that are resident at once
 };
 
