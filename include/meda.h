@@ -321,7 +321,7 @@ meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride,
  *   max_h sum_d (q_hd >= 0 ? q_hd * max_d : q_hd * min_d),
  * summed in 64 bits and rounded once to fp32; ties go to the lowest page, a NaN ranks highest.  The first n_first and
  * the last n_last pages are always among them (n_first + n_last <= keep).
- *   q      device, `dtype`, [n_seqs][n_q_heads][head_dim];  bounds: 16-byte aligned
+ *   q      device, `dtype`, [n_seqs][n_q_heads][head_dim];  q and bounds are 16-byte aligned (MEDA_ERR_SHAPE otherwise)
  *   sel    device int32 [n_seqs][n_kv_heads][keep]: min(keep, pages of the sequence) entries, the others untouched */
 meda_status meda_select_pages(meda_pages* pages, const void* q, const void* bounds, const int32_t* table,
                               const int32_t* lens, int32_t lens_stride, int32_t n_seqs, int32_t n_first,

@@ -409,7 +409,7 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
   const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
   if (r != MEDA_OK || n_seqs == 0) return r;
   if (!q || !bounds || !table || !lens || !sel) return MEDA_ERR_INVALID_ARG;
-  if (!aligned16(bounds)) return MEDA_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(bounds)) return MEDA_ERR_SHAPE;
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
   const meda_pages_config& c = pages->cfg;

@@ -736,6 +736,38 @@ def test_refusals(B):
     pg.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_vectors_off_their_boundary_are_refused(B, dtype):
+    """Every tensor that is read or written as 16-byte vectors, one element into its buffer: refused before any launch."""
+    pg, q, kp, vp, table, out, lse = attention_case(B, [20, 30], 4, 2, 64, dtype, 16)
+    t, n = i32(table.tolist()), i32([20, 30])
+    bd = torch.zeros((kp.shape[0], 2, 2, 64), dtype=kp.dtype, device="cuda")
+    sel = torch.zeros((2, 2, 1), dtype=torch.int32, device="cuda")
+    slots = torch.zeros(2, dtype=torch.int64, device="cuda")
+    k, v = torch.zeros((2, 2, 32, 64), dtype=kp.dtype, device="cuda"), torch.zeros((2, 2, 32, 64), dtype=kp.dtype, device="cuda")
+    kn, vn = k[:, :, 0].contiguous(), v[:, :, 0].contiguous()
+
+    def off(x):
+        y = torch.zeros(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+        assert y.is_contiguous() and y.data_ptr() % 16 != 0
+        return y
+
+    calls = [
+        (lambda q, bd: pg.select_pages(q, bd, t, n, 0, 1, sel), (q, bd)),
+        (lambda q, kp, vp, out: pg.paged_attention(q, kp, vp, t, n, out), (q, kp, vp, out)),
+        (lambda k, v, kp, vp, bd: pg.page_store(k, v, n, t, kp, vp, bd), (k, v, kp, vp, bd)),
+        (lambda kp, bd: pg.page_bounds(kp, t, None, n, bd), (kp, bd)),
+        (lambda q, k, v, out, kp, vp: pg.rope_append(q, k, v, None, slots, out, kp, vp), (q, kn, vn, out, kp, vp)),
+    ]
+    for call, args in calls:
+        for i in range(len(args)):
+            with pytest.raises(B.MedaError) as e:
+                call(*args[:i], off(args[i]), *args[i + 1:])
+            assert e.value.status == B.MEDA_ERR_SHAPE
+    assert pg.launch_count() == 0
+    pg.close()
+
+
 # ------------------------------------------------------------------------------------------ a run of them
 
 def decoder_case(keep_pages=0):
