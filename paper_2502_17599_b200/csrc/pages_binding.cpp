@@ -114,6 +114,16 @@ int64_t whole(PyObject* o, const char* what) {
 
 using Args = PyObject* const*;
 
+// One C call without the interpreter's lock: a launch waits where the stream's queue is full, and what it waits for may be
+// a host function that needs the lock.  (The arguments, which may use the interpreter, are ready before it is let go.)
+template <typename F, typename... A>
+meda_status unlocked(F f, A... a) {
+  PyThreadState* s = PyEval_SaveThread();
+  const meda_status r = f(a...);
+  PyEval_RestoreThread(s);
+  return r;
+}
+
 meda_status page_tables(Args a) {              // lens, new_lens, free_pages, free_top, free_top_out, table, cu_new, slots, stream
   Native* n = native_of(a[0]);
   const at::Tensor& nl = tensor(a[2], "new_lens");
@@ -129,7 +139,7 @@ meda_status page_tables(Args a) {              // lens, new_lens, free_pages, fr
   }
   const at::Tensor& sl = tensor(a[8], "slots");
   if (!on(n, sl, at::kLong) || sl.dim() != 1 || !sl.is_contiguous()) refuse(n, sl, at::kLong, "contiguous [capacity]", "slots");
-  return n->page_tables(n->h, lens, small(stride, "stride"), new_lens, small(nl.stride(0), "stride"), small(c, "n_seqs"),
+  return unlocked(n->page_tables, n->h, lens, small(stride, "stride"), new_lens, small(nl.stride(0), "stride"), small(c, "n_seqs"),
                         static_cast<int32_t*>(dense(n, a[3], at::kInt, {n->n_pages}, "free_pages")),
                         static_cast<const int32_t*>(dense(n, a[4], at::kInt, {1}, "free_top")),
                         static_cast<int32_t*>(dense(n, a[5], at::kInt, {1}, "free_top_out")),
@@ -150,7 +160,7 @@ meda_status page_store(Args a) {               // k, v, lens, table, k_pages, v_
       refuse(n, *t, n->dtype, "[" + std::to_string(c) + "][" + std::to_string(n->hkv) + "][capacity][" + std::to_string(n->d) +
              "], rows dense, k and v laid out alike,", what);
   }
-  return n->page_store(n->h, k.data_ptr(), v.data_ptr(), c > 1 ? k.stride(0) : 0, n->hkv > 1 ? k.stride(1) : 0, small(k.size(2), "capacity"),
+  return unlocked(n->page_store, n->h, k.data_ptr(), v.data_ptr(), c > 1 ? k.stride(0) : 0, n->hkv > 1 ? k.stride(1) : 0, small(k.size(2), "capacity"),
                        lengths(n, l, c, "lens"), small(l.stride(0), "stride"), small(c, "n_seqs"),
                        static_cast<const int32_t*>(dense(n, a[4], at::kInt, {c, n->width}, "table")),
                        dense(n, a[5], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
@@ -169,7 +179,7 @@ meda_status page_bounds(Args a) {              // k_pages, table, lens_from, len
     from = lengths(n, f, c, "lens_from");
     if (f.stride(0) != l.stride(0)) throw Refused("lens_from and lens have to have the same stride");
   }
-  return n->page_bounds(n->h, dense(n, a[1], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
+  return unlocked(n->page_bounds, n->h, dense(n, a[1], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
                         static_cast<const int32_t*>(dense(n, a[2], at::kInt, {c, n->width}, "table")), from, lengths(n, l, c, "lens"),
                         small(l.stride(0), "stride"), small(c, "n_seqs"), dense(n, a[5], n->dtype, {n->n_pages, n->hkv, 2, n->d}, "bounds"),
                         stream_of(n, a[6]));
@@ -199,7 +209,7 @@ meda_status rope_append(Args a) {              // q, k, v, positions, slots, q_o
     pos = static_cast<const int32_t*>(t.data_ptr());
     ax = t.stride(0);
   }
-  return n->rope_append(n->h, q, qs, k, ks, v, vs, pos, ax, static_cast<const int64_t*>(sl.data_ptr()), small(c, "n_tokens"), q_out,
+  return unlocked(n->rope_append, n->h, q, qs, k, ks, v, vs, pos, ax, static_cast<const int64_t*>(sl.data_ptr()), small(c, "n_tokens"), q_out,
                         dense(n, a[7], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
                         dense(n, a[8], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "v_pages"), stream_of(n, a[9]));
 }
@@ -210,7 +220,7 @@ meda_status select_pages(Args a) {             // q, bounds, table, lens, n_firs
   if (l.dim() != 1) refuse(n, l, at::kInt, "[n]", "lens");
   if (s.dim() != 3) refuse(n, s, at::kInt, "[n_seqs][n_kv_heads][keep]", "sel");
   const int64_t c = l.size(0), keep = s.size(2);
-  return n->select_pages(n->h, dense(n, a[1], n->dtype, {c, n->hq, n->d}, "q"), dense(n, a[2], n->dtype, {n->n_pages, n->hkv, 2, n->d}, "bounds"),
+  return unlocked(n->select_pages, n->h, dense(n, a[1], n->dtype, {c, n->hq, n->d}, "q"), dense(n, a[2], n->dtype, {n->n_pages, n->hkv, 2, n->d}, "bounds"),
                          static_cast<const int32_t*>(dense(n, a[3], at::kInt, {c, n->width}, "table")), lengths(n, l, c, "lens"),
                          small(l.stride(0), "stride"), small(c, "n_seqs"), small(whole(a[5], "n_first"), "n_first"),
                          small(whole(a[6], "n_last"), "n_last"), small(keep, "keep"),
@@ -230,7 +240,7 @@ meda_status paged_attention(Args a) {          // q, k_pages, v_pages, table, le
     keep = s.size(2);
     sel = static_cast<const int32_t*>(dense(n, a[8], at::kInt, {c, n->hkv, keep}, "sel"));
   }
-  return n->paged_attention(n->h, dense(n, a[1], n->dtype, {c, n->hq, n->d}, "q"),
+  return unlocked(n->paged_attention, n->h, dense(n, a[1], n->dtype, {c, n->hq, n->d}, "q"),
                             dense(n, a[2], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
                             dense(n, a[3], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "v_pages"),
                             static_cast<const int32_t*>(dense(n, a[4], at::kInt, {c, n->width}, "table")), lengths(n, l, c, "lens"),
