@@ -223,7 +223,8 @@ meda_status meda_decode_attention(meda_ctx* ctx, int32_t layer, const void* q, c
  * meda_pages may be used by one host thread and one stream at a time (CUDA graphs captured through the same
  * meda_pages share its scratch memory and must not run at the same time; give each stream its own).  Row
  * counts live on the device and are read there, so one captured graph serves every step while its buffers stay
- * in place.  Pool rows behind a sequence's length are never read: they may hold anything, NaN included, and
+ * in place.  No page stands twice in the table rows of a call that writes pages or bounds (the calls that only read may share
+ * them).  Pool rows behind a sequence's length are never read: they may hold anything, NaN included, and
  * stay as they are.  Errors only the device can see are recorded for meda_pages_poll_status: a length out of
  * range (taken as the nearest valid one; meda_page_tables and meda_page_store skip instead), a page or a slot outside the pool (its rows are skipped), a
  * free list that runs out.  The calls make the meda_pages' own device current for their duration.  n_seqs may
@@ -330,7 +331,7 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
 /* Attention of one new token's queries per sequence over its pages (Eq. 3, as meda_decode_attention):
  *   out[i][h] = softmax(q_ih . K^T / sqrt(head_dim)) V over rows [0, lens[i]) of KV head g of query head h, or, with
  *   sel (of meda_select_pages, `keep` entries per sequence and KV head), over those rows that lie in the
- *   min(keep, pages of the sequence) pages it names.
+ *   min(keep, pages of the sequence) pages it names, in any order, none of them twice.
  *   q    device, `dtype`, [n_seqs][n_q_heads][head_dim]; q and the pools are 16-byte aligned
  *   out  device, `dtype`, [n_seqs][n_q_heads][head_dim]
  *   lse  device fp32 [n_seqs][n_q_heads], may be NULL: the logarithm of the softmax's sum, ready to join with the

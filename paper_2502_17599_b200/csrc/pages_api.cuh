@@ -345,7 +345,7 @@ meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int
   if (!pages || rows_capacity < 0 || seq_stride < 0 || head_stride < 0) return MEDA_ERR_INVALID_ARG;
   const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
   if (r != MEDA_OK || n_seqs == 0) return r;
-  if (!k || !v || !lens || !table || !k_pages || !v_pages) return MEDA_ERR_INVALID_ARG;
+  if ((rows_capacity > 0 && (!k || !v)) || !lens || !table || !k_pages || !v_pages) return MEDA_ERR_INVALID_ARG;
   const meda_pages_config& c = pages->cfg;
   const int e = 16 / pages_element(pages);
   if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(bounds) || seq_stride % e != 0 ||

@@ -244,10 +244,13 @@ class PagedDecoder:
         L, R, hkv, d = wl.n_layers, int(max_requests), wl.n_kv_heads, wl.head_dim
         self.wl, self.n_layers, self.max_requests = wl, L, R
         self.keep_pages, self.n_first, self.n_last = int(keep_pages), n_first, n_last
+        if self.keep_pages < 0 or n_first < 0 or n_last < 0 or (self.keep_pages and n_first + n_last > self.keep_pages):
+            raise ValueError("keep_pages has to hold the n_first first and the n_last last pages")
         width = -(-int(max_rows) // page_size)
-        self.pages = binding.Pages(n_q_heads=wl.n_q_heads, n_kv_heads=hkv, head_dim=d, dtype=wl.dtype, page_size=page_size,
-                                   n_pages=n_pages, max_seqs=L * R, max_seq_pages=width, rope_theta=rope_theta,
-                                   rope_sections=rope_sections, rope_order=rope_order, rope_pairing=rope_pairing)
+        with torch.cuda.device(device):
+            self.pages = binding.Pages(n_q_heads=wl.n_q_heads, n_kv_heads=hkv, head_dim=d, dtype=wl.dtype, page_size=page_size,
+                                       n_pages=n_pages, max_seqs=L * R, max_seq_pages=width, rope_theta=rope_theta,
+                                       rope_sections=rope_sections, rope_order=rope_order, rope_pairing=rope_pairing)
         i32 = dict(dtype=torch.int32, device=device)
         dt = dict(dtype=wl.torch_dtype, device=device)
         self.k_pages = torch.empty((n_pages, hkv, page_size, d), **dt)

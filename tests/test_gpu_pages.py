@@ -1011,3 +1011,98 @@ def test_two_handles_on_two_streams_and_two_graphs(B):
         assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
     pg.close()
     other.close()
+
+
+FIRST_CAPTURE = """
+import torch
+from paper_2502_17599_b200 import binding as B
+pg = B.Pages(n_q_heads=14, n_kv_heads=2, head_dim=128, dtype="{dtype}", page_size=16, n_pages=64, max_seqs=3, max_seq_pages=20)
+dt = dict(bf16=torch.bfloat16, f32=torch.float32)["{dtype}"]
+torch.manual_seed(1)
+rand = lambda *s: torch.randn(s, device="cuda").to(dt)
+i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+q, k, v, kn, vn = rand(3, 14, 128), rand(3, 2, 320, 128), rand(3, 2, 320, 128), rand(3, 2, 128), rand(3, 2, 128)
+lens, more, none, zero = i32(300, 17, 0), i32(301, 18, 1), i32(0, 0, 0), i32(0)
+pos = i32(5, 6, 7).repeat(3, 1)
+
+def buffers():
+    z = lambda *s: torch.zeros(s, dtype=dt, device="cuda")
+    return dict(kp=z(64, 2, 16, 128), vp=z(64, 2, 16, 128), bd=z(64, 2, 2, 128), table=torch.full((3, 20), -1, dtype=torch.int32, device="cuda"),
+                free=torch.arange(64, dtype=torch.int32, device="cuda"), top=i32(0), top2=i32(0), cu=i32(0, 0, 0, 0),
+                slots=torch.zeros(3, dtype=torch.int64, device="cuda"), nothing=torch.empty(0, dtype=torch.int64, device="cuda"),
+                qr=z(3, 14, 128), sel=torch.zeros((3, 2, 4), dtype=torch.int32, device="cuda"), out=z(3, 14, 128), lse=torch.zeros((3, 14), device="cuda"))
+
+def body(b):
+    pg.page_tables(None, lens, b["free"], zero, b["top"], b["table"], b["cu"], b["nothing"])
+    pg.page_store(k, v, lens, b["table"], b["kp"], b["vp"], b["bd"])
+    pg.page_tables(lens, more, b["free"], b["top"], b["top2"], b["table"], b["cu"], b["slots"])
+    pg.rope_append(q, kn, vn, pos, b["slots"], b["qr"], b["kp"], b["vp"])
+    pg.page_bounds(b["kp"], b["table"], lens, more, b["bd"])
+    pg.select_pages(b["qr"], b["bd"], b["table"], more, 1, 1, b["sel"])
+    pg.paged_attention(b["qr"], b["kp"], b["vp"], b["table"], more, b["out"], b["lse"], sel=b["sel"])
+
+captured, eager = buffers(), buffers()
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    body(captured)
+graph.replay()
+pg.check()
+body(eager)
+pg.check()
+for name in captured:
+    assert torch.equal(captured[name], eager[name]), name
+assert captured["top2"].item() == 19 + 2 + 1 and captured["out"].float().abs().sum() > 0
+print("captured first")
+"""
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_first_calls_of_a_process_inside_a_capture(B, dtype):
+    """A server may capture its step before it ever ran one: no call may need anything a capture forbids (kernels are loaded then)."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CAPTURE.replace("{dtype}", dtype)], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured first" in r.stdout, r.stderr[-2000:]
+
+
+def test_sequences_may_share_pages_they_only_read(B):
+    """Two sequences whose table rows name the same pages, the second with fewer rows of the last one: as with pages of their own."""
+    lens = [100, 100, 70]
+    pg, q, kp, vp, table, out, lse = attention_case(B, lens, 8, 2, 128, "bf16", 16, seed=31)
+    own = torch.empty_like(out)
+    t = i32(table.tolist())
+    kp2, vp2 = kp.clone(), vp.clone()
+    for c in range(O.n_pages_of(70, 16)):                            # the third sequence's own copy of the first one's pages
+        kp2[int(table[2, c])], vp2[int(table[2, c])] = kp[int(table[0, c])], vp[int(table[0, c])]
+    pg.paged_attention(q, kp2, vp2, t, i32(lens), own)
+    shared = t.clone()
+    shared[2] = t[0]
+    pg.paged_attention(q, kp2, vp2, shared, i32(lens), out)
+    pg.check()
+    assert torch.equal(out, own)
+    pg.close()
+
+
+def test_page_store_of_a_cache_without_room(B):
+    """Capacity 0 (an empty tensor has no address): nothing is stored, and a length above it is reported."""
+    pg = make(B)
+    kp = torch.full((64, 2, 16, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    k = torch.empty((2, 2, 0, 64), dtype=torch.bfloat16, device="cuda")
+    t = torch.zeros((2, 16), dtype=torch.int32, device="cuda")
+    pg.page_store(k, k, i32([0, 0]), t, kp, kp.clone())
+    pg.check()
+    pg.page_store(k, k, i32([0, 1]), t, kp, kp.clone())
+    assert pg.poll_status() == B.MEDA_ERR_WORKSPACE
+    assert (kp == 3).all()
+    pg.close()
+
+
+def test_decoder_refuses_more_fixed_pages_than_it_keeps(B):
+    from paper_2502_17599_b200.pipeline import PagedDecoder
+    wl = W.small_variant("paged", window=32, seed=4)
+    for kw in (dict(keep_pages=2), dict(keep_pages=-1), dict(keep_pages=4, n_first=-1)):
+        with pytest.raises(ValueError):
+            PagedDecoder(wl, n_pages=10, max_requests=1, max_rows=100, **kw)
