@@ -90,17 +90,18 @@ __device__ __forceinline__ float exp2_fast(float x) {              // 2^x, off b
 
 __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
-// ---- bf16: D = head_dim, NH = groups of eight query heads ------------------------------------------------
+// ---- bf16: D = head_dim, NH = groups of eight query heads, R = rows worked on at a time (16 or 8) -----------------
 // Lane l: r = l / 4, c = l % 4.  Q K^T has A = queries (row r: head r, row r + 8: head r + 8), B = keys (column r: row r of
-// the tile's half); P V has A = V^T, B = P^T (row pairs 2c, 2c + 1 of both halves; column r: head r).
-template <int D, int NH>
+// the tile's half); P V has A = V^T, B = P^T (row pairs 2c, 2c + 1 of both halves; column r: head r).  With R = 8
+// there is one half: its P V takes both parts of the probabilities in one instruction, the values' fragment twice.
+template <int D, int NH, int R = 16>
 struct AttnTileBf16 {
   using T = __nv_bfloat16;
   static constexpr int kHeads = 8 * NH;
-  static constexpr int KC = D / 32, VC = D / 64;
+  static constexpr int KC = D / 32, VC = D / 64, KT = R / 8, kRows = R;
   uint4 q[NH][KC];
-  uint4 k[2][KC];
-  uint4 v[4][VC];
+  uint4 k[KT][KC];
+  uint4 v[2 * KT][VC];
   float o[VC][4][NH][4];
   float m[NH], l[NH];
 
@@ -131,29 +132,29 @@ struct AttnTileBf16 {
   }
   // Rows behind the nv that count are not read: their lanes read the last one that does, and its probability is 0 (its
   // value cannot add anything the row itself does not: 0 * NaN is NaN in both).
-  __device__ __forceinline__ void load_k(const T* rows, int nv, int lane) {
+  __device__ __forceinline__ void load_k(const T* rows, int r0, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const T* src = rows + min(t * 8 + r, nv - 1) * D + c * 8;
+    for (int t = 0; t < KT; ++t) {
+      const T* src = rows + min(r0 + t * 8 + r, nv - 1) * D + c * 8;
 #pragma unroll
       for (int x = 0; x < KC; ++x) k[t][x] = load_stream(reinterpret_cast<const uint4*>(src + x * 32));
     }
   }
-  __device__ __forceinline__ void load_v(const T* rows, int nv, int lane) {
+  __device__ __forceinline__ void load_v(const T* rows, int r0, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const T* src = rows + min(2 * c + (t & 1) + (t >> 1) * 8, nv - 1) * D + r * 8;
+    for (int t = 0; t < 2 * KT; ++t) {
+      const T* src = rows + min(r0 + 2 * c + (t & 1) + (t >> 1) * 8, nv - 1) * D + r * 8;
 #pragma unroll
       for (int y = 0; y < VC; ++y) v[t][y] = load_stream(reinterpret_cast<const uint4*>(src + y * 64));
     }
   }
-  // logits of the tile in k, in the log2 domain: s[t][0..1] head r, rows t * 8 + 2c, + 1; s[t][2..3] head r + 8
-  __device__ __forceinline__ void logits(float (&s)[2][4], float scale_log2, int nv, int lane) {
+  // logits of the rows in k (r0 and on of the tile), in the log2 domain: s[t][0..1] head r, rows t * 8 + 2c, + 1; s[t][2..3] head r + 8
+  __device__ __forceinline__ void logits(float (&s)[KT][4], float scale_log2, int r0, int nv, int lane) {
     const int c = lane % 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < KT; ++t) {
       float even[4] = {0.f, 0.f, 0.f, 0.f}, odd[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of dependent instructions
 #pragma unroll
       for (int x = 0; x < KC; ++x) {
@@ -163,20 +164,20 @@ struct AttnTileBf16 {
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[t][e] = (even[e] + odd[e]) * scale_log2;
     }
-    if (nv < kAttTile) {
+    if (nv < r0 + R) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (t * 8 + 2 * c + (e & 1) >= nv) s[t][e] = -INFINITY;
+          if (r0 + t * 8 + 2 * c + (e & 1) >= nv) s[t][e] = -INFINITY;
     }
   }
-  __device__ __forceinline__ void attend(float (&s)[2][4], int lane) {
+  __device__ __forceinline__ void attend(float (&s)[KT][4], int lane) {
     const int c = lane % 4;
-    uint32_t hi[NH][2], lo[NH][2];
+    uint32_t hi[NH][KT], lo[NH][KT];
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
-      float top = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[1][2 * n], s[1][2 * n + 1]));
+      float top = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[KT - 1][2 * n], s[KT - 1][2 * n + 1]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float mn = fmaxf(m[n], top);
@@ -197,7 +198,7 @@ struct AttnTileBf16 {
           }
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < KT; ++t) {
         const float p0 = exp2_fast(s[t][2 * n] - ref), p1 = exp2_fast(s[t][2 * n + 1] - ref);
         l[n] += p0 + p1;
         const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
@@ -210,13 +211,19 @@ struct AttnTileBf16 {
     for (int y = 0; y < VC; ++y)
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const uint32_t w0 = word_of(v[0][y], x), w1 = word_of(v[1][y], x), w2 = word_of(v[2][y], x), w3 = word_of(v[3][y], x);
+        const uint32_t w0 = word_of(v[0][y], x), w1 = word_of(v[1][y], x);
         const uint32_t a0 = __byte_perm(w0, w1, 0x5410), a1 = __byte_perm(w0, w1, 0x7632);
-        const uint32_t a2 = __byte_perm(w2, w3, 0x5410), a3 = __byte_perm(w2, w3, 0x7632);
+        if constexpr (KT == 2) {
+          const uint32_t w2 = word_of(v[2 * KT - 2][y], x), w3 = word_of(v[2 * KT - 1][y], x);
+          const uint32_t a2 = __byte_perm(w2, w3, 0x5410), a3 = __byte_perm(w2, w3, 0x7632);
 #pragma unroll
-        for (int n = 0; n < NH; ++n) {
-          mma_bf16(o[y][x][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-          mma_bf16(o[y][x][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+          for (int n = 0; n < NH; ++n) {
+            mma_bf16(o[y][x][n], a0, a1, a2, a3, hi[n][0], hi[n][KT - 1]);
+            mma_bf16(o[y][x][n], a0, a1, a2, a3, lo[n][0], lo[n][KT - 1]);
+          }
+        } else {                                               // both parts of the probabilities in one: the eight rows twice
+#pragma unroll
+          for (int n = 0; n < NH; ++n) mma_bf16(o[y][x][n], a0, a1, a0, a1, hi[n][0], lo[n][0]);
         }
       }
   }
@@ -517,11 +524,17 @@ paged_attention_kernel(AttnParams p) {
     const long long row_after = __shfl_sync(0xffffffffu, row_now, at);
     const int nv_after = __shfl_sync(0xffffffffu, nv_now, at);
     if constexpr (kBf16) {
-      float s[2][4];
-      if (nv > 0) tile.logits(s, p.scale_log2, nv, lane);
-      if (nv_after > 0) tile.load_k(kp + row_after * D, nv_after, lane);
-      if (nv > 0) tile.attend(s, lane);
-      if (nv_after > 0) tile.load_v(vp + row_after * D, nv_after, lane);
+      constexpr int R = Tile::kRows;
+#pragma unroll
+      for (int b = 0; b < kAttTile; b += R) {
+        float s[R / 8][4];
+        const bool last = b + R == kAttTile;                   // of this tile; then comes the next one's first
+        const int n = last ? nv_after : nv, r0 = last ? 0 : b + R;
+        if (b < nv) tile.logits(s, p.scale_log2, b, nv, lane);
+        if (r0 < n) tile.load_k(kp + (last ? row_after : row) * D, r0, n, lane);
+        if (b < nv) tile.attend(s, lane);
+        if (r0 < n) tile.load_v(vp + (last ? row_after : row) * D, r0, n, lane);
+      }
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {

@@ -107,6 +107,9 @@ struct AttnKernel {
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
 // At head_dim 128, eight warps against twelve: 947 rows 7.1 and 7.6 us, 4,000 rows 8.0 and 8.5, 129,072 rows 50.5 and 48.8, 64 sequences
 // of 36 to 18,944 rows 76 and 71.4; twelve are taken for the long ones.
+// At head_dim 256 a warp works on eight rows at a time: sixteen fill 224 registers before any temporary, and with the warps' states
+// beside them what is in flight no longer fits the L1 (400 MB, 7 heads per KV head: sixteen 98.1 us, eight 78.6; 947 rows 10.4 and
+// 9.0).  Elsewhere sixteen are better (head_dim 128: 67.8 and 80.2, the softmax's steps are per turn).
 // (More than eight query heads per KV head at head_dim 256 take two segments: the accumulators of sixteen do not fit.)
 template <typename F>
 meda_status with_attn_kernel(const meda_pages* p, F f) {
@@ -114,7 +117,7 @@ meda_status with_attn_kernel(const meda_pages* p, F f) {
   if (p->cfg.dtype == MEDA_BF16) {
     if (d == 64) return g <= 8 ? f(AttnKernel<AttnTileBf16<64, 1>, 64, 16>()) : f(AttnKernel<AttnTileBf16<64, 2>, 64, 16>());
     if (d == 128) return g <= 8 ? f(AttnKernel<AttnTileBf16<128, 1>, 128, 12>()) : f(AttnKernel<AttnTileBf16<128, 2>, 128, 8>());
-    return f(AttnKernel<AttnTileBf16<256, 1>, 256, 8>());
+    return f(AttnKernel<AttnTileBf16<256, 1, 8>, 256, 8>());
   }
   if (d == 64)
     return g == 1 ? f(AttnKernel<AttnTileF32<64, 1>, 64, 16>()) : g == 2 ? f(AttnKernel<AttnTileF32<64, 2>, 64, 16>())
