@@ -234,6 +234,7 @@ class PagedDecoder:
     and active request, `attend` (once per layer) rotates and appends the new rows and attends, `release` gives
     a request's pages back.  Everything runs on torch's current stream; nothing is copied to the host, so
     begin_step and the layers' attend calls can be captured into a CUDA graph (the lengths live on the device).
+    A request that cannot get its row keeps what it has: see begin_step.
 
     `keep_pages` > 0: attention reads at most that many pages per sequence and KV head, the ones whose key
     bounds promise the largest logits, the first and the last always among them."""
@@ -262,9 +263,12 @@ class PagedDecoder:
         self.free_pages = torch.arange(n_pages, **i32)
         self.free_top = torch.zeros(1, **i32)
         self.active = torch.zeros(R, **i32)                # 1: the request takes part in the next step
+        self._added = torch.zeros(L * R, **i32)            # rows of every sequence that the last step added
+        self.advanced = self._added[:R]                    # 1: the request got a row in the last step (in every layer: they grow together)
+        self._stalled = torch.zeros(R, dtype=torch.bool, device=device)    # active requests that got none in it
         self._top_out = torch.zeros(1, **i32)
         self._cu = torch.zeros(L * R + 1, **i32)
-        self._new_slots = torch.empty(L * R, dtype=torch.int64, device=device)
+        self._new_slots = torch.empty(L * R + 1, dtype=torch.int64, device=device)
         self._no_slots = torch.empty(0, dtype=torch.int64, device=device)
         self.slots = torch.full((L, R), -1, dtype=torch.int64, device=device)
         self.q_rot = torch.zeros((R, wl.n_q_heads, d), **dt)
@@ -274,8 +278,14 @@ class PagedDecoder:
         self.pages.close()
 
     def check(self):
-        """Synchronises and raises if a device-side error was recorded (a full pool among them)."""
-        self.pages.check()
+        """Synchronises and raises if a device-side error was recorded (a full pool among them) or an active request got no row in
+        the last step (the error names them)."""
+        status = self.pages.poll_status()
+        stalled = self._stalled.nonzero().flatten().tolist()
+        self._stalled.zero_()
+        if stalled:
+            raise binding.MedaError(status or binding.MEDA_ERR_WORKSPACE, f"no room for another row of requests {stalled}")
+        binding._check(status, "device status")
 
     def _move(self, new_lens, slots):
         """Page tables for lens -> new_lens.  A change the pool cannot serve is recorded and changes nothing."""
@@ -304,17 +314,25 @@ class PagedDecoder:
         self._move(new_lens, self._no_slots)
         self.lens.copy_(new_lens)
         self.active[request] = 0
+        self._stalled[request] = False
 
     def begin_step(self):
-        """Room for one more row in every layer of the active requests."""
+        """Room for one more row in every layer of the active requests.  A request with a layer that is full (max_rows, up to the end of
+        its last page) gets none and leaves the others alone; when the pool has too few pages for the rest, nobody gets any, and
+        the step can be begun again once a request has left.  `advanced` [R] is 1 for the requests that got their rows.  The query
+        of an active one that did not is NaN for this step, and so are its outputs; check() raises for it."""
         L, R = self.n_layers, self.max_requests
         self.lens_before.copy_(self.lens)
-        grow = self.active.repeat(L)
-        self._move(self.lens + grow, self._new_slots)
-        added = self._cu[1:] - self._cu[:-1]               # all 0 when the pool has run out: nothing is appended then
-        self.lens.copy_(self.lens + added)
-        at = self._cu[:-1].long().clamp(max=L * R - 1)
-        self.slots.copy_(torch.where(added > 0, self._new_slots[at], -1).view(L, R))
+        lens = self.lens.view(L, R)
+        room = lens.amax(0) < self.table.shape[1] * self.pages.cfg.page_size
+        self._move((lens + self.active * room).view(-1), self._new_slots)
+        torch.sub(self._cu[1:], self._cu[:-1], out=self._added)            # all 0 when the pool has run out: nothing is appended then
+        self.lens.add_(self._added)
+        slots = self.slots.view(-1)
+        torch.index_select(self._new_slots, 0, self._cu[:-1], out=slots)   # (behind the last sequence cu is at most L * R)
+        slots.masked_fill_(self._added == 0, -1)
+        torch.gt(self.active, self.advanced, out=self._stalled)
+        self.q_rot.masked_fill_(self._stalled[:, None, None], float("nan"))    # attend leaves the rows of tokens without a slot alone
 
     def attend(self, layer: int, q, k, v, positions, out, lse=None):
         """One layer of the step: q [R][Hq][d], k, v [R][Hkv][d] (any token stride) of the new tokens, positions int32
