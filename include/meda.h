@@ -336,7 +336,8 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
  *   out  device, `dtype`, [n_seqs][n_q_heads][head_dim]
  *   lse  device fp32 [n_seqs][n_q_heads], may be NULL: the logarithm of the softmax's sum, ready to join with the
  *        attention over rows kept elsewhere
- * A sequence of length 0 gets out = 0, lse = -inf. */
+ * A sequence of length 0 gets out = 0, lse = -inf.  An infinite value makes its dimension of the output infinite; both
+ * signs in one dimension, or a row whose weight is 0 in fp32 (below 2^-126 of the largest), make it NaN. */
 meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
                                  const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
                                  const int32_t* sel, int32_t keep, void* out, float* lse, void* stream);

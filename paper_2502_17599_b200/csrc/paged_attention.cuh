@@ -17,8 +17,9 @@
 // cp.async rings 6.0 to 6.3, through tiled or bulk TMA rings 5.3 to 6.1.)  The kernel is bound by reading the cache; the matrix instructions only have
 // to keep up (24 to 32 of them for 8 KB at head_dim 128), so the warp-level ones are used: eight query heads fill
 // their narrow side, where the tensor-memory instructions would want 128 rows of queries.
-// Probabilities enter P V as a sum of two bf16 numbers (16 bits of mantissa, 2^-17 relative), so that rounding
-// them stays below the rounding of the output; logits, maxima, sums and accumulators are fp32.
+// Probabilities enter P V as a sum of two bf16 numbers (2^-16 relative), so that rounding them stays below the rounding
+// of the output; logits, maxima, sums and accumulators are fp32.  Both parts of a positive probability are positive: an infinite
+// value then adds infinities of one sign (0 * inf and inf - inf are NaN).
 //
 // Measured with its second launch, 28 query and 4 KV heads of 128, bf16: one cache of 129,072 rows (264 MB) 48.0 us, 5.5 TB/s or
 // 86 % of a plain copy, about 7 us of it launches, look-ups and joining; 64 caches of 36 to 18,944 rows (410 MB) 71.5 us, 89 %;
@@ -88,6 +89,13 @@ __device__ __forceinline__ float exp2_fast(float x) {              // 2^x, off b
   return y;
 }
 
+// What cutting p to a bf16 leaves; where that is nothing, 2^-126 (0 for p = 0, which exp2_fast gives below 2^-126), far below the
+// rounding of a sum whose largest probability is 1.
+__device__ __forceinline__ float low_part(float p) {
+  const float rest = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+  return fmaxf(rest, fminf(p, 1.17549435e-38f));
+}
+
 __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
 // ---- bf16: D = head_dim, NH = groups of eight query heads, R = rows worked on at a time (16 or 8) -----------------
@@ -130,8 +138,8 @@ struct AttnTileBf16 {
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[y][x][n][e] = 0.f;
   }
-  // Rows behind the nv that count are not read: their lanes read the last one that does, and its probability is 0 (its
-  // value cannot add anything the row itself does not: 0 * NaN is NaN in both).
+  // Rows behind the nv that count are not read: their lanes read the last one that does, its logit is set to -inf and its
+  // value to 0 (an infinite one times a probability of 0 would be NaN).
   __device__ __forceinline__ void load_k(const T* rows, int r0, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
@@ -172,9 +180,16 @@ struct AttnTileBf16 {
           if (r0 + t * 8 + 2 * c + (e & 1) >= nv) s[t][e] = -INFINITY;
     }
   }
-  __device__ __forceinline__ void attend(float (&s)[KT][4], int lane) {
+  __device__ __forceinline__ void attend(float (&s)[KT][4], int r0, int nv, int lane) {
     const int c = lane % 4;
     uint32_t hi[NH][KT], lo[NH][KT];
+    if (nv < r0 + R) {
+#pragma unroll
+      for (int t = 0; t < 2 * KT; ++t)
+        if (r0 + 2 * c + (t & 1) + (t >> 1) * 8 >= nv)
+#pragma unroll
+          for (int y = 0; y < VC; ++y) v[t][y] = make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
       float top = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[KT - 1][2 * n], s[KT - 1][2 * n + 1]));
@@ -201,9 +216,8 @@ struct AttnTileBf16 {
       for (int t = 0; t < KT; ++t) {
         const float p0 = exp2_fast(s[t][2 * n] - ref), p1 = exp2_fast(s[t][2 * n + 1] - ref);
         l[n] += p0 + p1;
-        const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
-        const __nv_bfloat162 l2 = __floats2bfloat162_rn(p0 - __low2float(h2), p1 - __high2float(h2));
-        memcpy(&hi[n][t], &h2, 4);
+        hi[n][t] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);         // the upper 16 bits: cut, not rounded
+        const __nv_bfloat162 l2 = __floats2bfloat162_rn(low_part(p0), low_part(p1));
         memcpy(&lo[n][t], &l2, 4);
       }
     }
@@ -283,7 +297,7 @@ struct AttnTileF32 {
     m = -INFINITY;
     l = 0.f;
   }
-  // Rows r0 .. r0 + 3 of the tile; behind the last of nv that one again (see AttnTileBf16::load_k).
+  // Rows r0 .. r0 + 3 of the tile; behind the last of nv that one again (see AttnTileBf16::load_k; rows4 sets its value to 0).
   __device__ __forceinline__ static void load_rows(float (&x)[B][E], const T* rows, int r0, int nv, int lane) {
 #pragma unroll
     for (int b = 0; b < B; ++b) {
@@ -306,6 +320,13 @@ struct AttnTileF32 {
   }
   // One group of four rows, already in kx[cur], vx[cur], of which rows r0 + b < nv count.
   __device__ __forceinline__ void rows4(int cur, int r0, int nv, float scale_log2, int lane) {
+    if (nv < r0 + B) {
+#pragma unroll
+      for (int b = 1; b < B; ++b)
+        if (r0 + b >= nv)
+#pragma unroll
+          for (int e = 0; e < E; ++e) vx[cur][b][e] = 0.f;
+    }
     float part[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) part[i] = 0.f;
@@ -532,7 +553,7 @@ paged_attention_kernel(AttnParams p) {
         const int n = last ? nv_after : nv, r0 = last ? 0 : b + R;
         if (b < nv) tile.logits(s, p.scale_log2, b, nv, lane);
         if (r0 < n) tile.load_k(kp + (last ? row_after : row) * D, r0, n, lane);
-        if (b < nv) tile.attend(s, lane);
+        if (b < nv) tile.attend(s, b, nv, lane);
         if (r0 < n) tile.load_v(vp + (last ? row_after : row) * D, r0, n, lane);
       }
     } else {
