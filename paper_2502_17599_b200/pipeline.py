@@ -308,12 +308,13 @@ class PagedDecoder:
         self.active[request:request + 1] = moved.to(torch.int32)
 
     def release(self, request: int):
-        """Gives the request's pages back."""
+        """Gives the request's pages back.  Layers of a step in progress that are still to come append nothing of it."""
         new_lens = self.lens.clone()
         new_lens.view(self.n_layers, self.max_requests)[:, request] = 0
         self._move(new_lens, self._no_slots)
         self.lens.copy_(new_lens)
         self.active[request] = 0
+        self.slots[:, request] = -1                        # its pages may be another's before the step ends
         self._stalled[request] = False
 
     def begin_step(self):
@@ -336,8 +337,8 @@ class PagedDecoder:
 
     def attend(self, layer: int, q, k, v, positions, out, lse=None):
         """One layer of the step: q [R][Hq][d], k, v [R][Hkv][d] (any token stride) of the new tokens, positions int32
-        [3][R]; out [R][Hq][d], lse fp32 [R][Hq].  Rows of requests that are not active attend to what they hold,
-        with the query of an earlier call; their outputs mean nothing."""
+        [3][R]; out [R][Hq][d], lse fp32 [R][Hq].  Rows of requests that were not active when the step began (or have been
+        released or admitted since) attend to what they hold, with the query of an earlier call; their outputs mean nothing."""
         R = self.max_requests
         rows = slice(layer * R, (layer + 1) * R)
         table, lens = self.table[rows], self.lens[rows]

@@ -1,0 +1,50 @@
+"""What PagedDecoder.admit and release do with requests and caches that do not fit, and between the layers of a step."""
+import pytest
+import torch
+
+import paged_steps as S
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2502_17599_b200 import build, binding
+    build.build()
+    binding.load_library()
+    return binding
+
+
+@pytest.mark.parametrize("keep_pages", [0, 6])
+def test_leaving_between_the_layers_of_a_step(B, keep_pages):
+    """A request is released after a step has begun and its pages go to another: the layers still to come write nothing of the one
+    that left."""
+    wl = S.workload()
+    cp = S.compressed(wl)
+    dec = S.decoder(wl, 120, 3, 400, keep_pages=keep_pages)
+    st = S.Steps(wl, dec)
+    st.admit(0, cp)
+    st.admit(2, cp)
+    hq, hkv = wl.n_q_heads, wl.n_kv_heads
+    st.step([0, 2])
+    dec.begin_step()
+    st.release(0)
+    st.admit(1, cp)                                                # takes over the pages just given back
+    x = torch.full_like(st.qkv[0], 7.0)
+    at = dec.slots[:, 2].clone()
+    for l in range(wl.n_layers):
+        dec.attend(l, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], st.pos, st.out[l], st.lse[l])
+    dec.check()
+    st.check_caches([1])
+    assert torch.equal(at, dec.slots[:, 2]) and (at >= 0).all()    # the request that stayed got its rows
+    for l in range(wl.n_layers):
+        assert (dec.v_pages[at[l] // 16, :, at[l] % 16] == 7.0).all()
+    # a request that is replaced is one that left
+    dec.begin_step()
+    st.admit(1, cp)
+    for l in range(wl.n_layers):
+        dec.attend(l, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], st.pos, st.out[l], st.lse[l])
+    dec.check()
+    st.check_caches([1])
+    dec.close()
+    cp.close()
