@@ -292,9 +292,14 @@ class PagedDecoder:
         self.pages.page_tables(self.lens, new_lens, self.free_pages, self.free_top, self._top_out, self.table, self._cu, slots)
         self.free_top.copy_(self._top_out)
 
+    def _check_request(self, request: int):
+        if not 0 <= request < self.max_requests:
+            raise IndexError(f"request {request} of {self.max_requests}")
+
     def admit(self, request: int, cp: CompressionPass):
         """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back."""
         L, R = self.n_layers, self.max_requests
+        self._check_request(request)
         self.release(request)
         rows = cp.budgets[:, 0]
         new_lens = self.lens.clone()
@@ -309,6 +314,7 @@ class PagedDecoder:
 
     def release(self, request: int):
         """Gives the request's pages back.  Layers of a step in progress that are still to come append nothing of it."""
+        self._check_request(request)
         new_lens = self.lens.clone()
         new_lens.view(self.n_layers, self.max_requests)[:, request] = 0
         self._move(new_lens, self._no_slots)

@@ -15,6 +15,32 @@ def B():
     return binding
 
 
+def state(dec):
+    names = ("table", "lens", "free_pages", "free_top", "active", "slots", "k_pages", "v_pages")
+    return {x: getattr(dec, x).clone() for x in names}
+
+
+def same(dec, before):
+    return all(torch.equal(getattr(dec, x), y) for x, y in before.items() if x not in ("k_pages", "v_pages")) and all(
+        torch.equal(getattr(dec, x).view(torch.int16), before[x].view(torch.int16)) for x in ("k_pages", "v_pages"))
+
+
+@pytest.mark.parametrize("request_", [-1, -3, 3, 4])
+def test_requests_out_of_range_are_refused(B, request_):
+    wl = S.workload()
+    cp = S.compressed(wl)
+    dec = S.decoder(wl, 120, 3, 400)
+    dec.admit(2, cp)
+    before = state(dec)
+    for call in (lambda: dec.admit(request_, cp), lambda: dec.release(request_)):
+        with pytest.raises(IndexError):
+            call()
+    assert same(dec, before)
+    dec.check()
+    dec.close()
+    cp.close()
+
+
 @pytest.mark.parametrize("keep_pages", [0, 6])
 def test_leaving_between_the_layers_of_a_step(B, keep_pages):
     """A request is released after a step has begun and its pages go to another: the layers still to come write nothing of the one
