@@ -297,9 +297,15 @@ class PagedDecoder:
             raise IndexError(f"request {request} of {self.max_requests}")
 
     def admit(self, request: int, cp: CompressionPass):
-        """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back."""
+        """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back.  Caches of another
+        number of layers, KV heads, head size, type or device are refused (ValueError)."""
         L, R = self.n_layers, self.max_requests
         self._check_request(request)
+        _, hkv, _, d = self.k_pages.shape
+        for x in (cp.k_out, cp.v_out):
+            if x.shape[:2] != (L, hkv) or x.shape[3] != d or x.dtype != self.k_pages.dtype or x.device != self.k_pages.device:
+                raise ValueError(f"caches of {tuple(x.shape)} {x.dtype} on {x.device} for a decoder of [{L}][{hkv}][rows][{d}] "
+                                 f"{self.k_pages.dtype} on {self.k_pages.device}")
         self.release(request)
         rows = cp.budgets[:, 0]
         new_lens = self.lens.clone()

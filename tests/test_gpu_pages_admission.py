@@ -41,6 +41,25 @@ def test_requests_out_of_range_are_refused(B, request_):
     cp.close()
 
 
+def test_caches_of_another_shape_are_refused_and_change_nothing(B):
+    """The request keeps what it held, and nothing is taken from the pool."""
+    wl = S.workload()
+    cp = S.compressed(wl)
+    dec = S.decoder(wl, 120, 2, 400)
+    dec.admit(0, cp)
+    before = state(dec)
+    for kw in (dict(n_layers=1), dict(n_layers=4), dict(n_kv_heads=3), dict(n_kv_heads=1), dict(head_dim=64), dict(dtype="f32")):
+        other = S.compressed(wl.with_(**kw))
+        for r in (0, 1):
+            with pytest.raises(ValueError):
+                dec.admit(r, other)
+        assert same(dec, before), kw
+        other.close()
+    dec.check()
+    dec.close()
+    cp.close()
+
+
 @pytest.mark.parametrize("keep_pages", [0, 6])
 def test_leaving_between_the_layers_of_a_step(B, keep_pages):
     """A request is released after a step has begun and its pages go to another: the layers still to come write nothing of the one
