@@ -298,7 +298,8 @@ class PagedDecoder:
 
     def admit(self, request: int, cp: CompressionPass):
         """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back.  Caches of another
-        number of layers, KV heads, head size, type or device are refused (ValueError)."""
+        number of layers, KV heads, head size, type or device are refused (ValueError); budgets that the pool or the buffers
+        of `cp` (its row_capacity) cannot serve are recorded for check(), and the request stays empty."""
         L, R = self.n_layers, self.max_requests
         self._check_request(request)
         _, hkv, _, d = self.k_pages.shape
@@ -308,12 +309,13 @@ class PagedDecoder:
                                  f"{self.k_pages.dtype} on {self.k_pages.device}")
         self.release(request)
         rows = cp.budgets[:, 0]
+        over = rows > cp.cap                               # such a layer was not compacted: nothing is admitted then
         new_lens = self.lens.clone()
-        new_lens.view(L, R)[:, request] = rows
+        new_lens.view(L, R)[:, request] = torch.where(over.any(), 0, rows)
         self._move(new_lens, self._no_slots)               # whole pages are stored: no slot map is needed
-        moved = self._cu[-1] > 0                           # stays 0 when the pool could not serve the request
+        moved = self._cu[-1] > 0                           # stays 0 when the request could not be served
         self.lens.copy_(torch.where(moved, new_lens, self.lens))
-        held = torch.where(moved, rows, 0).to(torch.int32)
+        held = torch.where(moved | over, rows, 0).to(torch.int32)      # (page_store records a layer with too many rows, and skips it)
         table = self.table.view(L, R, -1)[:, request].contiguous()
         self.pages.page_store(cp.k_out, cp.v_out, held, table, self.k_pages, self.v_pages, self.bounds)
         self.active[request:request + 1] = moved.to(torch.int32)

@@ -60,6 +60,28 @@ def test_caches_of_another_shape_are_refused_and_change_nothing(B):
     cp.close()
 
 
+def test_a_compression_that_ran_out_of_rows_is_not_admitted(B):
+    """Its budgets name rows that its buffers do not have: the request stays empty, and check() says so."""
+    wl = S.workload()
+    good, short = S.compressed(wl), S.compressed(wl, row_capacity=20)
+    with pytest.raises(B.MedaError):
+        short.check()
+    assert int(short.budgets[:, 0].max()) > 20
+    dec = S.decoder(wl, 120, 2, 400)
+    dec.admit(0, good)
+    dec.check()
+    before = state(dec)
+    dec.admit(1, short)
+    with pytest.raises(B.MedaError) as e:
+        dec.check()
+    assert e.value.status == B.MEDA_ERR_WORKSPACE
+    assert same(dec, before)
+    dec.check()
+    dec.close()
+    good.close()
+    short.close()
+
+
 @pytest.mark.parametrize("keep_pages", [0, 6])
 def test_leaving_between_the_layers_of_a_step(B, keep_pages):
     """A request is released after a step has begun and its pages go to another: the layers still to come write nothing of the one
