@@ -279,7 +279,10 @@ meda_status meda_pages_poll_status(meda_pages* pages, void* stream);
  *                 slots_capacity 0 (slots is not read then): no slot map is wanted
  * When the list runs out (MEDA_ERR_WORKSPACE), slots_capacity is too small (MEDA_ERR_WORKSPACE), or a length or
  * the list's front is out of range (MEDA_ERR_INVALID_ARG) the table and the list stay as they are, *free_top_out = *free_top,
- * cu_new is 0 and every slot -1. */
+ * cu_new is 0 and every slot -1.
+ * The entries that are given back, taken or grown into are not looked through beforehand: one outside the pool is recorded
+ * (MEDA_ERR_INVALID_ARG) and goes on as -1, into the table or the list, and as slots of -1.  From the list a later call hands it
+ * out, which is recorded again; no call reads or writes a page for it. */
 meda_status meda_page_tables(meda_pages* pages, const int32_t* lens, int32_t lens_stride, const int32_t* new_lens,
                              int32_t new_stride, int32_t n_seqs, int32_t* free_pages, const int32_t* free_top,
                              int32_t* free_top_out, int32_t* table, int32_t* cu_new, int64_t* slots,

@@ -167,6 +167,7 @@ page_tables_kernel(TablesParams p) {
   __syncthreads();
   const int total_pops = (int)n_pops, total_pushes = (int)n_pushes, total_new = (int)n_fresh;
 
+  // (entries are looked at where they are moved: to look at all of them beforehand, every block would have to)
   auto checked = [&](int page) {
     if ((unsigned)page >= (unsigned)p.n_pages) {
       set_status(p.status, MEDA_ERR_INVALID_ARG);
