@@ -311,10 +311,15 @@ meda_status meda_pages_poll_status(meda_pages* pages, void* stream) {
   if (!pages) return MEDA_ERR_INVALID_ARG;
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
+  // on `stream` alone: work on the default stream would wait for other streams, and a clearing still under way there could
+  // take the error of the next call with it
   int code = 0;
+  MEDA_CUDA_TRY(cudaMemcpyAsync(&code, pages->status, sizeof(int), cudaMemcpyDeviceToHost, as_stream(stream)));
   MEDA_CUDA_TRY(cudaStreamSynchronize(as_stream(stream)));
-  MEDA_CUDA_TRY(cudaMemcpy(&code, pages->status, sizeof(int), cudaMemcpyDeviceToHost));
-  if (code != 0) MEDA_CUDA_TRY(cudaMemset(pages->status, 0, sizeof(int)));
+  if (code != 0) {
+    MEDA_CUDA_TRY(cudaMemsetAsync(pages->status, 0, sizeof(int), as_stream(stream)));
+    MEDA_CUDA_TRY(cudaStreamSynchronize(as_stream(stream)));
+  }
   return (meda_status)code;
 }
 
