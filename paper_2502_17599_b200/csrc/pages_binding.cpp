@@ -153,10 +153,15 @@ meda_status page_store(Args a) {               // k, v, lens, table, k_pages, v_
   const at::Tensor &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &l = tensor(a[3], "lens");
   if (l.dim() != 1) refuse(n, l, at::kInt, "[n]", "lens");
   const int64_t c = l.size(0);
+  const auto alike = [&k](const at::Tensor& t) {  // (the stride of an axis of one element means nothing)
+    for (int64_t x = 0; x < 4; ++x)
+      if (t.size(x) != k.size(x) || (t.size(x) > 1 && t.stride(x) != k.stride(x))) return false;
+    return true;
+  };
   for (const at::Tensor* t : {&k, &v}) {
     const char* what = t == &k ? "k" : "v";
-    if (!on(n, *t, n->dtype) || t->dim() != 4 || t->size(0) != c || t->size(1) != n->hkv || t->size(3) != n->d || t->sizes() != k.sizes() ||
-        t->strides() != k.strides() || t->stride(3) != 1 || (t->size(2) > 1 && t->stride(2) != n->d))
+    if (!on(n, *t, n->dtype) || k.dim() != 4 || t->dim() != 4 || t->size(0) != c || t->size(1) != n->hkv || t->size(3) != n->d ||
+        !alike(*t) || t->stride(3) != 1 || (t->size(2) > 1 && t->stride(2) != n->d))
       refuse(n, *t, n->dtype, "[" + std::to_string(c) + "][" + std::to_string(n->hkv) + "][capacity][" + std::to_string(n->d) +
              "], rows dense, k and v laid out alike,", what);
   }
@@ -177,7 +182,7 @@ meda_status page_bounds(Args a) {              // k_pages, table, lens_from, len
   if (a[3] != Py_None) {
     const at::Tensor& f = tensor(a[3], "lens_from");
     from = lengths(n, f, c, "lens_from");
-    if (f.stride(0) != l.stride(0)) throw Refused("lens_from and lens have to have the same stride");
+    if (c > 1 && f.stride(0) != l.stride(0)) throw Refused("lens_from and lens have to have the same stride");
   }
   return unlocked(n->page_bounds, n->h, dense(n, a[1], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
                         static_cast<const int32_t*>(dense(n, a[2], at::kInt, {c, n->width}, "table")), from, lengths(n, l, c, "lens"),
