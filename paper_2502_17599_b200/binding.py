@@ -300,10 +300,15 @@ def load_native():
     if _NATIVE is None:
         import importlib.machinery
         import importlib.util
+
+        from . import build
         path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_pages.so")
         if not os.path.exists(path):
             raise RuntimeError(f"{path} is missing: build it with `python -m paper_2502_17599_b200.build` "
                                "(or __graft_entry__.build()); there is no fallback implementation")
+        if not build.binding_matches():
+            raise RuntimeError(f"{path} was built for another torch or interpreter: build it again with "
+                               "`python -m paper_2502_17599_b200.build`")
         loader = importlib.machinery.ExtensionFileLoader("_pages", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_pages", loader))
         loader.exec_module(module)

@@ -316,4 +316,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pages", nullptr, -1, methods, nul
 
 }  // namespace
 
+// Read from the file by build.py before anything of it is loaded.
+extern "C" __attribute__((visibility("default"), used)) const char meda_pages_built_for[] = MEDA_BUILT_FOR;
+
 PyMODINIT_FUNC PyInit__pages() { return PyModule_Create(&module); }
