@@ -155,9 +155,12 @@ struct SelectPagesKernels {
 template <typename T, int D, typename F>
 meda_status with_select_group(const meda_pages* p, F f) {
   const int g = p->group;
-  if (sizeof(T) == 2) return g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
-  return g == 1 ? f(SelectPagesKernels<T, D, 1>()) : g <= 4 ? f(SelectPagesKernels<T, D, 4>())
-       : g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
+  if constexpr (sizeof(T) == 2) {
+    return g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
+  } else {
+    return g == 1 ? f(SelectPagesKernels<T, D, 1>()) : g <= 4 ? f(SelectPagesKernels<T, D, 4>())
+         : g <= 8 ? f(SelectPagesKernels<T, D, 8>()) : f(SelectPagesKernels<T, D, 16>());
+  }
 }
 
 template <typename F>
