@@ -406,7 +406,7 @@ meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride,
   RopeParams a = {q, k, v, positions, slots, q_out, k_pages, v_pages, pages->rope_freq, pages->rope_axis, pages->status,
                   q_stride / e, k_stride / e, v_stride / e, axis_stride, (long long)c.n_pages << pages->page_shift,
                   n_tokens, c.n_q_heads, c.n_kv_heads, half, pages->page_shift, tokens};
-  const int grid = (n_tokens + tokens - 1) / tokens;
+  const int grid = (int)(((int64_t)n_tokens + tokens - 1) / tokens);
   cudaStream_t st = as_stream(stream);
   const bool adjacent = c.rope_pairing == MEDA_ROPE_ADJACENT;
   if (c.dtype == MEDA_F32) return adjacent ? launch_rope<float, true>(pages, a, grid, st) : launch_rope<float, false>(pages, a, grid, st);

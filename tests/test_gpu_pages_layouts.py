@@ -53,3 +53,18 @@ def test_bounds_of_one_sequence_with_lengths_of_different_strides(B):
     with pytest.raises(ValueError):                                # there the strides count
         pg.page_bounds(k, T.i32([[5, 6, 7], [8, 9, 10]]), T.i32([1, 2]), T.i32([[3, 0], [4, 0]])[:, 0], bounds[1])
     pg.close()
+
+
+def test_the_largest_number_of_tokens(B):
+    """2^31 - 1 of them, nearly all padding: keys and values are one row each that every token shows (token stride 0)."""
+    pg, t = T.make(B), 2 ** 31 - 1
+    k, v = T.normal((1, 2, 64), torch.bfloat16, 1), T.normal((1, 2, 64), torch.bfloat16, 2)
+    slots = torch.full((t,), -1, dtype=torch.int64, device="cuda")
+    slots[0], slots[t // 2], slots[-1] = 5, 70, 1023
+    kp, vp = (torch.zeros((64, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    pg.rope_append(None, k.expand(t, 2, 64), v.expand(t, 2, 64), None, slots, None, kp, vp)
+    pg.check()
+    for pool, row in ((kp, k), (vp, v)):
+        cells = pool.transpose(1, 2).reshape(-1, 2, 64)
+        assert torch.equal(cells[[5, 70, 1023]], row.expand(3, 2, 64)) and (cells != 0).any(-1).any(-1).sum() == 3
+    pg.close()
