@@ -136,7 +136,7 @@ page_tables_kernel(TablesParams p) {
   const int stride = gridDim.x * kTabThreads;
   if (code != MEDA_OK) {
 #pragma unroll 1
-    for (int i = blockIdx.x * kTabThreads + threadIdx.x; i < p.slots_capacity; i += stride) p.slots[i] = -1;
+    for (long long i = blockIdx.x * kTabThreads + threadIdx.x; i < p.slots_capacity; i += stride) p.slots[i] = -1;
 #pragma unroll 1
     for (int i = blockIdx.x * kTabThreads + threadIdx.x; i <= n; i += stride) p.cu_new[i] = 0;
     if (first) {
@@ -211,30 +211,30 @@ page_tables_kernel(TablesParams p) {
       first_slot = fresh[i] + (r0 - a);
     }
     if (!p.slots) continue;
-    const int begin = __shfl_sync(0xffffffffu, first_slot, 0);
+    const unsigned begin = (unsigned)__shfl_sync(0xffffffffu, first_slot, 0);      // (the last round's slots may pass 2^31)
     const int last = 31 - __clz(__ballot_sync(0xffffffffu, rows_here > 0));
-    const int end = __shfl_sync(0xffffffffu, first_slot + rows_here, last);
+    const unsigned end = (unsigned)__shfl_sync(0xffffffffu, first_slot + rows_here, last);
 #pragma unroll 1
-    for (int t0 = begin; t0 < end; t0 += 128) {                // four slots of a lane at a time: their searches run side by side
+    for (unsigned t0 = begin; t0 < end; t0 += 128) {           // four slots of a lane at a time: their searches run side by side
       int owner[4] = {0, 0, 0, 0};                             // the lane whose page holds the slot
 #pragma unroll
       for (int step = 16; step > 0; step >>= 1)
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          if (__shfl_sync(0xffffffffu, first_slot, owner[y] + step) <= t0 + 32 * y + lane) owner[y] += step;
+          if ((unsigned)__shfl_sync(0xffffffffu, first_slot, owner[y] + step) <= t0 + 32 * y + lane) owner[y] += step;
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const int t = t0 + 32 * y + lane;
+        const unsigned t = t0 + 32 * y + lane;
         const int pg = __shfl_sync(0xffffffffu, page, owner[y]);
-        const int r = __shfl_sync(0xffffffffu, row0 - first_slot, owner[y]) + t;
+        const int r = __shfl_sync(0xffffffffu, row0 - first_slot, owner[y]) + (int)t;
         if (t < end) p.slots[t] = pg < 0 ? -1 : ((int64_t)pg << p.page_shift) + r;
       }
     }
   }
   // pages given back that nobody took onto the list; nothing in the slots behind the last row
 #pragma unroll 1
-  for (int j = total_pops + blockIdx.x * kTabThreads + threadIdx.x; j < total_pushes; j += stride)
-    p.free_pages[top - 1 - (j - total_pops)] = checked(*pushed(j));
+  for (long long j = (long long)total_pops + blockIdx.x * kTabThreads + threadIdx.x; j < total_pushes; j += stride)
+    p.free_pages[top - 1 - (j - total_pops)] = checked(*pushed((int)j));
 #pragma unroll 1
   for (long long t = (long long)total_new + blockIdx.x * kTabThreads + threadIdx.x; t < p.slots_capacity; t += stride) p.slots[t] = -1;
 }
