@@ -321,7 +321,8 @@ class Pages:
     Method names and argument order follow include/meda.h; shapes are read from the tensors and checked
     against the geometry (ValueError).  Lengths are 1-D int32 tensors of any stride (`budgets[:, 0]` as it is).  The handle
     belongs to the device that is current when it is made, and so do the tensors; without `stream` a call goes to
-    that device's current stream."""
+    that device's current stream.  The calls let go of the interpreter's lock while they launch: one thread at a time
+    may use a handle, close() included."""
 
     def __init__(self, *, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_seqs, max_seq_pages,
                  rope_theta=10000.0, rope_sections=None, rope_order=ROPE_RUNS, rope_pairing=ROPE_HALVES):

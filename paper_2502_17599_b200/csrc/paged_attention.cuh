@@ -21,12 +21,14 @@
 // of the output; logits, maxima, sums and accumulators are fp32.  Both parts of a positive probability are positive: an infinite
 // value then adds infinities of one sign (0 * inf and inf - inf are NaN).
 //
-// Measured with its second launch, 28 query and 4 KV heads of 128, bf16: one cache of 129,072 rows (264 MB) 48.0 us, 5.5 TB/s or
-// 86 % of a plain copy, about 7 us of it launches, look-ups and joining; 64 caches of 36 to 18,944 rows (410 MB) 71.5 us, 89 %;
-// one of 947 rows 8.0 us, latency alone.
+// Measured with its second launch, calls back to back, 28 query and 4 KV heads of 128, bf16: one cache of 129,072 rows (264 MB) 48.7 us,
+// 5.4 TB/s or 84 % of a plain copy, about 7 us of it launches, look-ups and joining; 64 caches of 36 to 18,944 rows (410 MB) 72.8 us,
+// 87 %; one of 947 rows 8.2 us, latency alone (7.5 replayed from a graph).  400 MB with 16 heads per KV head: 5.1 TB/s at head_dim 128,
+// 4.7 at 64; with 7 heads at head_dim 256 5.0, with 16, which read the cache twice there, 2.7.
 //
 // fp32 caches: the same walk with the products on the CUDA cores (see DecodeShape in decode.cuh for the reduction), whose
-// shuffles bound it from four query heads per KV head on (400 MB of caches, head_dim 128: 5.9 TB/s with one, 4.1 with four, 3.3 with seven).
+// shuffles bound it from four query heads per KV head on (400 MB of caches, head_dim 128: 5.9 TB/s with one, 4.1 with four, 3.3 with
+// seven, 1.7 with sixteen, which read the cache twice).
 #pragma once
 
 #include "decode.cuh"        // transpose_reduce
@@ -38,10 +40,11 @@ namespace meda {
 constexpr int kAttTile = 16;             // rows per tile; a page holds whole tiles
 // Empty tiles counted with every segment of a batch of sequences: what starting one and joining its warps' states takes,
 // in tiles of a block's time.  Without them a block whose share is many short segments works far longer than one inside
-// a long one (64 sequences of 36 to 18,944 rows: 96 us; 8 tiles: 87, 12: 80, 20: 71, 28: 72).
+// a long one (64 sequences of 36 to 18,944 rows: 96 us; 8 tiles: 87, 12: 80, 20: 71, 28: 72; seven bf16 heads of 128 to a KV head,
+// the one shape it was measured on: other tiles take another time each, and would want another number).
 constexpr int kAttSegment = 20;
-// Tiles per block where the GPU has more blocks than that fills.  One sequence of 947 rows, 4 KV heads: 4 tiles 7.2 us, 8: 7.6,
-// 16: 9.1; of 4,000 rows: 9.0, 8.5, 9.3.
+// Tiles per block where the GPU has more blocks than that fills.  One sequence of 947 rows, 4 KV heads, replayed from a graph: 4 tiles
+// 7.2 us, 8: 7.6, 16: 9.1; of 4,000 rows: 9.0, 8.5, 9.3.
 constexpr int kAttLeast = 8;
 
 // x / d for 0 <= x < 2^31 by a multiplication: with 2^s < d < 2^(s+1), mul = ceil(2^(32+s) / d) is off by less than d / 2^(32+s),

@@ -105,8 +105,8 @@ struct AttnKernel {
 };
 
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
-// At head_dim 128, eight warps against twelve: 947 rows 7.1 and 7.6 us, 4,000 rows 8.0 and 8.5, 129,072 rows 50.5 and 48.8, 64 sequences
-// of 36 to 18,944 rows 76 and 71.4; twelve are taken for the long ones.
+// At head_dim 128, eight warps against twelve, replayed from a graph: 947 rows 7.1 and 7.6 us, 4,000 rows 8.0 and 8.5, 129,072 rows 50.5
+// and 48.8, 64 sequences of 36 to 18,944 rows 76 and 71.4; twelve are taken for the long ones.
 // At head_dim 256 a warp works on eight rows at a time: sixteen fill 224 registers before any temporary, and with the warps' states
 // beside them what is in flight no longer fits the L1 (400 MB, 7 heads per KV head: sixteen 98.1 us, eight 78.6; 947 rows 10.4 and
 // 9.0).  Elsewhere sixteen are better (head_dim 128: 67.8 and 80.2, the softmax's steps are per turn).
