@@ -211,7 +211,7 @@ page_tables_kernel(TablesParams p) {
       first_slot = fresh[i] + (r0 - a);
     }
     if (!p.slots) continue;
-    const unsigned begin = (unsigned)__shfl_sync(0xffffffffu, first_slot, 0);      // (the last round's slots may pass 2^31)
+    const unsigned begin = (unsigned)__shfl_sync(0xffffffffu, first_slot, 0);      // (t0 and t may pass 2^31 behind the last slot)
     const int last = 31 - __clz(__ballot_sync(0xffffffffu, rows_here > 0));
     const unsigned end = (unsigned)__shfl_sync(0xffffffffu, first_slot + rows_here, last);
 #pragma unroll 1
