@@ -251,11 +251,26 @@ typedef struct {
   int32_t rope_pairing;  /* MEDA_ROPE_HALVES: (i, i + half); MEDA_ROPE_ADJACENT: (2 i, 2 i + 1) */
 } meda_pages_config;
 
-/* Validates the geometry and allocates scratch memory on the current device (the only allocating call).
+/* Validates the geometry and allocates scratch memory on the current device (with meda_pages_create_quantised the only allocating call).
  * max_seqs * (max_seq_pages * page_size / 16 + 20) * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query
  * heads per KV head in bf16 at head_dim 256 or in fp32; times up to four in fp32 at head_dim 256), n_pages * n_kv_heads * page_size below 2^40.
  * On failure *out is NULL and the status says why. */
 meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out);
+/* The same for pools that hold cache_bits = 4 or 8 bits per element.  Every call below then takes and fills such pools (k_pages,
+ * v_pages: device, 16-byte aligned, [n_pages][n_kv_heads][meda_pages_page_bytes]); `dtype` stays the type of queries, new rows, outputs
+ * and bounds.  Every 64 dimensions of a row share a step and a lowest value, both bf16:
+ *   low = min x rounded down,  step = max(2^-126, fl((max x - low) * fl(1 / (2^cache_bits - 1))) rounded up),
+ *   code = rint(fl(fl(x - low) * fl(1 / step))),  an element reads back as low + step * code,
+ * with fl the rounding of an fp32 operation: the same rows give the same bytes everywhere.  An element is off by half a step at most, and by
+ * the roundings.  If any of the 64 is NaN or of magnitude 2^126 or more, all of them read back as NaN.
+ * A page of a head: the codes of its rows [page_size][head_dim * cache_bits / 8], then [page_size][2][head_dim / 64] bf16, steps and
+ * lowest values.  Codes of a row: units of eight dimensions, unit i of group g at place i * (head_dim / 64) + g, in order from the lowest
+ * bits up.
+ * max_seqs * (max_seq_pages * page_size / 16 + 20) * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query heads per
+ * KV head, times up to four at head_dim 256). */
+meda_status meda_pages_create_quantised(const meda_pages_config* config, int32_t cache_bits, meda_pages** out);
+/* Bytes of one page of one KV head in a pool, whichever way it holds its rows. */
+int64_t meda_pages_page_bytes(const meda_pages* pages);
 /* Frees the scratch memory.  The caller must have synchronised the streams that used it. */
 void meda_pages_destroy(meda_pages* pages);
 int64_t meda_pages_workspace_bytes(const meda_pages* pages);
@@ -298,8 +313,20 @@ meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int
                             int32_t rows_capacity, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
                             const int32_t* table, void* k_pages, void* v_pages, void* bounds, void* stream);
 
+/* Rows [lens_from[i], lens[i]) of every sequence (lens_from NULL: from row 0) out of the pages into dense rows: what meda_page_store and
+ * meda_rope_append put there, or what their codes stand for, rounded once to `dtype`.
+ *   k, v   device, `dtype`: row lens_from[i] + j of a head at i * seq_stride + head * head_stride + j * head_dim; other rows are not
+ *          written.  Sequences and heads do not overlap.
+ * Both lengths are read with lens_stride; lens_from[i] >= lens[i]: no rows.  More than rows_capacity rows record MEDA_ERR_WORKSPACE, a
+ * length out of range MEDA_ERR_INVALID_ARG, and the sequence is skipped; of a page outside the pool no rows are written.  Alignment as for
+ * meda_page_store. */
+meda_status meda_page_load(meda_pages* pages, const void* k_pages, const void* v_pages, const int32_t* table,
+                           const int32_t* lens_from, const int32_t* lens, int32_t lens_stride, int32_t n_seqs, void* k, void* v,
+                           int64_t seq_stride, int64_t head_stride, int32_t rows_capacity, void* stream);
+
 /* Key bounds, recomputed for the pages that rows [lens_from[i], lens[i]) of each sequence touch (lens_from NULL: from
- * row 0), each over all of the page's rows below lens[i].  Both lengths are read with lens_stride. */
+ * row 0), each over all of the page's rows below lens[i].  Both lengths are read with lens_stride.  Here and in meda_page_store the bounds of
+ * quantised keys are those of what they read back as. */
 meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32_t* table, const int32_t* lens_from,
                              const int32_t* lens, int32_t lens_stride, int32_t n_seqs, void* bounds, void* stream);
 
@@ -313,7 +340,10 @@ meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32
  *   positions  device int32 [3][n_tokens], axis a at positions + a * axis_stride.  NULL: nothing is rotated.
  *   slots      device int64 [n_tokens]: where the token's key and value go.  Slots of one call are distinct.
  *   q_out      device, `dtype`, [n_tokens][n_q_heads][head_dim]; may be q itself when that is dense
- * A token with slot -1 is padding: neither q_out nor the pools are written for it. */
+ * A token with slot -1 is padding: neither q_out nor the pools are written for it.
+ * Into quantised pools the key goes as the pools of its type would hold it, rounded to `dtype`, and then into codes; cosine and sine are
+ * correctly rounded there (from 64-bit arithmetic), the two products and their sum are rounded one by one, so that the codes are the
+ * same everywhere. */
 meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                              const void* v, int64_t v_stride, const int32_t* positions, int64_t axis_stride,
                              const int64_t* slots, int32_t n_tokens, void* q_out, void* k_pages, void* v_pages,
@@ -339,7 +369,8 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
  *   out  device, `dtype`, [n_seqs][n_q_heads][head_dim]
  *   lse  device fp32 [n_seqs][n_q_heads], may be NULL: the logarithm of the softmax's sum, ready to join with the
  *        attention over rows kept elsewhere
- * A sequence of length 0 gets out = 0, lse = -inf.  An infinite value makes its dimension of the output infinite; both
+ * A sequence of length 0 gets out = 0, lse = -inf.  In quantised caches rows count as what they read back as, before it is rounded to
+ * `dtype`.  An infinite value makes its dimension of the output infinite; both
  * signs in one dimension, or a row whose weight is 0 in fp32 (below 2^-126 of the largest), make it NaN. */
 meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
                                  const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,

@@ -111,3 +111,88 @@ def attention(q_heads, k_rows, v_rows):
     p = e / z
     mag = (np.abs(q_heads) @ np.abs(k_rows).T / np.sqrt(d)).max(-1)
     return p @ v_rows, (m + np.log(z))[:, 0], dict(spread=p @ np.abs(v_rows), mag=mag)
+
+
+# ---- quantised pages: every 64 dimensions of a row share a step and a lowest value
+
+GROUP = 64
+
+
+def _bf16(x, up):
+    """fp32 -> the next bf16 value not below (up) or not above it, as fp32."""
+    bits = np.ascontiguousarray(x, np.float32).view(np.uint32)
+    cut = bits & np.uint32(0xffff0000)
+    away = (cut != bits) & ((bits >> 31 == 0) == up)
+    return (cut + np.where(away, np.uint32(0x10000), np.uint32(0))).view(np.float32)
+
+
+def quantise(x, bits):
+    """fp32 rows [..., d] -> (codes uint8 [..., d / 64, 64], step, low fp32 [..., d / 64]); every operation an fp32 one.  A group with a
+    NaN or an element of magnitude 2^126 or more has step = low = NaN (and codes of 0 here)."""
+    x = np.asarray(x, np.float32)
+    x = x.reshape(x.shape[:-1] + (x.shape[-1] // GROUP, GROUP))
+    with np.errstate(invalid="ignore", over="ignore"):
+        fine = (np.abs(x) < np.float32(2.0 ** 126)).all(-1)        # False for NaN
+        safe = np.where(fine[..., None], x, np.float32(0))
+        low = _bf16(safe.min(-1), False)
+        step = _bf16((safe.max(-1) - low) * (np.float32(1) / np.float32((1 << bits) - 1)), True)
+        step = np.maximum(step, np.float32(2.0 ** -126))
+        code = np.rint((safe - low[..., None]) * (np.float32(1) / step)[..., None])
+    nan = np.float32(np.nan)
+    return code.astype(np.uint8), np.where(fine, step, nan), np.where(fine, low, nan)
+
+
+def held(code, step, low):
+    """What the codes stand for, fp64 [..., d]."""
+    v = low[..., None].astype(np.float64) + step[..., None].astype(np.float64) * code
+    return v.reshape(v.shape[:-2] + (v.shape[-2] * GROUP,))
+
+
+def pack_page(code, step, low, bits):
+    """Codes [..., rows, groups, 64] and their steps and lowest values -> the bytes of a page [..., rows * row_bytes], written bit by bit."""
+    *lead, rows, groups, _ = code.shape
+    d = groups * GROUP
+    n = rows * d * bits // 8
+    out = np.zeros(lead + [n + rows * 4 * groups], np.uint8)
+    for r in range(rows):
+        for g in range(groups):
+            for x in range(GROUP):
+                bit = (((x // 8) * groups + g) * 8 + x % 8) * bits
+                out[..., r * d * bits // 8 + bit // 8] |= code[..., r, g, x] << (bit % 8)
+    half = np.stack([step, low], -2).astype(np.float32)              # [..., rows, 2, groups]
+    half = np.ascontiguousarray(half.view(np.uint32) >> 16, np.uint16)
+    out[..., n:] = half.reshape(lead + [rows * 2 * groups]).view(np.uint8)
+    return out
+
+
+def unpack_page(page, rows, d, bits):
+    """The inverse: (codes, step, low)."""
+    groups, n = d // GROUP, rows * d * bits // 8
+    lead = page.shape[:-1]
+    code = np.zeros(lead + (rows, groups, GROUP), np.uint8)
+    data = page[..., :n].reshape(lead + (rows, d * bits // 8))
+    for g in range(groups):
+        for x in range(GROUP):
+            bit = (((x // 8) * groups + g) * 8 + x % 8) * bits
+            code[..., g, x] = data[..., bit // 8] >> (bit % 8) & ((1 << bits) - 1)
+    half = np.ascontiguousarray(page[..., n:]).view(np.uint16).reshape(lead + (rows, 2, groups)).astype(np.uint32) << 16
+    half = half.view(np.float32)
+    return code, half[..., 0, :], half[..., 1, :]
+
+
+def rope_fp32(x, positions, sections, order, pairing, theta):
+    """rope() as the quantised pages define it: x fp32 [tokens][heads][D]; the angle in 64-bit fixed point, cosine and sine rounded to
+    fp32, two products and their sum rounded one by one.  The result is still to be rounded to the cache's type."""
+    half = sum(sections)
+    ax = axes(sections, order)
+    x = np.asarray(x, np.float32)
+    y = x.copy()
+    for i in range(half):
+        freq = int(theta ** (-i / half) / 6.283185307179586476925 * 18446744073709551616.0)
+        turn = [(int(p) * freq + (1 << 63)) % (1 << 64) - (1 << 63) for p in positions[ax[i]]]
+        angle = np.array(turn, np.float64) * (np.pi * 2.0 ** -63)
+        c, s = np.cos(angle).astype(np.float32)[:, None], np.sin(angle).astype(np.float32)[:, None]
+        a, b = (i, i + half) if pairing == 0 else (2 * i, 2 * i + 1)
+        y[..., a] = x[..., a] * c - x[..., b] * s
+        y[..., b] = x[..., b] * c + x[..., a] * s
+    return y

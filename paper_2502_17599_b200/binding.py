@@ -94,6 +94,8 @@ EXPORTS = {
     "meda_compress_layer": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int32] + [ctypes.c_void_p] * 8 +
                             [ctypes.c_int32, ctypes.c_void_p]),
     "meda_pages_create": (ctypes.c_int, [ctypes.POINTER(meda_pages_config), ctypes.POINTER(ctypes.c_void_p)]),
+    "meda_pages_create_quantised": (ctypes.c_int, [ctypes.POINTER(meda_pages_config), ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p)]),
+    "meda_pages_page_bytes": (ctypes.c_int64, [ctypes.c_void_p]),
     "meda_pages_destroy": (None, [ctypes.c_void_p]),
     "meda_pages_workspace_bytes": (ctypes.c_int64, [ctypes.c_void_p]),
     "meda_pages_launch_count": (ctypes.c_int64, [ctypes.c_void_p]),
@@ -102,6 +104,8 @@ EXPORTS = {
                                         ctypes.c_int32] + [ctypes.c_void_p] * 6 + [ctypes.c_int64, ctypes.c_void_p]),
     "meda_page_store": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p,
                                        ctypes.c_int32, ctypes.c_int32] + [ctypes.c_void_p] * 5),
+    "meda_page_load": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_int32] * 2 + [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 2 +
+                       [ctypes.c_int32, ctypes.c_void_p]),
     "meda_page_bounds": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int32] * 2 + [ctypes.c_void_p] * 2),
     "meda_rope_append": (ctypes.c_int, [ctypes.c_void_p] + [ctypes.c_void_p, ctypes.c_int64] * 4 +
                          [ctypes.c_void_p, ctypes.c_int32] + [ctypes.c_void_p] * 4),
@@ -322,15 +326,21 @@ class Pages:
     against the geometry (ValueError).  Lengths are 1-D int32 tensors of any stride (`budgets[:, 0]` as it is).  The handle
     belongs to the device that is current when it is made, and so do the tensors; without `stream` a call goes to
     that device's current stream.  The calls let go of the interpreter's lock while they launch: one thread at a time
-    may use a handle, close() included."""
+    may use a handle, close() included.
+
+    cache_bits 4 or 8: the pools hold codes of that many bits per element (include/meda.h says how), uint8
+    [n_pages][n_kv_heads][page_bytes()], 16-byte aligned."""
 
     def __init__(self, *, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_seqs, max_seq_pages,
-                 rope_theta=10000.0, rope_sections=None, rope_order=ROPE_RUNS, rope_pairing=ROPE_HALVES):
+                 rope_theta=10000.0, rope_sections=None, rope_order=ROPE_RUNS, rope_pairing=ROPE_HALVES,
+                 cache_bits=0):
         self._h = None
         lib = load_library()
         f32 = dtype in ("f32", torch.float32)
         if not f32 and dtype not in ("bf16", torch.bfloat16):
             raise ValueError("dtype is bf16 or f32")
+        if cache_bits not in (0, 4, 8):
+            raise ValueError("cache_bits is 4 or 8, or 0 for pools of the dtype itself")
         sections = (head_dim // 2, 0, 0) if rope_sections is None else tuple(int(x) for x in rope_sections)
         if len(sections) != 3:
             raise ValueError("rope_sections has three entries: time, height, width")
@@ -338,15 +348,20 @@ class Pages:
                                      max_seqs, max_seq_pages, float(rope_theta), (ctypes.c_int32 * 3)(*sections),
                                      rope_order, rope_pairing)
         handle = ctypes.c_void_p()
-        _check(lib.meda_pages_create(ctypes.byref(self.cfg), ctypes.byref(handle)), "meda_pages_create")
+        if cache_bits:
+            _check(lib.meda_pages_create_quantised(ctypes.byref(self.cfg), cache_bits, ctypes.byref(handle)), "meda_pages_create_quantised")
+        else:
+            _check(lib.meda_pages_create(ctypes.byref(self.cfg), ctypes.byref(handle)), "meda_pages_create")
+        self.cache_bits = int(cache_bits)
         self._h = handle.value
         self._lib = lib
         self._device = torch.cuda.current_device()
         native = load_native()
         address = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
         self._n = native.bind(self._h, self._device, f32, (n_pages, max_seq_pages, n_q_heads, n_kv_heads, page_size, head_dim),
-                              tuple(address(f"meda_{name}") for name in ("page_tables", "page_store", "page_bounds", "rope_append",
-                                                                         "select_pages", "paged_attention")))
+                              self.page_bytes() if cache_bits else 0,
+                              tuple(address(f"meda_{name}") for name in ("page_tables", "page_store", "page_load", "page_bounds",
+                                                                         "rope_append", "select_pages", "paged_attention")))
         self._native = native
 
     def close(self):
@@ -364,6 +379,10 @@ class Pages:
 
     def workspace_bytes(self) -> int:
         return int(self._lib.meda_pages_workspace_bytes(self._h))
+
+    def page_bytes(self) -> int:
+        """Bytes of one page of one KV head in a pool."""
+        return int(self._lib.meda_pages_page_bytes(self._h))
 
     def launch_count(self) -> int:
         return int(self._lib.meda_pages_launch_count(self._h))
@@ -386,6 +405,12 @@ class Pages:
         status = self._native.page_store(self._n, k, v, lens, table, k_pages, v_pages, bounds, stream)
         if status:
             _check(status, "meda_page_store")
+
+    def page_load(self, k_pages, v_pages, table, lens, k, v, lens_from=None, stream=None):
+        """Rows [lens_from, lens) of every sequence into k, v (laid out as for page_store), the first of them to row 0."""
+        status = self._native.page_load(self._n, k_pages, v_pages, table, lens_from, lens, k, v, stream)
+        if status:
+            _check(status, "meda_page_load")
 
     def page_bounds(self, k_pages, table, lens_from, lens, bounds, stream=None):
         """lens_from: None, or of the same stride as lens."""

@@ -1,0 +1,150 @@
+// Rotary positions with three axes (see rope_append.cuh), the new rows quantised into their pages.
+//
+// A key's codes hang on borders, so its rotation is stated to the bit: the angle is exact (64-bit fixed point), its sine and
+// cosine come from 64-bit arithmetic and are rounded to fp32, the two products and their sum are rounded one by one, and the key
+// is rounded to the cache's type before it is quantised.  A prompt appended here and one rotated elsewhere give the same pages.
+//
+// A block takes a few tokens.  Queries go by pairs of vectors (both read before either is written: q_out may be q), keys
+// and values by units of eight dimensions, eight neighbouring lanes to a group; a lane reads its unit and, with paired halves, the
+// unit's partner.
+#pragma once
+
+#include "page_codes.cuh"
+#include "rope_append.cuh"
+
+namespace meda {
+
+template <typename T, int D, int BITS, bool ADJACENT>
+__global__ void __launch_bounds__(kRopeThreads)
+coded_append_kernel(RopeParams p) {
+  constexpr int E = RopeVec<T>::E;
+  begin_grid();
+  constexpr int VR = D / E, U = D / 8;                         // vectors and units per head
+  constexpr int kTurns = ADJACENT ? 4 : 8;                     // frequencies of a unit: they lie half / kTurns apart
+  __shared__ float2 turn[kRopeMaxTokens][D / 2];               // (cos, sin) of the block's tokens
+  __shared__ int64_t slot_of[kRopeMaxTokens];
+  const int t0 = blockIdx.x * p.tokens_per_block;
+  const int n_tok = min(p.tokens_per_block, p.n_tokens - t0);
+  const int half = p.positions ? p.half : 0;
+  if ((int)threadIdx.x < n_tok) {
+    int64_t s = p.slots[t0 + threadIdx.x];
+    if (s >= p.n_slots || s < -1) {
+      set_status(p.status, MEDA_ERR_INVALID_ARG);
+      s = -1;
+    }
+    slot_of[threadIdx.x] = s;
+  }
+  const int apart = half / kTurns;
+#pragma unroll 1
+  for (int x = threadIdx.x; x < n_tok * half; x += kRopeThreads) {
+    const int tok = x / half, i = x - tok * half;
+    const long long pos = p.positions[p.axis[i] * p.axis_stride + t0 + tok];
+    const long long frac = (long long)((unsigned long long)pos * p.freq[i]);          // turns, as a signed 64-bit fraction
+    double s, c;
+    sincospi((double)frac * 1.0842021724855044e-19, &s, &c);                          // 2^-63: twice the turns
+    turn[tok][(i % kTurns) * apart + i / kTurns] = make_float2((float)c, (float)s);
+  }
+  __syncthreads();
+
+  // ---- queries
+  const int rot = ADJACENT ? 2 * half / E : half / E;          // items of a head that rotate
+  const int per_head = rot + (VR - 2 * half / E);
+  const int q_items = p.q ? p.n_q_heads * per_head : 0;
+  for (int x = threadIdx.x; x < n_tok * q_items; x += kRopeThreads) {
+    const int tok = x / q_items;
+    int item = x - tok * q_items;
+    if (slot_of[tok] < 0) continue;
+    const int h = item / per_head;
+    item -= h * per_head;
+    const uint4* src = static_cast<const uint4*>(p.q) + (t0 + tok) * p.q_stride + h * VR;
+    uint4* dst = static_cast<uint4*>(p.q_out) + ((size_t)(t0 + tok) * p.n_q_heads + h) * VR;
+    if (item >= rot) {
+      const int vec = 2 * half / E + (item - rot);
+      dst[vec] = src[vec];
+      continue;
+    }
+    if (ADJACENT) {
+      float f[E];
+      RopeVec<T>::unpack(src[item], f);
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+        const int i = item * (E / 2) + e;
+        const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+        const float a = f[2 * e], b = f[2 * e + 1];
+        f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
+        f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+      }
+      dst[item] = RopeVec<T>::pack(f);
+    } else {
+      float a[E], b[E];
+      const int other = item + half / E;
+      const uint4 xa = src[item], xb = src[other];
+      RopeVec<T>::unpack(xa, a);
+      RopeVec<T>::unpack(xb, b);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = item * E + e;
+        const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+        const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
+        b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
+        a[e] = y;
+      }
+      dst[item] = RopeVec<T>::pack(a);
+      dst[other] = RopeVec<T>::pack(b);
+    }
+  }
+
+  // ---- keys and values: a whole warp goes round together, its groups of eight lanes are all in or all out
+  const int page_size = 1 << p.page_shift;
+  const size_t page_bytes = (size_t)CodedRow<D, BITS>::kBytes << p.page_shift;
+  const int per_token = 2 * p.n_kv_heads * U, total = n_tok * per_token;
+  const int lane = threadIdx.x % 32;
+#pragma unroll 1
+  for (int x0 = threadIdx.x - lane; x0 < total; x0 += kRopeThreads) {
+    const int x = min(x0 + lane, total - 1);
+    const int tok = x / per_token, item = x - tok * per_token;
+    const int u = item % U, head = item / U;
+    const bool key = head < p.n_kv_heads;
+    const int g = key ? head : head - p.n_kv_heads;
+    const int64_t slot = slot_of[tok];
+    const T* src = key ? static_cast<const T*>(p.k) + (t0 + tok) * p.k_stride * E : static_cast<const T*>(p.v) + (t0 + tok) * p.v_stride * E;
+    src += (size_t)g * D;
+    Eight<T> v;
+    v.load(src + u * 8);
+    if (key && u * 8 < 2 * half) {
+      float f[8];
+      v.floats(f);
+      if (ADJACENT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 cs = turn[tok][e * apart + u];
+          const float a = f[2 * e], b = f[2 * e + 1];
+          f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
+          f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+        }
+      } else {
+        const bool second = u * 8 >= half;
+        const int at = second ? u - half / 8 : u;              // the pair's unit in the first half
+        Eight<T> o;
+        o.load(src + (second ? at : u + half / 8) * 8);
+        float y[8];
+        o.floats(y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 cs = turn[tok][e * apart + at];
+          const float mine = __fmul_rn(f[e], cs.x), other = __fmul_rn(y[e], cs.y);
+          f[e] = second ? __fadd_rn(mine, other) : __fsub_rn(mine, other);
+        }
+      }
+      v.round(f);
+    }
+    Unit<BITS> c;
+    c.encode(v);
+    if (slot < 0 || x0 + lane >= total) continue;
+    unsigned char* pool = static_cast<unsigned char*>(key ? p.k_pages : p.v_pages);
+    unsigned char* page = pool + ((size_t)(slot >> p.page_shift) * p.n_kv_heads + g) * page_bytes;
+    c.template put<D>(page, page_size, (int)(slot & (page_size - 1)), u);
+  }
+}
+
+}  // namespace meda

@@ -32,6 +32,7 @@
 #pragma once
 
 #include "decode.cuh"        // transpose_reduce
+#include "page_codes.cuh"
 #include "page_rows.cuh"     // load_stream
 #include "pages_common.cuh"
 
@@ -108,6 +109,7 @@ __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i ==
 template <int D, int NH, int R = 16>
 struct AttnTileBf16 {
   using T = __nv_bfloat16;
+  static constexpr bool kMma = true, kCoded = false;
   static constexpr int kHeads = 8 * NH;
   static constexpr int KC = D / 32, VC = D / 64, KT = R / 8, kRows = R;
   uint4 q[NH][KC];
@@ -278,6 +280,7 @@ struct AttnTileBf16 {
 template <int D, int GP>
 struct AttnTileF32 {
   using T = float;
+  static constexpr bool kMma = false, kCoded = false;
   static constexpr int kHeads = GP;
   static constexpr int E = D / 32, B = 4;
   static constexpr int P = GP * B <= 8 ? 8 : (GP * B <= 16 ? 16 : 32);
@@ -384,6 +387,42 @@ struct AttnTileF32 {
   }
 };
 
+// ---- quantised caches: read back into fp32, then as above -------------------------------------------------------
+template <typename TOUT, int D, int GP, int BITS>
+struct AttnTileCoded : AttnTileF32<D, GP> {
+  using T = TOUT;
+  using Base = AttnTileF32<D, GP>;
+  using Row = CodedRow<D, BITS>;
+  static constexpr bool kCoded = true;
+  static constexpr int E = Base::E, B = Base::B;
+  __device__ __forceinline__ void load_q(const T* qh, int heads, int lane) {
+#pragma unroll
+    for (int h = 0; h < GP; ++h)
+#pragma unroll
+      for (int e = 0; e < E; ++e) this->q[h][e] = h < heads ? to_f32<T>(qh[(size_t)h * D + lane * E + e]) : 0.f;
+  }
+  // Rows r0 .. r0 + 3 of the tile whose first row is `row` of the pool; behind the last of nv that one again.
+  __device__ __forceinline__ static void load_coded(float (&x)[B][E], const void* pool, long long row, int page_size, int r0, int nv,
+                                                    int lane) {
+    const int in = (int)row & (page_size - 1), u = lane * E / 8, e0 = lane * E % 8;
+    const unsigned char* page = static_cast<const unsigned char*>(pool) + (row - in) * Row::kBytes;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      Unit<BITS> c;
+      c.template get<D>(page, page_size, in + min(r0 + b, nv - 1), u);
+      float f[8];
+      c.values(f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[b][e] = f[e];
+#pragma unroll
+        for (int s = E; s < 8; s += E)
+          if (e0 == s) x[b][e] = f[s + e];
+      }
+    }
+  }
+};
+
 template <typename T>
 __device__ __forceinline__ void store4(T* dst, const float4& x);
 template <>
@@ -418,7 +457,6 @@ template <typename Tile, int D, int W>
 __global__ void __launch_bounds__(W * 32, 1)
 paged_attention_kernel(AttnParams p) {
   using T = typename Tile::T;
-  constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int HP = Tile::kHeads;
   constexpr int LD = D + 4;
   constexpr int kStates = attn_merge_floats(W, HP, D);
@@ -547,7 +585,7 @@ paged_attention_kernel(AttnParams p) {
     }
     const long long row_after = __shfl_sync(0xffffffffu, row_now, at);
     const int nv_after = __shfl_sync(0xffffffffu, nv_now, at);
-    if constexpr (kBf16) {
+    if constexpr (Tile::kMma) {
       constexpr int R = Tile::kRows;
 #pragma unroll
       for (int b = 0; b < kAttTile; b += R) {
@@ -564,8 +602,13 @@ paged_attention_kernel(AttnParams p) {
       for (int b = 0; b < 4; ++b) {
         const int r0 = b < 3 ? 4 * (b + 1) : 0, n = b < 3 ? nv : nv_after;
         if (r0 < n) {
-          tile.load_rows(tile.kx[(b + 1) & 1], kp + (b < 3 ? row : row_after) * D, r0, n, lane);
-          tile.load_rows(tile.vx[(b + 1) & 1], vp + (b < 3 ? row : row_after) * D, r0, n, lane);
+          if constexpr (Tile::kCoded) {
+            tile.load_coded(tile.kx[(b + 1) & 1], p.k, b < 3 ? row : row_after, page_size, r0, n, lane);
+            tile.load_coded(tile.vx[(b + 1) & 1], p.v, b < 3 ? row : row_after, page_size, r0, n, lane);
+          } else {
+            tile.load_rows(tile.kx[(b + 1) & 1], kp + (b < 3 ? row : row_after) * D, r0, n, lane);
+            tile.load_rows(tile.vx[(b + 1) & 1], vp + (b < 3 ? row : row_after) * D, r0, n, lane);
+          }
         }
         if (4 * b < nv) tile.rows4(b & 1, 4 * b, nv, p.scale_log2, lane);
       }

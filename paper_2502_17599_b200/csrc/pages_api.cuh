@@ -10,6 +10,8 @@
 #include <atomic>
 #include <new>
 
+#include "coded_append.cuh"
+#include "page_codes.cuh"
 #include "page_rows.cuh"
 #include "page_tables.cuh"
 #include "paged_attention.cuh"
@@ -104,6 +106,14 @@ struct AttnKernel {
   }
 };
 
+template <typename T, int BITS, typename F>
+meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
+  const int d = p->cfg.head_dim, g = p->group;
+  if (d == 64) return g == 1 ? f(AttnKernel<AttnTileCoded<T, 64, 1, BITS>, 64, 16>()) : f(AttnKernel<AttnTileCoded<T, 64, 8, BITS>, 64, 16>());
+  if (d == 128) return g == 1 ? f(AttnKernel<AttnTileCoded<T, 128, 1, BITS>, 128, 16>()) : f(AttnKernel<AttnTileCoded<T, 128, 8, BITS>, 128, 8>());
+  return g == 1 ? f(AttnKernel<AttnTileCoded<T, 256, 1, BITS>, 256, 8>()) : f(AttnKernel<AttnTileCoded<T, 256, 4, BITS>, 256, 8>());
+}
+
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
 // At head_dim 128, eight warps against twelve, replayed from a graph: 947 rows 7.1 and 7.6 us, 4,000 rows 8.0 and 8.5, 129,072 rows 50.5
 // and 48.8, 64 sequences of 36 to 18,944 rows 76 and 71.4; twelve are taken for the long ones.
@@ -114,6 +124,11 @@ struct AttnKernel {
 template <typename F>
 meda_status with_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
+  if (p->bits) {
+    if (p->cfg.dtype == MEDA_BF16)
+      return p->bits == 4 ? with_coded_attn_kernel<__nv_bfloat16, 4>(p, f) : with_coded_attn_kernel<__nv_bfloat16, 8>(p, f);
+    return p->bits == 4 ? with_coded_attn_kernel<float, 4>(p, f) : with_coded_attn_kernel<float, 8>(p, f);
+  }
   if (p->cfg.dtype == MEDA_BF16) {
     if (d == 64) return g <= 8 ? f(AttnKernel<AttnTileBf16<64, 1>, 64, 16>()) : f(AttnKernel<AttnTileBf16<64, 2>, 64, 16>());
     if (d == 128) return g <= 8 ? f(AttnKernel<AttnTileBf16<128, 1>, 128, 12>()) : f(AttnKernel<AttnTileBf16<128, 2>, 128, 8>());
@@ -197,11 +212,46 @@ meda_status launch_page_rows(meda_pages* p, const RowsParams& a, cudaStream_t st
                                                                            : go(page_rows_kernel<__nv_bfloat16, 32, STORE>);
 }
 
+// ---- quantised pages ---------------------------------------------------------------------------
+template <typename T, int BITS, CodedPass PASS>
+meda_status launch_coded_rows_of(meda_pages* p, const CodedParams& a, cudaStream_t st) {
+  const int blocks = p->sm_count * (PASS == kCodedBounds ? 4 : 16);        // as launch_page_rows
+  auto go = [&](auto kernel) { return launch_after(p, kernel, blocks, kRowsThreads, (size_t)(a.n_seqs + 1) * 4, st, a); };
+  const int d = p->cfg.head_dim;
+  return d == 64 ? go(coded_rows_kernel<T, 64, BITS, PASS>) : d == 128 ? go(coded_rows_kernel<T, 128, BITS, PASS>)
+                                                                     : go(coded_rows_kernel<T, 256, BITS, PASS>);
+}
+template <CodedPass PASS>
+meda_status launch_coded_rows(meda_pages* p, const CodedParams& a, cudaStream_t st) {
+  if (p->cfg.dtype == MEDA_F32)
+    return p->bits == 4 ? launch_coded_rows_of<float, 4, PASS>(p, a, st) : launch_coded_rows_of<float, 8, PASS>(p, a, st);
+  return p->bits == 4 ? launch_coded_rows_of<__nv_bfloat16, 4, PASS>(p, a, st) : launch_coded_rows_of<__nv_bfloat16, 8, PASS>(p, a, st);
+}
+
+meda_status launch_page_load(meda_pages* p, const LoadParams& a, cudaStream_t st) {
+  auto go = [&](auto kernel) { return launch_after(p, kernel, p->sm_count * 16, kRowsThreads, (size_t)(a.n_seqs + 1) * 4, st, a); };
+  const int vr = p->cfg.head_dim * pages_element(p) / 16;
+  return vr == 8 ? go(page_load_kernel<8>) : vr == 16 ? go(page_load_kernel<16>) : vr == 32 ? go(page_load_kernel<32>)
+                                                                                         : go(page_load_kernel<64>);
+}
+
+template <typename T, bool ADJACENT>
+meda_status launch_coded_append(meda_pages* p, const RopeParams& a, int grid, cudaStream_t st) {
+  auto go = [&](auto kernel) { return launch_after(p, kernel, grid, kRopeThreads, 0, st, a); };
+  const int d = p->cfg.head_dim;
+  if (p->bits == 4)
+    return d == 64 ? go(coded_append_kernel<T, 64, 4, ADJACENT>) : d == 128 ? go(coded_append_kernel<T, 128, 4, ADJACENT>)
+                                                                          : go(coded_append_kernel<T, 256, 4, ADJACENT>);
+  return d == 64 ? go(coded_append_kernel<T, 64, 8, ADJACENT>) : d == 128 ? go(coded_append_kernel<T, 128, 8, ADJACENT>)
+                                                                        : go(coded_append_kernel<T, 256, 8, ADJACENT>);
+}
+
 // (32 KB of prefixes at most: below the limit every kernel starts with)
 static_assert((kPagesMaxSeqs + 1) * 4 <= 48 * 1024, "page_rows_kernel would have to raise its shared memory");
 
 template <typename T, bool ADJACENT>
 meda_status launch_rope(meda_pages* p, const RopeParams& a, int grid, cudaStream_t st) {
+  if (p->bits) return launch_coded_append<T, ADJACENT>(p, a, grid, st);
   auto go = [&](auto kernel) { return launch_after(p, kernel, grid, kRopeThreads, 0, st, a); };
   const int d = p->cfg.head_dim;
   return d == 64 ? go(rope_append_kernel<T, 64, ADJACENT>) : d == 128 ? go(rope_append_kernel<T, 128, ADJACENT>)
@@ -213,12 +263,7 @@ void pages_release(meda_pages* p) {
   delete p;
 }
 
-}  // namespace
-
-#pragma GCC visibility push(default)
-extern "C" {
-
-meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out) {
+meda_status pages_create(const meda_pages_config* config, int bits, meda_pages** out) {
   if (out) *out = nullptr;
   if (!config || !out) return MEDA_ERR_INVALID_ARG;
   const meda_pages_config& c = *config;
@@ -258,6 +303,7 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
   meda_pages* p = new (std::nothrow) meda_pages();
   if (!p) return MEDA_ERR_CUDA;
   p->cfg = c;
+  p->bits = bits;
   p->group = c.n_q_heads / c.n_kv_heads;
   p->page_shift = 4;
   while ((1 << p->page_shift) < c.page_size) ++p->page_shift;
@@ -300,6 +346,25 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
   }
   *out = p;
   return MEDA_OK;
+}
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out) { return pages_create(config, 0, out); }
+
+meda_status meda_pages_create_quantised(const meda_pages_config* config, int32_t cache_bits, meda_pages** out) {
+  if (out) *out = nullptr;
+  if (cache_bits != 4 && cache_bits != 8) return MEDA_ERR_INVALID_ARG;
+  return pages_create(config, cache_bits, out);
+}
+
+int64_t meda_pages_page_bytes(const meda_pages* pages) {
+  if (!pages) return 0;
+  const meda_pages_config& c = pages->cfg;
+  return pages->bits ? coded_page_bytes(c.head_dim, pages->bits, c.page_size) : (int64_t)c.page_size * c.head_dim * pages_element(pages);
 }
 
 void meda_pages_destroy(meda_pages* pages) {
@@ -364,6 +429,12 @@ meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int
     return MEDA_ERR_SHAPE;
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
+  if (pages->bits) {
+    CodedParams a = {k, v, nullptr, nullptr, static_cast<unsigned char*>(k_pages), static_cast<unsigned char*>(v_pages), bounds, table, nullptr,
+                     lens, pages->status, seq_stride, head_stride, lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages,
+                     pages->page_shift, rows_capacity};
+    return launch_coded_rows<kCodedStore>(pages, a, as_stream(stream));
+  }
   RowsParams a = {k, v, k_pages, v_pages, bounds, table, nullptr, lens, pages->status, seq_stride / e, head_stride / e,
                   lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, rows_capacity};
   return launch_page_rows<true>(pages, a, as_stream(stream));
@@ -379,9 +450,39 @@ meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32
   PagesDevice dev(pages);
   if (!dev.ok) return MEDA_ERR_CUDA;
   const meda_pages_config& c = pages->cfg;
+  if (pages->bits) {                                           // (the pool is only read)
+    CodedParams a = {nullptr, nullptr, nullptr, nullptr, static_cast<unsigned char*>(const_cast<void*>(k_pages)), nullptr, bounds, table, lens_from,
+                     lens, pages->status, 0, 0, lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, 0};
+    return launch_coded_rows<kCodedBounds>(pages, a, as_stream(stream));
+  }
   RowsParams a = {k_pages, nullptr, nullptr, nullptr, bounds, table, lens_from, lens, pages->status, 0, 0,
                   lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, 0};
   return launch_page_rows<false>(pages, a, as_stream(stream));
+}
+
+meda_status meda_page_load(meda_pages* pages, const void* k_pages, const void* v_pages, const int32_t* table, const int32_t* lens_from,
+                           const int32_t* lens, int32_t lens_stride, int32_t n_seqs, void* k, void* v, int64_t seq_stride,
+                           int64_t head_stride, int32_t rows_capacity, void* stream) {
+  if (!pages || rows_capacity < 0 || seq_stride < 0 || head_stride < 0) return MEDA_ERR_INVALID_ARG;
+  const meda_status r = pages_batch_ok(pages, n_seqs, lens_stride);
+  if (r != MEDA_OK || n_seqs == 0) return r;
+  if ((rows_capacity > 0 && (!k || !v)) || !lens || !table || !k_pages || !v_pages) return MEDA_ERR_INVALID_ARG;
+  const meda_pages_config& c = pages->cfg;
+  const int e = 16 / pages_element(pages);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || seq_stride % e != 0 || head_stride % e != 0)
+    return MEDA_ERR_SHAPE;
+  PagesDevice dev(pages);
+  if (!dev.ok) return MEDA_ERR_CUDA;
+  if (pages->bits) {                                           // (the pools are only read)
+    CodedParams a = {nullptr, nullptr, k, v, static_cast<unsigned char*>(const_cast<void*>(k_pages)),
+                     static_cast<unsigned char*>(const_cast<void*>(v_pages)), nullptr, table, lens_from, lens, pages->status, seq_stride,
+                     head_stride, lens_stride, n_seqs, c.n_kv_heads, c.n_pages, c.max_seq_pages, pages->page_shift, rows_capacity};
+    return launch_coded_rows<kCodedLoad>(pages, a, as_stream(stream));
+  }
+  LoadParams a = {static_cast<const uint4*>(k_pages), static_cast<const uint4*>(v_pages), static_cast<uint4*>(k), static_cast<uint4*>(v),
+                  table, lens_from, lens, pages->status, seq_stride / e, head_stride / e, lens_stride, n_seqs, c.n_kv_heads, c.n_pages,
+                  c.max_seq_pages, pages->page_shift, rows_capacity};
+  return launch_page_load(pages, a, as_stream(stream));
 }
 
 meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

@@ -10,6 +10,7 @@
 #include <initializer_list>
 #include <sstream>
 #include <string>
+#include <utility>
 
 #include "../../include/meda.h"
 
@@ -26,8 +27,10 @@ struct Native {
   int device = 0;
   at::ScalarType dtype = at::kFloat;
   int64_t n_pages = 0, width = 0, hq = 0, hkv = 0, page = 0, d = 0;
+  int64_t coded = 0;                           // bytes of a page of quantised pools; 0: they hold rows of dtype
   decltype(&meda_page_tables) page_tables = nullptr;
   decltype(&meda_page_store) page_store = nullptr;
+  decltype(&meda_page_load) page_load = nullptr;
   decltype(&meda_page_bounds) page_bounds = nullptr;
   decltype(&meda_rope_append) rope_append = nullptr;
   decltype(&meda_select_pages) select_pages = nullptr;
@@ -75,10 +78,23 @@ void* dense(const Native* n, PyObject* o, at::ScalarType type, std::initializer_
   return t.data_ptr();
 }
 
+void* pool(const Native* n, PyObject* o, const char* what) {
+  return n->coded ? dense(n, o, at::kByte, {n->n_pages, n->hkv, n->coded}, what)
+                  : dense(n, o, n->dtype, {n->n_pages, n->hkv, n->page, n->d}, what);
+}
+
 // 1-D int32 lengths of any stride.
 const int32_t* lengths(const Native* n, const at::Tensor& t, int64_t count, const char* what) {
   if (!on(n, t, at::kInt) || t.dim() != 1 || t.size(0) != count) refuse(n, t, at::kInt, "[" + std::to_string(count) + "]", what);
   return static_cast<const int32_t*>(t.data_ptr());
+}
+
+// lens_from, read with the stride of lens.
+const int32_t* lengths_from(const Native* n, PyObject* o, const at::Tensor& lens) {
+  const at::Tensor& f = tensor(o, "lens_from");
+  const int32_t* from = lengths(n, f, lens.size(0), "lens_from");
+  if (lens.size(0) > 1 && f.stride(0) != lens.stride(0)) throw Refused("lens_from and lens have to have the same stride");
+  return from;
 }
 
 int32_t small(int64_t x, const char* what) {
@@ -94,6 +110,35 @@ void* heads_of(const Native* n, PyObject* o, int64_t count, int64_t heads, int64
     refuse(n, t, n->dtype, shape_text(at::IntArrayRef(want, 3)) + " with dense heads", what);
   *stride = count > 1 ? t.stride(0) : 0;
   return t.data_ptr();
+}
+
+// k, v: [count][n_kv_heads][capacity][head_dim], rows of a head dense, the outer strides free but alike.
+void rows_ok(const Native* n, const at::Tensor& k, const at::Tensor& v, int64_t c) {
+  const auto alike = [&k](const at::Tensor& t) {  // (the stride of an axis of one element means nothing)
+    for (int64_t x = 0; x < 4; ++x)
+      if (t.size(x) != k.size(x) || (t.size(x) > 1 && t.stride(x) != k.stride(x))) return false;
+    return true;
+  };
+  for (const at::Tensor* t : {&k, &v}) {
+    const char* what = t == &k ? "k" : "v";
+    if (!on(n, *t, n->dtype) || k.dim() != 4 || t->dim() != 4 || t->size(0) != c || t->size(1) != n->hkv || t->size(3) != n->d ||
+        !alike(*t) || t->stride(3) != 1 || (t->size(2) > 1 && t->stride(2) != n->d))
+      refuse(n, *t, n->dtype, "[" + std::to_string(c) + "][" + std::to_string(n->hkv) + "][capacity][" + std::to_string(n->d) +
+             "], rows dense, k and v laid out alike,", what);
+  }
+}
+
+// Whether x * sx + y * sy, for x < cx and y < cy, are at least `span` apart (rows that are written must not overlap).
+bool apart(int64_t cx, int64_t sx, int64_t cy, int64_t sy, int64_t span) {
+  if (cx < 2) sx = 0;
+  if (cy < 2) sy = 0;
+  if (sx > sy) {
+    std::swap(cx, cy);
+    std::swap(sx, sy);
+  }
+  if (cx > 1 && sx < span) return false;
+  if (cx > 1) span += (cx - 1) * sx;
+  return cy < 2 || sy >= span;
 }
 
 void* stream_of(const Native* n, PyObject* o) {
@@ -153,24 +198,29 @@ meda_status page_store(Args a) {               // k, v, lens, table, k_pages, v_
   const at::Tensor &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &l = tensor(a[3], "lens");
   if (l.dim() != 1) refuse(n, l, at::kInt, "[n]", "lens");
   const int64_t c = l.size(0);
-  const auto alike = [&k](const at::Tensor& t) {  // (the stride of an axis of one element means nothing)
-    for (int64_t x = 0; x < 4; ++x)
-      if (t.size(x) != k.size(x) || (t.size(x) > 1 && t.stride(x) != k.stride(x))) return false;
-    return true;
-  };
-  for (const at::Tensor* t : {&k, &v}) {
-    const char* what = t == &k ? "k" : "v";
-    if (!on(n, *t, n->dtype) || k.dim() != 4 || t->dim() != 4 || t->size(0) != c || t->size(1) != n->hkv || t->size(3) != n->d ||
-        !alike(*t) || t->stride(3) != 1 || (t->size(2) > 1 && t->stride(2) != n->d))
-      refuse(n, *t, n->dtype, "[" + std::to_string(c) + "][" + std::to_string(n->hkv) + "][capacity][" + std::to_string(n->d) +
-             "], rows dense, k and v laid out alike,", what);
-  }
+  rows_ok(n, k, v, c);
   return unlocked(n->page_store, n->h, k.data_ptr(), v.data_ptr(), c > 1 ? k.stride(0) : 0, n->hkv > 1 ? k.stride(1) : 0, small(k.size(2), "capacity"),
                        lengths(n, l, c, "lens"), small(l.stride(0), "stride"), small(c, "n_seqs"),
                        static_cast<const int32_t*>(dense(n, a[4], at::kInt, {c, n->width}, "table")),
-                       dense(n, a[5], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
-                       dense(n, a[6], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "v_pages"),
+                       pool(n, a[5], "k_pages"),
+                       pool(n, a[6], "v_pages"),
                        a[7] == Py_None ? nullptr : dense(n, a[7], n->dtype, {n->n_pages, n->hkv, 2, n->d}, "bounds"), stream_of(n, a[8]));
+}
+
+meda_status page_load(Args a) {                // k_pages, v_pages, table, lens_from, lens, k, v, stream
+  Native* n = native_of(a[0]);
+  const at::Tensor &l = tensor(a[5], "lens"), &k = tensor(a[6], "k"), &v = tensor(a[7], "v");
+  if (l.dim() != 1) refuse(n, l, at::kInt, "[n]", "lens");
+  const int64_t c = l.size(0);
+  const int32_t* from = a[4] == Py_None ? nullptr : lengths_from(n, a[4], l);
+  rows_ok(n, k, v, c);
+  for (const at::Tensor* t : {&k, &v})
+    if (!apart(c, t->stride(0), n->hkv, t->stride(1), t->size(2) * n->d))
+      throw Refused(std::string(t == &k ? "k" : "v") + ": sequences or heads overlap");
+  return unlocked(n->page_load, n->h, static_cast<const void*>(pool(n, a[1], "k_pages")), static_cast<const void*>(pool(n, a[2], "v_pages")),
+                  static_cast<const int32_t*>(dense(n, a[3], at::kInt, {c, n->width}, "table")), from, lengths(n, l, c, "lens"),
+                  small(l.stride(0), "stride"), small(c, "n_seqs"), k.data_ptr(), v.data_ptr(), c > 1 ? k.stride(0) : 0,
+                  n->hkv > 1 ? k.stride(1) : 0, small(k.size(2), "capacity"), stream_of(n, a[8]));
 }
 
 meda_status page_bounds(Args a) {              // k_pages, table, lens_from, lens, bounds, stream
@@ -178,13 +228,8 @@ meda_status page_bounds(Args a) {              // k_pages, table, lens_from, len
   const at::Tensor& l = tensor(a[4], "lens");
   if (l.dim() != 1) refuse(n, l, at::kInt, "[n]", "lens");
   const int64_t c = l.size(0);
-  const int32_t* from = nullptr;
-  if (a[3] != Py_None) {
-    const at::Tensor& f = tensor(a[3], "lens_from");
-    from = lengths(n, f, c, "lens_from");
-    if (c > 1 && f.stride(0) != l.stride(0)) throw Refused("lens_from and lens have to have the same stride");
-  }
-  return unlocked(n->page_bounds, n->h, dense(n, a[1], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
+  const int32_t* from = a[3] == Py_None ? nullptr : lengths_from(n, a[3], l);
+  return unlocked(n->page_bounds, n->h, pool(n, a[1], "k_pages"),
                         static_cast<const int32_t*>(dense(n, a[2], at::kInt, {c, n->width}, "table")), from, lengths(n, l, c, "lens"),
                         small(l.stride(0), "stride"), small(c, "n_seqs"), dense(n, a[5], n->dtype, {n->n_pages, n->hkv, 2, n->d}, "bounds"),
                         stream_of(n, a[6]));
@@ -215,8 +260,8 @@ meda_status rope_append(Args a) {              // q, k, v, positions, slots, q_o
     ax = t.stride(0);
   }
   return unlocked(n->rope_append, n->h, q, qs, k, ks, v, vs, pos, ax, static_cast<const int64_t*>(sl.data_ptr()), small(c, "n_tokens"), q_out,
-                        dense(n, a[7], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
-                        dense(n, a[8], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "v_pages"), stream_of(n, a[9]));
+                        pool(n, a[7], "k_pages"),
+                        pool(n, a[8], "v_pages"), stream_of(n, a[9]));
 }
 
 meda_status select_pages(Args a) {             // q, bounds, table, lens, n_first, n_last, sel, stream
@@ -246,8 +291,8 @@ meda_status paged_attention(Args a) {          // q, k_pages, v_pages, table, le
     sel = static_cast<const int32_t*>(dense(n, a[8], at::kInt, {c, n->hkv, keep}, "sel"));
   }
   return unlocked(n->paged_attention, n->h, dense(n, a[1], n->dtype, {c, n->hq, n->d}, "q"),
-                            dense(n, a[2], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "k_pages"),
-                            dense(n, a[3], n->dtype, {n->n_pages, n->hkv, n->page, n->d}, "v_pages"),
+                            pool(n, a[2], "k_pages"),
+                            pool(n, a[3], "v_pages"),
                             static_cast<const int32_t*>(dense(n, a[4], at::kInt, {c, n->width}, "table")), lengths(n, l, c, "lens"),
                             small(l.stride(0), "stride"), small(c, "n_seqs"), sel, small(keep, "keep"),
                             dense(n, a[6], n->dtype, {c, n->hq, n->d}, "out"),
@@ -272,12 +317,13 @@ PyObject* entry(PyObject*, Args a, Py_ssize_t n) {
 
 void drop(PyObject* o) { delete static_cast<Native*>(PyCapsule_GetPointer(o, kCapsule)); }
 
-// bind(handle, device, is_f32, (n_pages, width, hq, hkv, page_size, head_dim), (six addresses)) -> capsule
+// bind(handle, device, is_f32, (n_pages, width, hq, hkv, page_size, head_dim), page bytes if quantised, (seven addresses)) -> capsule
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long h, f[6];
+  unsigned long long h, f[7];
   int device, f32;
-  long long g[6];
-  if (!PyArg_ParseTuple(args, "Kip(LLLLLL)(KKKKKK)", &h, &device, &f32, g, g + 1, g + 2, g + 3, g + 4, g + 5, f, f + 1, f + 2, f + 3, f + 4, f + 5))
+  long long g[6], coded;
+  if (!PyArg_ParseTuple(args, "Kip(LLLLLL)L(KKKKKKK)", &h, &device, &f32, g, g + 1, g + 2, g + 3, g + 4, g + 5, &coded, f, f + 1, f + 2, f + 3,
+                        f + 4, f + 5, f + 6))
     return nullptr;
   auto* n = new (std::nothrow) Native();
   if (!n) return PyErr_NoMemory();
@@ -290,12 +336,14 @@ PyObject* bind(PyObject*, PyObject* args) {
   n->hkv = g[3];
   n->page = g[4];
   n->d = g[5];
+  n->coded = coded;
   n->page_tables = reinterpret_cast<decltype(n->page_tables)>(f[0]);
   n->page_store = reinterpret_cast<decltype(n->page_store)>(f[1]);
-  n->page_bounds = reinterpret_cast<decltype(n->page_bounds)>(f[2]);
-  n->rope_append = reinterpret_cast<decltype(n->rope_append)>(f[3]);
-  n->select_pages = reinterpret_cast<decltype(n->select_pages)>(f[4]);
-  n->paged_attention = reinterpret_cast<decltype(n->paged_attention)>(f[5]);
+  n->page_load = reinterpret_cast<decltype(n->page_load)>(f[2]);
+  n->page_bounds = reinterpret_cast<decltype(n->page_bounds)>(f[3]);
+  n->rope_append = reinterpret_cast<decltype(n->rope_append)>(f[4]);
+  n->select_pages = reinterpret_cast<decltype(n->select_pages)>(f[5]);
+  n->paged_attention = reinterpret_cast<decltype(n->paged_attention)>(f[6]);
   return PyCapsule_New(n, kCapsule, drop);
 }
 
@@ -309,7 +357,7 @@ PyObject* unbind(PyObject*, PyObject* o) {
 
 #define MEDA_ENTRY(name, count) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, count>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    MEDA_ENTRY(page_tables, 10), MEDA_ENTRY(page_store, 9), MEDA_ENTRY(page_bounds, 7), MEDA_ENTRY(rope_append, 10),
+    MEDA_ENTRY(page_tables, 10), MEDA_ENTRY(page_store, 9), MEDA_ENTRY(page_load, 9), MEDA_ENTRY(page_bounds, 7), MEDA_ENTRY(rope_append, 10),
     MEDA_ENTRY(select_pages, 9), MEDA_ENTRY(paged_attention, 10),
     {"bind", bind, METH_VARARGS, nullptr}, {"unbind", unbind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pages", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

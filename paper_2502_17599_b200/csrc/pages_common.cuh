@@ -11,6 +11,7 @@ struct meda_pages {
   int sm_count = 0;
   int group = 1;                       // query heads per KV head
   int page_shift = 4;                  // log2(page_size)
+  int bits = 0;                        // of an element of the pools: 4 or 8; 0: they hold rows of the geometry's type
   int64_t launches = 0;
   int64_t bytes = 0;
   void* slab = nullptr;                // the one allocation all pointers below lead into

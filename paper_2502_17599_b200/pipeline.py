@@ -237,11 +237,14 @@ class PagedDecoder:
     A request that cannot get its row keeps what it has: see begin_step.
 
     `keep_pages` > 0: attention reads at most that many pages per sequence and KV head, the ones whose key
-    bounds promise the largest logits, the first and the last always among them."""
+    bounds promise the largest logits, the first and the last always among them.
+
+    `cache_bits` 4 or 8: the pools hold that many bits per element (binding.Pages); rows are quantised as they are written, and
+    `read` gives them back."""
 
     def __init__(self, wl: Workload, n_pages: int, max_requests: int, max_rows: int, page_size: int = 16,
                  keep_pages: int = 0, n_first: int = 1, n_last: int = 2, rope_theta: float = 10000.0, rope_sections=None,
-                 rope_order: int = 0, rope_pairing: int = 0, device="cuda"):
+                 rope_order: int = 0, rope_pairing: int = 0, cache_bits: int = 0, device="cuda"):
         L, R, hkv, d = wl.n_layers, int(max_requests), wl.n_kv_heads, wl.head_dim
         self.wl, self.n_layers, self.max_requests = wl, L, R
         self.keep_pages, self.n_first, self.n_last = int(keep_pages), n_first, n_last
@@ -251,11 +254,14 @@ class PagedDecoder:
         with torch.cuda.device(device):
             self.pages = binding.Pages(n_q_heads=wl.n_q_heads, n_kv_heads=hkv, head_dim=d, dtype=wl.dtype, page_size=page_size,
                                        n_pages=n_pages, max_seqs=L * R, max_seq_pages=width, rope_theta=rope_theta,
-                                       rope_sections=rope_sections, rope_order=rope_order, rope_pairing=rope_pairing)
+                                       rope_sections=rope_sections, rope_order=rope_order, rope_pairing=rope_pairing,
+                                       cache_bits=cache_bits)
         i32 = dict(dtype=torch.int32, device=device)
         dt = dict(dtype=wl.torch_dtype, device=device)
-        self.k_pages = torch.empty((n_pages, hkv, page_size, d), **dt)
-        self.v_pages = torch.empty((n_pages, hkv, page_size, d), **dt)
+        if cache_bits:
+            self.k_pages, self.v_pages = (torch.empty((n_pages, hkv, self.pages.page_bytes()), dtype=torch.uint8, device=device) for _ in range(2))
+        else:
+            self.k_pages, self.v_pages = (torch.empty((n_pages, hkv, page_size, d), **dt) for _ in range(2))
         self.bounds = torch.empty((n_pages, hkv, 2, d), **dt) if self.keep_pages else None
         self.table = torch.full((L * R, width), -1, **i32)
         self.lens = torch.zeros(L * R, **i32)              # rows of every sequence
@@ -296,17 +302,20 @@ class PagedDecoder:
         if not 0 <= request < self.max_requests:
             raise IndexError(f"request {request} of {self.max_requests}")
 
+    def _check_dense(self, *caches):
+        L, hkv, d, dtype, device = self.n_layers, self.wl.n_kv_heads, self.wl.head_dim, self.wl.torch_dtype, self.k_pages.device
+        for x in caches:
+            if x.dim() != 4 or x.shape[:2] != (L, hkv) or x.shape[3] != d or x.dtype != dtype or x.device != device:
+                raise ValueError(f"caches of {tuple(x.shape)} {x.dtype} on {x.device} for a decoder of [{L}][{hkv}][rows][{d}] "
+                                 f"{dtype} on {device}")
+
     def admit(self, request: int, cp: CompressionPass):
         """The compacted caches of `cp` (all layers) become request `request`, whose earlier pages are given back.  Caches of another
         number of layers, KV heads, head size, type or device are refused (ValueError); budgets that the pool or the buffers
         of `cp` (its row_capacity) cannot serve are recorded for check(), and the request stays empty."""
         L, R = self.n_layers, self.max_requests
         self._check_request(request)
-        _, hkv, _, d = self.k_pages.shape
-        for x in (cp.k_out, cp.v_out):
-            if x.shape[:2] != (L, hkv) or x.shape[3] != d or x.dtype != self.k_pages.dtype or x.device != self.k_pages.device:
-                raise ValueError(f"caches of {tuple(x.shape)} {x.dtype} on {x.device} for a decoder of [{L}][{hkv}][rows][{d}] "
-                                 f"{self.k_pages.dtype} on {self.k_pages.device}")
+        self._check_dense(cp.k_out, cp.v_out)
         self.release(request)
         rows = cp.budgets[:, 0]
         over = rows > cp.cap                               # such a layer was not compacted: nothing is admitted then
@@ -330,6 +339,18 @@ class PagedDecoder:
         self.active[request] = 0
         self.slots[:, request] = -1                        # its pages may be another's before the step ends
         self._stalled[request] = False
+
+    def read(self, request: int, k, v, lens_from=None):
+        """The rows that `request` holds, of all layers, into k, v [L][Hkv][capacity][d], to hand the request on or to compress again what
+        it has gathered: rows [lens_from, length) of every layer to rows 0 and on, lens_from int32 [L] (None: all of them).  Returns
+        the rows' numbers, int32 [L].  A layer with more rows than `capacity` is recorded for check() and left out."""
+        L, R = self.n_layers, self.max_requests
+        self._check_request(request)
+        self._check_dense(k, v)
+        lens = self.lens.view(L, R)[:, request].contiguous()
+        table = self.table.view(L, R, -1)[:, request].contiguous()
+        self.pages.page_load(self.k_pages, self.v_pages, table, lens, k, v, lens_from=lens_from)
+        return lens if lens_from is None else (lens - lens_from).clamp_(min=0)
 
     def begin_step(self):
         """Room for one more row in every layer of the active requests.  A request with a layer that is full (max_rows, up to the end of
