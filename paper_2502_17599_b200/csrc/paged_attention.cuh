@@ -32,7 +32,6 @@
 #pragma once
 
 #include "decode.cuh"        // transpose_reduce
-#include "page_codes.cuh"
 #include "page_rows.cuh"     // load_stream
 #include "pages_common.cuh"
 
@@ -387,42 +386,6 @@ struct AttnTileF32 {
   }
 };
 
-// ---- quantised caches: read back into fp32, then as above -------------------------------------------------------
-template <typename TOUT, int D, int GP, int BITS>
-struct AttnTileCoded : AttnTileF32<D, GP> {
-  using T = TOUT;
-  using Base = AttnTileF32<D, GP>;
-  using Row = CodedRow<D, BITS>;
-  static constexpr bool kCoded = true;
-  static constexpr int E = Base::E, B = Base::B;
-  __device__ __forceinline__ void load_q(const T* qh, int heads, int lane) {
-#pragma unroll
-    for (int h = 0; h < GP; ++h)
-#pragma unroll
-      for (int e = 0; e < E; ++e) this->q[h][e] = h < heads ? to_f32<T>(qh[(size_t)h * D + lane * E + e]) : 0.f;
-  }
-  // Rows r0 .. r0 + 3 of the tile whose first row is `row` of the pool; behind the last of nv that one again.
-  __device__ __forceinline__ static void load_coded(float (&x)[B][E], const void* pool, long long row, int page_size, int r0, int nv,
-                                                    int lane) {
-    const int in = (int)row & (page_size - 1), u = lane * E / 8, e0 = lane * E % 8;
-    const unsigned char* page = static_cast<const unsigned char*>(pool) + (row - in) * Row::kBytes;
-#pragma unroll
-    for (int b = 0; b < B; ++b) {
-      Unit<BITS> c;
-      c.template get<D>(page, page_size, in + min(r0 + b, nv - 1), u);
-      float f[8];
-      c.values(f);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        x[b][e] = f[e];
-#pragma unroll
-        for (int s = E; s < 8; s += E)
-          if (e0 == s) x[b][e] = f[s + e];
-      }
-    }
-  }
-};
-
 template <typename T>
 __device__ __forceinline__ void store4(T* dst, const float4& x);
 template <>
@@ -597,18 +560,19 @@ paged_attention_kernel(AttnParams p) {
         if (b < nv) tile.attend(s, b, nv, lane);
         if (r0 < n) tile.load_v(vp + (last ? row_after : row) * D, r0, n, lane);
       }
+    } else if constexpr (Tile::kCoded) {
+      float s[HP / 8][4];
+      if (nv > 0) tile.logits(s, p.scale_log2, nv, lane);
+      if (nv_after > 0) tile.load_k(p.k, row_after, page_size, nv_after, lane);
+      if (nv > 0) tile.attend(s, nv, lane);
+      if (nv_after > 0) tile.load_v(p.v, row_after, page_size, nv_after, lane);
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int r0 = b < 3 ? 4 * (b + 1) : 0, n = b < 3 ? nv : nv_after;
         if (r0 < n) {
-          if constexpr (Tile::kCoded) {
-            tile.load_coded(tile.kx[(b + 1) & 1], p.k, b < 3 ? row : row_after, page_size, r0, n, lane);
-            tile.load_coded(tile.vx[(b + 1) & 1], p.v, b < 3 ? row : row_after, page_size, r0, n, lane);
-          } else {
-            tile.load_rows(tile.kx[(b + 1) & 1], kp + (b < 3 ? row : row_after) * D, r0, n, lane);
-            tile.load_rows(tile.vx[(b + 1) & 1], vp + (b < 3 ? row : row_after) * D, r0, n, lane);
-          }
+          tile.load_rows(tile.kx[(b + 1) & 1], kp + (b < 3 ? row : row_after) * D, r0, n, lane);
+          tile.load_rows(tile.vx[(b + 1) & 1], vp + (b < 3 ? row : row_after) * D, r0, n, lane);
         }
         if (4 * b < nv) tile.rows4(b & 1, 4 * b, nv, p.scale_log2, lane);
       }

@@ -11,6 +11,7 @@
 #include <new>
 
 #include "coded_append.cuh"
+#include "coded_attention.cuh"
 #include "page_codes.cuh"
 #include "page_rows.cuh"
 #include "page_tables.cuh"
@@ -109,9 +110,11 @@ struct AttnKernel {
 template <typename T, int BITS, typename F>
 meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
-  if (d == 64) return g == 1 ? f(AttnKernel<AttnTileCoded<T, 64, 1, BITS>, 64, 16>()) : f(AttnKernel<AttnTileCoded<T, 64, 8, BITS>, 64, 16>());
-  if (d == 128) return g == 1 ? f(AttnKernel<AttnTileCoded<T, 128, 1, BITS>, 128, 16>()) : f(AttnKernel<AttnTileCoded<T, 128, 8, BITS>, 128, 8>());
-  return g == 1 ? f(AttnKernel<AttnTileCoded<T, 256, 1, BITS>, 256, 8>()) : f(AttnKernel<AttnTileCoded<T, 256, 4, BITS>, 256, 8>());
+  constexpr bool kWide = sizeof(T) == 4;
+  if (d == 64) return g <= 8 ? f(AttnKernel<AttnTileCoded<T, 64, 1, BITS>, 64, 16>()) : f(AttnKernel<AttnTileCoded<T, 64, 2, BITS>, 64, 16>());
+  if (d == 128)
+    return g <= 8 ? f(AttnKernel<AttnTileCoded<T, 128, 1, BITS>, 128, kWide ? 12 : 16>()) : f(AttnKernel<AttnTileCoded<T, 128, 2, BITS>, 128, 8>());
+  return f(AttnKernel<AttnTileCoded<T, 256, 1, BITS>, 256, 8>());
 }
 
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
