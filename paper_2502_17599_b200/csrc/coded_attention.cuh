@@ -1,4 +1,4 @@
-// The attention's tile over quantised pages (the walk over the pages is paged_attention.cuh's).
+// Attention of one new token per sequence over quantised pages: the work split, the states and their joining are paged_attention.cuh's.
 //
 // A row's logit is the sum over its groups of step_g (q_g . codes_g) + low_g sum(q_g), an output the sum over the rows of
 // (p step_g) codes_g + p low_g.  So the matrix instructions multiply by the codes themselves, and a code is its own fp16 operand: the whole
@@ -19,8 +19,8 @@
 #pragma once
 
 #include "page_codes.cuh"
-#include "paged_attention.cuh"   // exp2_fast
-#include "pages_common.cuh"
+#include "paged_attention.cuh"   // the walk's numbers, exp2_fast, store4, the states' layout
+#include "sm100_primitives.cuh"
 
 namespace meda {
 
@@ -59,21 +59,33 @@ __device__ __forceinline__ uint32_t bf16_part(float& lo, float& hi) {
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }    // -126 <= e <= 127
 
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
+__device__ __forceinline__ void shared_words(uint32_t (&w)[N], const unsigned char* p) {
+  static_assert(N == 1 || N == 2 || N == 4, "one load");
   if constexpr (N == 1) {
-    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else if constexpr (N == 2) {
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
   } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const uint4 x = load_stream(reinterpret_cast<const uint4*>(p + 4 * i));
-      w[i] = x.x;
-      w[i + 1] = x.y;
-      w[i + 2] = x.z;
-      w[i + 3] = x.w;
-    }
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+    w[2] = x.z;
+    w[3] = x.w;
   }
+}
+template <int N>
+__device__ __forceinline__ void shared_piece(uint32_t (&w)[N], int i, const unsigned char* p) {
+  const uint4 x = *reinterpret_cast<const uint4*>(p);
+  w[i] = x.x;
+  w[i + 1] = x.y;
+  w[i + 2] = x.z;
+  w[i + 3] = x.w;
+}
+// 16 bytes from global to shared memory behind the thread's back; zeros where `live` is false.
+__device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(live ? 16 : 0) : "memory");
 }
 
 // T = type of queries and outputs, D = head_dim, NH = groups of eight query heads.
@@ -81,9 +93,10 @@ template <typename TOUT, int D, int NH, int BITS>
 struct AttnTileCoded {
   using T = TOUT;
   using Row = CodedRow<D, BITS>;
-  static constexpr bool kMma = false, kCoded = true;
   static constexpr int kHeads = 8 * NH;
   static constexpr int G = Row::kGroups, W = BITS / 4;           // groups, words per unit
+  static constexpr int kTileCodes = kAttTile * Row::kCodes, kTileMore = kAttTile * Row::kMore;
+  static constexpr int kHalf = kTileCodes + kTileMore, kStage = 2 * kHalf;       // bytes of a tile of keys or values, of both
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
   static constexpr int kScale = PARTS == 2 ? 13 : 5;             // weights reach 2^(kScale + 1) (times 2^kSlack)
   static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference may stay this far (log2) behind the maximum
@@ -91,8 +104,6 @@ struct AttnTileCoded {
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
   uint32_t qsum[NH][2];                  // sums over the groups, in bf16 parts
   float unscale[NH][2];                  // 2^-k of the scaled queries, of the lane's two heads
-  uint32_t k[2][2 * G * W], km[2][G];    // rows r, r + 8: codes of units 2c, 2c + 1; steps and lowest values
-  uint32_t v[4][G * W], vm[2][G];        // rows 2c, 2c + 1, 2c + 8, 2c + 9: codes of unit r; steps and lowest values of rows r, r + 8
   float o[G][4][NH][4];
   float low_sum[NH][2][G];               // sum of p low
   float m[NH][2], l[NH][2];
@@ -200,30 +211,33 @@ struct AttnTileCoded {
     step_top = 0.f;
     step_exp = kScale - 125;
   }
-  // Rows behind the nv that count are not read: their lanes read the last one that does (see logits and attend).
-  __device__ __forceinline__ void load_k(const void* pool, long long row, int page_size, int nv, int lane) {
-    const int r = lane / 4, c = lane % 4, in = (int)row & (page_size - 1);
-    const unsigned char* page = static_cast<const unsigned char*>(pool) + (row - in) * Row::kBytes;
-    const unsigned char *codes = page + in * Row::kCodes + c * (2 * G * BITS), *more = page + page_size * Row::kCodes + in * Row::kMore;
+  // A tile in shared memory: 16-byte pieces of its codes, then its steps and lowest values; keys first, then values.  The pieces are moved inside
+  // a row, and the values' rows are sorted even ones first in each eight, so that the lanes that read together meet different banks.
+  static constexpr int kPieces = Row::kCodes / 16;               // of a row
+  static constexpr int kKeyBytes = 2 * G * BITS, kValueBytes = G * BITS;         // a lane reads of a row
+  __device__ __forceinline__ static int key_piece(int row, int piece) {
+    const int moved = kKeyBytes == 32 ? row & 1 : kKeyBytes == 64 ? (row & 1) << 1 | (piece >> 3 & 1) : 0;
+    return row * kPieces + (piece ^ moved);
+  }
+  __device__ __forceinline__ static int value_piece(int row, int piece) {
+    const int at = (row & 8) | (row & 1) << 2 | (row >> 1 & 3);
+    const int moved = kValueBytes == 8 ? at & 2 : kValueBytes == 16 ? (at & 3) << 1 : kValueBytes == 32 ? (at & 1) | (at & 2) << 1 : 0;
+    return at * kPieces + (piece ^ moved);
+  }
+
+  // Logits in the log2 domain of the keys at `stage`, of which nv rows count: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
+  __device__ __forceinline__ void logits(float (&s)[NH][4], const unsigned char* stage, float scale_log2, int nv, int lane) {
+    const int r = lane / 4, c = lane % 4;
+    uint32_t k[2][2 * G * W], km[2][G];                        // rows r, r + 8: codes of units 2c, 2c + 1; steps and lowest values
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int y = min(r + 8 * t, nv - 1);
-      load_words(k[t], codes + y * Row::kCodes);
-      load_words(km[t], more + y * Row::kMore);
+      if constexpr (kKeyBytes == 8) shared_words(k[t], stage + (r + 8 * t) * Row::kCodes + c * 8);
+      else
+#pragma unroll
+        for (int x = 0; x < kKeyBytes / 16; ++x)
+          shared_piece(k[t], 4 * x, stage + 8 * t * Row::kCodes + 16 * key_piece(r, c * (kKeyBytes / 16) + x));
+      shared_words(km[t], stage + kTileCodes + (r + 8 * t) * Row::kMore);
     }
-  }
-  __device__ __forceinline__ void load_v(const void* pool, long long row, int page_size, int nv, int lane) {
-    const int r = lane / 4, c = lane % 4, in = (int)row & (page_size - 1);
-    const unsigned char* page = static_cast<const unsigned char*>(pool) + (row - in) * Row::kBytes;
-    const unsigned char *codes = page + in * Row::kCodes + r * (G * BITS), *more = page + page_size * Row::kCodes + in * Row::kMore;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) load_words(v[t], codes + min(2 * c + (t & 1) + (t >> 1) * 8, nv - 1) * Row::kCodes);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) load_words(vm[t], more + min(r + 8 * t, nv - 1) * Row::kMore);
-  }
-  // Logits in the log2 domain: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
-  __device__ __forceinline__ void logits(float (&s)[NH][4], float scale_log2, int nv, int lane) {
-    const int r = lane / 4;
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
 #pragma unroll
@@ -272,8 +286,20 @@ struct AttnTileCoded {
           if (r + (e >> 1) * 8 >= nv) s[n][e] = -INFINITY;
     }
   }
-  __device__ __forceinline__ void attend(float (&s)[NH][4], int nv, int lane) {
-    const int r = lane / 4;
+  // The values at `stage`, weighed.
+  __device__ __forceinline__ void attend(const float (&s)[NH][4], const unsigned char* stage, int nv, int lane) {
+    const int r = lane / 4, c = lane % 4;
+    uint32_t v[4][G * W], vm[2][G];                            // rows 2c, 2c + 1, 2c + 8, 2c + 9: codes of unit r; of rows r, r + 8 the rest
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const unsigned char* rows = stage + ((t & 1) * 4 + (t >> 1) * 8) * Row::kCodes;            // as value_piece() has row 2c + (t & 1) + 8 (t >> 1)
+      if constexpr (kValueBytes <= 8) shared_words(v[t], rows + 16 * value_piece(2 * c, r * kValueBytes / 16) + r * kValueBytes % 16);
+      else
+#pragma unroll
+        for (int x = 0; x < kValueBytes / 16; ++x) shared_piece(v[t], 4 * x, rows + 16 * value_piece(2 * c, r * (kValueBytes / 16) + x));
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) shared_words(vm[t], stage + kTileCodes + (r + 8 * t) * Row::kMore);
     if (nv < 16) {                                             // a weight of 0 times whatever is there has to be 0
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -413,5 +439,275 @@ struct AttnTileCoded {
       }
   }
 };
+
+// ---- the kernel ---------------------------------------------------------------------------------------------------
+// As paged_attention_kernel, tile by tile, but through a ring in shared memory: 4-bit rows are so short that a tile's arithmetic has to
+// fit 100 cycles of an SM to keep up with memory, and no register is left for the tiles on their way.  Every warp copies its own tiles ahead
+// (cp.async, 16 bytes a lane), p.stages of them at most; it waits for nobody but itself until a segment ends.
+constexpr int kCodedStages = 4;          // tiles of a warp in the ring at most
+
+template <int N>
+__device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Where the tiles of a launch lie: all (sequence, KV head, tile) triples in one list, of which block b takes the b-th equal part.
+// (All tile counts stay below 2^31: see meda_pages_create.)
+template <int HP>
+struct CodedWalk {
+  const AttnParams& p;
+  const int* pre;                        // [n + 1] tiles before sequence i
+  const int* rows_of;                    // [n] rows of sequence i
+  int chunks, H, gap, total, C, base, extra, t0, t1;
+
+  __device__ __forceinline__ CodedWalk(const AttnParams& params, const int* prefix) : p(params), pre(prefix), rows_of(prefix + params.n_seqs + 1) {
+    chunks = (p.group + HP - 1) / HP;
+    H = p.n_heads * chunks;
+    gap = p.n_seqs > 1 ? kAttSegment : 0;
+  }
+  __device__ __forceinline__ int block_start(int b) const { return base * b + div_small(extra * b, C); }
+  __device__ __forceinline__ int block_of(int x) const {
+    int b = min((int)((float)x * ((float)C / (float)total)), C - 1);
+    while (block_start(b) > x) --b;
+    while (b + 1 < C && block_start(b + 1) <= x) ++b;
+    return b;
+  }
+  __device__ __forceinline__ void share() {                    // (see paged_attention_kernel)
+    total = pre[p.n_seqs] * H;
+    const int most = max(p.n_seqs * H, 1), each = most * kAttLeast;
+    C = total == 0 ? 0 : min((int)gridDim.x, total <= (long long)each * gridDim.x ? most * (div_small(total - 1, each) + 1) : (int)gridDim.x);
+    base = C == (int)gridDim.x ? p.grid_div.of(total) : (C > 0 ? div_small(total, C) : 0);
+    extra = total - base * C;
+    const bool has_work = (int)blockIdx.x < C;
+    t0 = has_work ? block_start(blockIdx.x) : 0;
+    t1 = has_work ? block_start(blockIdx.x + 1) : 0;
+  }
+  // Tile x of this block: its first row in the pools, and in the lowest five bits the number of its rows that count (0: nothing to read).
+  __device__ __forceinline__ long long lookup(int x) const {
+    if (x >= t1) return 0;
+    long long row = 0;
+    int nv = 0;
+    const int tile_shift = p.page_shift - 4, page_size = 1 << p.page_shift;
+    const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(x));
+    const int tiles = pre[i + 1] - pre[i];
+    const int local = x - pre[i] * H;
+    const int sh = div_small(local, tiles), tile = local - sh * tiles, g = chunks == 1 ? sh : sh / chunks;
+    if (tile >= tiles - gap) return 0;
+    const int len = rows_of[i];
+    int col = tile >> tile_shift;
+    const int r0 = (tile & ((1 << tile_shift) - 1)) * kAttTile;
+    bool ok = true;
+    if (p.sel) {
+      col = p.sel[((size_t)i * p.n_heads + g) * p.keep + col];
+      ok = col >= 0 && col < (len + page_size - 1) >> p.page_shift;
+    }
+    if (ok) {
+      nv = min(kAttTile, max(0, len - ((col << p.page_shift) + r0)));
+      if (nv > 0) {
+        const int page = p.table[(size_t)i * p.width + col];
+        ok = (unsigned)page < (unsigned)p.n_pages;
+        row = (((long long)page * p.n_heads + g) << p.page_shift) + r0;
+      }
+    }
+    if (!ok) {
+      nv = 0;
+      set_status(p.status, MEDA_ERR_INVALID_ARG);
+    }
+    return row << 5 | nv;
+  }
+};
+
+template <typename Tile, int D, int W>
+__global__ void __launch_bounds__(W * 32, 1)
+coded_attention_kernel(AttnParams p) {
+  using T = typename Tile::T;
+  using Row = typename Tile::Row;
+  constexpr int HP = Tile::kHeads;
+  constexpr int LD = D + 4;
+  begin_grid();
+  extern __shared__ __align__(128) unsigned char coded_smem[];
+  __shared__ int scratch[W + 1];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int page_size = 1 << p.page_shift;
+  unsigned char* ring = coded_smem + (size_t)warp * p.stages * Tile::kStage;           // this warp's tiles
+  float* sm_m = reinterpret_cast<float*>(coded_smem + (size_t)W * p.stages * Tile::kStage);      // [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
+  float* sm_l = sm_m + W * HP;
+  float* sm_o = sm_l + W * HP;
+  int* pre = reinterpret_cast<int*>(sm_m + attn_merge_floats(W, HP, D));
+  CodedWalk<HP> walk(p, pre);
+  ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
+    bool bad = false;
+    const int len = clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad);
+    if (bad && blockIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
+    pre[p.n_seqs + 1 + i] = len;
+    const int tiles = p.sel ? min(p.keep, (len + page_size - 1) >> p.page_shift) << (p.page_shift - 4) : (len + kAttTile - 1) / kAttTile;
+    return tiles ? tiles + walk.gap : 0;
+  });
+  walk.share();
+  const int n_q_heads = p.n_heads * p.group;
+  const int state_heads = min(p.group, HP), state_floats = attn_state_floats(state_heads, D);
+  const int H = walk.H, gap = walk.gap, t0 = walk.t0, t1 = walk.t1;
+
+  // ---- copies.  Tile number i of the warp goes to stage i % p.stages; lane y of `now` has the look-up of the y-th of 32 tiles, the next 32 are
+  // looked up half way through them.  A copy of no rows is an empty group, so that the groups count the tiles.
+  int number = 0, into = 0, x_copy = t0 + warp;
+  uint32_t counts = 0;                                         // rows of the tiles on their way, the last one in the lowest byte
+  long long now = walk.lookup(t0 + (warp + lane * W)), next = 0;
+  auto copy_next = [&] {
+    if (number == 32) {
+      now = next;
+      number = 0;
+    }
+    const long long found = __shfl_sync(0xffffffffu, now, number);
+    const int nv = (int)found & 31;
+    counts = counts << 8 | nv;
+    if (nv > 0) {
+      const long long row = found >> 5;
+      const int in = (int)row & (page_size - 1);
+      const long long page = (row - in) * Row::kBytes;
+      const long long codes = page + in * Row::kCodes + lane * 16, more = page + page_size * Row::kCodes + in * Row::kMore;
+      const uint32_t to = sm100::smem_u32(ring + (size_t)into * Tile::kStage);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const unsigned char* pool = static_cast<const unsigned char*>(half ? p.v : p.k);
+#pragma unroll
+        for (int i = 0; i < Tile::kTileCodes / 512; ++i) {
+          const int piece = lane + 32 * i, y = piece / Tile::kPieces, z = piece % Tile::kPieces;
+          copy16(to + half * Tile::kHalf + 16 * (half ? Tile::value_piece(y, z) : Tile::key_piece(y, z)), pool + codes + i * 512, y < nv);
+        }
+      }
+      const int piece = lane % 16;                             // of the steps and lowest values: the keys' by the first 16 lanes
+      if (piece < Tile::kTileMore / 16)
+        copy16(to + lane / 16 * Tile::kHalf + Tile::kTileCodes + piece * 16, static_cast<const unsigned char*>(lane < 16 ? p.k : p.v) + more + piece * 16,
+               piece * 16 / Row::kMore < nv);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (++into == p.stages) into = 0;
+    if (++number == 16) {
+      x_copy += 32 * W;
+      next = walk.lookup(x_copy + lane * W);
+    }
+  };
+  for (int i = 1; i < p.stages; ++i) copy_next();
+
+  // ---- the segments (sequence, KV head) of this block
+  int seq = 0, sh = 0, seg0 = 0, seg_end = 0;
+  auto segment_end = [&] { seg_end = seg0 < t1 ? min(seg0 + pre[seq + 1] - pre[seq] - gap, t1) : t1; };
+  auto next_segment = [&] {                                    // the next one with tiles
+    seg0 += pre[seq + 1] - pre[seq];
+    if (++sh == H) {
+      sh = 0;
+#pragma unroll 1
+      do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
+    }
+    segment_end();
+  };
+  if (t0 < t1) {
+    seq = ragged_find(pre, p.n_seqs, p.heads_div.of(t0));
+    const int tiles = pre[seq + 1] - pre[seq];
+    sh = div_small(t0 - pre[seq] * H, tiles);
+    seg0 = pre[seq] * H + sh * tiles;
+    segment_end();
+    if (t0 >= seg0 + tiles - gap) next_segment();              // nothing but empty tiles of it here
+  }
+  Tile tile;
+  auto load_q = [&] {
+    const int g = walk.chunks == 1 ? sh : sh / walk.chunks, h0 = (sh - g * walk.chunks) * HP;
+    tile.load_q(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), lane);
+  };
+  if (seg0 < t1) load_q();                                     // (a block may hold nothing but the last segment's empty tiles)
+  tile.reset();
+  int x = t0 + warp, from = 0;
+  bool worked = false;
+  int4 split = make_int4(0, 0, 0, 0);
+#pragma unroll 1
+  while (seg0 < t1) {
+    if (x < seg_end) {
+      __syncwarp();                                            // the stage about to be filled has been read by every lane
+      copy_next();
+      switch (p.stages) {
+        case 4: copies_but<3>(); break;
+        case 3: copies_but<2>(); break;
+        case 2: copies_but<1>(); break;
+        default: copies_but<0>();
+      }
+      __syncwarp();
+      const int nv = counts >> 8 * (p.stages - 1) & 255;
+      if (nv > 0) {
+        const unsigned char* stage = ring + (size_t)from * Tile::kStage;
+        float s[HP / 8][4];
+        tile.logits(s, stage, p.scale_log2, nv, lane);
+        tile.attend(s, stage + Tile::kHalf, nv, lane);
+      }
+      worked = true;
+      if (++from == p.stages) from = 0;
+      x += W;
+      continue;
+    }
+    const int seg1 = seg0 + pre[seq + 1] - pre[seq] - gap, was_seg0 = seg0;
+    const int g = walk.chunks == 1 ? sh : sh / walk.chunks, h0 = (sh - g * walk.chunks) * HP;
+    const int heads = min(HP, p.group - h0);
+    const size_t first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
+    next_segment();
+    if (seg0 < t1) load_q();                                   // the next segment's queries can come already
+
+    // ---- the warps' states of this segment, joined in warp order.  A warp without tiles leaves a maximum of -inf, a sum of 0
+    // and no values; nobody reads those.
+    if (worked) tile.put(sm_m + warp * HP, sm_l + warp * HP, sm_o + warp * HP * LD, LD, heads, lane);
+    else if (lane < HP) {
+      sm_m[warp * HP + lane] = -INFINITY;
+      sm_l[warp * HP + lane] = 0.f;
+    }
+    __syncthreads();
+    tile.reset();
+    worked = false;
+    const bool whole = was_seg0 >= t0 && seg1 <= t1;
+    float* state = p.partial + ((size_t)blockIdx.x * 2 + (was_seg0 < t0 ? 0 : 1)) * state_floats;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
+      const int h = e / (D / 4), d = (e % (D / 4)) * 4;
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * HP + h]);
+      float ll = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int w = 0; w < W; ++w) {
+        const float mw = sm_m[w * HP + h], lw = sm_l[w * HP + h];
+        if (mw != -INFINITY || lw != 0.f) {                  // (a sum that is NaN has a maximum of -inf when all logits are)
+          const float f = exp2_fast(mw - mm);
+          const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * HP + h) * LD + d);
+          ll = fmaf(f, lw, ll);
+          acc.x = fmaf(f, y.x, acc.x);
+          acc.y = fmaf(f, y.y, acc.y);
+          acc.z = fmaf(f, y.z, acc.z);
+          acc.w = fmaf(f, y.w, acc.w);
+        }
+      }
+      if (whole) {
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+        if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
+      } else {
+        *reinterpret_cast<float4*>(state + h * D + d) = acc;
+        if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
+      }
+    }
+    if (was_seg0 >= t0 && seg1 > t1) split = make_int4(walk.block_of(seg1 - 1) - (int)blockIdx.x + 1, (int)first_head, heads, 0);
+    if (seg0 < t1) __syncthreads();                            // before the states are written again
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // sequences without rows
+#pragma unroll 1
+  for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
+    if (pre[i] == pre[i + 1]) {
+#pragma unroll 1
+      for (int e = threadIdx.x; e < n_q_heads * D / 4; e += W * 32)
+        store4<T>(static_cast<T*>(p.out) + (size_t)i * n_q_heads * D + e * 4, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (p.lse)
+#pragma unroll 1
+        for (int h = threadIdx.x; h < n_q_heads; h += W * 32) p.lse[(size_t)i * n_q_heads + h] = -INFINITY;
+    }
+  if (threadIdx.x == 0) p.split[blockIdx.x] = split;
+}
 
 }  // namespace meda

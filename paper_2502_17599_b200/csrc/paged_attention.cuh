@@ -76,6 +76,7 @@ struct AttnParams {
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep;
   float scale_log2;                      // log2(e) / sqrt(head_dim)
   InvariantDiv heads_div, grid_div;      // by the segments of a sequence, by the blocks of the launch
+  int stages = 0;                        // quantised pages: tiles of a warp that the ring holds
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -108,7 +109,7 @@ __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i ==
 template <int D, int NH, int R = 16>
 struct AttnTileBf16 {
   using T = __nv_bfloat16;
-  static constexpr bool kMma = true, kCoded = false;
+  static constexpr bool kMma = true;
   static constexpr int kHeads = 8 * NH;
   static constexpr int KC = D / 32, VC = D / 64, KT = R / 8, kRows = R;
   uint4 q[NH][KC];
@@ -279,7 +280,7 @@ struct AttnTileBf16 {
 template <int D, int GP>
 struct AttnTileF32 {
   using T = float;
-  static constexpr bool kMma = false, kCoded = false;
+  static constexpr bool kMma = false;
   static constexpr int kHeads = GP;
   static constexpr int E = D / 32, B = 4;
   static constexpr int P = GP * B <= 8 ? 8 : (GP * B <= 16 ? 16 : 32);
@@ -560,12 +561,6 @@ paged_attention_kernel(AttnParams p) {
         if (b < nv) tile.attend(s, b, nv, lane);
         if (r0 < n) tile.load_v(vp + (last ? row_after : row) * D, r0, n, lane);
       }
-    } else if constexpr (Tile::kCoded) {
-      float s[HP / 8][4];
-      if (nv > 0) tile.logits(s, p.scale_log2, nv, lane);
-      if (nv_after > 0) tile.load_k(p.k, row_after, page_size, nv_after, lane);
-      if (nv > 0) tile.attend(s, nv, lane);
-      if (nv_after > 0) tile.load_v(p.v, row_after, page_size, nv_after, lane);
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
