@@ -88,27 +88,30 @@ __device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from, b
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(live ? 16 : 0) : "memory");
 }
 
-// T = type of queries and outputs, D = head_dim, NH = groups of eight query heads.
-template <typename TOUT, int D, int NH, int BITS>
+// T = type of queries and outputs, D = head_dim, NH = groups of eight query heads, SUB = runs of sixteen rows in a tile (each lies in one page).
+template <typename TOUT, int D, int NH, int BITS, int SUBS>
 struct AttnTileCoded {
   using T = TOUT;
   using Row = CodedRow<D, BITS>;
+  static constexpr int SUB = SUBS;
   static constexpr int kHeads = 8 * NH;
   static constexpr int G = Row::kGroups, W = BITS / 4;           // groups, words per unit
-  static constexpr int kTileCodes = kAttTile * Row::kCodes, kTileMore = kAttTile * Row::kMore;
-  static constexpr int kHalf = kTileCodes + kTileMore, kStage = 2 * kHalf;       // bytes of a tile of keys or values, of both
+  static constexpr int kRunCodes = 16 * Row::kCodes, kRunMore = 16 * Row::kMore;
+  static constexpr int kHalf = kRunCodes + kRunMore;             // bytes of a run's keys or values
+  static constexpr int kStage = 2 * SUB * kHalf;                 // of a tile: keys and values of every run
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
   static constexpr int kScale = PARTS == 2 ? 13 : 5;             // weights reach 2^(kScale + 1) (times 2^kSlack)
   static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference may stay this far (log2) behind the maximum
 
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
   uint32_t qsum[NH][2];                  // sums over the groups, in bf16 parts
-  float unscale[NH][2];                  // 2^-k of the scaled queries, of the lane's two heads
+  float factor[NH][2];                   // from products of codes and scaled queries to logits (log2), of the lane's two heads
   float o[G][4][NH][4];
   float low_sum[NH][2][G];               // sum of p low
-  float m[NH][2], l[NH][2];
-  float step_top;                        // steps below this fit the weights' scale
-  int step_exp;                          // which is 2^(kScale - step_exp), 2^125 at most
+  float l[NH][2];                        // sum of p = 2^(logit - reference)
+  float ref[NH][2], limit[NH][2];        // reference; what a product may reach before the reference has to move (-inf: there is none yet)
+  float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
+  int step_exp;                          // of the largest step so far (kScale - 125 at least)
 
   // Pair j of a unit's eight codes, as the two halves of a word: elements (first, second).
   __device__ __forceinline__ static constexpr int pair_first(int j) { return BITS == 4 ? j : (j / 2) * 4 + j % 2; }
@@ -126,7 +129,7 @@ struct AttnTileCoded {
     else return __uint_as_float(g % 2 == 0 ? w[G / 2 + g / 2] << 16 : w[G / 2 + g / 2] & 0xffff0000u);
   }
 
-  __device__ __forceinline__ void load_q(const T* qh, int heads, int lane) {     // qh: the segment's first query head
+  __device__ __forceinline__ void load_q(const T* qh, int heads, float scale_log2, int lane) {     // qh: the segment's first query head
     const int r = lane / 4, c = lane % 4;
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
@@ -185,9 +188,9 @@ struct AttnTileCoded {
         qsum[n][0] = c == 0 ? hi : c == 1 ? lo : 0u;
         qsum[n][1] = c == 0 ? mid : 0u;
       }
-      const float back = scale == scale ? power_of_two(-k2) : NAN;
-      unscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * c);                     // head 2c is lane 4 * 2c's
-      unscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
+      const float back = scale == scale ? power_of_two(-k2) * (scale_log2 * 16777216.f) : NAN;       // 2^24: the codes' own scale
+      factor[n][0] = __shfl_sync(0xffffffffu, back, 8 * c);                      // head 2c is lane 4 * 2c's
+      factor[n][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
     }
   }
   __device__ __forceinline__ void reset() {
@@ -195,7 +198,8 @@ struct AttnTileCoded {
     for (int n = 0; n < NH; ++n)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        m[n][x] = -INFINITY;
+        ref[n][x] = 0.f;
+        limit[n][x] = -INFINITY;
         l[n][x] = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) low_sum[n][x][g] = 0.f;
@@ -210,8 +214,9 @@ struct AttnTileCoded {
           for (int e = 0; e < 4; ++e) o[g][t][n][e] = 0.f;
     step_top = 0.f;
     step_exp = kScale - 125;
+    weight = power_of_two(125);
   }
-  // A tile in shared memory: 16-byte pieces of its codes, then its steps and lowest values; keys first, then values.  The pieces are moved inside
+  // A run of rows in shared memory: 16-byte pieces of its codes, then its steps and lowest values.  The pieces are moved inside
   // a row, and the values' rows are sorted even ones first in each eight, so that the lanes that read together meet different banks.
   static constexpr int kPieces = Row::kCodes / 16;               // of a row
   static constexpr int kKeyBytes = 2 * G * BITS, kValueBytes = G * BITS;         // a lane reads of a row
@@ -225,8 +230,8 @@ struct AttnTileCoded {
     return at * kPieces + (piece ^ moved);
   }
 
-  // Logits in the log2 domain of the keys at `stage`, of which nv rows count: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
-  __device__ __forceinline__ void logits(float (&s)[NH][4], const unsigned char* stage, float scale_log2, int nv, int lane) {
+  // Logits over `factor` of the keys at `stage`, a run of which nv rows count: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
+  __device__ __forceinline__ void logits(float (&s)[NH][4], const unsigned char* stage, int nv, int lane) {
     const int r = lane / 4, c = lane % 4;
     uint32_t k[2][2 * G * W], km[2][G];                        // rows r, r + 8: codes of units 2c, 2c + 1; steps and lowest values
 #pragma unroll
@@ -236,7 +241,7 @@ struct AttnTileCoded {
 #pragma unroll
         for (int x = 0; x < kKeyBytes / 16; ++x)
           shared_piece(k[t], 4 * x, stage + 8 * t * Row::kCodes + 16 * key_piece(r, c * (kKeyBytes / 16) + x));
-      shared_words(km[t], stage + kTileCodes + (r + 8 * t) * Row::kMore);
+      shared_words(km[t], stage + kRunCodes + (r + 8 * t) * Row::kMore);
     }
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
@@ -273,11 +278,6 @@ struct AttnTileCoded {
         s[n][3] = fmaf(s1, acc[n][3], s[n][3]);
       }
     }
-    const float back = scale_log2 * 16777216.f;                                  // 2^24 (in two steps: 2^-k alone may fill fp32's range)
-#pragma unroll
-    for (int n = 0; n < NH; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = s[n][e] * back * unscale[n][e & 1];
     if (nv < 16) {
 #pragma unroll
       for (int n = 0; n < NH; ++n)
@@ -286,10 +286,81 @@ struct AttnTileCoded {
           if (r + (e >> 1) * 8 >= nv) s[n][e] = -INFINITY;
     }
   }
-  // The values at `stage`, weighed.
-  __device__ __forceinline__ void attend(const float (&s)[NH][4], const unsigned char* stage, int nv, int lane) {
+  // The tile at `stage`, of whose runs nv[] rows count.
+  __device__ __forceinline__ void work(const unsigned char* stage, const int (&nv)[SUB], int lane) {
+    const int r = lane / 4;
+    float s[SUB][NH][4];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) logits(s[u], stage + 2 * u * kHalf, nv[u], lane);
+    uint32_t vm[SUB][2][G];                                    // steps and lowest values of the values' rows r, r + 8
+    float top = 0.f;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) shared_words(vm[u][t], stage + (2 * u + 1) * kHalf + kRunCodes + (r + 8 * t) * Row::kMore);
+      if (nv[u] < 16) {                                        // a weight of 0 times whatever is there has to be 0
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (r + 8 * t >= nv[u])
+#pragma unroll
+            for (int g = 0; g < G; ++g) vm[u][t][g] = 0u;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int g = 0; g < G; ++g) top = fmaxf(top, step_of(vm[u][t], g));
+    }
+    bool moved = top >= step_top;
+#pragma unroll
+    for (int n = 0; n < NH; ++n)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
+        if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
+        moved |= most > limit[n][x];
+      }
+    if (__any_sync(0xffffffffu, moved)) {                      // a new reference, or larger values than before: bring the sums to them
+#pragma unroll
+      for (int y = 1; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+      const int to = max(step_exp, (int)(__float_as_uint(top) >> 23) - 127);
+      const float smaller = step_exp - to < -126 ? 0.f : power_of_two(step_exp - to);
+      step_exp = to;
+      step_top = to == 127 ? INFINITY : power_of_two(to + 1);
+      weight = power_of_two(kScale - to);
+#pragma unroll
+      for (int n = 0; n < NH; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
+          if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
+          most *= factor[n][x];
+#pragma unroll
+          for (int y = 4; y < 32; y <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, y));
+          const bool none = limit[n][x] == -INFINITY;
+          most = none ? most : fmaxf(most, ref[n][x]);
+          const float to_ref = most == -INFINITY ? 0.f : most;
+          const float f = none ? 0.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
+          limit[n][x] = most == -INFINITY ? -INFINITY : (most + kSlack) / factor[n][x];
+          ref[n][x] = to_ref;
+          l[n][x] = none ? l[n][x] : l[n][x] * f;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            low_sum[n][x][g] = none ? low_sum[n][x][g] : low_sum[n][x][g] * f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              o[g][t][n][x] = none ? o[g][t][n][x] : o[g][t][n][x] * (f * smaller);
+              o[g][t][n][2 + x] = none ? o[g][t][n][2 + x] : o[g][t][n][2 + x] * (f * smaller);
+            }
+          }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) attend(s[u], vm[u], stage + (2 * u + 1) * kHalf, lane);
+  }
+  // The values of a run, weighed.
+  __device__ __forceinline__ void attend(const float (&s)[NH][4], const uint32_t (&vm)[2][G], const unsigned char* stage, int lane) {
     const int r = lane / 4, c = lane % 4;
-    uint32_t v[4][G * W], vm[2][G];                            // rows 2c, 2c + 1, 2c + 8, 2c + 9: codes of unit r; of rows r, r + 8 the rest
+    uint32_t v[4][G * W];                                      // rows 2c, 2c + 1, 2c + 8, 2c + 9: codes of unit r
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const unsigned char* rows = stage + ((t & 1) * 4 + (t >> 1) * 8) * Row::kCodes;            // as value_piece() has row 2c + (t & 1) + 8 (t >> 1)
@@ -298,64 +369,12 @@ struct AttnTileCoded {
 #pragma unroll
         for (int x = 0; x < kValueBytes / 16; ++x) shared_piece(v[t], 4 * x, rows + 16 * value_piece(2 * c, r * (kValueBytes / 16) + x));
     }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) shared_words(vm[t], stage + kTileCodes + (r + 8 * t) * Row::kMore);
-    if (nv < 16) {                                             // a weight of 0 times whatever is there has to be 0
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (r + 8 * t >= nv)
-#pragma unroll
-          for (int g = 0; g < G; ++g) vm[t][g] = 0u;
-    }
-    float step[2][G], top = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        step[t][g] = step_of(vm[t], g);
-        top = fmaxf(top, step[t][g]);
-      }
-    bool moved = top >= step_top;
-#pragma unroll
-    for (int n = 0; n < NH; ++n)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) moved |= fmaxf(s[n][x], s[n][2 + x]) > m[n][x] + kSlack;
-    if (__any_sync(0xffffffffu, moved)) {                      // a new reference, or larger values than before: bring the sums to them
-#pragma unroll
-      for (int y = 1; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-      const int to = max(step_exp, (int)(__float_as_uint(top) >> 23) - 127);
-      const float smaller = step_exp - to < -126 ? 0.f : power_of_two(step_exp - to);
-      step_exp = to;
-      step_top = to == 127 ? INFINITY : power_of_two(to + 1);
-#pragma unroll
-      for (int n = 0; n < NH; ++n)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float mn = fmaxf(s[n][x], s[n][2 + x]);
-#pragma unroll
-          for (int y = 4; y < 32; y <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, y));
-          mn = fmaxf(mn, m[n][x]);
-          const float f = exp2_fast(m[n][x] - (mn == -INFINITY ? 0.f : mn));
-          m[n][x] = mn;
-          l[n][x] *= f;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            low_sum[n][x][g] *= f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              o[g][t][n][x] *= f * smaller;
-              o[g][t][n][2 + x] *= f * smaller;
-            }
-          }
-        }
-    }
-    const float weight = power_of_two(kScale - step_exp);      // step_exp >= kScale - 125
     uint32_t b[NH][PARTS][G][2];
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
       float p[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = exp2_fast(s[n][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
+      for (int e = 0; e < 4; ++e) p[e] = exp2_fast(fmaf(s[n][e], factor[n][e & 1], -ref[n][e & 1]));
       l[n][0] += p[0] + p[2];
       l[n][1] += p[1] + p[3];
 #pragma unroll
@@ -365,7 +384,7 @@ struct AttnTileCoded {
         for (int x = 0; x < 2; ++x) low_sum[n][x][g] = fmaf(p[2 + x], low1, fmaf(p[x], low0, low_sum[n][x][g]));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const float f = step[t][g] * weight, w0 = p[2 * t] * f, w1 = p[2 * t + 1] * f;
+          const float f = step_of(vm[t], g) * weight, w0 = p[2 * t] * f, w1 = p[2 * t + 1] * f;
           const uint32_t hi = halves(w0, w1);
           b[n][0][g][t] = transpose8(hi);
           if constexpr (PARTS == 2) b[n][PARTS - 1][g][t] = transpose8(halves(w0 - half_low(hi), w1 - half_high(hi)));
@@ -423,7 +442,7 @@ struct AttnTileCoded {
           for (int y = 4; y < 32; y <<= 1) low[g] += __shfl_xor_sync(0xffffffffu, low[g], y);
         }
         if (r == 0) {
-          sm[h] = m[n][x];
+          sm[h] = limit[n][x] == -INFINITY ? -INFINITY : ref[n][x];
           sl[h] = sum;
         }
         if (h < heads) {
@@ -443,25 +462,34 @@ struct AttnTileCoded {
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 // As paged_attention_kernel, tile by tile, but through a ring in shared memory: 4-bit rows are so short that a tile's arithmetic has to
 // fit 100 cycles of an SM to keep up with memory, and no register is left for the tiles on their way.  Every warp copies its own tiles ahead
-// (cp.async, 16 bytes a lane), p.stages of them at most; it waits for nobody but itself until a segment ends.
-constexpr int kCodedStages = 4;          // tiles of a warp in the ring at most
+// (cp.async, 16 bytes a lane) and waits for nobody but itself until a segment ends.
+// Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
+// kAttLeast but in rows.
+constexpr int kCodedSegment = 320, kCodedLeast = 128;
 
 template <int N>
 __device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Where the tiles of a launch lie: all (sequence, KV head, tile) triples in one list, of which block b takes the b-th equal part.
 // (All tile counts stay below 2^31: see meda_pages_create.)
-template <int HP>
+template <typename Tile>
 struct CodedWalk {
+  using Row = typename Tile::Row;
+  static constexpr int HP = Tile::kHeads, SUB = Tile::SUB, kRows = 16 * SUB;
   const AttnParams& p;
   const int* pre;                        // [n + 1] tiles before sequence i
-  const int* rows_of;                    // [n] rows of sequence i
   int chunks, H, gap, total, C, base, extra, t0, t1;
 
-  __device__ __forceinline__ CodedWalk(const AttnParams& params, const int* prefix) : p(params), pre(prefix), rows_of(prefix + params.n_seqs + 1) {
+  __device__ __forceinline__ CodedWalk(const AttnParams& params, const int* prefix) : p(params), pre(prefix) {
     chunks = (p.group + HP - 1) / HP;
     H = p.n_heads * chunks;
-    gap = p.n_seqs > 1 ? kAttSegment : 0;
+    gap = p.n_seqs > 1 ? kCodedSegment / kRows : 0;
+  }
+  __device__ __forceinline__ int length(int i, bool& bad) const { return clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad); }
+  // Runs of sixteen rows of a sequence that are attended to.
+  __device__ __forceinline__ int runs(int len) const {
+    const int per_page = p.page_shift - 4, pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+    return p.sel ? min(p.keep, pages) << per_page : (len + 15) / 16;
   }
   __device__ __forceinline__ int block_start(int b) const { return base * b + div_small(extra * b, C); }
   __device__ __forceinline__ int block_of(int x) const {
@@ -472,7 +500,7 @@ struct CodedWalk {
   }
   __device__ __forceinline__ void share() {                    // (see paged_attention_kernel)
     total = pre[p.n_seqs] * H;
-    const int most = max(p.n_seqs * H, 1), each = most * kAttLeast;
+    const int most = max(p.n_seqs * H, 1), each = most * (kCodedLeast / kRows);
     C = total == 0 ? 0 : min((int)gridDim.x, total <= (long long)each * gridDim.x ? most * (div_small(total - 1, each) + 1) : (int)gridDim.x);
     base = C == (int)gridDim.x ? p.grid_div.of(total) : (C > 0 ? div_small(total, C) : 0);
     extra = total - base * C;
@@ -480,65 +508,70 @@ struct CodedWalk {
     t0 = has_work ? block_start(blockIdx.x) : 0;
     t1 = has_work ? block_start(blockIdx.x + 1) : 0;
   }
-  // Tile x of this block: its first row in the pools, and in the lowest five bits the number of its rows that count (0: nothing to read).
-  __device__ __forceinline__ long long lookup(int x) const {
-    if (x >= t1) return 0;
-    long long row = 0;
-    int nv = 0;
-    const int tile_shift = p.page_shift - 4, page_size = 1 << p.page_shift;
+  // The runs of tile x of this block: where their codes begin in the pools, in units of 64 bytes, and (how far behind them their steps and lowest
+  // values are) * 32 + rows that count (0: nothing to read).
+  __device__ __forceinline__ void lookup(int x, unsigned (&at)[SUB], unsigned (&more)[SUB]) const {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) at[u] = more[u] = 0;
+    if (x >= t1) return;
+    const int per_page = p.page_shift - 4, page_size = 1 << p.page_shift;
     const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(x));
     const int tiles = pre[i + 1] - pre[i];
     const int local = x - pre[i] * H;
     const int sh = div_small(local, tiles), tile = local - sh * tiles, g = chunks == 1 ? sh : sh / chunks;
-    if (tile >= tiles - gap) return 0;
-    const int len = rows_of[i];
-    int col = tile >> tile_shift;
-    const int r0 = (tile & ((1 << tile_shift) - 1)) * kAttTile;
-    bool ok = true;
-    if (p.sel) {
-      col = p.sel[((size_t)i * p.n_heads + g) * p.keep + col];
-      ok = col >= 0 && col < (len + page_size - 1) >> p.page_shift;
-    }
-    if (ok) {
-      nv = min(kAttTile, max(0, len - ((col << p.page_shift) + r0)));
-      if (nv > 0) {
-        const int page = p.table[(size_t)i * p.width + col];
-        ok = (unsigned)page < (unsigned)p.n_pages;
-        row = (((long long)page * p.n_heads + g) << p.page_shift) + r0;
+    if (tile >= tiles - gap) return;
+    bool bad = false;
+    const int len = length(i, bad);
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int run = tile * SUB + u;
+      if (run >= runs(len)) break;
+      int col = run >> per_page;
+      const int r0 = (run & ((1 << per_page) - 1)) * 16;
+      bool ok = true;
+      if (p.sel) {
+        col = p.sel[((size_t)i * p.n_heads + g) * p.keep + col];
+        ok = col >= 0 && col < (len + page_size - 1) >> p.page_shift;
       }
+      if (ok) {
+        const int nv = min(16, max(0, len - ((col << p.page_shift) + r0)));
+        if (nv > 0) {
+          const int page = p.table[(size_t)i * p.width + col];
+          ok = (unsigned)page < (unsigned)p.n_pages;
+          if (ok) {
+            at[u] = (unsigned)(((((long long)page * p.n_heads + g) << p.page_shift) * Row::kBytes + r0 * Row::kCodes) / 64);
+            more[u] = (unsigned)(page_size * Row::kCodes - r0 * (Row::kCodes - Row::kMore)) << 5 | nv;
+          }
+        }
+      }
+      if (!ok) set_status(p.status, MEDA_ERR_INVALID_ARG);
     }
-    if (!ok) {
-      nv = 0;
-      set_status(p.status, MEDA_ERR_INVALID_ARG);
-    }
-    return row << 5 | nv;
   }
 };
 
-template <typename Tile, int D, int W>
+// S = tiles of a warp in the ring.
+template <typename Tile, int D, int W, int S>
 __global__ void __launch_bounds__(W * 32, 1)
 coded_attention_kernel(AttnParams p) {
   using T = typename Tile::T;
   using Row = typename Tile::Row;
-  constexpr int HP = Tile::kHeads;
+  constexpr int HP = Tile::kHeads, SUB = Tile::SUB;
   constexpr int LD = D + 4;
   begin_grid();
   extern __shared__ __align__(128) unsigned char coded_smem[];
   __shared__ int scratch[W + 1];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int page_size = 1 << p.page_shift;
-  unsigned char* ring = coded_smem + (size_t)warp * p.stages * Tile::kStage;           // this warp's tiles
-  float* sm_m = reinterpret_cast<float*>(coded_smem + (size_t)W * p.stages * Tile::kStage);      // [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
+  unsigned char* ring = coded_smem + warp * (S * Tile::kStage);                        // this warp's tiles
+  float* sm_m = reinterpret_cast<float*>(coded_smem + W * S * Tile::kStage);           // [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
   float* sm_l = sm_m + W * HP;
   float* sm_o = sm_l + W * HP;
   int* pre = reinterpret_cast<int*>(sm_m + attn_merge_floats(W, HP, D));
-  CodedWalk<HP> walk(p, pre);
+  CodedWalk<Tile> walk(p, pre);
   ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;
-    const int len = clamped_len(p.lens, p.lens_stride, i, p.width << p.page_shift, bad);
+    const int len = walk.length(i, bad);
     if (bad && blockIdx.x == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
-    pre[p.n_seqs + 1 + i] = len;
-    const int tiles = p.sel ? min(p.keep, (len + page_size - 1) >> p.page_shift) << (p.page_shift - 4) : (len + kAttTile - 1) / kAttTile;
+    const int tiles = (walk.runs(len) + SUB - 1) / SUB;
     return tiles ? tiles + walk.gap : 0;
   });
   walk.share();
@@ -546,47 +579,58 @@ coded_attention_kernel(AttnParams p) {
   const int state_heads = min(p.group, HP), state_floats = attn_state_floats(state_heads, D);
   const int H = walk.H, gap = walk.gap, t0 = walk.t0, t1 = walk.t1;
 
-  // ---- copies.  Tile number i of the warp goes to stage i % p.stages; lane y of `now` has the look-up of the y-th of 32 tiles, the next 32 are
+  // ---- copies.  Tile number i of the warp goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles, the next 32 are
   // looked up half way through them.  A copy of no rows is an empty group, so that the groups count the tiles.
   int number = 0, into = 0, x_copy = t0 + warp;
-  uint32_t counts = 0;                                         // rows of the tiles on their way, the last one in the lowest byte
-  long long now = walk.lookup(t0 + (warp + lane * W)), next = 0;
+  uint32_t counts = 0;                                         // rows of the runs on their way, 5 bits each, the last ones lowest
+  unsigned at_now[SUB], more_now[SUB], at_next[SUB], more_next[SUB];
+  walk.lookup(x_copy + lane * W, at_now, more_now);
+#pragma unroll
+  for (int u = 0; u < SUB; ++u) at_next[u] = more_next[u] = 0;
+  const unsigned char *k_lane = static_cast<const unsigned char*>(p.k) + lane * 16, *v_lane = static_cast<const unsigned char*>(p.v) + lane * 16;
+  constexpr int kMorePieces = Tile::kRunMore / 16;             // of a run of keys or values
   auto copy_next = [&] {
     if (number == 32) {
-      now = next;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        at_now[u] = at_next[u];
+        more_now[u] = more_next[u];
+      }
       number = 0;
     }
-    const long long found = __shfl_sync(0xffffffffu, now, number);
-    const int nv = (int)found & 31;
-    counts = counts << 8 | nv;
-    if (nv > 0) {
-      const long long row = found >> 5;
-      const int in = (int)row & (page_size - 1);
-      const long long page = (row - in) * Row::kBytes;
-      const long long codes = page + in * Row::kCodes + lane * 16, more = page + page_size * Row::kCodes + in * Row::kMore;
-      const uint32_t to = sm100::smem_u32(ring + (size_t)into * Tile::kStage);
+    const uint32_t to = sm100::smem_u32(ring) + into * Tile::kStage;
+    unsigned at[SUB], more[SUB];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const unsigned char* pool = static_cast<const unsigned char*>(half ? p.v : p.k);
+    for (int u = 0; u < SUB; ++u) {
+      at[u] = __shfl_sync(0xffffffffu, at_now[u], number);
+      more[u] = __shfl_sync(0xffffffffu, more_now[u], number);
+      const int nv = more[u] & 31;
+      counts = counts << 5 | nv;
+      const unsigned char *k = k_lane + (size_t)at[u] * 64, *v = v_lane + (size_t)at[u] * 64;
 #pragma unroll
-        for (int i = 0; i < Tile::kTileCodes / 512; ++i) {
-          const int piece = lane + 32 * i, y = piece / Tile::kPieces, z = piece % Tile::kPieces;
-          copy16(to + half * Tile::kHalf + 16 * (half ? Tile::value_piece(y, z) : Tile::key_piece(y, z)), pool + codes + i * 512, y < nv);
-        }
+      for (int i = 0; i < Tile::kRunCodes / 512; ++i) {
+        const int piece = lane + 32 * i, y = piece / Tile::kPieces, z = piece % Tile::kPieces;
+        copy16(to + 2 * u * Tile::kHalf + 16 * Tile::key_piece(y, z), k + i * 512, y < nv);
+        copy16(to + (2 * u + 1) * Tile::kHalf + 16 * Tile::value_piece(y, z), v + i * 512, y < nv);
       }
-      const int piece = lane % 16;                             // of the steps and lowest values: the keys' by the first 16 lanes
-      if (piece < Tile::kTileMore / 16)
-        copy16(to + lane / 16 * Tile::kHalf + Tile::kTileCodes + piece * 16, static_cast<const unsigned char*>(lane < 16 ? p.k : p.v) + more + piece * 16,
-               piece * 16 / Row::kMore < nv);
+    }
+    // steps and lowest values: keys and values of all runs side by side on the lanes
+#pragma unroll
+    for (int i = 0; i < (2 * SUB * kMorePieces + 31) / 32; ++i) {
+      const int e = lane + 32 * i, half = e / kMorePieces, piece = e % kMorePieces, u = SUB == 2 ? half >> 1 : 0;
+      const unsigned at_u = u ? at[SUB - 1] : at[0], more_u = u ? more[SUB - 1] : more[0];
+      const unsigned char* from = static_cast<const unsigned char*>(half & 1 ? p.v : p.k) + (size_t)at_u * 64 + (more_u >> 5) + piece * 16;
+      if (half < 2 * SUB) copy16(to + half * Tile::kHalf + Tile::kRunCodes + piece * 16, from, piece * 16 / Row::kMore < (more_u & 31));
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    if (++into == p.stages) into = 0;
+    into = into + 1 == S ? 0 : into + 1;
     if (++number == 16) {
       x_copy += 32 * W;
-      next = walk.lookup(x_copy + lane * W);
+      walk.lookup(x_copy + lane * W, at_next, more_next);
     }
   };
-  for (int i = 1; i < p.stages; ++i) copy_next();
+#pragma unroll 1
+  for (int i = 1; i < S; ++i) copy_next();
 
   // ---- the segments (sequence, KV head) of this block
   int seq = 0, sh = 0, seg0 = 0, seg_end = 0;
@@ -611,7 +655,7 @@ coded_attention_kernel(AttnParams p) {
   Tile tile;
   auto load_q = [&] {
     const int g = walk.chunks == 1 ? sh : sh / walk.chunks, h0 = (sh - g * walk.chunks) * HP;
-    tile.load_q(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), lane);
+    tile.load_q(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), p.scale_log2, lane);
   };
   if (seg0 < t1) load_q();                                     // (a block may hold nothing but the last segment's empty tiles)
   tile.reset();
@@ -623,22 +667,17 @@ coded_attention_kernel(AttnParams p) {
     if (x < seg_end) {
       __syncwarp();                                            // the stage about to be filled has been read by every lane
       copy_next();
-      switch (p.stages) {
-        case 4: copies_but<3>(); break;
-        case 3: copies_but<2>(); break;
-        case 2: copies_but<1>(); break;
-        default: copies_but<0>();
-      }
+      copies_but<S - 1>();
       __syncwarp();
-      const int nv = counts >> 8 * (p.stages - 1) & 255;
-      if (nv > 0) {
-        const unsigned char* stage = ring + (size_t)from * Tile::kStage;
-        float s[HP / 8][4];
-        tile.logits(s, stage, p.scale_log2, nv, lane);
-        tile.attend(s, stage + Tile::kHalf, nv, lane);
+      int nv[SUB], any = 0;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
+        any |= nv[u];
       }
+      if (any) tile.work(ring + from * Tile::kStage, nv, lane);
       worked = true;
-      if (++from == p.stages) from = 0;
+      from = from + 1 == S ? 0 : from + 1;
       x += W;
       continue;
     }

@@ -76,7 +76,6 @@ struct AttnParams {
   int lens_stride, n_seqs, n_heads, group, n_pages, width, page_shift, keep;
   float scale_log2;                      // log2(e) / sqrt(head_dim)
   InvariantDiv heads_div, grid_div;      // by the segments of a sequence, by the blocks of the launch
-  int stages = 0;                        // quantised pages: tiles of a warp that the ring holds
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,

@@ -107,27 +107,35 @@ struct AttnKernel {
   }
 };
 
-// Over quantised pages.  The ring gets what shared memory the batch's prefix sums and the warps' states leave.
-template <typename Tile, int D, int W>
+// Over quantised pages.  W warps with S tiles each in the ring; with more sequences than leave room for that, one.
+template <typename Tile, int D, int W, int S>
 struct CodedAttnKernel {
-  static constexpr auto kernel = coded_attention_kernel<Tile, D, W>;
-  static size_t fixed_smem(int n_seqs) { return (size_t)(attn_prefix_floats(n_seqs) + attn_merge_floats(W, Tile::kHeads, D)) * 4; }
-  static int stages(int n_seqs) {
-    return (int)std::min<int64_t>(kCodedStages, ((int64_t)kMaxDynSmem - 1024 - (int64_t)fixed_smem(n_seqs)) / (W * Tile::kStage));
+  static constexpr size_t smem(int n_seqs, int stages) {
+    return (size_t)W * stages * Tile::kStage + (size_t)attn_merge_floats(W, Tile::kHeads, D) * 4 + (size_t)(n_seqs + 1) * 4;
   }
+  static constexpr size_t kRoom = kMaxDynSmem - 1024;
+  static constexpr bool kAlways = smem(kPagesMaxSeqs, S) <= kRoom;
+  static_assert(smem(kPagesMaxSeqs, 1) <= kRoom, "the largest batch has to fit");
   static meda_status prepare(meda_pages* p) {
-    if (stages(p->cfg.max_seqs) < 1) return MEDA_ERR_SHAPE;
     const int64_t segments = (int64_t)p->cfg.n_kv_heads * ((p->group + Tile::kHeads - 1) / Tile::kHeads);     // (as AttnKernel)
     if (segments * p->cfg.max_seqs * ((int64_t)p->cfg.max_seq_pages * (p->cfg.page_size / kAttTile) + kAttSegment) >= (int64_t(1) << 31) - 65536)
       return MEDA_ERR_SHAPE;
     p->attn_blocks = p->sm_count;
-    return raise_once<kernel>();
+    meda_status r = raise_once<coded_attention_kernel<Tile, D, W, S>>();
+    if constexpr (!kAlways)
+      if (r == MEDA_OK) r = raise_once<coded_attention_kernel<Tile, D, W, 1>>();
+    return r;
   }
   static meda_status launch(meda_pages* p, AttnParams a, cudaStream_t st) {
     a.heads_div.set((unsigned)(a.n_heads * ((a.group + Tile::kHeads - 1) / Tile::kHeads)));
     a.grid_div.set((unsigned)p->attn_blocks);
-    a.stages = stages(a.n_seqs);
-    const meda_status r = launch_after(p, kernel, p->attn_blocks, W * 32, (size_t)W * a.stages * Tile::kStage + fixed_smem(a.n_seqs), st, a);
+    meda_status r;
+    if constexpr (kAlways) {
+      r = launch_after(p, coded_attention_kernel<Tile, D, W, S>, p->attn_blocks, W * 32, smem(a.n_seqs, S), st, a);
+    } else {
+      r = smem(a.n_seqs, S) <= kRoom ? launch_after(p, coded_attention_kernel<Tile, D, W, S>, p->attn_blocks, W * 32, smem(a.n_seqs, S), st, a)
+                                     : launch_after(p, coded_attention_kernel<Tile, D, W, 1>, p->attn_blocks, W * 32, smem(a.n_seqs, 1), st, a);
+    }
     if (r != MEDA_OK) return r;
     return launch_after(p, join_attention_kernel<typename Tile::T, D>, dim3(p->attn_blocks, std::min(a.group, Tile::kHeads)), kAttJoinThreads,
                         0, st, a);
@@ -138,12 +146,13 @@ template <typename T, int BITS, typename F>
 meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
   constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int kSub = BITS == 4 ? 2 : 1;
   if (d == 64)
-    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, BITS>, 64, 16>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, BITS>, 64, kF32 ? 12 : 16>());
+    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, BITS, kSub>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, BITS, kSub>, 64, kF32 ? 12 : 16, 3>());
   if (d == 128)
-    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS>, 128, kF32 || BITS == 8 ? 12 : 16>())
-                  : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS>, 128, kF32 ? 8 : 12>());
-  return f(CodedAttnKernel<AttnTileCoded<T, 256, 1, BITS>, 256, 8>());
+    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS, kSub>, 128, kF32 || BITS == 8 ? 12 : 16, 2>())
+                  : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS, kSub>, 128, 8, 3>());
+  return f(CodedAttnKernel<AttnTileCoded<T, 256, 1, BITS, 1>, 256, 8, BITS == 4 ? 3 : 2>());
 }
 
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
