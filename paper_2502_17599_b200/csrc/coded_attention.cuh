@@ -138,12 +138,16 @@ struct AttnTileCoded {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) {
+          Eight<T> w;
+          w.load(qh + (h < heads ? h : 0) * D + g * 64 + (2 * c + i) * 8);
+          w.floats(x[i][g]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            x[i][g][e] = h < heads ? to_f32<T>(qh[(size_t)h * D + g * 64 + (2 * c + i) * 8 + e]) : 0.f;
+            if (h >= heads) x[i][g][e] = 0.f;
             top = fmaxf(top, fabsf(x[i][g][e]));
           }
+        }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int k2 = min(126, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
@@ -423,8 +427,10 @@ struct AttnTileCoded {
             for (int x = 0; x < PARTS; ++x) mma_f16(o[g][2 * y + z][n], a[z][0], a[z][1], a[z][2], a[z][3], b[n][x][g][0], b[n][x][g][1]);
       }
   }
-  // state to shared memory: sm [kHeads], sl [kHeads], so [kHeads][ld]
-  __device__ __forceinline__ void put(float* sm, float* sl, float* so, int ld, int heads, int lane) {
+  // The sums of every lane's two heads: l and the lowest values' share over all rows, then f(head, its l, its reference, values of unit r of
+  // group g as 2^24 o + low) for heads below `heads`.  (A state without a reference has -inf.)
+  template <typename F>
+  __device__ __forceinline__ void finish(int heads, int lane, F f) {
     const int r = lane / 4, c = lane % 4;
     const float a = power_of_two(24 - kScale), e = power_of_two(step_exp), odd = BITS == 4 ? 0.0625f * a : a;
 #pragma unroll
@@ -441,18 +447,15 @@ struct AttnTileCoded {
 #pragma unroll
           for (int y = 4; y < 32; y <<= 1) low[g] += __shfl_xor_sync(0xffffffffu, low[g], y);
         }
-        if (r == 0) {
-          sm[h] = limit[n][x] == -INFINITY ? -INFINITY : ref[n][x];
-          sl[h] = sum;
-        }
         if (h < heads) {
+          const float m = limit[n][x] == -INFINITY ? -INFINITY : ref[n][x];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            float4* d = reinterpret_cast<float4*>(so + h * ld + g * 64 + r * 8);
-            d[0] = make_float4(fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),
-                               fmaf(o[g][0][n][2 + x] * a, e, low[g]), fmaf(o[g][1][n][2 + x] * odd, e, low[g]));
-            d[1] = make_float4(fmaf(o[g][2][n][x] * a, e, low[g]), fmaf(o[g][3][n][x] * odd, e, low[g]),
-                               fmaf(o[g][2][n][2 + x] * a, e, low[g]), fmaf(o[g][3][n][2 + x] * odd, e, low[g]));
+            const float y[8] = {fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),
+                                fmaf(o[g][0][n][2 + x] * a, e, low[g]), fmaf(o[g][1][n][2 + x] * odd, e, low[g]),
+                                fmaf(o[g][2][n][x] * a, e, low[g]), fmaf(o[g][3][n][x] * odd, e, low[g]),
+                                fmaf(o[g][2][n][2 + x] * a, e, low[g]), fmaf(o[g][3][n][2 + x] * odd, e, low[g])};
+            f(h, sum, m, g, r, y);
           }
         }
       }
@@ -460,12 +463,15 @@ struct AttnTileCoded {
 };
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------
-// As paged_attention_kernel, tile by tile, but through a ring in shared memory: 4-bit rows are so short that a tile's arithmetic has to
-// fit 100 cycles of an SM to keep up with memory, and no register is left for the tiles on their way.  Every warp copies its own tiles ahead
-// (cp.async, 16 bytes a lane) and waits for nobody but itself until a segment ends.
+// Every warp takes an equal run of the tiles of its block, whose share is that of paged_attention_kernel, and goes through it by itself: its
+// tiles come through a ring of its own in shared memory (cp.async, 16 bytes a lane: 4-bit rows are so short that a tile's arithmetic has
+// to fit 200 cycles of an SM to keep up with memory, and no register is left for tiles on their way), and segments (sequence, KV
+// head) that lie in its run are finished by it alone.  Those that cross warps leave states in shared memory, which the block joins in the
+// end, and those that cross blocks states in scratch, as there.  (With the tiles dealt round all warps and a joining at the end of every
+// segment a block of short segments took twice as long as one inside a long one.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
 // kAttLeast but in rows.
-constexpr int kCodedSegment = 320, kCodedLeast = 128;
+constexpr int kCodedSegment = 64, kCodedLeast = 128;
 
 template <int N>
 __device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -508,12 +514,12 @@ struct CodedWalk {
     t0 = has_work ? block_start(blockIdx.x) : 0;
     t1 = has_work ? block_start(blockIdx.x + 1) : 0;
   }
-  // The runs of tile x of this block: where their codes begin in the pools, in units of 64 bytes, and (how far behind them their steps and lowest
+  // The runs of tile x (nothing from `end` on): where their codes begin in the pools, in units of 64 bytes, and (how far behind them their steps and lowest
   // values are) * 32 + rows that count (0: nothing to read).
-  __device__ __forceinline__ void lookup(int x, unsigned (&at)[SUB], unsigned (&more)[SUB]) const {
+  __device__ __forceinline__ void lookup(int x, int end, unsigned (&at)[SUB], unsigned (&more)[SUB]) const {
 #pragma unroll
     for (int u = 0; u < SUB; ++u) at[u] = more[u] = 0;
-    if (x >= t1) return;
+    if (x >= end) return;
     const int per_page = p.page_shift - 4, page_size = 1 << p.page_shift;
     const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(x));
     const int tiles = pre[i + 1] - pre[i];
@@ -560,12 +566,15 @@ coded_attention_kernel(AttnParams p) {
   begin_grid();
   extern __shared__ __align__(128) unsigned char coded_smem[];
   __shared__ int scratch[W + 1];
+  __shared__ int4 part_of[2 * W];        // states, two per warp (the segment that ends in it, the one that goes on behind it): (first tile, one
+                                         // past the last, first query head of [n_seqs][n_q_heads], query heads or 0: there is none)
+  __shared__ int chain_of[2 * W + 1];    // first state of every segment that has some, and 2 W
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   unsigned char* ring = coded_smem + warp * (S * Tile::kStage);                        // this warp's tiles
-  float* sm_m = reinterpret_cast<float*>(coded_smem + W * S * Tile::kStage);           // [W][HP] maxima, [W][HP] sums, [W][HP][LD] values
-  float* sm_l = sm_m + W * HP;
-  float* sm_o = sm_l + W * HP;
-  int* pre = reinterpret_cast<int*>(sm_m + attn_merge_floats(W, HP, D));
+  constexpr int kState = attn_merge_floats(1, HP, D);                                  // a softmax state: [HP] maxima, [HP] sums, [HP][LD] values
+  static_assert(kState * 4 <= S * Tile::kStage, "a warp's last state goes where its tiles were");
+  float* heads_of = reinterpret_cast<float*>(coded_smem + W * S * Tile::kStage);       // [W] states of segments that end in a warp
+  int* pre = reinterpret_cast<int*>(heads_of + W * kState);
   CodedWalk<Tile> walk(p, pre);
   ragged_prefix<W * 32>(p.n_seqs, pre, scratch, [&](int i) {
     bool bad = false;
@@ -578,13 +587,14 @@ coded_attention_kernel(AttnParams p) {
   const int n_q_heads = p.n_heads * p.group;
   const int state_heads = min(p.group, HP), state_floats = attn_state_floats(state_heads, D);
   const int H = walk.H, gap = walk.gap, t0 = walk.t0, t1 = walk.t1;
+  const int w0 = t0 + (int)((long long)(t1 - t0) * warp / W), w1 = t0 + (int)((long long)(t1 - t0) * (warp + 1) / W);
 
-  // ---- copies.  Tile number i of the warp goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles, the next 32 are
+  // ---- copies.  Tile w0 + i goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles, the next 32 are
   // looked up half way through them.  A copy of no rows is an empty group, so that the groups count the tiles.
-  int number = 0, into = 0, x_copy = t0 + warp;
+  int number = 0, into = 0, x_copy = w0 + lane;
   uint32_t counts = 0;                                         // rows of the runs on their way, 5 bits each, the last ones lowest
   unsigned at_now[SUB], more_now[SUB], at_next[SUB], more_next[SUB];
-  walk.lookup(x_copy + lane * W, at_now, more_now);
+  walk.lookup(x_copy, w1, at_now, more_now);
 #pragma unroll
   for (int u = 0; u < SUB; ++u) at_next[u] = more_next[u] = 0;
   const unsigned char *k_lane = static_cast<const unsigned char*>(p.k) + lane * 16, *v_lane = static_cast<const unsigned char*>(p.v) + lane * 16;
@@ -625,16 +635,15 @@ coded_attention_kernel(AttnParams p) {
     asm volatile("cp.async.commit_group;" ::: "memory");
     into = into + 1 == S ? 0 : into + 1;
     if (++number == 16) {
-      x_copy += 32 * W;
-      walk.lookup(x_copy + lane * W, at_next, more_next);
+      x_copy += 32;
+      walk.lookup(x_copy, w1, at_next, more_next);
     }
   };
 #pragma unroll 1
   for (int i = 1; i < S; ++i) copy_next();
 
-  // ---- the segments (sequence, KV head) of this block
-  int seq = 0, sh = 0, seg0 = 0, seg_end = 0;
-  auto segment_end = [&] { seg_end = seg0 < t1 ? min(seg0 + pre[seq + 1] - pre[seq] - gap, t1) : t1; };
+  // ---- the segments (sequence, KV head) of this warp
+  int seq = 0, sh = 0, seg0 = w1, seg1 = w1;                   // tiles [seg0, seg1) count; w1: there is no segment
   auto next_segment = [&] {                                    // the next one with tiles
     seg0 += pre[seq + 1] - pre[seq];
     if (++sh == H) {
@@ -642,98 +651,149 @@ coded_attention_kernel(AttnParams p) {
 #pragma unroll 1
       do ++seq; while (seq < p.n_seqs && pre[seq] == pre[seq + 1]);
     }
-    segment_end();
+    seg1 = seg0 < w1 ? seg0 + pre[seq + 1] - pre[seq] - gap : seg0;
   };
-  if (t0 < t1) {
-    seq = ragged_find(pre, p.n_seqs, p.heads_div.of(t0));
+  if (w0 < w1) {
+    seq = ragged_find(pre, p.n_seqs, p.heads_div.of(w0));
     const int tiles = pre[seq + 1] - pre[seq];
-    sh = div_small(t0 - pre[seq] * H, tiles);
+    sh = div_small(w0 - pre[seq] * H, tiles);
     seg0 = pre[seq] * H + sh * tiles;
-    segment_end();
-    if (t0 >= seg0 + tiles - gap) next_segment();              // nothing but empty tiles of it here
+    seg1 = seg0 + tiles - gap;
+    if (w0 >= seg1) next_segment();                            // nothing but empty tiles of it here
   }
   Tile tile;
+  int heads = 0;
+  size_t first_head = 0;
   auto load_q = [&] {
     const int g = walk.chunks == 1 ? sh : sh / walk.chunks, h0 = (sh - g * walk.chunks) * HP;
-    tile.load_q(static_cast<const T*>(p.q) + ((size_t)seq * n_q_heads + (size_t)g * p.group + h0) * D, min(HP, p.group - h0), p.scale_log2, lane);
-  };
-  if (seg0 < t1) load_q();                                     // (a block may hold nothing but the last segment's empty tiles)
-  tile.reset();
-  int x = t0 + warp, from = 0;
-  bool worked = false;
-  int4 split = make_int4(0, 0, 0, 0);
-#pragma unroll 1
-  while (seg0 < t1) {
-    if (x < seg_end) {
-      __syncwarp();                                            // the stage about to be filled has been read by every lane
-      copy_next();
-      copies_but<S - 1>();
-      __syncwarp();
-      int nv[SUB], any = 0;
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
-        any |= nv[u];
-      }
-      if (any) tile.work(ring + from * Tile::kStage, nv, lane);
-      worked = true;
-      from = from + 1 == S ? 0 : from + 1;
-      x += W;
-      continue;
-    }
-    const int seg1 = seg0 + pre[seq + 1] - pre[seq] - gap, was_seg0 = seg0;
-    const int g = walk.chunks == 1 ? sh : sh / walk.chunks, h0 = (sh - g * walk.chunks) * HP;
-    const int heads = min(HP, p.group - h0);
-    const size_t first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
-    next_segment();
-    if (seg0 < t1) load_q();                                   // the next segment's queries can come already
-
-    // ---- the warps' states of this segment, joined in warp order.  A warp without tiles leaves a maximum of -inf, a sum of 0
-    // and no values; nobody reads those.
-    if (worked) tile.put(sm_m + warp * HP, sm_l + warp * HP, sm_o + warp * HP * LD, LD, heads, lane);
-    else if (lane < HP) {
-      sm_m[warp * HP + lane] = -INFINITY;
-      sm_l[warp * HP + lane] = 0.f;
-    }
-    __syncthreads();
+    heads = min(HP, p.group - h0);
+    first_head = (size_t)seq * n_q_heads + (size_t)g * p.group + h0;
+    tile.load_q(static_cast<const T*>(p.q) + first_head * D, heads, p.scale_log2, lane);
     tile.reset();
-    worked = false;
-    const bool whole = was_seg0 >= t0 && seg1 <= t1;
-    float* state = p.partial + ((size_t)blockIdx.x * 2 + (was_seg0 < t0 ? 0 : 1)) * state_floats;
-#pragma unroll 1
-    for (int e = threadIdx.x; e < heads * (D / 4); e += W * 32) {
-      const int h = e / (D / 4), d = (e % (D / 4)) * 4;
-      float mm = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * HP + h]);
-      float ll = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int w = 0; w < W; ++w) {
-        const float mw = sm_m[w * HP + h], lw = sm_l[w * HP + h];
-        if (mw != -INFINITY || lw != 0.f) {                  // (a sum that is NaN has a maximum of -inf when all logits are)
-          const float f = exp2_fast(mw - mm);
-          const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * HP + h) * LD + d);
-          ll = fmaf(f, lw, ll);
-          acc.x = fmaf(f, y.x, acc.x);
-          acc.y = fmaf(f, y.y, acc.y);
-          acc.z = fmaf(f, y.z, acc.z);
-          acc.w = fmaf(f, y.w, acc.w);
-        }
+  };
+  // what the warp has of the segment, as one of its two states
+  auto leave = [&](int which, float* state) {
+    tile.finish(heads, lane, [&](int h, float sum, float m, int g, int r, const float (&y)[8]) {
+      if (g == 0 && r == 0) {
+        state[h] = m;
+        state[HP + h] = sum;
       }
-      if (whole) {
-        const float inv = ll == 0.f ? 0.f : 1.f / ll;
-        store4<T>(static_cast<T*>(p.out) + (first_head + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-        if (p.lse && d == 0) p.lse[first_head + h] = (mm + log2f(ll)) * 0.6931471805599453f;
-      } else {
-        *reinterpret_cast<float4*>(state + h * D + d) = acc;
-        if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
-      }
+      float4* d = reinterpret_cast<float4*>(state + 2 * HP + h * LD + g * 64 + r * 8);
+      d[0] = make_float4(y[0], y[1], y[2], y[3]);
+      d[1] = make_float4(y[4], y[5], y[6], y[7]);
+    });
+    if (lane == 0) part_of[2 * warp + which] = make_int4(seg0, seg1, (int)first_head, heads);
+  };
+  auto close = [&] {                                           // the segment ends in this warp
+    if (seg0 < w0) {
+      leave(0, heads_of + warp * kState);
+      return;
     }
-    if (was_seg0 >= t0 && seg1 > t1) split = make_int4(walk.block_of(seg1 - 1) - (int)blockIdx.x + 1, (int)first_head, heads, 0);
-    if (seg0 < t1) __syncthreads();                            // before the states are written again
+    tile.finish(heads, lane, [&](int h, float sum, float m, int g, int r, const float (&y)[8]) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      float z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = y[e] * inv;
+      Eight<T> w;
+      w.round(z);
+      w.store(static_cast<T*>(p.out) + (first_head + h) * D + g * 64 + r * 8);
+      if (p.lse && g == 0 && r == 0) p.lse[first_head + h] = (m + log2f(sum)) * 0.6931471805599453f;
+    });
+  };
+  if (lane < 2) part_of[2 * warp + lane] = make_int4(0, 0, 0, 0);
+  __syncwarp();
+  if (seg0 < w1) load_q();                                     // (a warp may have nothing but the last segment's empty tiles)
+  int from = 0;
+#pragma unroll 1
+  for (int x = w0; x < w1; ++x) {
+    if (x == seg1) {
+      close();
+      next_segment();
+      if (seg0 < w1) load_q();
+    }
+    __syncwarp();                                              // the stage about to be filled has been read by every lane
+    copy_next();
+    int nv[SUB], any = 0;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
+      any |= nv[u];
+    }
+    copies_but<S - 1>();
+    __syncwarp();
+    if (any) tile.work(ring + from * Tile::kStage, nv, lane);
+    from = from + 1 == S ? 0 : from + 1;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+  if (seg0 < w1) {
+    if (seg1 <= w1) close();
+    else leave(1, reinterpret_cast<float*>(ring));
+  }
+  __syncthreads();
+
+  // ---- states of segments that cross warps, joined in the warps' order
+  if (warp == 0) {
+    const int4 part = lane < 2 * W ? part_of[lane] : make_int4(0, 0, 0, 0);
+    const unsigned there = __ballot_sync(0xffffffffu, part.w > 0), below = there & ((1u << lane) - 1);
+    const int before = __shfl_sync(0xffffffffu, part.x, below ? 31 - __clz(below) : 0);
+    const bool first = part.w > 0 && (!below || before != part.x);
+    const unsigned starts = __ballot_sync(0xffffffffu, first);
+    if (first) chain_of[__popc(starts & ((1u << lane) - 1))] = lane;
+    if (lane == 0) {
+      chain_of[__popc(starts)] = 2 * W;
+      scratch[0] = __popc(starts);
+    }
+  }
+  __syncthreads();
+  const int chains = scratch[0];
+  int4 split = make_int4(0, 0, 0, 0);
+  if (threadIdx.x == 0)
+#pragma unroll 1
+    for (int i = 0; i < chains; ++i) {                         // at most one goes on behind the block
+      const int4 part = part_of[chain_of[i]];
+      if (part.x >= t0 && part.y > t1) split = make_int4(walk.block_of(part.y - 1) - (int)blockIdx.x + 1, part.z, part.w, 0);
+    }
+#pragma unroll 1
+  for (int e = threadIdx.x; e < chains * state_heads * (D / 4); e += W * 32) {
+    const int i = e / (state_heads * (D / 4)), h = e / (D / 4) % state_heads, d = e % (D / 4) * 4;
+    const int begin = chain_of[i], end = chain_of[i + 1];
+    const int4 part = part_of[begin];
+    if (h >= part.w) continue;
+    auto state_of = [&](int z) {
+      return z & 1 ? reinterpret_cast<const float*>(coded_smem + (z >> 1) * (S * Tile::kStage)) : heads_of + (z >> 1) * kState;
+    };
+    float mm = -INFINITY;
+#pragma unroll 4
+    for (int z = begin; z < end; ++z)
+      if (part_of[z].w > 0) mm = fmaxf(mm, state_of(z)[h]);
+    float ll = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int z = begin; z < end; ++z) {
+      if (part_of[z].w == 0) continue;
+      const float* state = state_of(z);
+      const float mw = state[h], lw = state[HP + h];
+      if (mw != -INFINITY || lw != 0.f) {                      // (a sum that is NaN has a maximum of -inf when all logits are)
+        const float f = exp2_fast(mw - mm);
+        const float4 y = *reinterpret_cast<const float4*>(state + 2 * HP + h * LD + d);
+        ll = fmaf(f, lw, ll);
+        acc.x = fmaf(f, y.x, acc.x);
+        acc.y = fmaf(f, y.y, acc.y);
+        acc.z = fmaf(f, y.z, acc.z);
+        acc.w = fmaf(f, y.w, acc.w);
+      }
+    }
+    if (part.x >= t0 && part.y <= t1) {
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+      store4<T>(static_cast<T*>(p.out) + ((size_t)part.z + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      if (p.lse && d == 0) p.lse[part.z + h] = (mm + log2f(ll)) * 0.6931471805599453f;
+    } else {
+      float* state = p.partial + ((size_t)blockIdx.x * 2 + (part.x < t0 ? 0 : 1)) * state_floats;
+      *reinterpret_cast<float4*>(state + h * D + d) = acc;
+      if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
+    }
+  }
 
   // sequences without rows
 #pragma unroll 1
