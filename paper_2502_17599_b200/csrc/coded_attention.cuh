@@ -344,7 +344,7 @@ struct AttnTileCoded {
           most = none ? most : fmaxf(most, ref[n][x]);
           const float to_ref = most == -INFINITY ? 0.f : most;
           const float f = none ? 0.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
-          limit[n][x] = most == -INFINITY ? -INFINITY : (most + kSlack) / factor[n][x];
+          limit[n][x] = most == -INFINITY ? -INFINITY : __fdividef(most + kSlack, factor[n][x]);      // (need not be exact)
           ref[n][x] = to_ref;
           l[n][x] = none ? l[n][x] : l[n][x] * f;
 #pragma unroll
@@ -451,10 +451,10 @@ struct AttnTileCoded {
           const float m = limit[n][x] == -INFINITY ? -INFINITY : ref[n][x];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const float y[8] = {fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),
-                                fmaf(o[g][0][n][2 + x] * a, e, low[g]), fmaf(o[g][1][n][2 + x] * odd, e, low[g]),
-                                fmaf(o[g][2][n][x] * a, e, low[g]), fmaf(o[g][3][n][x] * odd, e, low[g]),
-                                fmaf(o[g][2][n][2 + x] * a, e, low[g]), fmaf(o[g][3][n][2 + x] * odd, e, low[g])};
+            float y[8] = {fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),
+                          fmaf(o[g][0][n][2 + x] * a, e, low[g]), fmaf(o[g][1][n][2 + x] * odd, e, low[g]),
+                          fmaf(o[g][2][n][x] * a, e, low[g]), fmaf(o[g][3][n][x] * odd, e, low[g]),
+                          fmaf(o[g][2][n][2 + x] * a, e, low[g]), fmaf(o[g][3][n][2 + x] * odd, e, low[g])};
             f(h, sum, m, g, r, y);
           }
         }
@@ -568,7 +568,8 @@ coded_attention_kernel(AttnParams p) {
   __shared__ int scratch[W + 1];
   __shared__ int4 part_of[2 * W];        // states, two per warp (the segment that ends in it, the one that goes on behind it): (first tile, one
                                          // past the last, first query head of [n_seqs][n_q_heads], query heads or 0: there is none)
-  __shared__ int chain_of[2 * W + 1];    // first state of every segment that has some, and 2 W
+  __shared__ int state_at[2 * W];        // where the states that are there lie, in floats
+  __shared__ int2 chain_of[2 * W + 1];   // of every segment that has some the first in that list and its place in part_of; and the list's end
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   unsigned char* ring = coded_smem + warp * (S * Tile::kStage);                        // this warp's tiles
   constexpr int kState = attn_merge_floats(1, HP, D);                                  // a softmax state: [HP] maxima, [HP] sums, [HP][LD] values
@@ -589,23 +590,18 @@ coded_attention_kernel(AttnParams p) {
   const int H = walk.H, gap = walk.gap, t0 = walk.t0, t1 = walk.t1;
   const int w0 = t0 + (int)((long long)(t1 - t0) * warp / W), w1 = t0 + (int)((long long)(t1 - t0) * (warp + 1) / W);
 
-  // ---- copies.  Tile w0 + i goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles, the next 32 are
-  // looked up half way through them.  A copy of no rows is an empty group, so that the groups count the tiles.
-  int number = 0, into = 0, x_copy = w0 + lane;
+  // ---- copies.  Tile w0 + i goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles.  A copy of no rows is an empty group,
+  // so that the groups count the tiles.  (One place each for look-ups, copies, queries and results: a short cache is over before a
+  // longer program is in the instruction cache.)
+  int number = 32, into = 0, x_copy = w0 + lane;
   uint32_t counts = 0;                                         // rows of the runs on their way, 5 bits each, the last ones lowest
-  unsigned at_now[SUB], more_now[SUB], at_next[SUB], more_next[SUB];
-  walk.lookup(x_copy, w1, at_now, more_now);
-#pragma unroll
-  for (int u = 0; u < SUB; ++u) at_next[u] = more_next[u] = 0;
+  unsigned at_now[SUB], more_now[SUB];
   const unsigned char *k_lane = static_cast<const unsigned char*>(p.k) + lane * 16, *v_lane = static_cast<const unsigned char*>(p.v) + lane * 16;
   constexpr int kMorePieces = Tile::kRunMore / 16;             // of a run of keys or values
   auto copy_next = [&] {
     if (number == 32) {
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        at_now[u] = at_next[u];
-        more_now[u] = more_next[u];
-      }
+      walk.lookup(x_copy, w1, at_now, more_now);
+      x_copy += 32;
       number = 0;
     }
     const uint32_t to = sm100::smem_u32(ring) + into * Tile::kStage;
@@ -634,13 +630,8 @@ coded_attention_kernel(AttnParams p) {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     into = into + 1 == S ? 0 : into + 1;
-    if (++number == 16) {
-      x_copy += 32;
-      walk.lookup(x_copy, w1, at_next, more_next);
-    }
+    ++number;
   };
-#pragma unroll 1
-  for (int i = 1; i < S; ++i) copy_next();
 
   // ---- the segments (sequence, KV head) of this warp
   int seq = 0, sh = 0, seg0 = w1, seg1 = w1;                   // tiles [seg0, seg1) count; w1: there is no segment
@@ -671,117 +662,120 @@ coded_attention_kernel(AttnParams p) {
     tile.load_q(static_cast<const T*>(p.q) + first_head * D, heads, p.scale_log2, lane);
     tile.reset();
   };
-  // what the warp has of the segment, as one of its two states
-  auto leave = [&](int which, float* state) {
-    tile.finish(heads, lane, [&](int h, float sum, float m, int g, int r, const float (&y)[8]) {
-      if (g == 0 && r == 0) {
-        state[h] = m;
-        state[HP + h] = sum;
-      }
-      float4* d = reinterpret_cast<float4*>(state + 2 * HP + h * LD + g * 64 + r * 8);
-      d[0] = make_float4(y[0], y[1], y[2], y[3]);
-      d[1] = make_float4(y[4], y[5], y[6], y[7]);
-    });
-    if (lane == 0) part_of[2 * warp + which] = make_int4(seg0, seg1, (int)first_head, heads);
-  };
-  auto close = [&] {                                           // the segment ends in this warp
-    if (seg0 < w0) {
-      leave(0, heads_of + warp * kState);
-      return;
+  auto finish = [&] {                                          // the segment ends in this warp, or the warp's run inside the segment
+    const bool ends = seg1 <= w1, whole = ends && seg0 >= w0;
+    float* state = ends ? heads_of + warp * kState : reinterpret_cast<float*>(ring);
+    if (!ends) {                                               // (copies of nothing may still be on their way there)
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
     }
-    tile.finish(heads, lane, [&](int h, float sum, float m, int g, int r, const float (&y)[8]) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      float z[8];
+    if (lane == 0 && !whole) part_of[2 * warp + (ends ? 0 : 1)] = make_int4(seg0, seg1, (int)first_head, heads);
+    tile.finish(heads, lane, [&](int h, float sum, float m, int g, int r, float (&y)[8]) {
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = y[e] * inv;
-      Eight<T> w;
-      w.round(z);
-      w.store(static_cast<T*>(p.out) + (first_head + h) * D + g * 64 + r * 8);
-      if (p.lse && g == 0 && r == 0) p.lse[first_head + h] = (m + log2f(sum)) * 0.6931471805599453f;
+        for (int e = 0; e < 8; ++e) y[e] *= inv;
+        Eight<T> w;
+        w.round(y);
+        w.store(static_cast<T*>(p.out) + (first_head + h) * D + g * 64 + r * 8);
+        if (p.lse && g == 0 && r == 0) p.lse[first_head + h] = (m + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        float4* d = reinterpret_cast<float4*>(state + 2 * HP + h * LD + g * 64 + r * 8);
+        d[0] = make_float4(y[0], y[1], y[2], y[3]);
+        d[1] = make_float4(y[4], y[5], y[6], y[7]);
+        if (g == 0 && r == 0) {
+          state[h] = m;
+          state[HP + h] = sum;
+        }
+      }
     });
   };
   if (lane < 2) part_of[2 * warp + lane] = make_int4(0, 0, 0, 0);
   __syncwarp();
-  if (seg0 < w1) load_q();                                     // (a warp may have nothing but the last segment's empty tiles)
   int from = 0;
+  bool fresh = true;                                           // the segment's queries are still to come
+  const int last = seg0 < w1 ? w1 : w0 - S;                    // (a warp may have nothing but the last segment's empty tiles)
 #pragma unroll 1
-  for (int x = w0; x < w1; ++x) {
-    if (x == seg1) {
-      close();
-      next_segment();
-      if (seg0 < w1) load_q();
-    }
+  for (int x = w0 - (S - 1); x < last; ++x) {
     __syncwarp();                                              // the stage about to be filled has been read by every lane
     copy_next();
-    int nv[SUB], any = 0;
+    if (x < w0) continue;
+    if (x >= seg0) {
+      if (fresh) load_q();
+      fresh = false;
+      int nv[SUB], any = 0;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
-      any |= nv[u];
+      for (int u = 0; u < SUB; ++u) {
+        nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
+        any |= nv[u];
+      }
+      copies_but<S - 1>();
+      __syncwarp();
+      if (any) tile.work(ring + from * Tile::kStage, nv, lane);
+      if (x + 1 == min(seg1, w1)) {
+        finish();
+        next_segment();
+        fresh = true;
+        if (seg0 >= w1) break;
+      }
     }
-    copies_but<S - 1>();
-    __syncwarp();
-    if (any) tile.work(ring + from * Tile::kStage, nv, lane);
     from = from + 1 == S ? 0 : from + 1;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncwarp();
-  if (seg0 < w1) {
-    if (seg1 <= w1) close();
-    else leave(1, reinterpret_cast<float*>(ring));
-  }
   __syncthreads();
 
-  // ---- states of segments that cross warps, joined in the warps' order
+  // ---- states of segments that cross warps, joined in the warps' order: a list of the states that are there, and where in it a segment begins
   if (warp == 0) {
     const int4 part = lane < 2 * W ? part_of[lane] : make_int4(0, 0, 0, 0);
     const unsigned there = __ballot_sync(0xffffffffu, part.w > 0), below = there & ((1u << lane) - 1);
     const int before = __shfl_sync(0xffffffffu, part.x, below ? 31 - __clz(below) : 0);
     const bool first = part.w > 0 && (!below || before != part.x);
     const unsigned starts = __ballot_sync(0xffffffffu, first);
-    if (first) chain_of[__popc(starts & ((1u << lane) - 1))] = lane;
+    if (part.w > 0)
+      state_at[__popc(below)] = lane & 1 ? (lane >> 1) * (S * Tile::kStage / 4) : W * S * Tile::kStage / 4 + (lane >> 1) * kState;
+    if (first) chain_of[__popc(starts & ((1u << lane) - 1))] = make_int2(__popc(below), lane);
     if (lane == 0) {
-      chain_of[__popc(starts)] = 2 * W;
+      chain_of[__popc(starts)] = make_int2(__popc(there), 0);
       scratch[0] = __popc(starts);
     }
   }
   __syncthreads();
   const int chains = scratch[0];
-  int4 split = make_int4(0, 0, 0, 0);
-  if (threadIdx.x == 0)
-#pragma unroll 1
-    for (int i = 0; i < chains; ++i) {                         // at most one goes on behind the block
-      const int4 part = part_of[chain_of[i]];
-      if (part.x >= t0 && part.y > t1) split = make_int4(walk.block_of(part.y - 1) - (int)blockIdx.x + 1, part.z, part.w, 0);
-    }
 #pragma unroll 1
   for (int e = threadIdx.x; e < chains * state_heads * (D / 4); e += W * 32) {
     const int i = e / (state_heads * (D / 4)), h = e / (D / 4) % state_heads, d = e % (D / 4) * 4;
-    const int begin = chain_of[i], end = chain_of[i + 1];
-    const int4 part = part_of[begin];
+    const int begin = chain_of[i].x, end = chain_of[i + 1].x;
+    const int4 part = part_of[chain_of[i].y];
     if (h >= part.w) continue;
-    auto state_of = [&](int z) {
-      return z & 1 ? reinterpret_cast<const float*>(coded_smem + (z >> 1) * (S * Tile::kStage)) : heads_of + (z >> 1) * kState;
-    };
+    const float* base = reinterpret_cast<const float*>(coded_smem) + h;
+    constexpr int kBatch = 4;                                  // states at a time; behind the last one that again, with a weight of 0
     float mm = -INFINITY;
-#pragma unroll 4
-    for (int z = begin; z < end; ++z)
-      if (part_of[z].w > 0) mm = fmaxf(mm, state_of(z)[h]);
+#pragma unroll 1
+    for (int z = begin; z < end; z += kBatch)
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) mm = fmaxf(mm, base[state_at[min(z + y, end - 1)]]);
     float ll = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int z = begin; z < end; ++z) {
-      if (part_of[z].w == 0) continue;
-      const float* state = state_of(z);
-      const float mw = state[h], lw = state[HP + h];
-      if (mw != -INFINITY || lw != 0.f) {                      // (a sum that is NaN has a maximum of -inf when all logits are)
-        const float f = exp2_fast(mw - mm);
-        const float4 y = *reinterpret_cast<const float4*>(state + 2 * HP + h * LD + d);
-        ll = fmaf(f, lw, ll);
-        acc.x = fmaf(f, y.x, acc.x);
-        acc.y = fmaf(f, y.y, acc.y);
-        acc.z = fmaf(f, y.z, acc.z);
-        acc.w = fmaf(f, y.w, acc.w);
+#pragma unroll 1
+    for (int z = begin; z < end; z += kBatch) {
+      float m[kBatch], l[kBatch];
+      float4 o[kBatch];
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const int at = state_at[min(z + y, end - 1)];
+        m[y] = base[at];
+        l[y] = base[at + HP];
+        o[y] = *reinterpret_cast<const float4*>(base + at + 2 * HP + h * (LD - 1) + d);
+      }
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        // (nothing is -inf with a sum of 0; a sum that is NaN has a maximum of -inf when all logits are)
+        const float f = z + y < end && (m[y] != -INFINITY || l[y] != 0.f) ? exp2_fast(m[y] - mm) : 0.f;
+        ll = fmaf(f, l[y], ll);
+        acc.x = fmaf(f, o[y].x, acc.x);
+        acc.y = fmaf(f, o[y].y, acc.y);
+        acc.z = fmaf(f, o[y].z, acc.z);
+        acc.w = fmaf(f, o[y].w, acc.w);
       }
     }
     if (part.x >= t0 && part.y <= t1) {
@@ -793,6 +787,15 @@ coded_attention_kernel(AttnParams p) {
       *reinterpret_cast<float4*>(state + h * D + d) = acc;
       if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
     }
+  }
+  if (threadIdx.x == W * 32 - 1) {
+    int4 split = make_int4(0, 0, 0, 0);
+#pragma unroll 1
+    for (int i = 0; i < chains; ++i) {                         // at most one goes on behind the block
+      const int4 part = part_of[chain_of[i].y];
+      if (part.x >= t0 && part.y > t1) split = make_int4(walk.block_of(part.y - 1) - (int)blockIdx.x + 1, part.z, part.w, 0);
+    }
+    p.split[blockIdx.x] = split;
   }
 
   // sequences without rows
@@ -806,7 +809,6 @@ coded_attention_kernel(AttnParams p) {
 #pragma unroll 1
         for (int h = threadIdx.x; h < n_q_heads; h += W * 32) p.lse[(size_t)i * n_q_heads + h] = -INFINITY;
     }
-  if (threadIdx.x == 0) p.split[blockIdx.x] = split;
 }
 
 }  // namespace meda
