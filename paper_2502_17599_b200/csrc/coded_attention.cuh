@@ -29,10 +29,16 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_low(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// The first products of a sum: d is written, not added to.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // The transpose of the 8 x 8 matrix of halves whose row l / 4, columns 2 (l % 4) and + 1 lane l holds.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -83,10 +89,12 @@ __device__ __forceinline__ void shared_piece(uint32_t (&w)[N], int i, const unsi
   w[i + 2] = x.z;
   w[i + 3] = x.w;
 }
-// 16 bytes from global to shared memory behind the thread's back; zeros where `live` is false.
-__device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(live ? 16 : 0) : "memory");
+// 16 bytes from global to shared memory behind the thread's back.
+__device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+// In a branch that is hardly ever taken: it stays one (selects in its place would cost every tile).
+__device__ __forceinline__ void keep_branch() { asm volatile(""); }
 
 // T = type of queries and outputs, D = head_dim, NH = groups of eight query heads, SUB = runs of sixteen rows in a tile (each lies in one page).
 template <typename TOUT, int D, int NH, int BITS, int SUBS>
@@ -100,7 +108,7 @@ struct AttnTileCoded {
   static constexpr int kHalf = kRunCodes + kRunMore;             // bytes of a run's keys or values
   static constexpr int kStage = 2 * SUB * kHalf;                 // of a tile: keys and values of every run
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
-  static constexpr int kScale = PARTS == 2 ? 13 : 5;             // weights reach 2^(kScale + 1) (times 2^kSlack)
+  static constexpr int kScale = PARTS == 2 ? 14 : 6;             // weights stay below 2^(kScale + 1) (times 2^kSlack)
   static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference may stay this far (log2) behind the maximum
 
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
@@ -111,7 +119,7 @@ struct AttnTileCoded {
   float l[NH][2];                        // sum of p = 2^(logit - reference)
   float ref[NH][2], limit[NH][2];        // reference; what a product may reach before the reference has to move (-inf: there is none yet)
   float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
-  int step_exp;                          // of the largest step so far (kScale - 125 at least)
+  int step_exp;                          // of twice the largest step when it was set (kScale - 125 at least)
 
   // Pair j of a unit's eight codes, as the two halves of a word: elements (first, second).
   __device__ __forceinline__ static constexpr int pair_first(int j) { return BITS == 4 ? j : (j / 2) * 4 + j % 2; }
@@ -234,8 +242,8 @@ struct AttnTileCoded {
     return at * kPieces + (piece ^ moved);
   }
 
-  // Logits over `factor` of the keys at `stage`, a run of which nv rows count: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
-  __device__ __forceinline__ void logits(float (&s)[NH][4], const unsigned char* stage, int nv, int lane) {
+  // Logits over `factor` of the run of keys at `stage`: s[n][0..1] row r, heads 2c, 2c + 1 (+ 8 n); s[n][2..3] row r + 8.
+  __device__ __forceinline__ void logits(float (&s)[NH][4], const unsigned char* stage, int lane) {
     const int r = lane / 4, c = lane % 4;
     uint32_t k[2][2 * G * W], km[2][G];                        // rows r, r + 8: codes of units 2c, 2c + 1; steps and lowest values
 #pragma unroll
@@ -249,18 +257,12 @@ struct AttnTileCoded {
     }
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
       constexpr int L0 = G / 2, L1 = G == 4 ? G / 2 + 1 : G / 2;                 // the words of the lowest values
-      mma_low(s[n], km[0][L0], km[1][L0], km[0][L1], km[1][L1], qsum[n][0], qsum[n][1]);
+      mma_bf16_first(s[n], km[0][L0], km[1][L0], km[0][L1], km[1][L1], qsum[n][0], qsum[n][1]);
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       float acc[NH][4];
-#pragma unroll
-      for (int n = 0; n < NH; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t *u0 = &k[0][(i * G + g) * W], *u1 = &k[1][(i * G + g) * W];
@@ -270,7 +272,10 @@ struct AttnTileCoded {
 #pragma unroll
           for (int n = 0; n < NH; ++n)
 #pragma unroll
-            for (int x = 0; x < PARTS; ++x) mma_f16(acc[n], a0, a1, a2, a3, q[n][x][i][g][j], q[n][x][i][g][j + 1]);
+            for (int x = 0; x < PARTS; ++x) {
+              if (i == 0 && j == 0 && x == 0) mma_f16_first(acc[n], a0, a1, a2, a3, q[n][x][i][g][j], q[n][x][i][g][j + 1]);
+              else mma_f16(acc[n], a0, a1, a2, a3, q[n][x][i][g][j], q[n][x][i][g][j + 1]);
+            }
         }
       }
       const float s0 = step_of(km[0], g), s1 = step_of(km[1], g);
@@ -282,38 +287,39 @@ struct AttnTileCoded {
         s[n][3] = fmaf(s1, acc[n][3], s[n][3]);
       }
     }
-    if (nv < 16) {
-#pragma unroll
-      for (int n = 0; n < NH; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r + (e >> 1) * 8 >= nv) s[n][e] = -INFINITY;
-    }
   }
-  // The tile at `stage`, of whose runs nv[] rows count.
-  __device__ __forceinline__ void work(const unsigned char* stage, const int (&nv)[SUB], int lane) {
+  // The tile at `stage`; `rows`: how many rows of each run count, five bits each, the last run's lowest.
+  static constexpr unsigned kFull = SUB == 2 ? 16 << 5 | 16 : 16;
+  __device__ __forceinline__ void work(const unsigned char* stage, unsigned rows, int lane) {
     const int r = lane / 4;
     float s[SUB][NH][4];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) logits(s[u], stage + 2 * u * kHalf, nv[u], lane);
+    for (int u = 0; u < SUB; ++u) logits(s[u], stage + 2 * u * kHalf, lane);
     uint32_t vm[SUB][2][G];                                    // steps and lowest values of the values' rows r, r + 8
     float top = 0.f;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t) shared_words(vm[u][t], stage + (2 * u + 1) * kHalf + kRunCodes + (r + 8 * t) * Row::kMore);
-      if (nv[u] < 16) {                                        // a weight of 0 times whatever is there has to be 0
+    if (rows != kFull) {                                       // rows that do not count: logits of -inf, and 0 for the weight of 0 to meet
+      keep_branch();
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          if (r + 8 * t >= nv[u])
+          if (r + 8 * t >= (int)(rows >> 5 * (SUB - 1 - u) & 31)) {
+#pragma unroll
+            for (int n = 0; n < NH; ++n) s[u][n][2 * t] = s[u][n][2 * t + 1] = -INFINITY;
 #pragma unroll
             for (int g = 0; g < G; ++g) vm[u][t][g] = 0u;
-      }
+          }
+    }
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int g = 0; g < G; ++g) top = fmaxf(top, step_of(vm[u][t], g));
-    }
     bool moved = top >= step_top;
 #pragma unroll
     for (int n = 0; n < NH; ++n)
@@ -326,7 +332,7 @@ struct AttnTileCoded {
     if (__any_sync(0xffffffffu, moved)) {                      // a new reference, or larger values than before: bring the sums to them
 #pragma unroll
       for (int y = 1; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-      const int to = max(step_exp, (int)(__float_as_uint(top) >> 23) - 127);
+      const int to = top >= step_top ? max(step_exp, min(127, (int)(__float_as_uint(top) >> 23) - 126)) : step_exp;
       const float smaller = step_exp - to < -126 ? 0.f : power_of_two(step_exp - to);
       step_exp = to;
       step_top = to == 127 ? INFINITY : power_of_two(to + 1);
@@ -343,17 +349,17 @@ struct AttnTileCoded {
           const bool none = limit[n][x] == -INFINITY;
           most = none ? most : fmaxf(most, ref[n][x]);
           const float to_ref = most == -INFINITY ? 0.f : most;
-          const float f = none ? 0.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
+          const float f = none ? 1.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
           limit[n][x] = most == -INFINITY ? -INFINITY : __fdividef(most + kSlack, factor[n][x]);      // (need not be exact)
           ref[n][x] = to_ref;
-          l[n][x] = none ? l[n][x] : l[n][x] * f;
+          l[n][x] *= f;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            low_sum[n][x][g] = none ? low_sum[n][x][g] : low_sum[n][x][g] * f;
+            low_sum[n][x][g] *= f;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              o[g][t][n][x] = none ? o[g][t][n][x] : o[g][t][n][x] * (f * smaller);
-              o[g][t][n][2 + x] = none ? o[g][t][n][2 + x] : o[g][t][n][2 + x] * (f * smaller);
+              o[g][t][n][x] *= f * smaller;
+              o[g][t][n][2 + x] *= f * smaller;
             }
           }
         }
@@ -471,10 +477,17 @@ struct AttnTileCoded {
 // segment a block of short segments took twice as long as one inside a long one.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
 // kAttLeast but in rows.
-constexpr int kCodedSegment = 64, kCodedLeast = 128;
+constexpr int kCodedSegment = 128, kCodedLeast = 384;
 
 template <int N>
 __device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Where a tile's runs of sixteen rows are: where their codes begin in the pools, in units of 64 bytes, and how far behind that their steps and lowest
+// values do (20 bits; above those, with the first run, how many rows of each run count, 0: nothing to read, five bits each, the last run's lowest).
+template <int SUB>
+struct __align__(8 * SUB) CodedRuns {
+  uint2 run[SUB];
+};
 
 // Where the tiles of a launch lie: all (sequence, KV head, tile) triples in one list, of which block b takes the b-th equal part.
 // (All tile counts stay below 2^31: see meda_pages_create.)
@@ -514,11 +527,16 @@ struct CodedWalk {
     t0 = has_work ? block_start(blockIdx.x) : 0;
     t1 = has_work ? block_start(blockIdx.x + 1) : 0;
   }
-  // The runs of tile x (nothing from `end` on): where their codes begin in the pools, in units of 64 bytes, and (how far behind them their steps and lowest
-  // values are) * 32 + rows that count (0: nothing to read).
-  __device__ __forceinline__ void lookup(int x, int end, unsigned (&at)[SUB], unsigned (&more)[SUB]) const {
+  // The runs of tile x (nothing from `end` on) to `found`.
+  __device__ __forceinline__ void lookup(int x, int end, CodedRuns<SUB>& found) const {
+    unsigned rows = 0, at[SUB], more[SUB];
 #pragma unroll
     for (int u = 0; u < SUB; ++u) at[u] = more[u] = 0;
+    find(x, end, at, more, rows);
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) found.run[u] = make_uint2(at[u], u == 0 ? more[u] | rows << 20 : more[u]);
+  }
+  __device__ __forceinline__ void find(int x, int end, unsigned (&at)[SUB], unsigned (&more)[SUB], unsigned& rows) const {
     if (x >= end) return;
     const int per_page = p.page_shift - 4, page_size = 1 << p.page_shift;
     const int i = ragged_find(pre, p.n_seqs, p.heads_div.of(x));
@@ -546,7 +564,8 @@ struct CodedWalk {
           ok = (unsigned)page < (unsigned)p.n_pages;
           if (ok) {
             at[u] = (unsigned)(((((long long)page * p.n_heads + g) << p.page_shift) * Row::kBytes + r0 * Row::kCodes) / 64);
-            more[u] = (unsigned)(page_size * Row::kCodes - r0 * (Row::kCodes - Row::kMore)) << 5 | nv;
+            more[u] = (unsigned)(page_size * Row::kCodes - r0 * (Row::kCodes - Row::kMore));
+            rows |= nv << 5 * (SUB - 1 - u);
           }
         }
       }
@@ -568,6 +587,7 @@ coded_attention_kernel(AttnParams p) {
   __shared__ int scratch[W + 1];
   __shared__ int4 part_of[2 * W];        // states, two per warp (the segment that ends in it, the one that goes on behind it): (first tile, one
                                          // past the last, first query head of [n_seqs][n_q_heads], query heads or 0: there is none)
+  __shared__ CodedRuns<SUB> table[W][32];
   __shared__ int state_at[2 * W];        // where the states that are there lie, in floats
   __shared__ int2 chain_of[2 * W + 1];   // of every segment that has some the first in that list and its place in part_of; and the list's end
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -588,46 +608,58 @@ coded_attention_kernel(AttnParams p) {
   const int n_q_heads = p.n_heads * p.group;
   const int state_heads = min(p.group, HP), state_floats = attn_state_floats(state_heads, D);
   const int H = walk.H, gap = walk.gap, t0 = walk.t0, t1 = walk.t1;
-  const int w0 = t0 + (int)((long long)(t1 - t0) * warp / W), w1 = t0 + (int)((long long)(t1 - t0) * (warp + 1) / W);
+  const int each = (t1 - t0) / W, more = (t1 - t0) % W;        // tiles of a warp, and how many warps have one more
+  const int w0 = t0 + each * warp + min(warp, more), w1 = w0 + each + (warp < more);
 
-  // ---- copies.  Tile w0 + i goes to stage i % S; lane y holds the look-up of the y-th of 32 tiles.  A copy of no rows is an empty group,
-  // so that the groups count the tiles.  (One place each for look-ups, copies, queries and results: a short cache is over before a
-  // longer program is in the instruction cache.)
+  // ---- copies.  Tile w0 + i goes to stage i % S; 32 tiles are looked up at a time, one by each lane, into `table`.  A copy of no rows is an
+  // empty group, so that the groups count the tiles.
   int number = 32, into = 0, x_copy = w0 + lane;
-  uint32_t counts = 0;                                         // rows of the runs on their way, 5 bits each, the last ones lowest
-  unsigned at_now[SUB], more_now[SUB];
+  static_assert(5 * SUB * S <= 32, "`counts` has the rows of all tiles in the ring");
+  unsigned counts = 0;                                         // rows of the tiles on their way, the last one's lowest
+  const uint32_t ring_at = sm100::smem_u32(ring);
+  constexpr int kMorePieces = Tile::kRunMore / 16;             // of a run of keys or values: side by side on the lanes, keys, values, the next run's
+  const int more_half = lane / kMorePieces, more_run = SUB == 2 ? more_half >> 1 & 1 : 0;
   const unsigned char *k_lane = static_cast<const unsigned char*>(p.k) + lane * 16, *v_lane = static_cast<const unsigned char*>(p.v) + lane * 16;
-  constexpr int kMorePieces = Tile::kRunMore / 16;             // of a run of keys or values
+  const unsigned char* more_lane = static_cast<const unsigned char*>(more_half & 1 ? p.v : p.k) + lane % kMorePieces * 16;
   auto copy_next = [&] {
     if (number == 32) {
-      walk.lookup(x_copy, w1, at_now, more_now);
+      __syncwarp();
+      walk.lookup(x_copy, w1, table[warp][lane]);
+      __syncwarp();
       x_copy += 32;
       number = 0;
     }
-    const uint32_t to = sm100::smem_u32(ring) + into * Tile::kStage;
-    unsigned at[SUB], more[SUB];
+    const uint32_t to = ring_at + into * Tile::kStage;
+    const CodedRuns<SUB> found = table[warp][number];
+    const uint2 mine = found.run[more_run];
+    const unsigned rows = found.run[0].y >> 20;
+    counts = counts << 5 * SUB | rows;
+    auto copies = [&](auto live) {
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      at[u] = __shfl_sync(0xffffffffu, at_now[u], number);
-      more[u] = __shfl_sync(0xffffffffu, more_now[u], number);
-      const int nv = more[u] & 31;
-      counts = counts << 5 | nv;
-      const unsigned char *k = k_lane + (size_t)at[u] * 64, *v = v_lane + (size_t)at[u] * 64;
+      for (int u = 0; u < SUB; ++u) {
+        const unsigned char *k = k_lane + (size_t)found.run[u].x * 64, *v = v_lane + (size_t)found.run[u].x * 64;
 #pragma unroll
-      for (int i = 0; i < Tile::kRunCodes / 512; ++i) {
-        const int piece = lane + 32 * i, y = piece / Tile::kPieces, z = piece % Tile::kPieces;
-        copy16(to + 2 * u * Tile::kHalf + 16 * Tile::key_piece(y, z), k + i * 512, y < nv);
-        copy16(to + (2 * u + 1) * Tile::kHalf + 16 * Tile::value_piece(y, z), v + i * 512, y < nv);
+        for (int i = 0; i < Tile::kRunCodes / 512; ++i) {
+          const int piece = lane + 32 * i, y = piece / Tile::kPieces, z = piece % Tile::kPieces;
+          if (live(u, y)) {
+            copy16(to + 2 * u * Tile::kHalf + 16 * Tile::key_piece(y, z), k + i * 512);
+            copy16(to + (2 * u + 1) * Tile::kHalf + 16 * Tile::value_piece(y, z), v + i * 512);
+          }
+        }
       }
-    }
-    // steps and lowest values: keys and values of all runs side by side on the lanes
+      // steps and lowest values: with 32 pieces or fewer one goes for each lane, else a turn for each run
+      constexpr int kAll = 2 * SUB * kMorePieces;
 #pragma unroll
-    for (int i = 0; i < (2 * SUB * kMorePieces + 31) / 32; ++i) {
-      const int e = lane + 32 * i, half = e / kMorePieces, piece = e % kMorePieces, u = SUB == 2 ? half >> 1 : 0;
-      const unsigned at_u = u ? at[SUB - 1] : at[0], more_u = u ? more[SUB - 1] : more[0];
-      const unsigned char* from = static_cast<const unsigned char*>(half & 1 ? p.v : p.k) + (size_t)at_u * 64 + (more_u >> 5) + piece * 16;
-      if (half < 2 * SUB) copy16(to + half * Tile::kHalf + Tile::kRunCodes + piece * 16, from, piece * 16 / Row::kMore < (more_u & 31));
-    }
+      for (int i = 0; i < (kAll + 31) / 32; ++i) {
+        const int u = kAll > 32 ? i : more_run;
+        const uint2 run = kAll > 32 ? found.run[i] : mine;
+        if ((kAll >= 32 || lane < kAll) && live(u, lane % kMorePieces * 16 / Row::kMore))
+          copy16(to + (kAll > 32 ? 2 * i + (more_half & 1) : more_half) * Tile::kHalf + Tile::kRunCodes + lane % kMorePieces * 16,
+                 more_lane + ((size_t)run.x * 64 + (run.y & 0xfffffu)));
+      }
+    };
+    if (rows == Tile::kFull) copies([](int, int) { return true; });
+    else copies([&](int u, int y) { return y < (int)(rows >> 5 * (SUB - 1 - u) & 31); });
     asm volatile("cp.async.commit_group;" ::: "memory");
     into = into + 1 == S ? 0 : into + 1;
     ++number;
@@ -692,34 +724,25 @@ coded_attention_kernel(AttnParams p) {
   };
   if (lane < 2) part_of[2 * warp + lane] = make_int4(0, 0, 0, 0);
   __syncwarp();
-  int from = 0;
-  bool fresh = true;                                           // the segment's queries are still to come
-  const int last = seg0 < w1 ? w1 : w0 - S;                    // (a warp may have nothing but the last segment's empty tiles)
+  int from = 0, x = w0 - (S - 1);
 #pragma unroll 1
-  for (int x = w0 - (S - 1); x < last; ++x) {
-    __syncwarp();                                              // the stage about to be filled has been read by every lane
-    copy_next();
-    if (x < w0) continue;
-    if (x >= seg0) {
-      if (fresh) load_q();
-      fresh = false;
-      int nv[SUB], any = 0;
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        nv[u] = counts >> 5 * ((S - 1) * SUB + SUB - 1 - u) & 31;
-        any |= nv[u];
-      }
+  while (seg0 < w1) {                                          // (a warp may have nothing but the last segment's empty tiles)
+#pragma unroll 1
+    for (; x < w0; ++x) copy_next();
+    load_q();
+    const int end = min(seg1, w1);
+#pragma unroll 1
+    for (; x < end; ++x) {
+      __syncwarp();                                            // the stage about to be filled has been read by every lane
+      copy_next();
+      const unsigned rows = counts >> 5 * (S - 1) * SUB & ((1u << 5 * SUB) - 1);
       copies_but<S - 1>();
       __syncwarp();
-      if (any) tile.work(ring + from * Tile::kStage, nv, lane);
-      if (x + 1 == min(seg1, w1)) {
-        finish();
-        next_segment();
-        fresh = true;
-        if (seg0 >= w1) break;
-      }
+      if (rows) tile.work(ring + from * Tile::kStage, rows, lane);
+      from = from + 1 == S ? 0 : from + 1;
     }
-    from = from + 1 == S ? 0 : from + 1;
+    finish();
+    next_segment();
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();

@@ -113,7 +113,7 @@ struct CodedAttnKernel {
   static constexpr size_t smem(int n_seqs, int stages) {
     return (size_t)W * stages * Tile::kStage + (size_t)attn_merge_floats(W, Tile::kHeads, D) * 4 + (size_t)(n_seqs + 1) * 4;
   }
-  static constexpr size_t kRoom = kMaxDynSmem - 1024;
+  static constexpr size_t kRoom = kMaxDynSmem - 2048 - W * 32 * sizeof(CodedRuns<Tile::SUB>);          // without the kernel's own arrays
   static constexpr bool kAlways = smem(kPagesMaxSeqs, S) <= kRoom;
   static_assert(smem(kPagesMaxSeqs, 1) <= kRoom, "the largest batch has to fit");
   static meda_status prepare(meda_pages* p) {
@@ -145,14 +145,14 @@ struct CodedAttnKernel {
 template <typename T, int BITS, typename F>
 meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
-  constexpr bool kF32 = sizeof(T) == 4;
   constexpr int kSub = BITS == 4 ? 2 : 1;
-  if (d == 64)
-    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, BITS, kSub>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, BITS, kSub>, 64, kF32 ? 12 : 16, 3>());
+  if (d == 64) {
+    if constexpr (BITS == 4) return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, 4, 2>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, 4, 2>, 64, 12, 3>());
+    else return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, 8, 1>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, 8, 1>, 64, 12, 4>());
+  }
   if (d == 128)
-    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS, kSub>, 128, kF32 || BITS == 8 ? 12 : 16, 2>())
-                  : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS, kSub>, 128, 8, 3>());
-  return f(CodedAttnKernel<AttnTileCoded<T, 256, 1, BITS, 1>, 256, 8, BITS == 4 ? 3 : 2>());
+    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS, kSub>, 128, 12, 2>()) : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS, kSub>, 128, 8, 3>());
+  return f(CodedAttnKernel<AttnTileCoded<T, 256, 1, BITS, kSub>, 256, 8, 2>());
 }
 
 // Calls f with the AttnKernel for the handle's geometry.  Warps per block: what the registers of one block per SM allow.
