@@ -748,78 +748,70 @@ coded_attention_kernel(AttnParams p) {
   __syncthreads();
 
   // ---- states of segments that cross warps, joined in the warps' order: a list of the states that are there, and where in it a segment begins
-  if (warp == 0) {
-    const int4 part = lane < 2 * W ? part_of[lane] : make_int4(0, 0, 0, 0);
-    const unsigned there = __ballot_sync(0xffffffffu, part.w > 0), below = there & ((1u << lane) - 1);
-    const int before = __shfl_sync(0xffffffffu, part.x, below ? 31 - __clz(below) : 0);
-    const bool first = part.w > 0 && (!below || before != part.x);
-    const unsigned starts = __ballot_sync(0xffffffffu, first);
-    if (part.w > 0)
-      state_at[__popc(below)] = lane & 1 ? (lane >> 1) * (S * Tile::kStage / 4) : W * S * Tile::kStage / 4 + (lane >> 1) * kState;
-    if (first) chain_of[__popc(starts & ((1u << lane) - 1))] = make_int2(__popc(below), lane);
-    if (lane == 0) {
-      chain_of[__popc(starts)] = make_int2(__popc(there), 0);
-      scratch[0] = __popc(starts);
-    }
-  }
-  __syncthreads();
-  const int chains = scratch[0];
+  // (every warp writes the same)
+  const int4 part = lane < 2 * W ? part_of[lane] : make_int4(0, 0, 0, 0);
+  const unsigned there = __ballot_sync(0xffffffffu, part.w > 0), below = there & ((1u << lane) - 1);
+  const int before = __shfl_sync(0xffffffffu, part.x, below ? 31 - __clz(below) : 0);
+  const unsigned starts = __ballot_sync(0xffffffffu, part.w > 0 && (!below || before != part.x));
+  const int chains = __popc(starts);
+  if (part.w > 0)
+    state_at[__popc(below)] = lane & 1 ? (lane >> 1) * (S * Tile::kStage / 4) : W * S * Tile::kStage / 4 + (lane >> 1) * kState;
+  if (starts >> lane & 1) chain_of[__popc(starts & ((1u << lane) - 1))] = make_int2(__popc(below), lane);
+  if (lane == 0) chain_of[chains] = make_int2(__popc(there), 0);
+  __syncwarp();
+  int4 split = make_int4(0, 0, 0, 0);
 #pragma unroll 1
-  for (int e = threadIdx.x; e < chains * state_heads * (D / 4); e += W * 32) {
-    const int i = e / (state_heads * (D / 4)), h = e / (D / 4) % state_heads, d = e % (D / 4) * 4;
+  for (int i = 0; i < chains; ++i) {
     const int begin = chain_of[i].x, end = chain_of[i + 1].x;
     const int4 part = part_of[chain_of[i].y];
-    if (h >= part.w) continue;
-    const float* base = reinterpret_cast<const float*>(coded_smem) + h;
-    constexpr int kBatch = 4;                                  // states at a time; behind the last one that again, with a weight of 0
-    float mm = -INFINITY;
 #pragma unroll 1
-    for (int z = begin; z < end; z += kBatch)
-#pragma unroll
-      for (int y = 0; y < kBatch; ++y) mm = fmaxf(mm, base[state_at[min(z + y, end - 1)]]);
-    float ll = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int e = threadIdx.x; e < part.w * (D / 4); e += W * 32) {
+      const int h = e / (D / 4), d = e % (D / 4) * 4;
+      const float* base = reinterpret_cast<const float*>(coded_smem) + h;
+      constexpr int kBatch = 4;                                // states at a time; behind the last one that again, with a weight of 0
+      float mm = -INFINITY;
 #pragma unroll 1
-    for (int z = begin; z < end; z += kBatch) {
-      float m[kBatch], l[kBatch];
-      float4 o[kBatch];
+      for (int z = begin; z < end; z += kBatch)
 #pragma unroll
-      for (int y = 0; y < kBatch; ++y) {
-        const int at = state_at[min(z + y, end - 1)];
-        m[y] = base[at];
-        l[y] = base[at + HP];
-        o[y] = *reinterpret_cast<const float4*>(base + at + 2 * HP + h * (LD - 1) + d);
+        for (int y = 0; y < kBatch; ++y) mm = fmaxf(mm, base[state_at[min(z + y, end - 1)]]);
+      float ll = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int z = begin; z < end; z += kBatch) {
+        float m[kBatch], l[kBatch];
+        float4 o[kBatch];
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+          const int at = state_at[min(z + y, end - 1)];
+          m[y] = base[at];
+          l[y] = base[at + HP];
+          o[y] = *reinterpret_cast<const float4*>(base + at + 2 * HP + h * (LD - 1) + d);
+        }
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+          // (no state is -inf with a sum of 0; a sum that is NaN has a maximum of -inf when all logits are)
+          const float f = z + y < end && (m[y] != -INFINITY || l[y] != 0.f) ? exp2_fast(m[y] - mm) : 0.f;
+          ll = fmaf(f, l[y], ll);
+          acc.x = fmaf(f, o[y].x, acc.x);
+          acc.y = fmaf(f, o[y].y, acc.y);
+          acc.z = fmaf(f, o[y].z, acc.z);
+          acc.w = fmaf(f, o[y].w, acc.w);
+        }
       }
-#pragma unroll
-      for (int y = 0; y < kBatch; ++y) {
-        // (nothing is -inf with a sum of 0; a sum that is NaN has a maximum of -inf when all logits are)
-        const float f = z + y < end && (m[y] != -INFINITY || l[y] != 0.f) ? exp2_fast(m[y] - mm) : 0.f;
-        ll = fmaf(f, l[y], ll);
-        acc.x = fmaf(f, o[y].x, acc.x);
-        acc.y = fmaf(f, o[y].y, acc.y);
-        acc.z = fmaf(f, o[y].z, acc.z);
-        acc.w = fmaf(f, o[y].w, acc.w);
+      if (part.x >= t0 && part.y <= t1) {
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        store4<T>(static_cast<T*>(p.out) + ((size_t)part.z + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+        if (p.lse && d == 0) p.lse[part.z + h] = (mm + log2f(ll)) * 0.6931471805599453f;
+      } else {
+        float* state = p.partial + ((size_t)blockIdx.x * 2 + (part.x < t0 ? 0 : 1)) * state_floats;
+        *reinterpret_cast<float4*>(state + h * D + d) = acc;
+        if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
       }
     }
-    if (part.x >= t0 && part.y <= t1) {
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;
-      store4<T>(static_cast<T*>(p.out) + ((size_t)part.z + h) * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (p.lse && d == 0) p.lse[part.z + h] = (mm + log2f(ll)) * 0.6931471805599453f;
-    } else {
-      float* state = p.partial + ((size_t)blockIdx.x * 2 + (part.x < t0 ? 0 : 1)) * state_floats;
-      *reinterpret_cast<float4*>(state + h * D + d) = acc;
-      if (d == 0) *reinterpret_cast<float2*>(state + state_heads * D + 2 * h) = make_float2(mm, ll);
-    }
+    if (threadIdx.x == W * 32 - 1 && part.x >= t0 && part.y > t1)               // at most one goes on behind the block
+      split = make_int4(walk.block_of(part.y - 1) - (int)blockIdx.x + 1, part.z, part.w, 0);
   }
-  if (threadIdx.x == W * 32 - 1) {
-    int4 split = make_int4(0, 0, 0, 0);
-#pragma unroll 1
-    for (int i = 0; i < chains; ++i) {                         // at most one goes on behind the block
-      const int4 part = part_of[chain_of[i].y];
-      if (part.x >= t0 && part.y > t1) split = make_int4(walk.block_of(part.y - 1) - (int)blockIdx.x + 1, part.z, part.w, 0);
-    }
-    p.split[blockIdx.x] = split;
-  }
+  if (threadIdx.x == W * 32 - 1) p.split[blockIdx.x] = split;
 
   // sequences without rows
 #pragma unroll 1
