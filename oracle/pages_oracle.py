@@ -134,7 +134,7 @@ def quantise(x, bits):
     with np.errstate(invalid="ignore", over="ignore"):
         fine = (np.abs(x) < np.float32(2.0 ** 126)).all(-1)        # False for NaN
         safe = np.where(fine[..., None], x, np.float32(0))
-        low = _bf16(safe.min(-1), False)
+        low = _bf16(safe.min(-1), False) + np.float32(0)           # a zero counts as +0
         step = _bf16((safe.max(-1) - low) * (np.float32(1) / np.float32((1 << bits) - 1)), True)
         step = np.maximum(step, np.float32(2.0 ** -126))
         code = np.rint((safe - low[..., None]) * (np.float32(1) / step)[..., None])

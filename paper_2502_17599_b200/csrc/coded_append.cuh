@@ -139,11 +139,13 @@ coded_append_kernel(RopeParams p) {
       v.round(f);
     }
     Unit<BITS> c;
-    c.encode(v);
+    const CodeScale by = c.encode(v);
     if (slot < 0 || x0 + lane >= total) continue;
     unsigned char* pool = static_cast<unsigned char*>(key ? p.k_pages : p.v_pages);
     unsigned char* page = pool + ((size_t)(slot >> p.page_shift) * p.n_kv_heads + g) * page_bytes;
-    c.template put<D>(page, page_size, (int)(slot & (page_size - 1)), u);
+    const int row = (int)(slot & (page_size - 1));
+    c.template put_codes<D>(page, row, u);
+    if (u % 8 == 0) Unit<BITS>::template put_more<D>(page, page_size, row, u / 8, by.more);
   }
 }
 

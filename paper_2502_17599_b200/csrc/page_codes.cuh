@@ -71,15 +71,32 @@ struct Eight<__nv_bfloat16> {
     w = make_uint4(v[0], v[1], v[2], v[3]);
   }
   __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = w; }
-  __device__ __forceinline__ void extremes(float& lo, float& hi) const {         // a NaN wins
-    VecBounds<__nv_bfloat16> b;
-    b.reset();
-    b.add(w);
-    const __nv_bfloat162 l = __hmin2_nan(__hmin2_nan(b.lo[0], b.lo[1]), __hmin2_nan(b.lo[2], b.lo[3]));
-    const __nv_bfloat162 h = __hmax2_nan(__hmax2_nan(b.hi[0], b.hi[1]), __hmax2_nan(b.hi[2], b.hi[3]));
-    lo = __bfloat162float(__hmin_nan(l.x, l.y));
-    hi = __bfloat162float(__hmax_nan(h.x, h.y));
+  // The eight's extremes as (minimum, -maximum); a NaN wins.
+  using Range = uint32_t;
+  __device__ __forceinline__ Range range() const {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    __nv_bfloat162 x[4];
+    memcpy(x, v, 16);
+    const __nv_bfloat162 l = __hmin2_nan(__hmin2_nan(x[0], x[1]), __hmin2_nan(x[2], x[3]));
+    const __nv_bfloat162 h = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
+    uint32_t lw, hw;
+    memcpy(&lw, &l, 4);
+    memcpy(&hw, &h, 4);
+    hw ^= 0x80008000u;
+    return join(__byte_perm(lw, hw, 0x5410), __byte_perm(lw, hw, 0x7632));
   }
+  __device__ __forceinline__ static Range join(Range a, Range b) {
+    __nv_bfloat162 x, y;
+    memcpy(&x, &a, 4);
+    memcpy(&y, &b, 4);
+    const __nv_bfloat162 m = __hmin2_nan(x, y);
+    uint32_t r;
+    memcpy(&r, &m, 4);
+    return r;
+  }
+  __device__ __forceinline__ static Range other(Range a, int mask) { return __shfl_xor_sync(0xffffffffu, a, mask); }
+  __device__ __forceinline__ static float low_of(Range a) { return __uint_as_float(a << 16); }
+  __device__ __forceinline__ static float high_of(Range a) { return -__uint_as_float(a & 0xffff0000u); }
 };
 template <>
 struct Eight<float> {
@@ -101,15 +118,58 @@ struct Eight<float> {
     reinterpret_cast<float4*>(p)[0] = a;
     reinterpret_cast<float4*>(p)[1] = b;
   }
-  __device__ __forceinline__ void extremes(float& lo, float& hi) const {
-    float x[8];
-    floats(x);
-    lo = hi = x[0];
-#pragma unroll
-    for (int e = 1; e < 8; ++e) {
-      lo = min_nan(lo, x[e]);
-      hi = max_nan(hi, x[e]);
-    }
+  using Range = float2;
+  __device__ __forceinline__ static float least(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  }
+  __device__ __forceinline__ Range range() const {
+    const float2 x = make_float2(a.x, -a.x), y = make_float2(a.y, -a.y), z = make_float2(a.z, -a.z), w = make_float2(a.w, -a.w);
+    const float2 p = make_float2(b.x, -b.x), q = make_float2(b.y, -b.y), r = make_float2(b.z, -b.z), t = make_float2(b.w, -b.w);
+    return join(join(join(x, y), join(z, w)), join(join(p, q), join(r, t)));
+  }
+  __device__ __forceinline__ static Range join(Range a, Range b) { return make_float2(least(a.x, b.x), least(a.y, b.y)); }
+  __device__ __forceinline__ static Range other(Range a, int mask) {
+    return make_float2(__shfl_xor_sync(0xffffffffu, a.x, mask), __shfl_xor_sync(0xffffffffu, a.y, mask));
+  }
+  __device__ __forceinline__ static float low_of(Range a) { return a.x; }
+  __device__ __forceinline__ static float high_of(Range a) { return -a.y; }
+};
+
+// Two fp32 operations in one instruction, each rounded as by itself.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// What a group of 64 elements is quantised by.
+struct CodeScale {
+  uint32_t more;                 // step and lowest value, as a page has them: bf16, the step in the lower half
+  float inverse;                 // 1 / step
+  __device__ __forceinline__ float step() const { return __uint_as_float(more << 16); }
+  __device__ __forceinline__ float low() const { return __uint_as_float(more & 0xffff0000u); }
+  template <int BITS>
+  __device__ __forceinline__ static CodeScale of(float lo, float hi) {
+    const bool fine = lo > -kCodeMost && hi < kCodeMost;
+    const float low = bf16_down(lo) + 0.f;       // (a zero counts as +0)
+    const float step = fmaxf(bf16_up(__fmul_rn(__fsub_rn(hi, low), 1.f / ((1 << BITS) - 1))), kCodeLeast);
+    CodeScale s;
+    s.more = fine ? __float_as_uint(step) >> 16 | __float_as_uint(low) : 0x7fff7fffu;
+    s.inverse = __frcp_rn(step);
+    return s;
   }
 };
 
@@ -122,57 +182,69 @@ struct Unit {
 
   // The eight lanes of a group call this together (and the other lanes of the warp at the same time).
   template <typename T>
-  __device__ __forceinline__ void encode(const Eight<T>& v) {
-    float lo, hi;
-    v.extremes(lo, hi);
+  __device__ __forceinline__ CodeScale encode(const Eight<T>& v) {
+    auto range = v.range();
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    const bool fine = lo > -kCodeMost && hi < kCodeMost;
-    low = fine ? bf16_down(lo) : NAN;
-    step = fmaxf(bf16_up(__fmul_rn(__fsub_rn(hi, low), 1.f / ((1 << BITS) - 1))), kCodeLeast);
-    if (!fine) step = NAN;
-    const float inv = __frcp_rn(step);
+    for (int o = 1; o < 8; o <<= 1) range = Eight<T>::join(range, Eight<T>::other(range, o));
+    const CodeScale by = CodeScale::of<BITS>(Eight<T>::low_of(range), Eight<T>::high_of(range));
+    encode(v, by);
+    return by;
+  }
+  template <typename T>
+  __device__ __forceinline__ void encode(const Eight<T>& v, const CodeScale& by) {
+    step = by.step();
+    low = by.low();
     float x[8];
     v.floats(x);
+    const uint64_t minus_low = pair(-by.low(), -by.low()), inverse = pair(by.inverse, by.inverse), magic = pair(8388608.f, 8388608.f);
+    // The product is a sum with -0, which leaves it as it is, and in words that the compiler does not see through (the inverse is positive): a
+    // plain mul.rn.f32x2 it puts together with the sum behind it, into one rounding.
+    const float zero = __uint_as_float(~__float_as_uint(by.inverse) & 0x80000000u);
+    const uint64_t minus_zero = pair(zero, zero);
     uint32_t u[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)                  // 2^23 + t: the sum's rounding is rint, its lower bits are the code
-      u[e] = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x[e], low), inv), 8388608.f));
+    for (int e = 0; e < 8; e += 2) {             // 2^23 + t: the sum's rounding is rint, its lower bits are the code
+      float a, b;
+      unpair(add2(fma2(add2(pair(x[e], x[e + 1]), minus_low), inverse, minus_zero), magic), a, b);
+      u[e] = __float_as_uint(a);
+      u[e + 1] = __float_as_uint(b);
+    }
     if constexpr (BITS == 4) {
-      w[0] = 0u - 0xfb000000u;                   // the exponents 0x4b000000 of the first two, shifted (the others' leave the word)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[0] += u[e] << (4 * e);
+      // the exponents 0x4b000000 of the first two, shifted, come off again (the others' leave the word)
+      w[0] = ((u[0] - 0xfb000000u + (u[1] << 4)) + ((u[2] << 8) + (u[3] << 12))) + (((u[4] << 16) + (u[5] << 20)) + ((u[6] << 24) + (u[7] << 28)));
     } else {
 #pragma unroll
-      for (int j = 0; j < kWords; ++j) {
-        w[j] = 0u - 0x4b000000u;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[j] += u[4 * j + e] << (8 * e);
-      }
+      for (int j = 0; j < kWords; ++j)
+        w[j] = __byte_perm(__byte_perm(u[4 * j], u[4 * j + 1], 0x0040), __byte_perm(u[4 * j + 2], u[4 * j + 3], 0x0040), 0x5410);
     }
   }
   __device__ __forceinline__ void values(float (&x)[8]) const {
+    const uint64_t steps = pair(step, step), lows = pair(low, low), magic = pair(-8388608.f, -8388608.f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t code = BITS == 4 ? w[0] >> (4 * e) & 15u : w[e / 4] >> (8 * (e % 4)) & 255u;
-      x[e] = fmaf(step, __uint_as_float(0x4b000000u | code) - 8388608.f, low);
+    for (int e = 0; e < 8; e += 2) {
+      uint32_t c[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (BITS == 4) c[i] = w[0] >> (4 * (e + i)) & 15u | 0x4b000000u;
+        else c[i] = __byte_perm(w[e / 4], 0x4b000000u, 0x7440 | (e + i) % 4);
+      }
+      unpair(fma2(steps, add2(pair(__uint_as_float(c[0]), __uint_as_float(c[1])), magic), lows), x[e], x[e + 1]);
     }
   }
   // page: a page of one head; r: row in it; u: unit of the row
   template <int D>
-  __device__ __forceinline__ void put(unsigned char* page, int page_size, int r, int u) const {
+  __device__ __forceinline__ void put_codes(unsigned char* page, int r, int u) const {
     using Row = CodedRow<D, BITS>;
     unsigned char* at = page + (size_t)r * Row::kCodes + Row::place(u);
     if constexpr (BITS == 4) *reinterpret_cast<uint32_t*>(at) = w[0];
     else *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[kWords - 1]);
-    if (u % 8 == 0) {
-      unsigned char* more = page + (size_t)page_size * Row::kCodes + (size_t)r * Row::kMore + (u / 8) * 2;
-      *reinterpret_cast<uint16_t*>(more) = (uint16_t)(__float_as_uint(step) >> 16);
-      *reinterpret_cast<uint16_t*>(more + 2 * Row::kGroups) = (uint16_t)(__float_as_uint(low) >> 16);
-    }
+  }
+  template <int D>
+  __device__ __forceinline__ static void put_more(unsigned char* page, int page_size, int r, int group, uint32_t value) {
+    using Row = CodedRow<D, BITS>;
+    unsigned char* more = page + (size_t)page_size * Row::kCodes + (size_t)r * Row::kMore + group * 2;
+    *reinterpret_cast<uint16_t*>(more) = (uint16_t)value;
+    *reinterpret_cast<uint16_t*>(more + 2 * Row::kGroups) = (uint16_t)(value >> 16);
   }
   template <int D>
   __device__ __forceinline__ void get(const unsigned char* page, int page_size, int r, int u) {
@@ -323,29 +395,46 @@ coded_rows_kernel(CodedParams p) {
 #pragma unroll 1
     for (int base = first; base < live; base += kRows * kBatch) {          // (all lanes together: encode() exchanges between them)
       if constexpr (PASS == kCodedStore) {
-        Eight<T> kx[kBatch], vx[kBatch];
+        static_assert(kBatch == 4, "a group's eight lanes, eight scales");
+        Eight<T> x[2 * kBatch];                          // four rows of keys, four of values
+        typename Eight<T>::Range range[2 * kBatch];
 #pragma unroll
         for (int y = 0; y < kBatch; ++y) {
           const int r = min(base + y * kRows + sub, live - 1);             // behind the last row: that one again, not written
-          kx[y].load(static_cast<const T*>(p.k) + dense + (long long)r * D);
-          vx[y].load(static_cast<const T*>(p.v) + dense + (long long)r * D);
+          x[y].load(static_cast<const T*>(p.k) + dense + (long long)r * D);
+          x[kBatch + y].load(static_cast<const T*>(p.v) + dense + (long long)r * D);
         }
 #pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-          const int r = base + y * kRows + sub;
-          if (base + y * kRows >= live) break;
+        for (int y = 0; y < 2 * kBatch; ++y) range[y] = x[y].range();
+        // each of the group's eight lanes ends up with one of the eight scales, and works it out for all
+        const int mine = lane & 7;
+#pragma unroll
+        for (int half = kBatch; half >= 1; half >>= 1)
+#pragma unroll
+          for (int y = 0; y < half; ++y) {
+            const bool upper = (mine & half) != 0;
+            const auto send = upper ? range[y] : range[y + half], keep = upper ? range[y + half] : range[y];
+            range[y] = Eight<T>::join(keep, Eight<T>::other(send, half));
+          }
+        const CodeScale scale = CodeScale::of<BITS>(Eight<T>::low_of(range[0]), Eight<T>::high_of(range[0]));
+        const int row = base + mine % kBatch * kRows + sub;
+        if (row < live) Unit<BITS>::template put_more<D>(mine < kBatch ? kpage : vpage, page_size, row, unit / 8, scale.more);
+#pragma unroll
+        for (int y = 0; y < 2 * kBatch; ++y) {
+          CodeScale by;
+          by.more = __shfl_sync(0xffffffffu, scale.more, (lane & 24) | y);
+          by.inverse = __shfl_sync(0xffffffffu, scale.inverse, (lane & 24) | y);
+          const int r = base + y % kBatch * kRows + sub;
           Unit<BITS> c;
-          c.encode(kx[y]);
-          if (r < live) c.template put<D>(kpage, page_size, r, unit);
-          if (p.bounds) {                                // (a row met twice changes no bound)
+          c.encode(x[y], by);
+          if (r < live) c.template put_codes<D>(y < kBatch ? kpage : vpage, r, unit);
+          if (y < kBatch && p.bounds) {                  // (a row met twice changes no bound)
             float f[8];
             c.values(f);
             Eight<T> back;
             back.round(f);
             b.add(back);
           }
-          c.encode(vx[y]);
-          if (r < live) c.template put<D>(vpage, page_size, r, unit);
         }
       } else {
         Unit<BITS> kc[kBatch], vc[kBatch];
