@@ -49,61 +49,77 @@ coded_append_kernel(RopeParams p) {
   // ---- queries
   const int rot = ADJACENT ? 2 * half / E : half / E;          // items of a head that rotate
   const int per_head = rot + (VR - 2 * half / E);
-  const int q_items = p.q ? p.n_q_heads * per_head : 0;
-  for (int x = threadIdx.x; x < n_tok * q_items; x += kRopeThreads) {
-    const int tok = x / q_items;
-    int item = x - tok * q_items;
-    if (slot_of[tok] < 0) continue;
-    const int h = item / per_head;
-    item -= h * per_head;
-    const uint4* src = static_cast<const uint4*>(p.q) + (t0 + tok) * p.q_stride + h * VR;
-    uint4* dst = static_cast<uint4*>(p.q_out) + ((size_t)(t0 + tok) * p.n_q_heads + h) * VR;
-    if (item >= rot) {
-      const int vec = 2 * half / E + (item - rot);
-      dst[vec] = src[vec];
-      continue;
-    }
-    if (ADJACENT) {
-      float f[E];
-      RopeVec<T>::unpack(src[item], f);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) {
-        const int i = item * (E / 2) + e;
-        const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
-        const float a = f[2 * e], b = f[2 * e + 1];
-        f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
-        f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+  // (indexes go up by what a turn of the block adds to them: divisions in every turn would cost more than the rotation)
+  if (p.q) {
+    const int turn_heads = kRopeThreads / per_head, turn_items = kRopeThreads % per_head;
+    int h = threadIdx.x / per_head, item = threadIdx.x % per_head, tok = 0;
+    for (;; h += turn_heads, item += turn_items) {
+      if (item >= per_head) {
+        item -= per_head;
+        ++h;
       }
-      dst[item] = RopeVec<T>::pack(f);
-    } else {
-      float a[E], b[E];
-      const int other = item + half / E;
-      const uint4 xa = src[item], xb = src[other];
-      RopeVec<T>::unpack(xa, a);
-      RopeVec<T>::unpack(xb, b);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int i = item * E + e;
-        const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
-        const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
-        b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
-        a[e] = y;
+      while (h >= p.n_q_heads) {
+        h -= p.n_q_heads;
+        ++tok;
       }
-      dst[item] = RopeVec<T>::pack(a);
-      dst[other] = RopeVec<T>::pack(b);
+      if (tok >= n_tok) break;
+      if (slot_of[tok] < 0) continue;
+      const uint4* src = static_cast<const uint4*>(p.q) + (t0 + tok) * p.q_stride + h * VR;
+      uint4* dst = static_cast<uint4*>(p.q_out) + ((size_t)(t0 + tok) * p.n_q_heads + h) * VR;
+      if (item >= rot) {
+        const int vec = 2 * half / E + (item - rot);
+        dst[vec] = src[vec];
+        continue;
+      }
+      if (ADJACENT) {
+        float f[E];
+        RopeVec<T>::unpack(src[item], f);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) {
+          const int i = item * (E / 2) + e;
+          const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+          const float a = f[2 * e], b = f[2 * e + 1];
+          f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
+          f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+        }
+        dst[item] = RopeVec<T>::pack(f);
+      } else {
+        float a[E], b[E];
+        const int other = item + half / E;
+        const uint4 xa = src[item], xb = src[other];
+        RopeVec<T>::unpack(xa, a);
+        RopeVec<T>::unpack(xb, b);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int i = item * E + e;
+          const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+          const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
+          b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
+          a[e] = y;
+        }
+        dst[item] = RopeVec<T>::pack(a);
+        dst[other] = RopeVec<T>::pack(b);
+      }
     }
   }
 
   // ---- keys and values: a whole warp goes round together, its groups of eight lanes are all in or all out
   const int page_size = 1 << p.page_shift;
   const size_t page_bytes = (size_t)CodedRow<D, BITS>::kBytes << p.page_shift;
-  const int per_token = 2 * p.n_kv_heads * U, total = n_tok * per_token;
-  const int lane = threadIdx.x % 32;
+  const int u = threadIdx.x % U, heads = 2 * p.n_kv_heads;            // keys' heads, then values'
+  int tok = 0;
 #pragma unroll 1
-  for (int x0 = threadIdx.x - lane; x0 < total; x0 += kRopeThreads) {
-    const int x = min(x0 + lane, total - 1);
-    const int tok = x / per_token, item = x - tok * per_token;
-    const int u = item % U, head = item / U;
+  for (int head = threadIdx.x / U; ; head += kRopeThreads / U) {
+    while (head >= heads && tok < n_tok) {
+      head -= heads;
+      ++tok;
+    }
+    const bool there = tok < n_tok;
+    if (!__any_sync(0xffffffffu, there)) break;
+    if (!there) {                                              // beside lanes that are: the last head again, not written
+      tok = n_tok - 1;
+      head = heads - 1;
+    }
     const bool key = head < p.n_kv_heads;
     const int g = key ? head : head - p.n_kv_heads;
     const int64_t slot = slot_of[tok];
@@ -140,7 +156,12 @@ coded_append_kernel(RopeParams p) {
     }
     Unit<BITS> c;
     const CodeScale by = c.encode(v);
-    if (slot < 0 || x0 + lane >= total) continue;
+    if (!there) {
+      tok = n_tok;
+      head = heads;
+      continue;
+    }
+    if (slot < 0) continue;
     unsigned char* pool = static_cast<unsigned char*>(key ? p.k_pages : p.v_pages);
     unsigned char* page = pool + ((size_t)(slot >> p.page_shift) * p.n_kv_heads + g) * page_bytes;
     const int row = (int)(slot & (page_size - 1));

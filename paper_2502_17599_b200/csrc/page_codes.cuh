@@ -247,7 +247,7 @@ struct Unit {
     *reinterpret_cast<uint16_t*>(more + 2 * Row::kGroups) = (uint16_t)(value >> 16);
   }
   template <int D>
-  __device__ __forceinline__ void get(const unsigned char* page, int page_size, int r, int u) {
+  __device__ __forceinline__ void get_codes(const unsigned char* page, int r, int u) {
     using Row = CodedRow<D, BITS>;
     const unsigned char* at = page + (size_t)r * Row::kCodes + Row::place(u);
     if constexpr (BITS == 4) w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
@@ -256,9 +256,17 @@ struct Unit {
       w[0] = x.x;
       w[kWords - 1] = x.y;
     }
-    const unsigned char* more = page + (size_t)page_size * Row::kCodes + (size_t)r * Row::kMore + (u / 8) * 2;
-    step = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(more)) << 16);
-    low = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(more + 2 * Row::kGroups)) << 16);
+  }
+  template <int D>
+  __device__ __forceinline__ static uint32_t get_more(const unsigned char* page, int page_size, int r, int group) {
+    using Row = CodedRow<D, BITS>;
+    const unsigned char* more = page + (size_t)page_size * Row::kCodes + (size_t)r * Row::kMore + group * 2;
+    return (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(more)) |
+           (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(more + 2 * Row::kGroups)) << 16;
+  }
+  __device__ __forceinline__ void scale(uint32_t more) {       // as CodeScale has it
+    step = __uint_as_float(more << 16);
+    low = __uint_as_float(more & 0xffff0000u);
   }
 };
 
@@ -437,27 +445,25 @@ coded_rows_kernel(CodedParams p) {
           }
         }
       } else {
-        Unit<BITS> kc[kBatch], vc[kBatch];
+        constexpr int kItems = PASS == kCodedLoad ? 2 * kBatch : kBatch;           // four rows of keys, and of values if they are wanted
+        Unit<BITS> c[kItems];
 #pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-          const int r = min(base + y * kRows + sub, live - 1);
-          kc[y].template get<D>(kpage, page_size, r, unit);
-          if (PASS == kCodedLoad) vc[y].template get<D>(vpage, page_size, r, unit);
-        }
+        for (int y = 0; y < kItems; ++y)
+          c[y].template get_codes<D>(y < kBatch ? kpage : vpage, min(base + y % kBatch * kRows + sub, live - 1), unit);
+        // the scales of a group's eight items, one by each of its lanes
+        const int mine = lane & 7;
+        const uint32_t more = Unit<BITS>::template get_more<D>(PASS == kCodedLoad && mine >= kBatch ? vpage : kpage, page_size,
+                                                               min(base + mine % kBatch * kRows + sub, live - 1), unit / 8);
 #pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-          const int r = base + y * kRows + sub;
+        for (int y = 0; y < kItems; ++y) {
+          const int r = base + y % kBatch * kRows + sub;
+          c[y].scale(__shfl_sync(0xffffffffu, more, (lane & 24) | y));
           float f[8];
+          c[y].values(f);
           Eight<T> back;
-          kc[y].values(f);
           back.round(f);
           if (PASS == kCodedBounds) b.add(back);
-          else if (r < live) {
-            back.store(static_cast<T*>(p.k_rows) + dense + (long long)r * D);
-            vc[y].values(f);
-            back.round(f);
-            back.store(static_cast<T*>(p.v_rows) + dense + (long long)r * D);
-          }
+          else if (r < live) back.store(static_cast<T*>(y < kBatch ? p.k_rows : p.v_rows) + dense + (long long)r * D);
         }
       }
     }
