@@ -71,13 +71,14 @@ coded_append_kernel(RopeParams p) {
         dst[vec] = src[vec];
         continue;
       }
+      // the item's frequencies: in fp32 a vector has half a unit's
+      const float2* turns = E == 8 ? turn[tok] + item : turn[tok] + (item & 1) * (kTurns / 2) * apart + (item >> 1);
       if (ADJACENT) {
         float f[E];
         RopeVec<T>::unpack(src[item], f);
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) {
-          const int i = item * (E / 2) + e;
-          const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+          const float2 cs = turns[e * apart];
           const float a = f[2 * e], b = f[2 * e + 1];
           f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
           f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
@@ -91,8 +92,7 @@ coded_append_kernel(RopeParams p) {
         RopeVec<T>::unpack(xb, b);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int i = item * E + e;
-          const float2 cs = turn[tok][(i % kTurns) * apart + i / kTurns];
+          const float2 cs = turns[e * apart];
           const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
           b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
           a[e] = y;
