@@ -259,7 +259,7 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
 /* The same for pools that hold cache_bits = 4 or 8 bits per element.  Every call below then takes and fills such pools (k_pages,
  * v_pages: device, 16-byte aligned, [n_pages][n_kv_heads][meda_pages_page_bytes]); `dtype` stays the type of queries, new rows, outputs
  * and bounds.  Every 64 dimensions of a row share a step and a lowest value, both bf16:
- *   low = min x rounded down,  step = max(2^-126, fl((max x - low) * fl(1 / (2^cache_bits - 1))) rounded up),
+ *   low = min x rounded down (a zero counts as +0),  step = max(2^-126, fl((max x - low) * fl(1 / (2^cache_bits - 1))) rounded up),
  *   code = rint(fl(fl(x - low) * fl(1 / step))),  an element reads back as low + step * code,
  * with fl the rounding of an fp32 operation: the same rows give the same bytes everywhere.  An element is off by half a step at most, and by
  * the roundings.  If any of the 64 is NaN or of magnitude 2^126 or more, all of them read back as NaN.
@@ -267,7 +267,7 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
  * lowest values.  Codes of a row: units of eight dimensions, unit i of group g at place i * (head_dim / 64) + g, in order from the lowest
  * bits up.
  * max_seqs * (max_seq_pages * page_size / 16 + 20) * n_kv_heads stays below 2^31 - 2^16 (times two with more than eight query heads per
- * KV head, times up to four at head_dim 256). */
+ * KV head at head_dim 256), a pool below 256 GiB. */
 meda_status meda_pages_create_quantised(const meda_pages_config* config, int32_t cache_bits, meda_pages** out);
 /* Bytes of one page of one KV head in a pool, whichever way it holds its rows. */
 int64_t meda_pages_page_bytes(const meda_pages* pages);
@@ -370,8 +370,10 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
  *   lse  device fp32 [n_seqs][n_q_heads], may be NULL: the logarithm of the softmax's sum, ready to join with the
  *        attention over rows kept elsewhere
  * A sequence of length 0 gets out = 0, lse = -inf.  In quantised caches rows count as what they read back as, before it is rounded to
- * `dtype`.  An infinite value makes its dimension of the output infinite; both
- * signs in one dimension, or a row whose weight is 0 in fp32 (below 2^-126 of the largest), make it NaN. */
+ * `dtype`; rows that read back as NaN make the outputs NaN that they have a part in (keys all of their KV head's, values those of their 64
+ * dimensions), and so does a query with an element that is not finite or of magnitude 2^110 or more, its own.  In other caches an
+ * infinite value makes its dimension of the output infinite; both signs in one dimension, or a row whose weight is 0 in fp32 (below
+ * 2^-126 of the largest), make it NaN. */
 meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
                                  const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
                                  const int32_t* sel, int32_t keep, void* out, float* lse, void* stream);

@@ -18,6 +18,8 @@
 // fp16's range.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "page_codes.cuh"
 #include "paged_attention.cuh"   // the walk's numbers, exp2_fast, store4, the states' layout
 #include "sm100_primitives.cuh"
@@ -109,6 +111,7 @@ struct AttnTileCoded {
   static constexpr int kStage = 2 * SUB * kHalf;                 // of a tile: keys and values of every run
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
   static constexpr int kScale = PARTS == 2 ? 14 : 6;             // weights stay below 2^(kScale + 1) (times 2^kSlack)
+  static constexpr float kMostQuery = 1.2980742e33f;             // 2^110: `factor` and its inverse stay in fp32's range
   static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference may stay this far (log2) behind the maximum
 
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
@@ -121,13 +124,26 @@ struct AttnTileCoded {
   float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
   int step_exp;                          // of twice the largest step when it was set (kScale - 125 at least)
 
+  // Two codes in the lower bits of a word's halves as an operand: as they are, c 2^-24, or for fp32 as normal numbers (1024 + c, less 1024).
+  static constexpr float kCodeScale = PARTS == 2 ? 1.f : 5.9604644775390625e-8f;
+  __device__ __forceinline__ static uint32_t operand(uint32_t codes) {
+    if constexpr (PARTS == 1) return codes;
+    const uint32_t x = codes | 0x64006400u, offset = 0x64006400u;
+    __half2 a, b;
+    memcpy(&a, &x, 4);
+    memcpy(&b, &offset, 4);
+    a = __hsub2(a, b);
+    uint32_t y;
+    memcpy(&y, &a, 4);
+    return y;
+  }
   // Pair j of a unit's eight codes, as the two halves of a word: elements (first, second).
   __device__ __forceinline__ static constexpr int pair_first(int j) { return BITS == 4 ? j : (j / 2) * 4 + j % 2; }
   __device__ __forceinline__ static constexpr int pair_second(int j) { return BITS == 4 ? j + 4 : (j / 2) * 4 + j % 2 + 2; }
   __device__ __forceinline__ static constexpr float pair_factor(int j) { return BITS == 4 && j % 2 == 1 ? 0.0625f : 1.f; }
   __device__ __forceinline__ static uint32_t pair_of(const uint32_t* unit, int j) {
-    if constexpr (BITS == 4) return (j < 2 ? unit[0] : unit[0] >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu);
-    else return (j % 2 ? unit[j / 2] >> 8 : unit[j / 2]) & 0x00ff00ffu;
+    if constexpr (BITS == 4) return operand((j < 2 ? unit[0] : unit[0] >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu));
+    else return operand((j % 2 ? unit[j / 2] >> 8 : unit[j / 2]) & 0x00ff00ffu);
   }
   __device__ __forceinline__ static float step_of(const uint32_t (&w)[G], int g) {
     return __uint_as_float(g % 2 == 0 ? w[g / 2] << 16 : w[g / 2] & 0xffff0000u);
@@ -159,7 +175,7 @@ struct AttnTileCoded {
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int k2 = min(126, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
-      const float scale = top < INFINITY ? power_of_two(k2) : NAN;               // a query that is not finite makes its logits NaN
+      const float scale = top < kMostQuery ? power_of_two(k2) : NAN;             // a query that is not finite, or huge, makes its logits NaN
       float sum[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) sum[g] = 0.f;
@@ -180,7 +196,7 @@ struct AttnTileCoded {
       for (int g = 0; g < G; ++g) {
         sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
         sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
-        sum[g] *= 5.9604644775390625e-8f;                                        // 2^-24, as the products with codes have it
+        sum[g] *= kCodeScale;                                                    // as the products with codes have it
       }
       // A has the lowest values twice (G <= 2) or two pairs of them (G = 4) in every lane's columns; B the parts, one after the other
       if constexpr (G == 4) {
@@ -200,7 +216,7 @@ struct AttnTileCoded {
         qsum[n][0] = c == 0 ? hi : c == 1 ? lo : 0u;
         qsum[n][1] = c == 0 ? mid : 0u;
       }
-      const float back = scale == scale ? power_of_two(-k2) * (scale_log2 * 16777216.f) : NAN;       // 2^24: the codes' own scale
+      const float back = scale == scale ? power_of_two(-k2) * (scale_log2 / kCodeScale) : NAN;
       factor[n][0] = __shfl_sync(0xffffffffu, back, 8 * c);                      // head 2c is lane 4 * 2c's
       factor[n][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
     }
@@ -262,22 +278,30 @@ struct AttnTileCoded {
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      float acc[NH][4];
+      float acc[NH][4], low_parts[NH][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t *u0 = &k[0][(i * G + g) * W], *u1 = &k[1][(i * G + g) * W];
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           const uint32_t a0 = pair_of(u0, j), a1 = pair_of(u1, j), a2 = pair_of(u0, j + 1), a3 = pair_of(u1, j + 1);
+          const bool first = i == 0 && j == 0;
 #pragma unroll
-          for (int n = 0; n < NH; ++n)
-#pragma unroll
-            for (int x = 0; x < PARTS; ++x) {
-              if (i == 0 && j == 0 && x == 0) mma_f16_first(acc[n], a0, a1, a2, a3, q[n][x][i][g][j], q[n][x][i][g][j + 1]);
-              else mma_f16(acc[n], a0, a1, a2, a3, q[n][x][i][g][j], q[n][x][i][g][j + 1]);
+          for (int n = 0; n < NH; ++n) {
+            if (first) mma_f16_first(acc[n], a0, a1, a2, a3, q[n][0][i][g][j], q[n][0][i][g][j + 1]);
+            else mma_f16(acc[n], a0, a1, a2, a3, q[n][0][i][g][j], q[n][0][i][g][j + 1]);
+            if constexpr (PARTS == 2) {                        // a sum by itself
+              if (first) mma_f16_first(low_parts[n], a0, a1, a2, a3, q[n][PARTS - 1][i][g][j], q[n][PARTS - 1][i][g][j + 1]);
+              else mma_f16(low_parts[n], a0, a1, a2, a3, q[n][PARTS - 1][i][g][j], q[n][PARTS - 1][i][g][j + 1]);
             }
+          }
         }
       }
+      if constexpr (PARTS == 2)
+#pragma unroll
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[n][e] += low_parts[n][e];
       const float s0 = step_of(km[0], g), s1 = step_of(km[1], g);
 #pragma unroll
       for (int n = 0; n < NH; ++n) {
@@ -350,7 +374,8 @@ struct AttnTileCoded {
           most = none ? most : fmaxf(most, ref[n][x]);
           const float to_ref = most == -INFINITY ? 0.f : most;
           const float f = none ? 1.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
-          limit[n][x] = most == -INFINITY ? -INFINITY : __fdividef(most + kSlack, factor[n][x]);      // (need not be exact)
+          // (rather too low, by more than the quotient may be off: a logit beyond it would overflow the weights)
+          limit[n][x] = most == -INFINITY ? -INFINITY : __fdividef(most + kSlack - 1.9073486e-6f * fabsf(most), factor[n][x]);
           ref[n][x] = to_ref;
           l[n][x] *= f;
 #pragma unroll
@@ -414,23 +439,31 @@ struct AttnTileCoded {
           x1 = t0 >> 8;
           x2 = t1;
           x3 = t1 >> 8;
-          a[0][0] = x0 & 0x000f000fu; a[0][1] = x1 & 0x000f000fu; a[0][2] = x2 & 0x000f000fu; a[0][3] = x3 & 0x000f000fu;
-          a[1][0] = x0 & 0x00f000f0u; a[1][1] = x1 & 0x00f000f0u; a[1][2] = x2 & 0x00f000f0u; a[1][3] = x3 & 0x00f000f0u;
+          a[0][0] = operand(x0 & 0x000f000fu); a[0][1] = operand(x1 & 0x000f000fu); a[0][2] = operand(x2 & 0x000f000fu); a[0][3] = operand(x3 & 0x000f000fu);
+          a[1][0] = operand(x0 & 0x00f000f0u); a[1][1] = operand(x1 & 0x00f000f0u); a[1][2] = operand(x2 & 0x00f000f0u); a[1][3] = operand(x3 & 0x00f000f0u);
         } else {
           const int w = g * W + (W - 1) * y;
           x0 = __byte_perm(v[0][w], v[1][w], 0x5410);
           x1 = __byte_perm(v[0][w], v[1][w], 0x7632);
           x2 = __byte_perm(v[2][w], v[3][w], 0x5410);
           x3 = __byte_perm(v[2][w], v[3][w], 0x7632);
-          a[0][0] = x0 & 0x00ff00ffu; a[0][1] = x1 & 0x00ff00ffu; a[0][2] = x2 & 0x00ff00ffu; a[0][3] = x3 & 0x00ff00ffu;
-          a[1][0] = x0 >> 8 & 0x00ff00ffu; a[1][1] = x1 >> 8 & 0x00ff00ffu; a[1][2] = x2 >> 8 & 0x00ff00ffu; a[1][3] = x3 >> 8 & 0x00ff00ffu;
+          a[0][0] = operand(x0 & 0x00ff00ffu); a[0][1] = operand(x1 & 0x00ff00ffu); a[0][2] = operand(x2 & 0x00ff00ffu); a[0][3] = operand(x3 & 0x00ff00ffu);
+          a[1][0] = operand(x0 >> 8 & 0x00ff00ffu); a[1][1] = operand(x1 >> 8 & 0x00ff00ffu);
+          a[1][2] = operand(x2 >> 8 & 0x00ff00ffu); a[1][3] = operand(x3 >> 8 & 0x00ff00ffu);
         }
 #pragma unroll
         for (int z = 0; z < 2; ++z)
 #pragma unroll
-          for (int n = 0; n < NH; ++n)
+          for (int n = 0; n < NH; ++n) {
+            if constexpr (PARTS == 1) mma_f16(o[g][2 * y + z][n], a[z][0], a[z][1], a[z][2], a[z][3], b[n][0][g][0], b[n][0][g][1]);
+            else {
+              float part[4];
+              mma_f16_first(part, a[z][0], a[z][1], a[z][2], a[z][3], b[n][0][g][0], b[n][0][g][1]);
+              mma_f16(part, a[z][0], a[z][1], a[z][2], a[z][3], b[n][PARTS - 1][g][0], b[n][PARTS - 1][g][1]);
 #pragma unroll
-            for (int x = 0; x < PARTS; ++x) mma_f16(o[g][2 * y + z][n], a[z][0], a[z][1], a[z][2], a[z][3], b[n][x][g][0], b[n][x][g][1]);
+              for (int e = 0; e < 4; ++e) o[g][2 * y + z][n][e] += part[e];
+            }
+          }
       }
   }
   // The sums of every lane's two heads: l and the lowest values' share over all rows, then f(head, its l, its reference, values of unit r of
@@ -438,7 +471,7 @@ struct AttnTileCoded {
   template <typename F>
   __device__ __forceinline__ void finish(int heads, int lane, F f) {
     const int r = lane / 4, c = lane % 4;
-    const float a = power_of_two(24 - kScale), e = power_of_two(step_exp), odd = BITS == 4 ? 0.0625f * a : a;
+    const float a = power_of_two(PARTS == 2 ? -kScale : 24 - kScale), e = power_of_two(step_exp), odd = BITS == 4 ? 0.0625f * a : a;
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll

@@ -322,6 +322,8 @@ meda_status pages_create(const meda_pages_config* config, int bits, meda_pages**
   if ((int64_t)c.max_seqs * c.max_seq_pages * (c.page_size / 16) * c.n_kv_heads >= (int64_t(1) << 31) ||
       (int64_t)c.n_pages * c.n_kv_heads * c.page_size >= (int64_t(1) << 40))
     return MEDA_ERR_SHAPE;
+  // quantised pages are addressed in 32 bits, in units of 64 bytes
+  if (bits && (int64_t)c.n_pages * c.n_kv_heads * (coded_page_bytes(c.head_dim, bits, c.page_size) / 64) >= (int64_t(1) << 32)) return MEDA_ERR_SHAPE;
   int64_t half = 0;
   for (int a = 0; a < 3; ++a) {
     if (c.rope_sections[a] < 0 || c.rope_sections[a] > c.head_dim / 2) return MEDA_ERR_SHAPE;

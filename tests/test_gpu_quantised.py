@@ -562,6 +562,64 @@ def test_queries_of_every_size(B, bits, dtype):
     pg.close()
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_huge_logits_and_queries(B, bits, dtype):
+    """Logits of up to 10^8 in an order that moves the maximum in every tile (weights in fp16 must not overflow), queries of 2^100 with keys as small,
+    and of 2^110, which are refused as NaN."""
+    lens, hq, hkv, d, page = [300, 300, 300, 40], 2, 1, 64, 16
+    pg, q, kp, vp, table, out, lse = attention_case(B, lens, hq, hkv, d, dtype, page, bits, seed=12)
+    k = np.zeros((kp.shape[0], hkv, page, d))
+    rows = np.arange(300)
+    for i, top in ((0, 1e8), (1, 1e4), (2, 2.0 ** -90)):
+        for c in range(O.n_pages_of(300, page)):
+            at = rows[c * page:(c + 1) * page]
+            k[table[i, c], 0, :len(at), 0] = top * (at + 1) / 300
+    k[table[0, 18], 0, 5] = 0.0
+    kp.copy_(torch.as_tensor(O.pack_page(*O.quantise(k.astype(np.float32), bits), bits)))
+    q.zero_()
+    q[0, :, 0], q[1, :, 0], q[2, :, 0], q[3, 0, 3], q[3, 1, 3] = 1.0, 1.0, 2.0 ** 100, 2.0 ** 110, -(2.0 ** 109)
+    pg.paged_attention(q, kp, vp, T.i32(table.tolist()), T.i32(lens), out, lse)
+    pg.check()
+    check_attention(out[:3], lse[:3], q[:3], kp, vp, table[:3], lens[:3], page, bits, dtype)
+    assert out[3, 0].isnan().all() and lse[3, 0].isnan() and not out[3, 1].isnan().any()       # (keys of 0 there)
+    pg.close()
+
+
+@pytest.mark.parametrize("dtype,bits,hq,d", [("bf16", 4, 1, 256), ("f32", 4, 2, 256), ("bf16", 8, 1, 256), ("bf16", 4, 16, 128), ("f32", 8, 9, 64)])
+def test_attention_of_the_largest_batch(B, dtype, bits, hq, d):
+    """8,192 sequences of 0 to 40 rows: the prefix sums leave the least shared memory to the rings.  Outputs by a plain form on the device in
+    64 bits, to the bound of check_attention, with the keys' and values' sizes as they are."""
+    page, n = 16, 8192
+    lens = np.random.default_rng(1).integers(0, 41, n)
+    n_pages = 700
+    pg = T.make(B, n_q_heads=hq, n_kv_heads=1, head_dim=d, dtype=dtype, page_size=page, n_pages=n_pages, max_seqs=n, max_seq_pages=3, cache_bits=bits)
+    rng = np.random.default_rng(2)
+    pools, held = [], []
+    for std in (0.3, 0.5):
+        code, step, low = O.quantise(rng.normal(0.1, std, (n_pages, 1, page, d)).astype(np.float32), bits)
+        pools.append(torch.as_tensor(O.pack_page(code, step, low, bits), device="cuda"))
+        sizes = O.held(code, step, 0 * low) + np.abs(O.held(0 * code, step, low))
+        held += [torch.as_tensor(x, device="cuda") for x in (O.held(code, step, low)[:, 0], sizes[:, 0])]
+    table = torch.as_tensor(rng.integers(0, n_pages, (n, 3)).astype(np.int32), device="cuda")          # (read only: pages may be shared)
+    q = T.normal((n, hq, d), DT[dtype], 3, 0.0, 2.0)
+    out, lse = torch.full_like(q, math.nan), torch.full((n, hq), math.nan, device="cuda")
+    pg.paged_attention(q, *pools, table, T.i32(lens.tolist()), out, lse)
+    pg.check()
+    k, k_size, v, v_size = (x[table.long()].flatten(1, 2) for x in held)
+    live = torch.arange(48, device="cuda")[None] < torch.as_tensor(lens, device="cuda")[:, None]
+    s = torch.where(live[:, None], q.double() @ k.transpose(1, 2) / math.sqrt(d), -math.inf)
+    p = torch.where(live.any(1)[:, None, None], torch.softmax(s, -1), 0.0)
+    want, mag = p @ v, torch.where(live[:, None], q.double().abs() @ k_size.transpose(1, 2) / math.sqrt(d), 0.0).amax(-1, keepdim=True)
+    delta = (d + 32) * 2.0 ** -22 * mag
+    tol = (p @ v_size) * (2 * delta * (1 + delta) + 2.0 ** -15 + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 1.01) + T.HALF_STEP[dtype] * 1.01 * want.abs() + 1e-6
+    assert ((out.double() - want).abs() <= tol).all()
+    norm = torch.logsumexp(s, -1)
+    assert torch.equal(lse.isinf(), norm.isinf())
+    assert ((lse.double() - norm).abs() <= delta[..., 0] + 2.0 ** -15 + 2.0 ** -21 * norm.abs())[~norm.isinf()].all()
+    pg.close()
+
+
 def test_bad_pages_and_lengths_are_reported_and_skipped(B):
     page, d, lens, bits = 16, 64, [48, 33], 4
     pg, q, kp, vp, table, out, lse = attention_case(B, lens, 2, 1, d, "bf16", page, bits, seed=8)

@@ -35,6 +35,19 @@ def test_create_refuses_what_other_handles_refuse(B, status, kw, bits):
     assert e.value.status == status
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_pools_of_256_gib_are_refused(B, bits):
+    geometry = dict(n_q_heads=16, n_kv_heads=8, head_dim=256, dtype="bf16", page_size=256, max_seqs=1, max_seq_pages=1)
+    n_pages = -(-2 ** 38 // (8 * 256 * (256 * bits // 8 + 16)))
+    with pytest.raises(B.MedaError) as e:
+        B.Pages(**geometry, n_pages=n_pages, cache_bits=bits)
+    assert e.value.status == B.MEDA_ERR_SHAPE
+    try:
+        B.Pages(**geometry, n_pages=n_pages - 1, cache_bits=bits).close()
+    except B.MedaError as e:                                       # (without a GPU, but past the shapes)
+        assert e.status == B.MEDA_ERR_CUDA
+
+
 def test_null_handles(B):
     lib = B.load_library()
     one = 256                                                      # never dereferenced
