@@ -3,10 +3,17 @@
 // A key's codes hang on borders, so its rotation is stated to the bit: the angle is exact (64-bit fixed point), its sine and
 // cosine come from 64-bit arithmetic and are rounded to fp32, the two products and their sum are rounded one by one, and the key
 // is rounded to the cache's type before it is quantised.  A prompt appended here and one rotated elsewhere give the same pages.
+// (64-bit sines cost 0.8 us of a prompt's 65: a block works each out once for all heads.)
 //
-// A block takes a few tokens.  Queries go by pairs of vectors (both read before either is written: q_out may be q), keys
-// and values by units of eight dimensions, eight neighbouring lanes to a group; a lane reads its unit and, with paired halves, the
-// unit's partner.
+// A block takes a few tokens.  Keys and values go by units of eight dimensions, eight neighbouring lanes to a group; a lane reads its
+// unit and, with paired halves, the unit's partner (taking it from the other lane by shuffles measured the same).  Queries go by pairs of
+// vectors (both read before either is written: q_out may be q).
+//
+// Bound by memory with its latency: 18,944 tokens of 28 + 4 + 4 heads of 128 at 4 bits, 322 MB, in 59.8 us, 82 % of a plain copy; 64 tokens 3.4 us.
+// What helps is warps, not loads ahead.  Keys first, and the 32 registers that eight blocks per SM leave: 64.6 -> 62.4 -> 59.8 us (9,000
+// tokens in fp32 53.7 -> 50.7); the first units fetched before the sines 65.9, four tokens' units and queries on their way at once, their
+// scales shared out among a group's lanes, 74 to 90.  It is the other way with neighbouring pairs in bf16 (40 registers 64.9 us, 32 66.5) and
+// where keys and values outweigh the queries (9,000 tokens of 32 + 32 + 32 heads 92 -> 98 us).
 #pragma once
 
 #include "page_codes.cuh"
@@ -15,7 +22,7 @@
 namespace meda {
 
 template <typename T, int D, int BITS, bool ADJACENT>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 8)
 coded_append_kernel(RopeParams p) {
   constexpr int E = RopeVec<T>::E;
   begin_grid();
@@ -45,63 +52,6 @@ coded_append_kernel(RopeParams p) {
     turn[tok][(i % kTurns) * apart + i / kTurns] = make_float2((float)c, (float)s);
   }
   __syncthreads();
-
-  // ---- queries
-  const int rot = ADJACENT ? 2 * half / E : half / E;          // items of a head that rotate
-  const int per_head = rot + (VR - 2 * half / E);
-  // (indexes go up by what a turn of the block adds to them: divisions in every turn would cost more than the rotation)
-  if (p.q) {
-    const int turn_heads = kRopeThreads / per_head, turn_items = kRopeThreads % per_head;
-    int h = threadIdx.x / per_head, item = threadIdx.x % per_head, tok = 0;
-    for (;; h += turn_heads, item += turn_items) {
-      if (item >= per_head) {
-        item -= per_head;
-        ++h;
-      }
-      while (h >= p.n_q_heads) {
-        h -= p.n_q_heads;
-        ++tok;
-      }
-      if (tok >= n_tok) break;
-      if (slot_of[tok] < 0) continue;
-      const uint4* src = static_cast<const uint4*>(p.q) + (t0 + tok) * p.q_stride + h * VR;
-      uint4* dst = static_cast<uint4*>(p.q_out) + ((size_t)(t0 + tok) * p.n_q_heads + h) * VR;
-      if (item >= rot) {
-        const int vec = 2 * half / E + (item - rot);
-        dst[vec] = src[vec];
-        continue;
-      }
-      // the item's frequencies: in fp32 a vector has half a unit's
-      const float2* turns = E == 8 ? turn[tok] + item : turn[tok] + (item & 1) * (kTurns / 2) * apart + (item >> 1);
-      if (ADJACENT) {
-        float f[E];
-        RopeVec<T>::unpack(src[item], f);
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          const float2 cs = turns[e * apart];
-          const float a = f[2 * e], b = f[2 * e + 1];
-          f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
-          f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
-        }
-        dst[item] = RopeVec<T>::pack(f);
-      } else {
-        float a[E], b[E];
-        const int other = item + half / E;
-        const uint4 xa = src[item], xb = src[other];
-        RopeVec<T>::unpack(xa, a);
-        RopeVec<T>::unpack(xb, b);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float2 cs = turns[e * apart];
-          const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
-          b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
-          a[e] = y;
-        }
-        dst[item] = RopeVec<T>::pack(a);
-        dst[other] = RopeVec<T>::pack(b);
-      }
-    }
-  }
 
   // ---- keys and values: a whole warp goes round together, its groups of eight lanes are all in or all out
   const int page_size = 1 << p.page_shift;
@@ -168,6 +118,63 @@ coded_append_kernel(RopeParams p) {
     c.template put_codes<D>(page, row, u);
     if (u % 8 == 0) Unit<BITS>::template put_more<D>(page, page_size, row, u / 8, by.more);
   }
+  // ---- queries
+  const int rot = ADJACENT ? 2 * half / E : half / E;          // items of a head that rotate
+  const int per_head = rot + (VR - 2 * half / E);
+  // (indexes go up by what a turn of the block adds to them: divisions in every turn would cost more than the rotation)
+  if (p.q) {
+    const int turn_heads = kRopeThreads / per_head, turn_items = kRopeThreads % per_head;
+    int h = threadIdx.x / per_head, item = threadIdx.x % per_head, tok = 0;
+    for (;; h += turn_heads, item += turn_items) {
+      if (item >= per_head) {
+        item -= per_head;
+        ++h;
+      }
+      while (h >= p.n_q_heads) {
+        h -= p.n_q_heads;
+        ++tok;
+      }
+      if (tok >= n_tok) break;
+      if (slot_of[tok] < 0) continue;
+      const uint4* src = static_cast<const uint4*>(p.q) + (t0 + tok) * p.q_stride + h * VR;
+      uint4* dst = static_cast<uint4*>(p.q_out) + ((size_t)(t0 + tok) * p.n_q_heads + h) * VR;
+      if (item >= rot) {
+        const int vec = 2 * half / E + (item - rot);
+        dst[vec] = src[vec];
+        continue;
+      }
+      // the item's frequencies: in fp32 a vector has half a unit's
+      const float2* turns = E == 8 ? turn[tok] + item : turn[tok] + (item & 1) * (kTurns / 2) * apart + (item >> 1);
+      if (ADJACENT) {
+        float f[E];
+        RopeVec<T>::unpack(src[item], f);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) {
+          const float2 cs = turns[e * apart];
+          const float a = f[2 * e], b = f[2 * e + 1];
+          f[2 * e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
+          f[2 * e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+        }
+        dst[item] = RopeVec<T>::pack(f);
+      } else {
+        float a[E], b[E];
+        const int other = item + half / E;
+        const uint4 xa = src[item], xb = src[other];
+        RopeVec<T>::unpack(xa, a);
+        RopeVec<T>::unpack(xb, b);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float2 cs = turns[e * apart];
+          const float y = __fsub_rn(__fmul_rn(a[e], cs.x), __fmul_rn(b[e], cs.y));
+          b[e] = __fadd_rn(__fmul_rn(b[e], cs.x), __fmul_rn(a[e], cs.y));
+          a[e] = y;
+        }
+        dst[item] = RopeVec<T>::pack(a);
+        dst[other] = RopeVec<T>::pack(b);
+      }
+    }
+  }
+
 }
 
 }  // namespace meda
