@@ -343,11 +343,13 @@ class PagedDecoder:
     def read(self, request: int, k, v, lens_from=None):
         """The rows that `request` holds, of all layers, into k, v [L][Hkv][capacity][d], to hand the request on or to compress again what
         it has gathered: rows [lens_from, length) of every layer to rows 0 and on, lens_from int32 [L] (None: all of them).  Returns
-        the rows' numbers, int32 [L].  A layer with more rows than `capacity` is recorded for check() and left out."""
+        the rows' numbers, int32 [L].  A layer with more rows than `capacity` is recorded for check() and left out.  (Between begin_step and a
+        layer's attend the layer's newest row is not there yet.)"""
         L, R = self.n_layers, self.max_requests
         self._check_request(request)
         self._check_dense(k, v)
-        lens = self.lens.view(L, R)[:, request].contiguous()
+        lens = self.lens.view(L, R)[:, request].clone(memory_format=torch.contiguous_format)     # (the caller's: later steps leave it alone)
+        lens_from = None if lens_from is None else lens_from.contiguous()
         table = self.table.view(L, R, -1)[:, request].contiguous()
         self.pages.page_load(self.k_pages, self.v_pages, table, lens, k, v, lens_from=lens_from)
         return lens if lens_from is None else (lens - lens_from).clamp_(min=0)

@@ -163,6 +163,27 @@ def test_read_gives_rows_from_anywhere_and_refuses(B, bits):
     cp.close()
 
 
+def test_read_of_the_only_request(B):
+    """The numbers of rows are the caller's own: a release later on does not change them.  Where reading begins may be a column."""
+    wl = S.workload()
+    cp = S.compressed(wl)
+    dec = S.decoder(wl, 60, 1, 400, cache_bits=4)
+    dec.admit(0, cp)
+    b = cp.budgets[:, 0].tolist()
+    whole = torch.zeros((2, wl.n_layers, wl.n_kv_heads, max(b), wl.head_dim), dtype=wl.torch_dtype, device="cuda")
+    count = dec.read(0, whole[0], whole[1])
+    tail = torch.full_like(whole, 5.0)
+    first = T.i32([[x - 3, 0] for x in b])[:, 0]
+    assert dec.read(0, tail[0], tail[1], first).tolist() == [3] * wl.n_layers
+    dec.check()
+    for l in range(wl.n_layers):
+        assert torch.equal(tail[:, l, :, :3], whole[:, l, :, b[l] - 3:b[l]]) and (tail[:, l, :, 3:] == 5).all()
+    dec.release(0)
+    assert count.tolist() == b
+    dec.close()
+    cp.close()
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_two_handles_on_two_streams_and_two_graphs(B, bits):
     lens = [3000, 17, 900]
