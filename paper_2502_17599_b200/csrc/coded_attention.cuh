@@ -4,7 +4,12 @@
 // (p step_g) codes_g + p low_g.  So the matrix instructions multiply by the codes themselves, and a code is its own fp16 operand: the whole
 // number c in the lower bits of a half is the subnormal c 2^-24, exact, and needs no conversion, offset or scale, only a mask
 // (and at 4 bits c << 4, a nibble further up, is 16 c 2^-24: the factor goes into the queries and out of the result).  Steps, lowest
-// values, logits, maxima and sums are fp32; products of the queries with codes are exact and added in fp32.
+// values, logits, maxima and sums are fp32.
+//
+// The matrix instructions cut off what a product's sum has below its largest term, and take a subnormal for as large as the smallest
+// normal number: with codes as they are a logit is off by some 2^-20 of its products' sum.  In bf16 that is far below the output's own
+// rounding; for fp32 outputs (2e-6 to 5e-6 over 30,000 rows) it is not.  There codes become normal numbers (one more instruction for two), the
+// low parts of queries add up by themselves, and a run's values are added to the sums outside: 5e-7 to 1.5e-6, at 443 MB 111 -> 146 us.
 //
 // Fragments, lane l: r = l / 4, c = l % 4.  Q K^T has A = codes of the keys (rows r and r + 8 of the tile), B = queries (column r: head r),
 // group by group; sum(q) low is one instruction of bf16, the sums in three parts.  P V has A = codes of the values, transposed
@@ -15,7 +20,13 @@
 // that matters exactly (the rest is below 2^-38 of the largest); fp32 ones go in two parts.  A weight p step is rounded to
 // fp16 (2^-11 of itself: a quarter of the output's own rounding in bf16 at worst, and it averages out over the rows), for fp32 caches to two
 // such parts; weights are scaled by a power of two that follows the largest step a warp has met, so that neither tiny nor huge values leave
-// fp16's range.
+// fp16's range.  The reference of the exponentials moves only when a logit passes it by 2^8 (bf16; in fp32 at once, the parts need the range):
+// bringing the sums to a new one costs as much as a tile.
+//
+// Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 9.2 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
+// rows, 28 / 4 heads of 128, 443 MB: 83 us, 82 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
+// ten of up to 32,768 rows, 32 heads, 765 MB: 123 us, 95 %; 192 of 36 to 18,944 rows, 342 MB: 71 us, 74 %; one of 129,072 rows, 74 MB: 25 us, 45 %
+// (copies alone 22.5); one of 947 rows 9.8 us.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -503,13 +514,15 @@ struct AttnTileCoded {
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 // Every warp takes an equal run of the tiles of its block, whose share is that of paged_attention_kernel, and goes through it by itself: its
-// tiles come through a ring of its own in shared memory (cp.async, 16 bytes a lane: 4-bit rows are so short that a tile's arithmetic has
-// to fit 200 cycles of an SM to keep up with memory, and no register is left for tiles on their way), and segments (sequence, KV
+// tiles come through a ring of its own in shared memory (cp.async, 16 bytes a lane: no register is left for tiles on their way.  A warp that
+// loaded for the others with bulk copies, four a tile, took 390 cycles for each whatever its size), and segments (sequence, KV
 // head) that lie in its run are finished by it alone.  Those that cross warps leave states in shared memory, which the block joins in the
 // end, and those that cross blocks states in scratch, as there.  (With the tiles dealt round all warps and a joining at the end of every
-// segment a block of short segments took twice as long as one inside a long one.)
+// segment the 192 ragged caches took 167 us against 77 then.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
-// kAttLeast but in rows.
+// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches took 82.5, 77, 71.5 and 71.9 us; with blocks of 64, 128,
+// 256, 384 and 512 rows at least one cache of 947 rows took 8.8, 9.6, 9.3, 9.8 and 11.3 us, one of 4,000 11.2, 10.5, 9.7, 10.5 and 11.6, and
+// long ones want the larger.
 constexpr int kCodedSegment = 128, kCodedLeast = 384;
 
 template <int N>

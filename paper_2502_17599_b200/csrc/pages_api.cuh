@@ -142,16 +142,23 @@ struct CodedAttnKernel {
   }
 };
 
+// Rows of a tile, warps and ring by head size, bits and group; one block per SM.  A tile has 32 rows at 4 bits and 16 at 8, which are about as many
+// bytes: at 4 bits and 16 rows the work of a tile that does not depend on its rows shows.  Warps are what the registers allow without spills in
+// bf16, stages what the warps leave of shared memory (with the largest batches one at head_dim 256).  443 MB at 4 bits, 28 / 4 heads: head_dim
+// 128, eight warps with three tiles each 95 us, twelve with two 83.0, with three 83.4, sixteen with two 85; head_dim 64, twelve warps 110,
+// sixteen 101.
 template <typename T, int BITS, typename F>
 meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
   constexpr int kSub = BITS == 4 ? 2 : 1;
   if (d == 64) {
-    if constexpr (BITS == 4) return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, 4, 2>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, 4, 2>, 64, 12, 3>());
-    else return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, 8, 1>, 64, 16, 3>()) : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, 8, 1>, 64, 12, 4>());
+    constexpr int kMany = BITS == 4 ? 3 : 4;                   // (`counts` has no room for four of 32 rows)
+    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 64, 1, BITS, kSub>, 64, 16, 3>())
+                  : f(CodedAttnKernel<AttnTileCoded<T, 64, 2, BITS, kSub>, 64, 12, kMany>());
   }
   if (d == 128)
-    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS, kSub>, 128, 12, 2>()) : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS, kSub>, 128, 8, 3>());
+    return g <= 8 ? f(CodedAttnKernel<AttnTileCoded<T, 128, 1, BITS, kSub>, 128, 12, 2>())
+                  : f(CodedAttnKernel<AttnTileCoded<T, 128, 2, BITS, kSub>, 128, 8, 3>());
   return f(CodedAttnKernel<AttnTileCoded<T, 256, 1, BITS, kSub>, 256, 8, 2>());
 }
 
@@ -323,7 +330,8 @@ meda_status pages_create(const meda_pages_config* config, int bits, meda_pages**
       (int64_t)c.n_pages * c.n_kv_heads * c.page_size >= (int64_t(1) << 40))
     return MEDA_ERR_SHAPE;
   // quantised pages are addressed in 32 bits, in units of 64 bytes
-  if (bits && (int64_t)c.n_pages * c.n_kv_heads * (coded_page_bytes(c.head_dim, bits, c.page_size) / 64) >= (int64_t(1) << 32)) return MEDA_ERR_SHAPE;
+  if (bits && (int64_t)c.n_pages * c.n_kv_heads * (coded_page_bytes(c.head_dim, bits, c.page_size) / 64) >= (int64_t(1) << 32))
+    return MEDA_ERR_SHAPE;
   int64_t half = 0;
   for (int a = 0; a < 3; ++a) {
     if (c.rope_sections[a] < 0 || c.rope_sections[a] > c.head_dim / 2) return MEDA_ERR_SHAPE;
