@@ -16,8 +16,8 @@
 // Bound by memory where the arithmetic lets it: some 60 instructions go into eight elements of bf16 with bounds, so it is fp32 pairs in one
 // instruction (f32x2), extremes of two bf16 at once, sums with 2^23 in place of conversions, and one scale per lane for eight rows of a
 // group, handed round, in place of eight equal ones.  28 layers of a 19K-token prompt (4 heads of 128, bf16, 4 bits): stored with
-// their bounds, 330 MB, in 83 us, 61 % of a plain copy (116 before those; without bounds 72), read back, 315 MB, in 54 us, 88 %; 64 caches read
-// back from 8 bits, 629 MB, in 103 us, 93 %.  The same prompt in fp32 125 and 116 us.
+// their bounds, 330 MB, in 72 us, 70 % of a plain copy (without bounds 62), read back, 315 MB, in 54 us, 88 %; 64 caches read
+// back from 8 bits, 629 MB, in 103 us, 93 %.  The same prompt in fp32 122 and 100 us.
 #pragma once
 
 #include "page_rows.cuh"
@@ -341,8 +341,15 @@ __device__ __forceinline__ void load_span(const int32_t* lens_from, const int32_
   if (from >= rows) from = rows = 0;
 }
 
+// Blocks per SM that the registers are to leave room for.  Storing from bf16, four instead of the two of 104 registers: the 19K-token prompt 83.4 -> 72.8
+// us (five 81), from fp32 two (120 us, three 146); loading into fp32 three instead of four 116 -> 101.5 us, into bf16 no matter.
+template <typename T, int BITS, CodedPass PASS>
+constexpr int kCodedBlocks = PASS == kCodedStore ? (sizeof(T) == 2 ? 4 : 2) : sizeof(T) == 4 ? 3 : BITS == 4 ? 5 : 4;
+
+// (Several warps to a page where there are fewer pages than warps: a prompt of 592 pages read back 17 -> 11.5 us by itself but 72.3 -> 71.1 behind its
+// append, a step of 64 tokens with its reading back 8.5 -> 10.1: more code to fetch.)
 template <typename T, int D, int BITS, CodedPass PASS>
-__global__ void __launch_bounds__(kRowsThreads)
+__global__ void __launch_bounds__(kRowsThreads, kCodedBlocks<T, BITS, PASS>)
 coded_rows_kernel(CodedParams p) {
   begin_grid();
   using Row = CodedRow<D, BITS>;
@@ -381,17 +388,16 @@ coded_rows_kernel(CodedParams p) {
     span(i, from, rows);
     return ((rows + page_size - 1) >> p.page_shift) - (from >> p.page_shift);
   });
-  const long long total = (long long)rows_smem[p.n_seqs] * p.n_heads;
+  const unsigned total = (unsigned)rows_smem[p.n_seqs] * p.n_heads;              // (below 2^31, as all sequences' tiles together)
   const int warps = gridDim.x * (kRowsThreads / 32);
 #pragma unroll 1
-  for (long long x = (long long)blockIdx.x * (kRowsThreads / 32) + warp; x < total; x += warps) {
-    const int i = ragged_find(rows_smem, p.n_seqs, (int)(x / p.n_heads));
-    const int count = rows_smem[i + 1] - rows_smem[i];
-    const long long local = x - (long long)rows_smem[i] * p.n_heads;
+  for (unsigned x = blockIdx.x * (kRowsThreads / 32) + warp; x < total; x += warps) {
+    const int i = ragged_find(rows_smem, p.n_seqs, (int)(x / (unsigned)p.n_heads));
+    const unsigned count = rows_smem[i + 1] - rows_smem[i], local = x - (unsigned)rows_smem[i] * p.n_heads;
     const int g = (int)(local / count);
     int from, rows;
     span(i, from, rows);
-    const int col = (from >> p.page_shift) + (int)(local % count);
+    const int col = (from >> p.page_shift) + (int)(local - g * count);
     const int page = p.table[(size_t)i * p.width + col];
     if ((unsigned)page >= (unsigned)p.n_pages) {
       if (lane == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
@@ -515,17 +521,16 @@ page_load_kernel(LoadParams p) {
     span(i, from, rows);
     return ((rows + page_size - 1) >> p.page_shift) - (from >> p.page_shift);
   });
-  const long long total = (long long)rows_smem[p.n_seqs] * p.n_heads;
+  const unsigned total = (unsigned)rows_smem[p.n_seqs] * p.n_heads;              // (below 2^31, as all sequences' tiles together)
   const int warps = gridDim.x * (kRowsThreads / 32);
 #pragma unroll 1
-  for (long long x = (long long)blockIdx.x * (kRowsThreads / 32) + warp; x < total; x += warps) {
-    const int i = ragged_find(rows_smem, p.n_seqs, (int)(x / p.n_heads));
-    const int count = rows_smem[i + 1] - rows_smem[i];
-    const long long local = x - (long long)rows_smem[i] * p.n_heads;
+  for (unsigned x = blockIdx.x * (kRowsThreads / 32) + warp; x < total; x += warps) {
+    const int i = ragged_find(rows_smem, p.n_seqs, (int)(x / (unsigned)p.n_heads));
+    const unsigned count = rows_smem[i + 1] - rows_smem[i], local = x - (unsigned)rows_smem[i] * p.n_heads;
     const int g = (int)(local / count);
     int from, rows;
     span(i, from, rows);
-    const int col = (from >> p.page_shift) + (int)(local % count);
+    const int col = (from >> p.page_shift) + (int)(local - g * count);
     const int page = p.table[(size_t)i * p.width + col];
     if ((unsigned)page >= (unsigned)p.n_pages) {
       if (lane == 0) set_status(p.status, MEDA_ERR_INVALID_ARG);
