@@ -131,7 +131,7 @@ struct AttnTileCoded {
   float o[G][4][NH][4];
   float low_sum[NH][2][G];               // sum of p low
   float l[NH][2];                        // sum of p = 2^(logit - reference)
-  float ref[NH][2], limit[NH][2];        // reference; what a product may reach before the reference has to move (-inf: there is none yet)
+  float ref[NH][2], limit[NH][2];        // reference; what a logit may reach before the reference has to move (-inf: there is none yet)
   float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
   int step_exp;                          // of twice the largest step when it was set (kScale - 125 at least)
 
@@ -329,7 +329,15 @@ struct AttnTileCoded {
     const int r = lane / 4;
     float s[SUB][NH][4];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) logits(s[u], stage + 2 * u * kHalf, lane);
+    for (int u = 0; u < SUB; ++u) {
+      logits(s[u], stage + 2 * u * kHalf, lane);
+      // Rounded here, once: the reference is one of these numbers, and its own row's weight 1.  (Inside the exponential's subtraction the product
+      // would not be rounded, and from 5e7 on that weight 2 to the power of what rounding the reference had cut off.)
+#pragma unroll
+      for (int n = 0; n < NH; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[u][n][e] = __fmul_rn(s[u][n][e], factor[n][e & 1]);
+    }
     uint32_t vm[SUB][2][G];                                    // steps and lowest values of the values' rows r, r + 8
     float top = 0.f;
 #pragma unroll
@@ -378,15 +386,13 @@ struct AttnTileCoded {
         for (int x = 0; x < 2; ++x) {
           float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
           if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
-          most *= factor[n][x];
 #pragma unroll
           for (int y = 4; y < 32; y <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, y));
           const bool none = limit[n][x] == -INFINITY;
           most = none ? most : fmaxf(most, ref[n][x]);
           const float to_ref = most == -INFINITY ? 0.f : most;
           const float f = none ? 1.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
-          // (rather too low, by more than the quotient may be off: a logit beyond it would overflow the weights)
-          limit[n][x] = most == -INFINITY ? -INFINITY : __fdividef(most + kSlack - 1.9073486e-6f * fabsf(most), factor[n][x]);
+          limit[n][x] = __fadd_rd(most, kSlack);               // (a logit beyond it would overflow the weights)
           ref[n][x] = to_ref;
           l[n][x] *= f;
 #pragma unroll
@@ -420,7 +426,7 @@ struct AttnTileCoded {
     for (int n = 0; n < NH; ++n) {
       float p[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = exp2_fast(fmaf(s[n][e], factor[n][e & 1], -ref[n][e & 1]));
+      for (int e = 0; e < 4; ++e) p[e] = exp2_fast(s[n][e] - ref[n][e & 1]);
       l[n][0] += p[0] + p[2];
       l[n][1] += p[1] + p[3];
 #pragma unroll

@@ -1,0 +1,84 @@
+"""Attention over quantised pages where numbers are far apart or large."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import parity as P
+import test_gpu_pages as T
+from oracle import pages_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2502_17599_b200 import build, binding
+    build.build()
+    binding.load_library()
+    return binding
+
+
+def pool(x, bits):
+    return torch.as_tensor(O.pack_page(*O.quantise(np.asarray(x).astype(np.float32), bits), bits), device="cuda")
+
+
+def attend(B, q, k, v, dtype, bits, times=1):
+    """k, v [n][rows][d], q [n][hq][d]: every sequence one page of one KV head, all of them `times` over (a batch large enough that a warp goes
+    through several tiles of one) -> out, lse [times][n][hq]..."""
+    (n, rows, d), hq = k.shape, q.shape[1]
+    page = max(16, 1 << (rows - 1).bit_length())
+    kp, vp = (pool(np.concatenate([x, np.zeros((n, page - rows, d))], 1)[:, None], bits) for x in (k, v))
+    pg = T.make(B, n_q_heads=hq, n_kv_heads=1, head_dim=d, dtype=dtype, page_size=page, n_pages=n, max_seqs=n * times, max_seq_pages=1, cache_bits=bits)
+    many = q.repeat(times, 1, 1)
+    out, lse = torch.full_like(many, math.nan), torch.full(many.shape[:2], math.nan, device="cuda")
+    pg.paged_attention(many, kp, vp, T.i32([[i] for i in range(n)]).repeat(times, 1), T.i32([rows] * (n * times)), out, lse)
+    pg.check()
+    pg.close()
+    return out.view(times, *q.shape), lse.view(times, n, hq)
+
+
+def parts(v, bits):
+    """What rows of values [..., d] read back as, and the sizes of their code and low parts."""
+    code, step, low = O.quantise(np.asarray(v).astype(np.float32), bits)
+    return O.held(code, step, low), O.held(code, step, 0 * low), O.held(0 * code, step, np.abs(low))
+
+
+BOTH = [pytest.mark.parametrize("bits", [4, 8]), pytest.mark.parametrize("dtype", ["bf16", "f32"])]
+
+
+def both(f):
+    for m in BOTH:
+        f = m(f)
+    return f
+
+
+@both
+@pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
+def test_logits_far_beyond_the_mantissa(B, dtype, bits, order):
+    """Logits of 10^6 to 10^30, a dozen in every binade up to 10^11: the row that sets the reference has a weight of 1, whatever the rounding of its logit.
+    What rows read back as differs by 2^-9 or more of the largest, so one row decides (or several alike): the output is their values' mean.  Its weight
+    is exact (a step is a bf16), the sums are off by 2^-22 of their size for each row and for each of the 64 products beside it, and the result is
+    rounded once."""
+    rows, d = 40, 64
+    tops = np.concatenate([8e6 * 2.0 ** (np.arange(200) / 12), 8e12 * 10.0 ** np.arange(18)])
+    n = len(tops)
+    rng = np.random.default_rng(bits)
+    ranks = {"rising": np.arange(rows), "falling": np.arange(rows)[::-1], "mixed": rng.permutation(rows)}[order]
+    k = np.zeros((n, rows, d))
+    k[:, :, 0] = tops[:, None] * (ranks + 1) / rows
+    v = rng.normal(0.3, 1, (n, rows, d))
+    q = torch.zeros((n, 1, d), dtype=T.DT[dtype], device="cuda")
+    q[:, :, 0] = 1.0
+    out, lse = attend(B, q, k, v, dtype, bits, 30)
+    s = parts(k, bits)[0][:, :, 0] / 8
+    at = s == s.max(1, keepdims=True)
+    assert (np.where(at, -np.inf, s).max(1) <= s.max(1) * (1 - 2.0 ** -9)).all()
+    p = at / at.sum(1, keepdims=True)
+    vr, vc, vl = parts(v, bits)
+    want, size = np.einsum("nr,nrd->nd", p, vr), np.einsum("nr,nrd->nd", p, vc + vl)
+    tol = size * (rows + 64) * 2.0 ** -22 + T.HALF_STEP[dtype] * 1.01 * np.abs(want)
+    off = np.abs(P.np64(out[:, :, 0]) - want)
+    assert (off <= tol).all(), float((off / tol).max())
+    assert (np.abs(P.np64(lse[:, :, 0]) - s.max(1) - np.log(at.sum(1))) <= 2.0 ** -21 * s.max(1)).all()
