@@ -373,7 +373,8 @@ meda_status meda_select_pages(meda_pages* pages, const void* q, const void* boun
  * `dtype`; rows that read back as NaN make the outputs NaN that they have a part in (keys all of their KV head's, values those of their 64
  * dimensions), and so does a query with an element that is not finite or of magnitude 2^110 or more, its own.  In other caches an
  * infinite value makes its dimension of the output infinite; both signs in one dimension, or a row whose weight is 0 in fp32 (below
- * 2^-126 of the largest), make it NaN. */
+ * 2^-126 of the largest), make it NaN.  Values are added up in fp32 with weights of at most 1 and divided in the end: in caches of either kind
+ * such a sum beyond 2^128 is infinite. */
 meda_status meda_paged_attention(meda_pages* pages, const void* q, const void* k_pages, const void* v_pages,
                                  const int32_t* table, const int32_t* lens, int32_t lens_stride, int32_t n_seqs,
                                  const int32_t* sel, int32_t keep, void* out, float* lse, void* stream);

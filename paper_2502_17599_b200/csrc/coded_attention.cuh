@@ -20,8 +20,8 @@
 // that matters exactly (the rest is below 2^-38 of the largest); fp32 ones go in two parts.  A weight p step is rounded to
 // fp16 (2^-11 of itself: a quarter of the output's own rounding in bf16 at worst, and it averages out over the rows), for fp32 caches to two
 // such parts; weights are scaled by a power of two that follows the largest step a warp has met, so that neither tiny nor huge values leave
-// fp16's range.  The reference of the exponentials moves only when a logit passes it by 2^8 (bf16; in fp32 at once, the parts need the range):
-// bringing the sums to a new one costs as much as a tile.
+// fp16's range.  The reference of the exponentials is set 2^8 above the largest logit met (bf16; in fp32 on it, the parts need the range) and moves
+// when one passes it: bringing the sums to a new one costs as much as a tile.  No weight is ever above 1, so the sums reach no further than values times rows.
 //
 // Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 9.2 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
 // rows, 28 / 4 heads of 128, 443 MB: 83 us, 82 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
@@ -121,9 +121,9 @@ struct AttnTileCoded {
   static constexpr int kHalf = kRunCodes + kRunMore;             // bytes of a run's keys or values
   static constexpr int kStage = 2 * SUB * kHalf;                 // of a tile: keys and values of every run
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
-  static constexpr int kScale = PARTS == 2 ? 14 : 6;             // weights stay below 2^(kScale + 1) (times 2^kSlack)
+  static constexpr int kScale = 14;                              // weights stay below 2^(kScale + 1)
   static constexpr float kMostQuery = 1.2980742e33f;             // 2^110: `factor` and its inverse stay in fp32's range
-  static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference may stay this far (log2) behind the maximum
+  static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference is put this far (log2) above the maximum
 
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
   uint32_t qsum[NH][2];                  // sums over the groups, in bf16 parts
@@ -131,7 +131,7 @@ struct AttnTileCoded {
   float o[G][4][NH][4];
   float low_sum[NH][2][G];               // sum of p low
   float l[NH][2];                        // sum of p = 2^(logit - reference)
-  float ref[NH][2], limit[NH][2];        // reference; what a logit may reach before the reference has to move (-inf: there is none yet)
+  float ref[NH][2];                      // reference: no logit so far is above it (-inf: there is none yet)
   float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
   int step_exp;                          // of twice the largest step when it was set (kScale - 125 at least)
 
@@ -237,8 +237,7 @@ struct AttnTileCoded {
     for (int n = 0; n < NH; ++n)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        ref[n][x] = 0.f;
-        limit[n][x] = -INFINITY;
+        ref[n][x] = -INFINITY;
         l[n][x] = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) low_sum[n][x][g] = 0.f;
@@ -370,7 +369,7 @@ struct AttnTileCoded {
       for (int x = 0; x < 2; ++x) {
         float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
         if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
-        moved |= most > limit[n][x];
+        moved |= most > ref[n][x];
       }
     if (__any_sync(0xffffffffu, moved)) {                      // a new reference, or larger values than before: bring the sums to them
 #pragma unroll
@@ -388,11 +387,8 @@ struct AttnTileCoded {
           if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
 #pragma unroll
           for (int y = 4; y < 32; y <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, y));
-          const bool none = limit[n][x] == -INFINITY;
-          most = none ? most : fmaxf(most, ref[n][x]);
-          const float to_ref = most == -INFINITY ? 0.f : most;
-          const float f = none ? 1.f : exp2_fast(ref[n][x] - to_ref);            // (without a reference the sums are 0, or NaN)
-          limit[n][x] = __fadd_rd(most, kSlack);               // (a logit beyond it would overflow the weights)
+          // (with nothing but NaN so far there is still no reference, and f is NaN too)
+          const float to_ref = most > ref[n][x] ? most + kSlack : ref[n][x], f = exp2_fast(ref[n][x] - to_ref);
           ref[n][x] = to_ref;
           l[n][x] *= f;
 #pragma unroll
@@ -504,7 +500,7 @@ struct AttnTileCoded {
           for (int y = 4; y < 32; y <<= 1) low[g] += __shfl_xor_sync(0xffffffffu, low[g], y);
         }
         if (h < heads) {
-          const float m = limit[n][x] == -INFINITY ? -INFINITY : ref[n][x];
+          const float m = ref[n][x];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             float y[8] = {fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),

@@ -1,4 +1,12 @@
-"""Attention over quantised pages where numbers are far apart or large."""
+"""Attention over quantised pages where numbers are far apart or large: logits beyond 2^26, rows that count for nothing beside rows that do, keys and
+values next to fp32's end.
+
+Tolerances.  A logit is the sum over the groups of step * (q . codes) and low * (sum of q), d + d / 64 products added up in fp32 (2^-22 for each, which also
+covers an accumulator that truncates), and is rounded once more: off by at most delta = (d + 34) 2^-22 sum |q| (step code + |low|) / sqrt(d); that moves a
+probability by exp(delta) and its normaliser by as much.  exp2 is off by 2^-22, sums of `rows` terms by rows 2^-22.  The weight p * step of a row's codes
+enters its product in fp16, off by 2^-11 of itself for bf16 outputs and by 2^-22 for fp32 ones (two parts), and no finer than 2^-38 of the largest weight of
+its head and 64 dimensions.  The result is rounded once.  All of it is relative to what is added up, p * step * code and p * |low|: a row without weight
+is not in it."""
 import math
 
 import numpy as np
@@ -45,6 +53,31 @@ def parts(v, bits):
     return O.held(code, step, low), O.held(code, step, 0 * low), O.held(0 * code, step, np.abs(low))
 
 
+def check(out, lse, q, k, v, bits, dtype):
+    """out [times][n][hq][d] against softmax over the rows k, v [n][rows][d], q [n][hq][d]; see the file's head."""
+    rows, d = k.shape[1:]
+    kr, kc, kl = parts(k, bits)
+    vr, vc, vl = parts(v, bits)
+    s = np.einsum("nhd,nrd->nhr", q, kr) / math.sqrt(d)
+    top = s.max(-1, keepdims=True)
+    e = np.exp(s - top)
+    z = e.sum(-1, keepdims=True)
+    p = e / z
+    mag = (np.einsum("nhd,nrd->nhr", np.abs(q), kc + kl) / math.sqrt(d)).max(-1, keepdims=True)
+    delta = (d + 34) * 2.0 ** -22 * mag
+    rel = 2 * delta * (1 + delta) + (rows + 64) * 2.0 ** -22
+    codes, lows = p @ vc, p @ vl
+    step = O.quantise(np.asarray(v).astype(np.float32), bits)[1]                    # [n][rows][groups]
+    weight = (p[..., None] * step[:, None]).max(2).repeat(64, -1)                   # the largest of each head and group
+    fine = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 1.01 * codes + rows * 2.0 ** -38 * weight * (1 << bits)
+    want = p @ vr
+    tol = (codes + lows) * rel + fine + T.HALF_STEP[dtype] * 1.01 * np.abs(want) + 1e-30
+    off = np.abs(P.np64(out) - want)
+    assert (off <= tol).all(), float((off / tol).max())
+    norm = (top + np.log(z))[..., 0]
+    assert (np.abs(P.np64(lse) - norm) <= delta[..., 0] + (rows + 64) * 2.0 ** -22 + 2.0 ** -21 * np.abs(norm) + 1e-6).all()
+
+
 BOTH = [pytest.mark.parametrize("bits", [4, 8]), pytest.mark.parametrize("dtype", ["bf16", "f32"])]
 
 
@@ -82,3 +115,19 @@ def test_logits_far_beyond_the_mantissa(B, dtype, bits, order):
     off = np.abs(P.np64(out[:, :, 0]) - want)
     assert (off <= tol).all(), float((off / tol).max())
     assert (np.abs(P.np64(lse[:, :, 0]) - s.max(1) - np.log(at.sum(1))) <= 2.0 ** -21 * s.max(1)).all()
+
+
+@both
+def test_values_near_the_end_of_fp32(B, dtype, bits):
+    """256 rows of 2^117: their sum is within fp32 as long as no weight is above 1, however the rows come (here later logits are above the first ones, by
+    less than what would move a reference that may stay behind)."""
+    rows, d, n = 256, 64, 3
+    rng = np.random.default_rng(1)
+    k, v = np.zeros((n, rows, d)), (2 + rng.random((n, rows, d))) * 2.0 ** 116
+    k[0, 40:, 0], k[1, 40:, 0], k[2, 40:, 0] = 5.0, 5.5, 7.0
+    v[2] *= -1
+    q = torch.zeros((n, 1, d), dtype=T.DT[dtype], device="cuda")
+    q[:, 0, 0] = 8.0
+    out, lse = attend(B, q, k, v, dtype, bits, 1000)
+    assert torch.isfinite(out).all()
+    check(out, lse, P.np64(q), k, v, bits, dtype)
