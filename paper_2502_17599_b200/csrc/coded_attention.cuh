@@ -18,10 +18,11 @@
 //
 // Roundings.  Queries are scaled by a power of two per head, their largest element between 2^14 and 2^15: fp16 then holds every bf16 element
 // that matters exactly (the rest is below 2^-38 of the largest); fp32 ones go in two parts.  A weight p step is rounded to
-// fp16 (2^-11 of itself: a quarter of the output's own rounding in bf16 at worst, and it averages out over the rows), for fp32 caches to two
-// such parts; weights are scaled by a power of two that follows the largest step a warp has met, so that neither tiny nor huge values leave
-// fp16's range.  The reference of the exponentials is set 2^8 above the largest logit met (bf16; in fp32 on it, the parts need the range) and moves
-// when one passes it: bringing the sums to a new one costs as much as a tile.  No weight is ever above 1, so the sums reach no further than values times rows.
+// fp16 (2^-11 of itself, so of the codes' part of the output: it averages out over the rows), for fp32 caches to two
+// such parts.  Weights are scaled by a power of two for every head and group, which goes by the weights met (p step, not the step alone: a row with huge
+// values and no weight takes nothing from the others), so that neither tiny nor huge values leave fp16's range: see settle().
+// The reference of the exponentials is set 2^8 above the largest logit met (fp32: 2^6) and moves when one passes it: bringing the sums to a new one
+// costs as much as a tile or two.  No weight is ever above 1, so the sums reach no further than values times rows.
 //
 // Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 9.2 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
 // rows, 28 / 4 heads of 128, 443 MB: 83 us, 82 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
@@ -75,6 +76,11 @@ __device__ __forceinline__ uint32_t bf16_part(float& lo, float& hi) {
   memcpy(&y, &x, 4);
   return y;
 }
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b, float c, float d) {       // (a c, b d) in one instruction
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a, b)), "l"(pair(c, d)));
+  unpair(r, x, y);
+}
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }    // -126 <= e <= 127
 
 template <int N>
@@ -121,9 +127,9 @@ struct AttnTileCoded {
   static constexpr int kHalf = kRunCodes + kRunMore;             // bytes of a run's keys or values
   static constexpr int kStage = 2 * SUB * kHalf;                 // of a tile: keys and values of every run
   static constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;           // fp16 parts of a query element and of a weight
-  static constexpr int kScale = 14;                              // weights stay below 2^(kScale + 1)
   static constexpr float kMostQuery = 1.2980742e33f;             // 2^110: `factor` and its inverse stay in fp32's range
-  static constexpr float kSlack = PARTS == 2 ? 0.f : 8.f;        // the reference is put this far (log2) above the maximum
+  static constexpr int kMostScale = 126;
+  static constexpr float kSlack = PARTS == 2 ? 6.f : 8.f;        // the reference is put this far (log2) above the maximum
 
   uint32_t q[NH][PARTS][2][G][4];        // unit 2c + i of group g: the four pairs that go with pair_of()
   uint32_t qsum[NH][2];                  // sums over the groups, in bf16 parts
@@ -132,8 +138,7 @@ struct AttnTileCoded {
   float low_sum[NH][2][G];               // sum of p low
   float l[NH][2];                        // sum of p = 2^(logit - reference)
   float ref[NH][2];                      // reference: no logit so far is above it (-inf: there is none yet)
-  float weight, step_top;                // 2^(kScale - step_exp); steps below this fit it
-  int step_exp;                          // of twice the largest step when it was set (kScale - 125 at least)
+  float scale[NH][2][G];                 // of the weights in o, a power of two: p step scale is 2^15 at most for the tile at hand
 
   // Two codes in the lower bits of a word's halves as an operand: as they are, c 2^-24, or for fp32 as normal numbers (1024 + c, less 1024).
   static constexpr float kCodeScale = PARTS == 2 ? 1.f : 5.9604644775390625e-8f;
@@ -240,7 +245,10 @@ struct AttnTileCoded {
         ref[n][x] = -INFINITY;
         l[n][x] = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) low_sum[n][x][g] = 0.f;
+        for (int g = 0; g < G; ++g) {
+          low_sum[n][x][g] = 0.f;
+          scale[n][x][g] = power_of_two(kMostScale);
+        }
       }
 #pragma unroll
     for (int g = 0; g < G; ++g)
@@ -250,9 +258,6 @@ struct AttnTileCoded {
         for (int n = 0; n < NH; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[g][t][n][e] = 0.f;
-    step_top = 0.f;
-    step_exp = kScale - 125;
-    weight = power_of_two(125);
   }
   // A run of rows in shared memory: 16-byte pieces of its codes, then its steps and lowest values.  The pieces are moved inside
   // a row, and the values' rows are sorted even ones first in each eight, so that the lanes that read together meet different banks.
@@ -330,15 +335,14 @@ struct AttnTileCoded {
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
       logits(s[u], stage + 2 * u * kHalf, lane);
-      // Rounded here, once: the reference is one of these numbers, and its own row's weight 1.  (Inside the exponential's subtraction the product
-      // would not be rounded, and from 5e7 on that weight 2 to the power of what rounding the reference had cut off.)
+      // Rounded here, once: the reference goes by one of these numbers, and its own row's weight is what kSlack makes it.  (Were the product formed with the
+      // exponential's subtraction, unrounded, that weight would be off by 2 to the power of what rounding had cut off: too large for fp16 from 5e7 on.)
 #pragma unroll
       for (int n = 0; n < NH; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[u][n][e] = __fmul_rn(s[u][n][e], factor[n][e & 1]);
+        for (int e = 0; e < 4; e += 2) mul2(s[u][n][e], s[u][n][e + 1], s[u][n][e], s[u][n][e + 1], factor[n][0], factor[n][1]);
     }
     uint32_t vm[SUB][2][G];                                    // steps and lowest values of the values' rows r, r + 8
-    float top = 0.f;
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -356,57 +360,101 @@ struct AttnTileCoded {
             for (int g = 0; g < G; ++g) vm[u][t][g] = 0u;
           }
     }
+    bool unsettled = false;                                    // a logit above its reference, or a step whose row could weigh too much for fp16
+#pragma unroll
+    for (int n = 0; n < NH; ++n)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) unsettled |= largest(s, n, x) > ref[n][x];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float most = scale[0][0][g];
+#pragma unroll
+      for (int n = 0; n < NH; ++n) most = fmaxf(most, fmaxf(scale[n][0][g], scale[n][1][g]));
+      unsettled |= largest_step(vm, g) * most > 32768.f;
+    }
+    if (__any_sync(0xffffffffu, unsettled)) settle(s, vm);
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int n = 0; n < NH; ++n) {
+        float (&p)[4] = s[u][n];
 #pragma unroll
-        for (int g = 0; g < G; ++g) top = fmaxf(top, step_of(vm[u][t], g));
-    bool moved = top >= step_top;
+        for (int e = 0; e < 4; ++e) p[e] = exp2_fast(p[e] - ref[n][e & 1]);
+        l[n][0] += p[0] + p[2];
+        l[n][1] += p[1] + p[3];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float low0 = low_of(vm[u][0], g), low1 = low_of(vm[u][1], g);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) low_sum[n][x][g] = fmaf(p[2 + x], low1, fmaf(p[x], low0, low_sum[n][x][g]));
+        }
+      }
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) attend(s[u], vm[u], stage + (2 * u + 1) * kHalf, lane);
+  }
+  __device__ __forceinline__ static float largest(const float (&s)[SUB][NH][4], int n, int x) {
+    float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
+    if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
+    return most;
+  }
+  __device__ __forceinline__ static float largest_step(const uint32_t (&vm)[SUB][2][G], int g) {
+    float most = fmaxf(step_of(vm[0][0], g), step_of(vm[0][1], g));
+    if (SUB == 2) most = fmaxf(most, fmaxf(step_of(vm[SUB - 1][0], g), step_of(vm[SUB - 1][1], g)));
+    return most;
+  }
+  __device__ __forceinline__ static int exponent(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }       // of x >= 0
+  __device__ __forceinline__ static float over_rows(float most) {
+#pragma unroll
+    for (int y = 4; y < 32; y <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, y));
+    return most;
+  }
+  // References at or above the tile's logits `s`, the sums brought to them; and scales for the tile's weights p step, which then are at most 2^15.
+  // Where a reference moves the scale is set anew: kRoom bits below what would fit the tile's largest step with a weight of 1, so that the next tiles need not be
+  // looked at this closely, but not so low that its largest weight p step would be below 2^kLeast.  Elsewhere it comes down only for a weight that
+  // is too large: a huge step alone, of a row that does not count, leaves it alone.
+  static constexpr int kRoom = PARTS == 2 ? 3 : 6, kLeast = PARTS == 2 ? 0 : -6;
+  __device__ __forceinline__ void settle(const float (&s)[SUB][NH][4], const uint32_t (&vm)[SUB][2][G]) {
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
-        if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
-        moved |= most > ref[n][x];
-      }
-    if (__any_sync(0xffffffffu, moved)) {                      // a new reference, or larger values than before: bring the sums to them
+        const float most = over_rows(largest(s, n, x)), from = ref[n][x];
+        const bool moved = most > from;                        // (with nothing but NaN so far there is no reference, and the sums become NaN)
+        const float to = moved ? most + kSlack : from, f = exp2_fast(from - to);
+        ref[n][x] = to;
+        l[n][x] *= f;
+        const int by = (int)fminf(to - from, 400.f);           // (more than fp32 has)
 #pragma unroll
-      for (int y = 1; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-      const int to = top >= step_top ? max(step_exp, min(127, (int)(__float_as_uint(top) >> 23) - 126)) : step_exp;
-      const float smaller = step_exp - to < -126 ? 0.f : power_of_two(step_exp - to);
-      step_exp = to;
-      step_top = to == 127 ? INFINITY : power_of_two(to + 1);
-      weight = power_of_two(kScale - to);
+        for (int g = 0; g < G; ++g) {
+          low_sum[n][x][g] *= f;
+          float weight = 0.f;
 #pragma unroll
-      for (int n = 0; n < NH; ++n)
+          for (int u = 0; u < SUB; ++u)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float most = fmaxf(s[0][n][x], s[0][n][2 + x]);
-          if (SUB == 2) most = fmaxf(most, fmaxf(s[SUB - 1][n][x], s[SUB - 1][n][2 + x]));
+            for (int t = 0; t < 2; ++t) weight = fmaxf(weight, exp2_fast(s[u][n][2 * t + x] - to) * step_of(vm[u][t], g));
+          const int weight_exp = exponent(over_rows(weight)), step_exp = exponent(over_rows(largest_step(vm, g)));
+          const int now = exponent(scale[n][x][g]);
+          int e = min(max(14 - kRoom - step_exp, kLeast - weight_exp), kMostScale);
+          float high = 0.f;
 #pragma unroll
-          for (int y = 4; y < 32; y <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, y));
-          // (with nothing but NaN so far there is still no reference, and f is NaN too)
-          const float to_ref = most > ref[n][x] ? most + kSlack : ref[n][x], f = exp2_fast(ref[n][x] - to_ref);
-          ref[n][x] = to_ref;
-          l[n][x] *= f;
+          for (int t = 0; t < 4; ++t) high = fmaxf(high, fmaxf(fabsf(o[g][t][n][x]), fabsf(o[g][t][n][2 + x])));
+          high = over_rows(high);                              // (by all lanes: which heads move differs among them)
+          if (moved) e = min(e, now + by + 60 - exponent(high));                 // o, as it is in the new scale, below 2^60
+          else if (weight_exp + now < 15) e = now;
+          e = max(e, -126);
+          scale[n][x][g] = power_of_two(e);
+          const int up = min(e - now, 200);                    // (beyond 126 in two steps; f is 0 where it could be more)
+          const float change = up < -126 ? 0.f : f * power_of_two(min(up, 100)) * power_of_two(max(up, 100) - 100);
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            low_sum[n][x][g] *= f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              o[g][t][n][x] *= f * smaller;
-              o[g][t][n][2 + x] *= f * smaller;
-            }
+          for (int t = 0; t < 4; ++t) {
+            o[g][t][n][x] *= change;
+            o[g][t][n][2 + x] *= change;
           }
         }
-    }
-#pragma unroll
-    for (int u = 0; u < SUB; ++u) attend(s[u], vm[u], stage + (2 * u + 1) * kHalf, lane);
+      }
   }
   // The values of a run, weighed.
-  __device__ __forceinline__ void attend(const float (&s)[NH][4], const uint32_t (&vm)[2][G], const unsigned char* stage, int lane) {
+  __device__ __forceinline__ void attend(const float (&p)[NH][4], const uint32_t (&vm)[2][G], const unsigned char* stage, int lane) {
     const int r = lane / 4, c = lane % 4;
     uint32_t v[4][G * W];                                      // rows 2c, 2c + 1, 2c + 8, 2c + 9: codes of unit r
 #pragma unroll
@@ -419,26 +467,20 @@ struct AttnTileCoded {
     }
     uint32_t b[NH][PARTS][G][2];
 #pragma unroll
-    for (int n = 0; n < NH; ++n) {
-      float p[4];
+    for (int n = 0; n < NH; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = exp2_fast(s[n][e] - ref[n][e & 1]);
-      l[n][0] += p[0] + p[2];
-      l[n][1] += p[1] + p[3];
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const float low0 = low_of(vm[0], g), low1 = low_of(vm[1], g);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) low_sum[n][x][g] = fmaf(p[2 + x], low1, fmaf(p[x], low0, low_sum[n][x][g]));
+      for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const float f = step_of(vm[t], g) * weight, w0 = p[2 * t] * f, w1 = p[2 * t + 1] * f;
+          // (p scale is at most 2^126: a weight of 0 stays 0 whatever its step)
+          const float step = step_of(vm[t], g);
+          float w0, w1;
+          mul2(w0, w1, p[n][2 * t], p[n][2 * t + 1], scale[n][0][g], scale[n][1][g]);
+          mul2(w0, w1, w0, w1, step, step);
           const uint32_t hi = halves(w0, w1);
           b[n][0][g][t] = transpose8(hi);
           if constexpr (PARTS == 2) b[n][PARTS - 1][g][t] = transpose8(halves(w0 - half_low(hi), w1 - half_high(hi)));
         }
-      }
-    }
     // dimensions of a unit: (0, 2), (1, 3), (4, 6), (5, 7) side by side; at 4 bits the odd ones come out sixteen times too large
 #pragma unroll
     for (int g = 0; g < G; ++g)
@@ -484,7 +526,7 @@ struct AttnTileCoded {
   template <typename F>
   __device__ __forceinline__ void finish(int heads, int lane, F f) {
     const int r = lane / 4, c = lane % 4;
-    const float a = power_of_two(PARTS == 2 ? -kScale : 24 - kScale), e = power_of_two(step_exp), odd = BITS == 4 ? 0.0625f * a : a;
+    constexpr float a = 1.f / kCodeScale, odd = BITS == 4 ? 0.0625f * a : a;
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll
@@ -503,6 +545,7 @@ struct AttnTileCoded {
           const float m = ref[n][x];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
+            const float e = __uint_as_float((254u << 23) - __float_as_uint(scale[n][x][g]));     // 1 / scale
             float y[8] = {fmaf(o[g][0][n][x] * a, e, low[g]), fmaf(o[g][1][n][x] * odd, e, low[g]),
                           fmaf(o[g][0][n][2 + x] * a, e, low[g]), fmaf(o[g][1][n][2 + x] * odd, e, low[g]),
                           fmaf(o[g][2][n][x] * a, e, low[g]), fmaf(o[g][3][n][x] * odd, e, low[g]),

@@ -4,8 +4,8 @@ values next to fp32's end.
 Tolerances.  A logit is the sum over the groups of step * (q . codes) and low * (sum of q), d + d / 64 products added up in fp32 (2^-22 for each, which also
 covers an accumulator that truncates), and is rounded once more: off by at most delta = (d + 34) 2^-22 sum |q| (step code + |low|) / sqrt(d); that moves a
 probability by exp(delta) and its normaliser by as much.  exp2 is off by 2^-22, sums of `rows` terms by rows 2^-22.  The weight p * step of a row's codes
-enters its product in fp16, off by 2^-11 of itself for bf16 outputs and by 2^-22 for fp32 ones (two parts), and no finer than 2^-38 of the largest weight of
-its head and 64 dimensions.  The result is rounded once.  All of it is relative to what is added up, p * step * code and p * |low|: a row without weight
+enters its product in fp16, off by 2^-11 of itself for bf16 outputs and by 2^-22 for fp32 ones (two parts), and no finer than 2^-25 where the largest weight of
+its head and 64 dimensions is 2^-6 or more (fp32: 1 or more).  The result is rounded once.  All of it is relative to what is added up, p * step * code and p * |low|: a row without weight
 is not in it."""
 import math
 
@@ -69,7 +69,7 @@ def check(out, lse, q, k, v, bits, dtype):
     codes, lows = p @ vc, p @ vl
     step = O.quantise(np.asarray(v).astype(np.float32), bits)[1]                    # [n][rows][groups]
     weight = (p[..., None] * step[:, None]).max(2).repeat(64, -1)                   # the largest of each head and group
-    fine = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 1.01 * codes + rows * 2.0 ** -38 * weight * (1 << bits)
+    fine = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * 1.01 * codes + rows * (2.0 ** -19 if dtype == "bf16" else 2.0 ** -25) * weight * (1 << bits)
     want = p @ vr
     tol = (codes + lows) * rel + fine + T.HALF_STEP[dtype] * 1.01 * np.abs(want) + 1e-30
     off = np.abs(P.np64(out) - want)
@@ -115,6 +115,46 @@ def test_logits_far_beyond_the_mantissa(B, dtype, bits, order):
     off = np.abs(P.np64(out[:, :, 0]) - want)
     assert (off <= tol).all(), float((off / tol).max())
     assert (np.abs(P.np64(lse[:, :, 0]) - s.max(1) - np.log(at.sum(1))) <= 2.0 ** -21 * s.max(1)).all()
+
+
+@both
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_huge_values_of_rows_that_count_for_nothing(B, dtype, bits, d):
+    """A row with a step of 2^26 to 2^60 times the others' whose logit is 100 below theirs (a weight of 2^-144: nothing), at the front, in the middle, at the
+    end; in all groups of 64 dimensions and in one of them.  A third head has that row and nothing else."""
+    rows, hq, n = 120, 3, 0
+    rng = np.random.default_rng(d + bits)
+    ks, vs = [], []
+    q = rng.normal(0, 1, (hq, d))
+    q[:2, 0], q[2, 0] = 8.0, -8.0
+    for where in (0, 15, 33, 63, 64, 119):
+        for far in (26, 31, 40, 60):
+            for group in (None, 0):
+                k, v = rng.normal(0, 0.05, (rows, d)), rng.normal(0.2, 1, (rows, d))
+                k[:, 0] = 3.0
+                k[where, 0] = 3.0 - 110 * math.sqrt(d) / 8
+                v[where, slice(None) if group is None else slice(0, 64)] *= 2.0 ** far
+                ks.append(k), vs.append(v)
+                n += 1
+    k, v = np.stack(ks), np.stack(vs)
+    qd = torch.as_tensor(np.broadcast_to(q, (n, hq, d)).copy()).to(T.DT[dtype]).cuda()
+    out, lse = attend(B, qd, k, v, dtype, bits, 50)
+    s = np.einsum("hd,nrd->nhr", P.np64(qd)[0], parts(k, bits)[0]) / math.sqrt(d)
+    assert all((s[i, :2, w] < s[i, :2].max(-1) - 95).all() and s[i, 2].argmax() == w for i, w in enumerate(np.repeat((0, 15, 33, 63, 64, 119), 8)))
+    check(out, lse, P.np64(qd), k, v, bits, dtype)
+
+
+@both
+def test_groups_of_very_different_sizes(B, dtype, bits):
+    """Values whose second 64 dimensions are 2^-30 of the first ones: each group is as exact as if it were alone."""
+    rows, hq, d, n = 50, 3, 128, 4
+    rng = np.random.default_rng(bits)
+    k, v = rng.normal(0, 0.3, (n, rows, d)), rng.normal(0.2, 1, (n, rows, d))
+    v[:2, :, 64:] *= 2.0 ** -30
+    v[2:, :, :64] *= 2.0 ** -30
+    q = T.normal((n, hq, d), T.DT[dtype], 3)
+    out, lse = attend(B, q, k, v, dtype, bits, 50)
+    check(out, lse, P.np64(q), k, v, bits, dtype)
 
 
 @both
