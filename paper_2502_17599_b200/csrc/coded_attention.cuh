@@ -16,7 +16,7 @@
 // (rows are dimensions; a byte permute pairs the codes of neighbouring cache rows), B = (p step_g)^T, from the logits' layout by an 8 x 8
 // transposition per group.  Columns are heads on both sides, so a lane's maxima, sums and results belong to the same two heads.
 //
-// Roundings.  Queries are scaled by a power of two per head, their largest element between 2^14 and 2^15: fp16 then holds every bf16 element
+// Roundings.  Queries are scaled by a power of two per head, their largest element between 2^14 and 2^15 (fp32: 2^5 and 2^6): fp16 then holds every bf16 element
 // that matters exactly (the rest is below 2^-38 of the largest); fp32 ones go in two parts.  A weight p step is rounded to
 // fp16 (2^-11 of itself, so of the codes' part of the output: it averages out over the rows), for fp32 caches to two
 // such parts.  Weights are scaled by a power of two for every head and group, which goes by the weights met (p step, not the step alone: a row with huge
@@ -140,15 +140,17 @@ struct AttnTileCoded {
   float ref[NH][2];                      // reference: no logit so far is above it (-inf: there is none yet)
   float scale[NH][2][G];                 // of the weights in o, a power of two: p step scale is 2^15 at most for the tile at hand
 
-  // Two codes in the lower bits of a word's halves as an operand: as they are, c 2^-24, or for fp32 as normal numbers (1024 + c, less 1024).
-  static constexpr float kCodeScale = PARTS == 2 ? 1.f : 5.9604644775390625e-8f;
+  // Two codes in the lower bits of a word's halves as an operand: as they are, c 2^-24, or for fp32 as normal numbers c 2^-14 ((1024 + c) 2^-14 - 2^-4).
+  // A sum of products is multiplied by its step before `factor` takes the scale of queries and codes out again; the two keep it below fp32's end for
+  // keys of up to 2^126: 4 groups of 64 products of 2^(kQueryTop + 1) with 3 2^126 (codes' part and lowest values) times kCodeScale.
+  static constexpr float kCodeScale = PARTS == 2 ? 6.103515625e-5f : 5.9604644775390625e-8f;
+  static constexpr int kQueryTop = PARTS == 2 ? 5 : 14;          // log2 of a head's largest query element as the operands have it, rounded down
   __device__ __forceinline__ static uint32_t operand(uint32_t codes) {
     if constexpr (PARTS == 1) return codes;
-    const uint32_t x = codes | 0x64006400u, offset = 0x64006400u;
-    __half2 a, b;
+    const uint32_t x = codes | 0x64006400u;
+    __half2 a;
     memcpy(&a, &x, 4);
-    memcpy(&b, &offset, 4);
-    a = __hsub2(a, b);
+    a = __hfma2(a, __float2half2_rn(kCodeScale), __float2half2_rn(-0.0625f));
     uint32_t y;
     memcpy(&y, &a, 4);
     return y;
@@ -190,7 +192,7 @@ struct AttnTileCoded {
         }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int k2 = min(126, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
+      const int k2 = min(126, kQueryTop - ((int)(__float_as_uint(top) >> 23) - 127));
       const float scale = top < kMostQuery ? power_of_two(k2) : NAN;             // a query that is not finite, or huge, makes its logits NaN
       float sum[G];
 #pragma unroll

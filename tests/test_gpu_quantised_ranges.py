@@ -158,6 +158,21 @@ def test_groups_of_very_different_sizes(B, dtype, bits):
 
 
 @both
+@pytest.mark.parametrize("d", [64, 256])
+def test_keys_up_to_the_largest_that_are_held(B, dtype, bits, d):
+    """Keys of 2^100 to just below 2^126 with queries as small: logits of some 16."""
+    sizes = [100, 105, 107, 112, 120, 125.9]
+    rows, hq, n = 40, 2, len(sizes)
+    rng = np.random.default_rng(d)
+    k, v = rng.uniform(-1, 1, (n, rows, d)), rng.normal(0.2, 1, (n, rows, d))
+    k[n - 1] = np.abs(k[n - 1])                                    # all of one sign: the largest sums
+    big = 2.0 ** np.array(sizes)[:, None, None]
+    q = torch.as_tensor(rng.uniform(0.5, 1, (n, hq, d)) * 4 / big).to(T.DT[dtype]).cuda()
+    out, lse = attend(B, q, k * big, v, dtype, bits)
+    check(out, lse, P.np64(q), k * big, v, bits, dtype)
+
+
+@both
 def test_values_near_the_end_of_fp32(B, dtype, bits):
     """256 rows of 2^117: their sum is within fp32 as long as no weight is above 1, however the rows come (here later logits are above the first ones, by
     less than what would move a reference that may stay behind)."""
