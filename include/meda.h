@@ -316,7 +316,7 @@ meda_status meda_page_store(meda_pages* pages, const void* k, const void* v, int
 /* Rows [lens_from[i], lens[i]) of every sequence (lens_from NULL: from row 0) out of the pages into dense rows: what meda_page_store and
  * meda_rope_append put there, or what their codes stand for, rounded once to `dtype`.
  *   k, v   device, `dtype`: row lens_from[i] + j of a head at i * seq_stride + head * head_stride + j * head_dim; other rows are not
- *          written.  Sequences and heads do not overlap.
+ *          written.  Sequences and heads do not overlap, nor do k and v.
  * Both lengths are read with lens_stride; lens_from[i] >= lens[i]: no rows.  More than rows_capacity rows record MEDA_ERR_WORKSPACE, a
  * length out of range MEDA_ERR_INVALID_ARG, and the sequence is skipped; of a page outside the pool no rows are written.  Alignment as for
  * meda_page_store. */

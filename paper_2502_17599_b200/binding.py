@@ -407,7 +407,7 @@ class Pages:
             _check(status, "meda_page_store")
 
     def page_load(self, k_pages, v_pages, table, lens, k, v, lens_from=None, stream=None):
-        """Rows [lens_from, lens) of every sequence into k, v (laid out as for page_store), the first of them to row 0."""
+        """Rows [lens_from, lens) of every sequence into k, v (laid out as for page_store, not over one another), the first of them to row 0."""
         status = self._native.page_load(self._n, k_pages, v_pages, table, lens_from, lens, k, v, stream)
         if status:
             _check(status, "meda_page_load")

@@ -6,6 +6,8 @@
 
 #include <c10/cuda/CUDAStream.h>
 
+#include <algorithm>
+#include <cstdlib>
 #include <exception>
 #include <initializer_list>
 #include <sstream>
@@ -141,6 +143,23 @@ bool apart(int64_t cx, int64_t sx, int64_t cy, int64_t sy, int64_t span) {
   return cy < 2 || sy >= span;
 }
 
+// Whether no run of `span` elements at `by` + x * sx + y * sy lies over one at x' * sx + y' * sy (x, x' < cx; y, y' < cy): two tensors laid out alike,
+// the second `by` elements behind the first.
+bool beside(int64_t by, int64_t cx, int64_t sx, int64_t cy, int64_t sy, int64_t span) {
+  if (cx < 1 || cy < 1 || span < 1) return true;
+  if (cx < 2) sx = 0;
+  if (cy < 2) sy = 0;
+  by = by < 0 ? -by : by;
+  if (by >= (cx - 1) * sx + (cy - 1) * sy + span) return true;
+  for (int64_t x = 1 - cx; x < cx; ++x) {
+    const int64_t left = by - x * sx;
+    const int64_t y = sy ? std::min(std::max(left / sy, 1 - cy), cy - 1) : 0;
+    for (int64_t z = std::max(y - 1, 1 - cy); z <= std::min(y + 1, cy - 1); ++z)           // (the nearest is one of these)
+      if (std::abs(left - z * sy) < span) return false;
+  }
+  return true;
+}
+
 void* stream_of(const Native* n, PyObject* o) {
   if (o == Py_None) return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)n->device).stream();
   PyObject* v = PyObject_GetAttrString(o, "cuda_stream");
@@ -217,6 +236,9 @@ meda_status page_load(Args a) {                // k_pages, v_pages, table, lens_
   for (const at::Tensor* t : {&k, &v})
     if (!apart(c, t->stride(0), n->hkv, t->stride(1), t->size(2) * n->d))
       throw Refused(std::string(t == &k ? "k" : "v") + ": sequences or heads overlap");
+  // (both are of one type and 16-byte aligned, or the call refuses them)
+  const int64_t by = (static_cast<const char*>(v.data_ptr()) - static_cast<const char*>(k.data_ptr())) / (int64_t)k.element_size();
+  if (!beside(by, c, k.stride(0), n->hkv, k.stride(1), k.size(2) * n->d)) throw Refused("k and v overlap");
   return unlocked(n->page_load, n->h, static_cast<const void*>(pool(n, a[1], "k_pages")), static_cast<const void*>(pool(n, a[2], "v_pages")),
                   static_cast<const int32_t*>(dense(n, a[3], at::kInt, {c, n->width}, "table")), from, lengths(n, l, c, "lens"),
                   small(l.stride(0), "stride"), small(c, "n_seqs"), k.data_ptr(), v.data_ptr(), c > 1 ? k.stride(0) : 0,
