@@ -108,7 +108,6 @@ __device__ __forceinline__ uint32_t word_of(const uint4& x, int i) { return i ==
 template <int D, int NH, int R = 16>
 struct AttnTileBf16 {
   using T = __nv_bfloat16;
-  static constexpr bool kMma = true;
   static constexpr int kHeads = 8 * NH;
   static constexpr int KC = D / 32, VC = D / 64, KT = R / 8, kRows = R;
   uint4 q[NH][KC];
@@ -279,7 +278,6 @@ struct AttnTileBf16 {
 template <int D, int GP>
 struct AttnTileF32 {
   using T = float;
-  static constexpr bool kMma = false;
   static constexpr int kHeads = GP;
   static constexpr int E = D / 32, B = 4;
   static constexpr int P = GP * B <= 8 ? 8 : (GP * B <= 16 ? 16 : 32);
@@ -420,6 +418,7 @@ template <typename Tile, int D, int W>
 __global__ void __launch_bounds__(W * 32, 1)
 paged_attention_kernel(AttnParams p) {
   using T = typename Tile::T;
+  constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int HP = Tile::kHeads;
   constexpr int LD = D + 4;
   constexpr int kStates = attn_merge_floats(W, HP, D);
@@ -548,7 +547,7 @@ paged_attention_kernel(AttnParams p) {
     }
     const long long row_after = __shfl_sync(0xffffffffu, row_now, at);
     const int nv_after = __shfl_sync(0xffffffffu, nv_now, at);
-    if constexpr (Tile::kMma) {
+    if constexpr (kBf16) {
       constexpr int R = Tile::kRows;
 #pragma unroll
       for (int b = 0; b < kAttTile; b += R) {
