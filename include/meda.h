@@ -262,7 +262,8 @@ meda_status meda_pages_create(const meda_pages_config* config, meda_pages** out)
  *   low = min x rounded down (a zero counts as +0),  step = max(2^-126, fl((max x - low) * fl(1 / (2^cache_bits - 1))) rounded up),
  *   code = rint(fl(fl(x - low) * fl(1 / step))),  an element reads back as low + step * code,
  * with fl the rounding of an fp32 operation: the same rows give the same bytes everywhere.  An element is off by half a step at most, and by
- * the roundings.  If any of the 64 is NaN or of magnitude 2^126 or more, all of them read back as NaN.
+ * the roundings.  If any of the 64 is NaN or of magnitude 2^126 or more, all of them read back as NaN (step and lowest value are, the codes mean
+ * nothing).
  * A page of a head: the codes of its rows [page_size][head_dim * cache_bits / 8], then [page_size][2][head_dim / 64] bf16, steps and
  * lowest values.  Codes of a row: units of eight dimensions, unit i of group g at place i * (head_dim / 64) + g, in order from the lowest
  * bits up.
@@ -341,9 +342,10 @@ meda_status meda_page_bounds(meda_pages* pages, const void* k_pages, const int32
  *   slots      device int64 [n_tokens]: where the token's key and value go.  Slots of one call are distinct.
  *   q_out      device, `dtype`, [n_tokens][n_q_heads][head_dim]; may be q itself when that is dense
  * A token with slot -1 is padding: neither q_out nor the pools are written for it.
- * Into quantised pools the key goes as the pools of its type would hold it, rounded to `dtype`, and then into codes; cosine and sine are
- * correctly rounded there (from 64-bit arithmetic), the two products and their sum are rounded one by one, so that the codes are the
- * same everywhere. */
+ * Into quantised pools the key goes rotated, rounded to `dtype`, and then into codes, step by step: frequency i is the whole number of 2^-64
+ * turns below rope_theta^(-i / half) / (2 pi) as fp64 arithmetic gives it, the angle position times that modulo 2^64, cosine and sine those
+ * of fp64 arithmetic rounded to fp32; the two products and their sum are rounded one by one.  Whoever follows these steps gets the same codes, unless
+ * the last bits of pow, cosine or sine in fp64 differ and decide. */
 meda_status meda_rope_append(meda_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                              const void* v, int64_t v_stride, const int32_t* positions, int64_t axis_stride,
                              const int64_t* slots, int32_t n_tokens, void* q_out, void* k_pages, void* v_pages,

@@ -1,8 +1,10 @@
 // Rotary positions with three axes (see rope_append.cuh), the new rows quantised into their pages.
 //
-// A key's codes hang on borders, so its rotation is stated to the bit: the angle is exact (64-bit fixed point), its sine and
+// A key's codes hang on borders, so its rotation is stated step by step: a frequency is the 64-bit fraction of a turn that the handle was made
+// with (from fp64: good to 2^-53 of itself), the angle is position times frequency modulo a turn, without rounding, its sine and
 // cosine come from 64-bit arithmetic and are rounded to fp32, the two products and their sum are rounded one by one, and the key
-// is rounded to the cache's type before it is quantised.  A prompt appended here and one rotated elsewhere give the same pages.
+// is rounded to the cache's type before it is quantised.  A prompt rotated elsewhere by the same steps gives the same pages, but for a sine or
+// cosine so near the middle of two fp32 numbers that the last bits of the 64-bit one decide (one in 10^8).
 // (64-bit sines cost 0.8 us of a prompt's 65: a block works each out once for all heads.)
 //
 // A block takes a few tokens.  Keys and values go by units of eight dimensions, eight neighbouring lanes to a group; a lane reads its
