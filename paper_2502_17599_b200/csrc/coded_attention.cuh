@@ -567,10 +567,11 @@ struct AttnTileCoded {
 // end, and those that cross blocks states in scratch, as there.  (With the tiles dealt round all warps and a joining at the end of every
 // segment the 192 ragged caches took 167 us against 77 then.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
-// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches took 82.5, 77, 71.5 and 71.9 us; with blocks of 64, 128,
-// 256, 384 and 512 rows at least one cache of 947 rows took 8.8, 9.6, 9.3, 9.8 and 11.3 us, one of 4,000 11.2, 10.5, 9.7, 10.5 and 11.6, and
-// long ones want the larger.
-constexpr int kCodedSegment = 128, kCodedLeast = 384;
+// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches took 82.5, 77, 71.5 and 71.9 us (before weights were scaled by
+// head and group).  With blocks of 64, 128, 256, 384 and 512 rows at least one cache of 947 rows takes 8.9, 9.0, 9.4, 10.1 and 11.1 us, one of 4,000 10.5, 9.9,
+// 9.8, 10.6 and 11.5, one of 16,000 13.7, 13.7, 13.7, 13.7 and 13.0, nine in fp32 of up to 1,024 9.5, 9.5, 9.6, 10.2 and 10.2; longer ones and larger
+// batches fill all blocks with any of them.
+constexpr int kCodedSegment = 128, kCodedLeast = 128;
 
 template <int N>
 __device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
