@@ -11,7 +11,8 @@
 // unit and, with paired halves, the unit's partner (taking it from the other lane by shuffles measured the same).  Queries go by pairs of
 // vectors (both read before either is written: q_out may be q).
 //
-// Bound by memory with its latency: 18,944 tokens of 28 + 4 + 4 heads of 128 at 4 bits, 322 MB, in 59.8 us, 82 % of a plain copy; 64 tokens 3.4 us.
+// Bound by memory with its latency: 18,944 tokens of 28 + 4 + 4 heads of 128 at 4 bits, 322 MB, in 60 to 65 us, 76 to 82 % of a plain copy, at 8 bits, 331
+// MB, 61 to 65; 9,000 tokens in fp32 at 8 bits, 305 MB, 51.5 us, 90 %; 64 tokens 3.5 us.
 // What helps is warps, not loads ahead.  Keys first, and the 32 registers that eight blocks per SM leave: 64.6 -> 62.4 -> 59.8 us (9,000
 // tokens in fp32 53.7 -> 50.7); the first units fetched before the sines 65.9, four tokens' units and queries on their way at once, their
 // scales shared out among a group's lanes, 74 to 90.  It is the other way with neighbouring pairs in bf16 (40 registers 64.9 us, 32 66.5) and

@@ -9,25 +9,28 @@
 // The matrix instructions cut off what a product's sum has below its largest term, and take a subnormal for as large as the smallest
 // normal number: with codes as they are a logit is off by some 2^-20 of its products' sum.  In bf16 that is far below the output's own
 // rounding; for fp32 outputs (2e-6 to 5e-6 over 30,000 rows) it is not.  There codes become normal numbers (one more instruction for two), the
-// low parts of queries add up by themselves, and a run's values are added to the sums outside: 5e-7 to 1.5e-6, at 443 MB 111 -> 146 us.
+// low parts of queries add up by themselves, and a run's values are added to the sums outside: 6.5e-7 to 1.0e-6, at 443 MB 111 -> 146 us then.
 //
 // Fragments, lane l: r = l / 4, c = l % 4.  Q K^T has A = codes of the keys (rows r and r + 8 of the tile), B = queries (column r: head r),
 // group by group; sum(q) low is one instruction of bf16, the sums in three parts.  P V has A = codes of the values, transposed
 // (rows are dimensions; a byte permute pairs the codes of neighbouring cache rows), B = (p step_g)^T, from the logits' layout by an 8 x 8
 // transposition per group.  Columns are heads on both sides, so a lane's maxima, sums and results belong to the same two heads.
 //
-// Roundings.  Queries are scaled by a power of two per head, their largest element between 2^14 and 2^15 (fp32: 2^5 and 2^6): fp16 then holds every bf16 element
-// that matters exactly (the rest is below 2^-38 of the largest); fp32 ones go in two parts.  A weight p step is rounded to
-// fp16 (2^-11 of itself, so of the codes' part of the output: it averages out over the rows), for fp32 caches to two
-// such parts.  Weights are scaled by a power of two for every head and group, which goes by the weights met (p step, not the step alone: a row with huge
-// values and no weight takes nothing from the others), so that neither tiny nor huge values leave fp16's range: see settle().
+// Roundings.  Queries are scaled by a power of two per head, their largest element between 2^14 and 2^15 (fp32: 2^5 and 2^6).  fp16 then holds a bf16
+// element exactly down to 2^-31 of the largest and cuts smaller ones off at 2^-39 of it (at 4 bits half of them carry the nibble's 1/16: 2^-27 and 2^-35); fp32
+// ones go in two parts, 22 bits.  A weight p step is rounded to fp16, 2^-11 of itself, for fp32 outputs to two such parts, 2^-22; caches of 16 bits
+// have theirs in two parts of bf16, which here costs 15 % (443 MB at 4 bits 86 -> 99 us).  The error goes with the codes' part of the sum, which lies within
+// the values' range and averages out over the rows: the outputs' error against 64 bits is that of a computation in fp32, 0.0017 (the type's own), and
+// one to three in a hundred come out as the neighbouring number.  Weights are scaled by a power of two for every head and group, which goes by the weights
+// met (p step, not the step alone: a row with huge values and no weight takes nothing from the others): see settle().
 // The reference of the exponentials is set 2^8 above the largest logit met (fp32: 2^6) and moves when one passes it: bringing the sums to a new one
-// costs as much as a tile or two.  No weight is ever above 1, so the sums reach no further than values times rows.
+// costs as much as a tile or two (with none at all in fp32 144 -> 155 us, at head_dim 256 151 -> 174).  No weight is ever above 1, so the sums reach no
+// further than values times rows.
 //
-// Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 9.2 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
-// rows, 28 / 4 heads of 128, 443 MB: 83 us, 82 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
-// ten of up to 32,768 rows, 32 heads, 765 MB: 123 us, 95 %; 192 of 36 to 18,944 rows, 342 MB: 71 us, 74 %; one of 129,072 rows, 74 MB: 25 us, 45 %
-// (copies alone 22.5); one of 947 rows 9.8 us.
+// Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 4.6 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
+// rows, 28 / 4 heads of 128, 443 MB: 86 us, 79 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
+// ten of up to 32,768 rows, 32 heads, 765 MB: 122 to 134 us, 87 to 95 %; 192 of 36 to 18,944 rows, 342 MB: 73 to 80 us, 65 to 71 %; one of
+// 129,072 rows, 74 MB: 26 us, 44 % (copies alone 22.5); one of 947 rows 9.0 us, more than the same rows in 16 bits take (8.2).
 #pragma once
 
 #include <cuda_fp16.h>
@@ -411,9 +414,10 @@ struct AttnTileCoded {
     return most;
   }
   // References at or above the tile's logits `s`, the sums brought to them; and scales for the tile's weights p step, which then are at most 2^15.
-  // Where a reference moves the scale is set anew: kRoom bits below what would fit the tile's largest step with a weight of 1, so that the next tiles need not be
-  // looked at this closely, but not so low that its largest weight p step would be below 2^kLeast.  Elsewhere it comes down only for a weight that
-  // is too large: a huge step alone, of a row that does not count, leaves it alone.
+  // Where a reference moves the scale is set anew: kRoom bits below what would fit the tile's largest step with a p of 1, so that the next tiles, whose steps
+  // are much alike, need not be looked at this closely (with no room at all 443 MB 86 -> 106 us, in fp32 144 -> 165), but not so low that the tile's largest
+  // weight p step would be below 2^kLeast.  Elsewhere it comes down only for a weight that is too large: a huge step alone, of a row that does not
+  // count, leaves it alone.
   static constexpr int kRoom = PARTS == 2 ? 3 : 6, kLeast = PARTS == 2 ? 0 : -6;
   __device__ __forceinline__ void settle(const float (&s)[SUB][NH][4], const uint32_t (&vm)[SUB][2][G]) {
 #pragma unroll
@@ -567,8 +571,7 @@ struct AttnTileCoded {
 // end, and those that cross blocks states in scratch, as there.  (With the tiles dealt round all warps and a joining at the end of every
 // segment the 192 ragged caches took 167 us against 77 then.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
-// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches took 82.5, 77, 71.5 and 71.9 us (before weights were scaled by
-// head and group).  With blocks of 64, 128, 256, 384 and 512 rows at least one cache of 947 rows takes 8.9, 9.0, 9.4, 10.1 and 11.1 us, one of 4,000 10.5, 9.9,
+// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches take 84.5, 78.4, 73.2 and 73.6 us.  With blocks of 64, 128, 256, 384 and 512 rows at least one cache of 947 rows takes 8.9, 9.0, 9.4, 10.1 and 11.1 us, one of 4,000 10.5, 9.9,
 // 9.8, 10.6 and 11.5, one of 16,000 13.7, 13.7, 13.7, 13.7 and 13.0, nine in fp32 of up to 1,024 9.5, 9.5, 9.6, 10.2 and 10.2; longer ones and larger
 // batches fill all blocks with any of them.
 constexpr int kCodedSegment = 128, kCodedLeast = 128;

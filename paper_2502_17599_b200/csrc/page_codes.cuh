@@ -16,8 +16,10 @@
 // Bound by memory where the arithmetic lets it: some 60 instructions go into eight elements of bf16 with bounds, so it is fp32 pairs in one
 // instruction (f32x2), extremes of two bf16 at once, sums with 2^23 in place of conversions, and one scale per lane for eight rows of a
 // group, handed round, in place of eight equal ones.  28 layers of a 19K-token prompt (4 heads of 128, bf16, 4 bits): stored with
-// their bounds, 330 MB, in 72 us, 70 % of a plain copy (without bounds 62), read back, 315 MB, in 54 us, 88 %; 64 caches read
-// back from 8 bits, 629 MB, in 103 us, 93 %.  The same prompt in fp32 122 and 100 us.
+// their bounds, 330 MB, in 71 to 75 us, 67 to 71 % of a plain copy (without bounds 61 to 69), read back, 315 MB, in 54 us, 88 %; at 8 bits, 392 and 376
+// MB, in 72 to 78 us, 77 to 83 %, and 63 us, 92 %; 64 caches read back from 8 bits, 629 MB, in 103 us, 93 %.  The same prompt in fp32 119 to 133 us and 98
+// at 4 bits, 122 to 131 and 110 at 8.  Its keys' bounds alone: 33 to 40 us at 4 bits, 26 at 8 (arithmetic: 8 and 12 us of reading), in fp32 64 and 60; those of
+// the last pages of 28 sequences 3.5 and 3.0 us.
 #pragma once
 
 #include "page_rows.cuh"
@@ -342,7 +344,8 @@ __device__ __forceinline__ void load_span(const int32_t* lens_from, const int32_
 }
 
 // Blocks per SM that the registers are to leave room for.  Storing from bf16, four instead of the two of 104 registers: the 19K-token prompt 83.4 -> 72.8
-// us (five 81), from fp32 two (120 us, three 146); loading into fp32 three instead of four 116 -> 101.5 us, into bf16 no matter.
+// us (64 registers, with 24 bytes of spills at 4 bits and 32 at 8; five 81), from fp32 two (120 us, three 146); loading into fp32 three instead of four
+// 116 -> 101.5 us, into bf16 no matter.
 template <typename T, int BITS, CodedPass PASS>
 constexpr int kCodedBlocks = PASS == kCodedStore ? (sizeof(T) == 2 ? 4 : 2) : sizeof(T) == 4 ? 3 : BITS == 4 ? 5 : 4;
 
@@ -490,7 +493,8 @@ coded_rows_kernel(CodedParams p) {
 }
 
 // ---- rows of pages that hold them as they are, read back ------------------------------------------------------------------
-// VR = 16-byte vectors per row.
+// VR = 16-byte vectors per row.  Bound by memory: 28 layers of a 19K-token prompt (4 heads of 128), 491 MB in bf16, in 79 us, 95 % of a plain copy, 983 MB
+// in fp32 in 156 us, 96 %; the last 33 rows of each 3.9 and 5.3 us.
 struct LoadParams {
   const uint4* k_pages;
   const uint4* v_pages;

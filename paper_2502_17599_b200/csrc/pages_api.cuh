@@ -145,8 +145,8 @@ struct CodedAttnKernel {
 // Rows of a tile, warps and ring by head size, bits and group; one block per SM.  A tile has 32 rows at 4 bits and 16 at 8, which are about as many
 // bytes: at 4 bits and 16 rows the work of a tile that does not depend on its rows shows.  Warps are what the registers allow without spills in
 // bf16, stages what the warps leave of shared memory (with the largest batches one at head_dim 256).  443 MB at 4 bits, 28 / 4 heads: head_dim
-// 128, eight warps with three tiles each 95 us, twelve with two 83.0, with three 83.4, sixteen with two 85; head_dim 64, twelve warps 110,
-// sixteen 101.
+// 128, eight warps with three tiles each 97.7 us, twelve with two 86.0, with three 87.2, sixteen with two 87.5; head_dim 64, twelve warps 109,
+// sixteen 102.  In fp32 with its spills the same order: 147.5, 144, 146, 159.
 template <typename T, int BITS, typename F>
 meda_status with_coded_attn_kernel(const meda_pages* p, F f) {
   const int d = p->cfg.head_dim, g = p->group;
