@@ -416,14 +416,22 @@ struct AttnTileCoded {
   // References at or above the tile's logits `s`, the sums brought to them; and scales for the tile's weights p step, which then are at most 2^15.
   // Where a reference moves the scale is set anew: kRoom bits below what would fit the tile's largest step with a p of 1, so that the next tiles, whose steps
   // are much alike, need not be looked at this closely (with no room at all 443 MB 86 -> 106 us, in fp32 144 -> 165), but not so low that the tile's largest
-  // weight p step would be below 2^kLeast.  Elsewhere it comes down only for a weight that is too large: a huge step alone, of a row that does not
-  // count, leaves it alone.
+  // weight p step would be below 2^kLeast, and no higher than leaves what o has where it is: weights that are too small for that are small beside it
+  // for good.  Elsewhere it comes down only for a weight that is too large: a huge step alone, of a row that does not count, leaves it alone.
   static constexpr int kRoom = PARTS == 2 ? 3 : 6, kLeast = PARTS == 2 ? 0 : -6;
   __device__ __forceinline__ void settle(const float (&s)[SUB][NH][4], const uint32_t (&vm)[SUB][2][G]) {
+    // The groups' exponents once for all heads where there are registers for them (64 / 4 heads of 128 at 8 bits 94.4 -> 89.6 us, 28 / 4 at 4 bits 86.2 ->
+    // 85.4; but 64 / 4 at 4 bits 131 -> 134, 16 / 4 of 256 81.0 -> 84.0).
+    constexpr bool kOnce = G * NH * SUB <= 4;
+    int step_exp[G];
+    if constexpr (kOnce)
+#pragma unroll
+      for (int g = 0; g < G; ++g) step_exp[g] = exponent(over_rows(largest_step(vm, g)));
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        // (which heads move differs among the lanes: no exchange below depends on it)
         const float most = over_rows(largest(s, n, x)), from = ref[n][x];
         const bool moved = most > from;                        // (with nothing but NaN so far there is no reference, and the sums become NaN)
         const float to = moved ? most + kSlack : from, f = exp2_fast(from - to);
@@ -438,19 +446,12 @@ struct AttnTileCoded {
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int t = 0; t < 2; ++t) weight = fmaxf(weight, exp2_fast(s[u][n][2 * t + x] - to) * step_of(vm[u][t], g));
-          const int weight_exp = exponent(over_rows(weight)), step_exp = exponent(over_rows(largest_step(vm, g)));
-          const int now = exponent(scale[n][x][g]);
-          int e = min(max(14 - kRoom - step_exp, kLeast - weight_exp), kMostScale);
-          float high = 0.f;
-#pragma unroll
-          for (int t = 0; t < 4; ++t) high = fmaxf(high, fmaxf(fabsf(o[g][t][n][x]), fabsf(o[g][t][n][2 + x])));
-          high = over_rows(high);                              // (by all lanes: which heads move differs among them)
-          if (moved) e = min(e, now + by + 60 - exponent(high));                 // o, as it is in the new scale, below 2^60
-          else if (weight_exp + now < 15) e = now;
-          e = max(e, -126);
+          if constexpr (!kOnce) step_exp[g] = exponent(over_rows(largest_step(vm, g)));
+          const int weight_exp = exponent(over_rows(weight)), now = exponent(scale[n][x][g]);
+          const int anew = min(max(14 - kRoom - step_exp[g], kLeast - weight_exp), moved ? now + by : now);
+          const int e = max(moved || weight_exp + now >= 15 ? min(anew, kMostScale) : now, -126);
           scale[n][x][g] = power_of_two(e);
-          const int up = min(e - now, 200);                    // (beyond 126 in two steps; f is 0 where it could be more)
-          const float change = up < -126 ? 0.f : f * power_of_two(min(up, 100)) * power_of_two(max(up, 100) - 100);
+          const float change = e - now < -126 ? 0.f : f * power_of_two(min(e - now, 126));                       // (beyond 126 only where f is 0)
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             o[g][t][n][x] *= change;

@@ -186,3 +186,24 @@ def test_values_near_the_end_of_fp32(B, dtype, bits):
     out, lse = attend(B, q, k, v, dtype, bits, 1000)
     assert torch.isfinite(out).all()
     check(out, lse, P.np64(q), k, v, bits, dtype)
+
+
+@both
+def test_a_row_that_counts_less_and_less(B, dtype, bits):
+    """A row of 2^40 times the others' values that counts when it is met and is left behind by logits that rise: in the end its part of the sum is far above, about,
+    or far below the others'.  What came before, between and after is as exact as the largest part lets it be seen."""
+    rows, hq, d = 120, 2, 64
+    rng = np.random.default_rng(bits)
+    ks, vs = [], []
+    for where in (0, 20, 50):
+        for far in (5, 20, 35, 38, 40, 42, 45, 60, 100, 140):
+            k, v = rng.normal(0, 0.01, (rows, d)), rng.normal(0.2, 1, (rows, d))
+            k[:, 0] = np.maximum(0, np.arange(rows) - where) / (rows - 1 - where) * far * math.log(2)
+            v[where] *= 2.0 ** 40
+            ks.append(k), vs.append(v)
+    k, v = np.stack(ks), np.stack(vs)
+    q = np.zeros((len(k), hq, d))
+    q[:, 0, 0], q[:, 1, 0], q[:, :, 1:] = 8.0, 4.0, rng.normal(0, 0.1, (len(k), hq, d - 1))
+    q = torch.as_tensor(q).to(T.DT[dtype]).cuda()
+    out, lse = attend(B, q, k, v, dtype, bits, 50)
+    check(out, lse, P.np64(q), k, v, bits, dtype)
