@@ -28,9 +28,9 @@
 // further than values times rows.
 //
 // Bound by issue slots beside memory: a 4-bit tile of 32 rows at head_dim 128 is 4.6 KB, 200 cycles of an SM's share of memory.  64 caches of 12,000
-// rows, 28 / 4 heads of 128, 443 MB: 86 us, 79 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
-// ten of up to 32,768 rows, 32 heads, 765 MB: 122 to 134 us, 87 to 95 %; 192 of 36 to 18,944 rows, 342 MB: 73 to 80 us, 65 to 71 %; one of
-// 129,072 rows, 74 MB: 26 us, 44 % (copies alone 22.5); one of 947 rows 9.0 us, more than the same rows in 16 bits take (8.2).
+// rows, 28 / 4 heads of 128, 443 MB: 85 us, 79 % of a plain copy (the same copies without arithmetic 76.7); at 8 bits, 418 MB: 73 us, 87 %;
+// ten of up to 32,768 rows, 32 heads, 765 MB: 122 to 134 us, 87 to 95 %; 192 of 36 to 18,944 rows, 342 MB: 73 to 82 us, 64 to 72 %; one of
+// 129,072 rows, 74 MB: 26 us, 44 % (copies alone 22.5); one of 947 rows 8.9 us, more than the same rows in 16 bits take (8.2).
 #pragma once
 
 #include <cuda_fp16.h>
@@ -572,9 +572,10 @@ struct AttnTileCoded {
 // end, and those that cross blocks states in scratch, as there.  (With the tiles dealt round all warps and a joining at the end of every
 // segment the 192 ragged caches took 167 us against 77 then.)
 // Empty tiles counted with every segment, and tiles per block where the GPU has more blocks than that fills, as kAttSegment and
-// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches take 84.5, 78.4, 73.2 and 73.6 us.  With blocks of 64, 128, 256, 384 and 512 rows at least one cache of 947 rows takes 8.9, 9.0, 9.4, 10.1 and 11.1 us, one of 4,000 10.5, 9.9,
-// 9.8, 10.6 and 11.5, one of 16,000 13.7, 13.7, 13.7, 13.7 and 13.0, nine in fp32 of up to 1,024 9.5, 9.5, 9.6, 10.2 and 10.2; longer ones and larger
-// batches fill all blocks with any of them.
+// kAttLeast but in rows.  Of 32, 64, 128 and 192 rows with a segment the 192 ragged caches take 84.5, 78.4, 73.2 and 73.6 us.  With blocks of 64, 128,
+// 256, 384 and 512 rows at least one cache of 947 rows takes 8.9, 9.0, 9.4, 10.1 and 11.1 us, one of 4,000 10.5, 9.9, 9.8, 10.6 and 11.5, one of
+// 16,000 13.7, 13.7, 13.7, 13.7 and 13.0, nine in fp32 of up to 1,024 9.5, 9.5, 9.6, 10.2 and 10.2; longer ones and larger batches fill all blocks
+// with any of them.
 constexpr int kCodedSegment = 128, kCodedLeast = 128;
 
 template <int N>
