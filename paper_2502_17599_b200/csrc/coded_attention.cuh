@@ -79,7 +79,8 @@ __device__ __forceinline__ uint32_t bf16_part(float& lo, float& hi) {
   memcpy(&y, &x, 4);
   return y;
 }
-__device__ __forceinline__ void mul2(float& x, float& y, float a, float b, float c, float d) {       // (a c, b d) in one instruction
+// (a c, b d) in one instruction, which may be put together with a sum behind it, into one rounding.
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b, float c, float d) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a, b)), "l"(pair(c, d)));
   unpair(r, x, y);
@@ -345,7 +346,7 @@ struct AttnTileCoded {
 #pragma unroll
       for (int n = 0; n < NH; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) mul2(s[u][n][e], s[u][n][e + 1], s[u][n][e], s[u][n][e + 1], factor[n][0], factor[n][1]);
+        for (int e = 0; e < 4; ++e) s[u][n][e] = __fmul_rn(s[u][n][e], factor[n][e & 1]);
     }
     uint32_t vm[SUB][2][G];                                    // steps and lowest values of the values' rows r, r + 8
 #pragma unroll
@@ -420,13 +421,6 @@ struct AttnTileCoded {
   // for good.  Elsewhere it comes down only for a weight that is too large: a huge step alone, of a row that does not count, leaves it alone.
   static constexpr int kRoom = PARTS == 2 ? 3 : 6, kLeast = PARTS == 2 ? 0 : -6;
   __device__ __forceinline__ void settle(const float (&s)[SUB][NH][4], const uint32_t (&vm)[SUB][2][G]) {
-    // The groups' exponents once for all heads where there are registers for them (64 / 4 heads of 128 at 8 bits 94.4 -> 89.6 us, 28 / 4 at 4 bits 86.2 ->
-    // 85.4; but 64 / 4 at 4 bits 131 -> 134, 16 / 4 of 256 81.0 -> 84.0).
-    constexpr bool kOnce = G * NH * SUB <= 4;
-    int step_exp[G];
-    if constexpr (kOnce)
-#pragma unroll
-      for (int g = 0; g < G; ++g) step_exp[g] = exponent(over_rows(largest_step(vm, g)));
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll
@@ -446,9 +440,8 @@ struct AttnTileCoded {
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int t = 0; t < 2; ++t) weight = fmaxf(weight, exp2_fast(s[u][n][2 * t + x] - to) * step_of(vm[u][t], g));
-          if constexpr (!kOnce) step_exp[g] = exponent(over_rows(largest_step(vm, g)));
-          const int weight_exp = exponent(over_rows(weight)), now = exponent(scale[n][x][g]);
-          const int anew = min(max(14 - kRoom - step_exp[g], kLeast - weight_exp), moved ? now + by : now);
+          const int weight_exp = exponent(over_rows(weight)), step_exp = exponent(over_rows(largest_step(vm, g))), now = exponent(scale[n][x][g]);
+          const int anew = min(max(14 - kRoom - step_exp, kLeast - weight_exp), moved ? now + by : now);
           const int e = max(moved || weight_exp + now >= 15 ? min(anew, kMostScale) : now, -126);
           scale[n][x][g] = power_of_two(e);
           const float change = e - now < -126 ? 0.f : f * power_of_two(min(e - now, 126));                       // (beyond 126 only where f is 0)

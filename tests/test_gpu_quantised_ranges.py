@@ -4,9 +4,9 @@ values next to fp32's end.
 Tolerances.  A logit is the sum over the groups of step * (q . codes) and low * (sum of q), d + d / 64 products added up in fp32 (2^-22 for each, which also
 covers an accumulator that truncates), and is rounded once more: off by at most delta = (d + 34) 2^-22 sum |q| (step code + |low|) / sqrt(d); that moves a
 probability by exp(delta) and its normaliser by as much.  exp2 is off by 2^-22, sums of `rows` terms by rows 2^-22.  The weight p * step of a row's codes
-enters its product in fp16, off by 2^-11 of itself for bf16 outputs and by 2^-22 for fp32 ones (two parts), and no finer than 2^-25 where the largest weight of
-its head and 64 dimensions is 2^-6 or more (fp32: 1 or more).  The result is rounded once.  All of it is relative to what is added up, p * step * code and p * |low|: a row without weight
-is not in it."""
+enters its product in fp16, off by 2^-11 of itself for bf16 outputs and by 2^-22 for fp32 ones (two parts), and no finer than 2^-25 where the largest
+weight of its head and 64 dimensions is 2^-6 or more (fp32: 1 or more).  The result is rounded once.  All of it is relative to what is added up,
+p * step * code and p * |low|: a row without weight is not in it."""
 import math
 
 import numpy as np
@@ -88,13 +88,14 @@ def both(f):
 
 
 @both
-@pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
-def test_logits_far_beyond_the_mantissa(B, dtype, bits, order):
+@pytest.mark.parametrize("order,d,hq", [("rising", 64, 1), ("falling", 64, 1), ("mixed", 64, 1), ("mixed", 64, 16), ("rising", 128, 3), ("mixed", 128, 9),
+                                        ("rising", 256, 2), ("mixed", 256, 11)])
+def test_logits_far_beyond_the_mantissa(B, dtype, bits, order, d, hq):
     """Logits of 10^6 to 10^30, a dozen in every binade up to 10^11: the row that sets the reference has a weight of 1, whatever the rounding of its logit.
     What rows read back as differs by 2^-9 or more of the largest, so one row decides (or several alike): the output is their values' mean.  Its weight
-    is exact (a step is a bf16), the sums are off by 2^-22 of their size for each row and for each of the 64 products beside it, and the result is
+    is exact (a step is a bf16), the sums are off by 2^-22 of their size for each row and for 64 products beside it, and the result is
     rounded once."""
-    rows, d = 40, 64
+    rows = 40
     tops = np.concatenate([8e6 * 2.0 ** (np.arange(200) / 12), 8e12 * 10.0 ** np.arange(18)])
     n = len(tops)
     rng = np.random.default_rng(bits)
@@ -102,19 +103,20 @@ def test_logits_far_beyond_the_mantissa(B, dtype, bits, order):
     k = np.zeros((n, rows, d))
     k[:, :, 0] = tops[:, None] * (ranks + 1) / rows
     v = rng.normal(0.3, 1, (n, rows, d))
-    q = torch.zeros((n, 1, d), dtype=T.DT[dtype], device="cuda")
+    q = torch.zeros((n, hq, d), dtype=T.DT[dtype], device="cuda")
     q[:, :, 0] = 1.0
     out, lse = attend(B, q, k, v, dtype, bits, 30)
-    s = parts(k, bits)[0][:, :, 0] / 8
+    s = parts(k, bits)[0][:, :, 0] / math.sqrt(d)
     at = s == s.max(1, keepdims=True)
     assert (np.where(at, -np.inf, s).max(1) <= s.max(1) * (1 - 2.0 ** -9)).all()
     p = at / at.sum(1, keepdims=True)
     vr, vc, vl = parts(v, bits)
     want, size = np.einsum("nr,nrd->nd", p, vr), np.einsum("nr,nrd->nd", p, vc + vl)
     tol = size * (rows + 64) * 2.0 ** -22 + T.HALF_STEP[dtype] * 1.01 * np.abs(want)
-    off = np.abs(P.np64(out[:, :, 0]) - want)
-    assert (off <= tol).all(), float((off / tol).max())
-    assert (np.abs(P.np64(lse[:, :, 0]) - s.max(1) - np.log(at.sum(1))) <= 2.0 ** -21 * s.max(1)).all()
+    off = np.abs(P.np64(out) - want[:, None])
+    assert (off <= tol[:, None]).all(), float((off / tol[:, None]).max())
+    norm = s.max(1) + np.log(at.sum(1))
+    assert (np.abs(P.np64(lse) - norm[:, None]) <= 2.0 ** -21 * norm[:, None]).all()
 
 
 @both
